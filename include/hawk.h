@@ -424,6 +424,119 @@ int hawk_generate_spatial(hawk_ctx* ctx, const float* cond, int n_cond, int grid
                           const void* W_heads, const void* W_out, int HD, int VSD, uint64_t seed, void* workspace,
                           size_t workspace_bytes, int32_t* out_grid, int64_t* out_stats);
 
+/* ---- A target pass over a paged cache -----------------------------------------------------------
+ * For callers that run a target model of their own over many sequences: the cache of keys and values, the
+ * attention that reads it, and the two forms of verification of this library (a drafted chain, a candidate
+ * tree) on top of it.  One step of such a model: per layer hawk_paged_append and hawk_paged_attention over
+ * the step's rows - the last committed token of every sequence and what was drafted behind it, or a piece of
+ * a prompt -, then hawk_verify_chains (or hawk_multi_verify along a tree, and hawk_paged_keep).
+ * No context: all pointers are DEVICE pointers unless stated (the structures themselves are host memory, read
+ * during the call), the caller owns every buffer, nothing is allocated, launches are asynchronous on `stream`
+ * (a hipStream_t of the current device, NULL: the default stream), and every call may be captured into a graph.
+ * What the host does not see - tables, row starts, lengths - is checked on the device: nothing outside the
+ * pools, tables and rows described is read or written, whatever they hold. */
+
+enum { HAWK_FP16 = 2 };   /* next to HAWK_FP32 and HAWK_BF16, in the structures below only */
+
+/* A pool of pages of keys and values and which pages hold which sequence.  Entry e of sequence s lies in page
+ * table[s * table_stride + e / page_size] at place e % page_size; key (or value) of head h of that entry starts
+ *   layer * layer_stride + page * page_stride + h * head_stride + (e % page_size) * entry_stride
+ * elements behind k (or v), head_dim elements in a row.  An entry exists if 0 <= e < max_pages * page_size and
+ * 0 <= page < n_pages; entries that do not exist are neither written nor attended.
+ * head_dim: a multiple of 8, at most 256; strides: multiples of 8 elements, not below head_dim (layer_stride: not
+ * below 0); k and v 16-byte aligned; max_pages * page_size <= 2^30; any page_size. */
+typedef struct {
+    void *k, *v;
+    int64_t layer_stride, page_stride, head_stride, entry_stride;
+    const int32_t* table;
+    int64_t table_stride;
+    int32_t dtype;                  /* HAWK_FP32, HAWK_BF16 or HAWK_FP16 */
+    int32_t n_layers, n_pages, page_size, n_heads, head_dim, n_seq, max_pages;
+} hawk_paged_cache;
+
+/* The rows of a step: rows row_start[s] .. row_start[s + 1] - 1 (row_start [n_seq + 1], ascending from 0; a
+ * sequence may have none) belong to sequence s, which has n_past[s] committed entries [n_seq]; row i of a
+ * sequence is its entry n_past + i.  rows: how many rows the buffers have; rows behind the last sequence's are
+ * left as they are (a batch padded to a fixed size). */
+typedef struct {
+    const int32_t *row_start, *n_past;
+    int32_t rows;
+} hawk_paged_rows;
+
+/* Vectors of head_dim elements, one per row and head: row * row_stride + head * head_stride elements behind
+ * data (columns of a fused projection are row_stride apart).  data 16-byte aligned, strides multiples of 8. */
+typedef struct {
+    void* data;
+    int64_t row_stride, head_stride;
+    int32_t n_heads, dtype;
+} hawk_heads;
+
+/* Rotary table: fp32 [n_pos][rot_dim / 2][2], cos and sin of position * theta^(-2 j / rot_dim), angles in fp64.
+ * rot_dim even.  (Any table of that shape may be passed on, e.g. one for two-dimensional positions.) */
+int hawk_rotary_table(float* table, int n_pos, int rot_dim, double theta, void* stream);
+
+/* Queries and keys of one layer are normalised per head and rotated, keys and values appended to the cache.
+ *   normalised: x / sqrt(mean(x^2) + eps) * gain (q_gain, k_gain fp32 [head_dim]; NULL: not normalised);
+ *   rotated by row `position` of the table: (a, b) -> (a cos - b sin, a sin + b cos) for pairs j < rot_dim / 2 of
+ *   the first rot_dim elements, pair j = elements 2 j, 2 j + 1 (pairs = 0) or j, j + rot_dim / 2 (pairs = 1);
+ *   position = pos[row] (pos NULL: n_past + i).  rot NULL: not rotated.
+ * In fp32, rounded once to the cache's type.  k, v: cache->n_heads heads each, q (may be NULL with q_out) any
+ * number; q, k, v of one type, q_out of the cache's.  q_out may be q itself (same data, strides and type), no other
+ * buffers overlap.  A row whose position is outside the table is left out altogether: neither its q_out nor its
+ * entry is written.  Rows of different sequences that share an entry race.
+ * rot_dim: a multiple of 8, at most head_dim. */
+int hawk_paged_append(const hawk_paged_cache* cache, int layer, const hawk_paged_rows* rows, const hawk_heads* q,
+                      const hawk_heads* k, const hawk_heads* v, const float* q_gain, const float* k_gain, float eps,
+                      const float* rot, int n_pos, int rot_dim, int pairs, const int32_t* pos, const hawk_heads* q_out,
+                      void* stream);
+
+/* Attention of the step's rows over one layer of the cache, which holds the rows' own entries already:
+ *   out[row][h] = sum_e softmax_e(scale * q[row][h] . k[e][h / group]) v[e][h / group],  group = q heads / cache heads,
+ * over the entries e that exist and that the row sees: e <= n_past + i; or, with tree (uint64 [rows]), the
+ * committed entries e < n_past, those of the step's rows j < 64 whose bit j is set in tree[row] (e = n_past + j; the
+ * ancestors of hawk_tree_layout) and its own.  A row that sees nothing (or whose every score is minus infinity) gives zeros.  What
+ * a row does not see has no part in its result, whatever values it holds.
+ * q of the cache's type; out of any of the three types, not overlapping q.  Scores, maximum, sums and results in
+ * fp32; the weights reach the products with about 16 bits for rows of few, with the type's own for many (see below).
+ * scale > 0.  max_len (host): the longest n_past + rows of a sequence, for the choice of the kernel only: any value
+ * gives the right results (at most max_pages * page_size is assumed).
+ * workspace (may be NULL where the size function says 0; 16-byte aligned): hawk_paged_attention_workspace_bytes
+ * for the same cache, rows and max_len; nothing in it has to be cleared or is kept from call to call. */
+size_t hawk_paged_attention_workspace_bytes(const hawk_paged_cache* cache, int rows, int n_q_heads, int max_len);
+int hawk_paged_attention(const hawk_paged_cache* cache, int layer, const hawk_paged_rows* rows, const hawk_heads* q,
+                         const uint64_t* tree, float scale, int max_len, const hawk_heads* out, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/* After a tree step: the entries of the accepted path move to their positions, in every layer.  For sequence s and
+ * j = 0 .. n_keep[s] - 1 (n_keep clamped to 0..depth): entry n_past[s] + path[s * depth + j] goes to
+ * n_past[s] + j + 1 (path: node numbers as in hawk_tree_layout, the root's own entry stays).  Nodes below j + 1, which
+ * a path never has, and entries that do not exist are skipped.  depth 1..64. */
+int hawk_paged_keep(const hawk_paged_cache* cache, const int32_t* n_past, const int32_t* path, const int32_t* n_keep,
+                    int depth, void* stream);
+
+/* Where entry e of a sequence whose pages are table_row (HOST, [max_pages]) lies: elements behind k (head 0), -1 if
+ * the entry does not exist (host arithmetic only; the kernels use the same function). */
+int64_t hawk_paged_entry(const hawk_paged_cache* cache, const int32_t* table_row, int layer, int64_t e);
+
+/* Verification of drafted chains (Preliminary, "Speculative Sampling"), the rule of hawk_verify for logits that
+ * the caller has: sequence s has n_draft[s] drafts (NULL: k; clamped to k; negative: the sequence is
+ * left out, count and tokens -1), draft[s * k + i] judged by row i of its k + 1 target rows.
+ * Draft i is accepted iff u_acc[s * k + i] * q_i(d) < p_i(d); at the first rejection the next token is drawn with
+ * u_final[s] from norm(max(0, p_i - q_i)) (from p_i if that has no mass), after n_draft acceptances from the next
+ * target row.  p = warp(p_logits), q = warp(q_logits), warp and draws as in hawk_multi_verify; probabilities and
+ * sums in fp64.  A draft outside 0..n-1 is rejected.
+ *   p_logits fp32: row i of sequence s starts (p_start ? p_start[s] + i : s * (k + 1) + i) * p_stride elements in; p_rows
+ *     rows in all (a sequence with drafts whose rows are not all among them is left out);
+ *   q_logits fp32: s * q_seq_stride + i * q_stride elements in, or NULL: every proposal is the point mass on its draft;
+ *   out_n_accept [n_seq], out_tokens [n_seq][k + 1]: accepted drafts and the token drawn, -1 behind.
+ * k 0..63, n 1..2^20, n_seq * (2 k + 1) <= 2^21, strides not below n, top_k >= 1, temperature >= 0.  workspace
+ * (16-byte aligned): hawk_verify_chains_workspace_bytes; nothing in it has to be cleared. */
+size_t hawk_verify_chains_workspace_bytes(int n_seq, int k, int n);
+int hawk_verify_chains(const float* p_logits, int64_t p_stride, const int32_t* p_start, int p_rows, const float* q_logits,
+                       int64_t q_seq_stride, int64_t q_stride, const int32_t* draft, const int32_t* n_draft,
+                       const float* u_acc, const float* u_final, int n_seq, int k, int n, float temperature, int top_k,
+                       int32_t* out_n_accept, int32_t* out_tokens, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -14,11 +14,14 @@ from .hawk import (  # noqa: F401
     multi_verify_static,
     multi_verify_workspace_bytes,
     plan_info,
+    rotary_table,
     sample_rows,
     spatial_heads,
     spec_cache_bytes,
     spec_cache_slot,
     tree_layout,
+    verify_chains,
+    PagedCache,
     SpecCache,
     workspace_bytes,
 )

@@ -10,6 +10,7 @@
 #include <new>
 
 #include "chain.h"
+#include "paged.h"
 
 #include <vector>
 
@@ -574,6 +575,61 @@ int hawk_sample_rows(const float* logits, const int32_t* skip, const float* u, i
     if (rows == 0) return HAWK_OK;
     return hawk::launch_sample_rows(logits, skip, u, rows, n, temperature, top_k, out_token,
                                     static_cast<hipStream_t>(stream));
+}
+
+int hawk_rotary_table(float* table, int n_pos, int rot_dim, double theta, void* stream) {
+    return hawk::launch_rotary_table(table, n_pos, rot_dim, theta, static_cast<hipStream_t>(stream));
+}
+
+int hawk_paged_append(const hawk_paged_cache* cache, int layer, const hawk_paged_rows* rows, const hawk_heads* q,
+                      const hawk_heads* k, const hawk_heads* v, const float* q_gain, const float* k_gain, float eps,
+                      const float* rot, int n_pos, int rot_dim, int pairs, const int32_t* pos, const hawk_heads* q_out,
+                      void* stream) {
+    return hawk::launch_paged_append(cache, layer, rows, q, k, v, q_gain, k_gain, eps, rot, n_pos, rot_dim, pairs, pos, q_out,
+                                     static_cast<hipStream_t>(stream));
+}
+
+size_t hawk_paged_attention_workspace_bytes(const hawk_paged_cache* cache, int rows, int n_q_heads, int max_len) {
+    return hawk::paged_attention_workspace_bytes(cache, rows, n_q_heads, max_len);
+}
+
+int hawk_paged_attention(const hawk_paged_cache* cache, int layer, const hawk_paged_rows* rows, const hawk_heads* q,
+                         const uint64_t* tree, float scale, int max_len, const hawk_heads* out, void* workspace,
+                         size_t workspace_bytes, void* stream) {
+    return hawk::launch_paged_attention(cache, layer, rows, q, tree, scale, max_len, out, workspace, workspace_bytes,
+                                        static_cast<hipStream_t>(stream));
+}
+
+int hawk_paged_keep(const hawk_paged_cache* cache, const int32_t* n_past, const int32_t* path, const int32_t* n_keep,
+                    int depth, void* stream) {
+    return hawk::launch_paged_keep(cache, n_past, path, n_keep, depth, static_cast<hipStream_t>(stream));
+}
+
+int64_t hawk_paged_entry(const hawk_paged_cache* cache, const int32_t* table_row, int layer, int64_t e) {
+    hawk::PagedView c;
+    if (!table_row || !hawk::paged_view(cache, layer, &c)) return -1;
+    const int64_t at = hawk::entry_at(c, table_row, e);
+    return at < 0 ? -1 : layer * cache->layer_stride + at;
+}
+
+size_t hawk_verify_chains_workspace_bytes(int n_seq, int k, int n) {
+    return n_seq > 0 && k >= 0 && k <= hawk::kMaxK && n >= 1 && n <= (1 << 20) ? hawk::verify_chains_workspace_bytes(n_seq, k, n) : 0;
+}
+
+int hawk_verify_chains(const float* p_logits, int64_t p_stride, const int32_t* p_start, int p_rows, const float* q_logits,
+                       int64_t q_seq_stride, int64_t q_stride, const int32_t* draft, const int32_t* n_draft,
+                       const float* u_acc, const float* u_final, int n_seq, int k, int n, float temperature, int top_k,
+                       int32_t* out_n_accept, int32_t* out_tokens, void* workspace, size_t workspace_bytes, void* stream) {
+    if (n_seq < 0 || k < 0 || k > hawk::kMaxK || n < 1 || n > (1 << 20) || top_k < 1 || !(temperature >= 0.0f)) return HAWK_EINVAL;
+    if (p_stride < n || p_rows < 0 || (int64_t)n_seq * (2 * k + 1) > (1 << 21)) return HAWK_EINVAL;   // a launch has fewer than 2^32 threads
+    if (k > 0 && q_logits && (q_stride < n || q_seq_stride < 0)) return HAWK_EINVAL;
+    if (n_seq == 0) return HAWK_OK;
+    if (!p_logits || !u_final || !out_n_accept || !out_tokens || (k > 0 && (!draft || !u_acc))) return HAWK_EINVAL;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15)) return HAWK_EINVAL;
+    if (workspace_bytes < hawk::verify_chains_workspace_bytes(n_seq, k, n)) return HAWK_ENOMEM;
+    return hawk::launch_verify_chains(p_logits, p_stride, p_start, p_rows, q_logits, q_seq_stride, q_stride, draft, n_draft, u_acc,
+                                      u_final, n_seq, k, n, temperature, top_k, out_n_accept, out_tokens, workspace,
+                                      workspace_bytes, static_cast<hipStream_t>(stream));
 }
 
 int hawk_load(hawk_ctx* c, const void* host_blob, size_t nbytes) {

@@ -304,4 +304,11 @@ int launch_spec_pool(const void* cache, int IW, int IH, int VSD, int Vs, const i
                      size_t horiz_stride, int n, float* pool_logits, int32_t* pool_m, int32_t* pool_delta,
                      hipStream_t stream);
 
+// ---- verification of drafted chains, implemented in chains.hip (arguments checked by the caller) ----
+size_t verify_chains_workspace_bytes(int n_seq, int k, int n);
+int launch_verify_chains(const float* p_logits, int64_t p_stride, const int32_t* p_start, int p_rows, const float* q_logits,
+                         int64_t q_seq_stride, int64_t q_stride, const int32_t* draft, const int32_t* n_draft,
+                         const float* u_acc, const float* u_final, int n_seq, int k, int n, float temperature, int top_k,
+                         int32_t* out_n_accept, int32_t* out_tokens, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
 }  // namespace hawk

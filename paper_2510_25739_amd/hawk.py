@@ -11,7 +11,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libhawk.so")
 _lib = None
 
-HAWK_FP32, HAWK_BF16 = 0, 1
+HAWK_FP32, HAWK_BF16, HAWK_FP16 = 0, 1, 2
 
 
 class HawkError(RuntimeError):
@@ -42,6 +42,21 @@ class HawkStats(C.Structure):
 
     def as_dict(self):
         return {n: getattr(self, n) for n, _ in self._fields_}
+
+
+class HawkPagedCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("layer_stride", C.c_int64), ("page_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("entry_stride", C.c_int64), ("table", C.c_void_p), ("table_stride", C.c_int64)] + [
+        (n, C.c_int32) for n in ("dtype", "n_layers", "n_pages", "page_size", "n_heads", "head_dim", "n_seq", "max_pages")]
+
+
+class HawkPagedRows(C.Structure):
+    _fields_ = [("row_start", C.c_void_p), ("n_past", C.c_void_p), ("rows", C.c_int32)]
+
+
+class HawkHeads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64), ("n_heads", C.c_int32),
+                ("dtype", C.c_int32)]
 
 
 EXPORTS = {
@@ -98,6 +113,18 @@ EXPORTS = {
                                  C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
     "hawk_sample_rows": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_float, C.c_int,
                                    C.c_void_p, C.c_void_p]),
+    "hawk_rotary_table": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_double, C.c_void_p]),
+    "hawk_paged_append": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                    C.c_float, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "hawk_paged_attention_workspace_bytes": (C.c_size_t, [C.c_void_p, C.c_int, C.c_int, C.c_int]),
+    "hawk_paged_attention": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float, C.c_int, C.c_void_p,
+                                       C.c_void_p, C.c_size_t, C.c_void_p]),
+    "hawk_paged_keep": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p]),
+    "hawk_paged_entry": (C.c_int64, [C.c_void_p, C.c_void_p, C.c_int, C.c_int64]),
+    "hawk_verify_chains_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int]),
+    "hawk_verify_chains": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p,
+                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_float, C.c_int,
+                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "hawk_generate_spatial_workspace_bytes": (C.c_size_t, [C.c_void_p, C.c_int, C.c_int, C.c_int]),
     "hawk_generate_spatial": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_float, C.c_int, C.c_void_p,
                                         C.c_void_p, C.c_int, C.c_int, C.c_uint64, C.c_void_p, C.c_size_t, C.c_void_p,
@@ -211,6 +238,16 @@ def tree_layout(m_depth):
     return parent[:n], depth[:n], cand[:n], anc[:n]
 
 
+def _int32():
+    import torch
+    return torch.int32
+
+
+def _float32():
+    import torch
+    return torch.float32
+
+
 def _stream_of(t):
     import torch  # device memory and stream only
     return torch.cuda.current_stream(t.device).cuda_stream
@@ -313,6 +350,213 @@ def sample_rows(logits, u, temperature: float, top_k: int, skip=None):
     if rc != 0:
         raise HawkError(rc, "hawk_sample_rows")
     return out
+
+_DTYPES = None   # torch dtype -> HAWK_*
+
+
+def _dtype_of(t):
+    global _DTYPES
+    if _DTYPES is None:
+        import torch
+        _DTYPES = {torch.float32: HAWK_FP32, torch.bfloat16: HAWK_BF16, torch.float16: HAWK_FP16}
+    return _DTYPES.get(t.dtype, -1)
+
+
+def _on_device(device, call):
+    """`call` with `device` current: launches go to the current device, whatever stream they are given."""
+    import torch  # device memory and stream only
+    if device.index is None or device.index == torch.cuda.current_device():
+        return call()
+    with torch.cuda.device(device):
+        return call()
+
+
+def rotary_table(n_pos: int, rot_dim: int, theta: float = 10000.0, device: str = "cuda:0"):
+    """hawk_rotary_table: fp32 device tensor [n_pos, rot_dim // 2, 2] of cos and sin of position * theta^(-2 j / rot_dim)."""
+    import torch  # device memory and stream only
+    out = torch.empty((n_pos, rot_dim // 2, 2), dtype=torch.float32, device=device)
+    rc = _on_device(out.device, lambda: load_library().hawk_rotary_table(out.data_ptr(), n_pos, rot_dim, float(theta), _stream_of(out)))
+    if rc != 0:
+        raise HawkError(rc, "hawk_rotary_table")
+    return out
+
+
+class PagedCache:
+    """Keys and values of many sequences in pages (hawk_paged_cache) and the calls on them.
+
+    k, v: device tensors [n_layers, n_pages, n_heads, page_size, head_dim] (or without the first axis) of the same strides,
+    fp32, bf16 or fp16, the last axis contiguous - any other order of the axes is a permuted view.  table [n_seq, max_pages]
+    int32: the pages of every sequence.  The tensors stay the caller's: their contents may change between calls (new pages
+    in the table), and `table` may be replaced by another tensor.
+    Calls launch on torch's current stream of the cache's device.  `row_start` [n_seq + 1] and `n_past` [n_seq] are int32 device
+    tensors: rows row_start[s] .. row_start[s + 1] - 1 of a call belong to sequence s, which has n_past[s] committed entries."""
+
+    def __init__(self, k, v, table):
+        if k.dim() == 4:
+            k, v = k.unsqueeze(0), v.unsqueeze(0)
+        if not (k.is_cuda and v.device == k.device and k.dim() == 5 and v.shape == k.shape and v.dtype == k.dtype
+                and _dtype_of(k) >= 0 and k.stride() == v.stride() and k.stride(4) == 1):
+            raise HawkError(-1, "PagedCache", "k and v must be device tensors [layers, pages, heads, page_size, head_dim] of one type and one layout")
+        self._L = load_library()
+        self.k, self.v = k, v
+        self.device = k.device
+        n_layers, n_pages, n_heads, page_size, head_dim = k.shape
+        sl, sp, sh, se, _ = k.stride()
+        # the stride of an axis of one is not used
+        sp, sh, se = (st if n > 1 else max(st, head_dim) for st, n in ((sp, n_pages), (sh, n_heads), (se, page_size)))
+        self._c = HawkPagedCache(k=k.data_ptr(), v=v.data_ptr(), layer_stride=sl if n_layers > 1 else 0, page_stride=(sp + 7) // 8 * 8 if n_pages == 1 else sp,
+                                 head_stride=(sh + 7) // 8 * 8 if n_heads == 1 else sh,
+                                 entry_stride=(se + 7) // 8 * 8 if page_size == 1 else se, dtype=_dtype_of(k), n_layers=n_layers,
+                                 n_pages=n_pages, page_size=page_size, n_heads=n_heads, head_dim=head_dim)
+        self._ref = C.byref(self._c)
+        self.table = table
+
+    @property
+    def table(self):
+        return self._table
+
+    @table.setter
+    def table(self, t):
+        if not (_dev_ok(t, _int32()) and t.dim() == 2 and t.device == self.device):
+            raise HawkError(-1, "PagedCache", "table must be a contiguous int32 tensor [n_seq, max_pages] on the cache's device")
+        self._table = t
+        self._c.table, self._c.table_stride = t.data_ptr(), max(t.shape[1], 1)
+        self._c.n_seq, self._c.max_pages = t.shape
+
+    def _rows(self, where, rows, row_start, n_past):
+        n, i32 = self._c.n_seq, _int32()
+        if not (row_start.dtype == i32 and n_past.dtype == i32 and row_start.device == self.device and n_past.device == self.device
+                and row_start.shape == (n + 1,) and n_past.shape == (n,) and row_start.is_contiguous() and n_past.is_contiguous()):
+            raise HawkError(-1, where, "row_start [n_seq + 1] and n_past [n_seq] must be contiguous int32 tensors on the cache's device")
+        return HawkPagedRows(row_start.data_ptr(), n_past.data_ptr(), rows)
+
+    def _heads(self, where, t, heads=None):
+        if not (t.dim() == 3 and t.device == self.device and t.shape[2] == self._c.head_dim and (t.stride(2) == 1 or t.numel() == 0)
+                and (heads is None or t.shape[1] == heads) and t.shape[1] > 0 and _dtype_of(t) >= 0):
+            raise HawkError(-1, where, "vectors must be tensors [rows, heads, head_dim] of a supported type on the cache's device, the last axis contiguous")
+        rs, hs = t.stride(0), t.stride(1)
+        return HawkHeads(t.data_ptr(), rs if t.shape[0] > 1 else t.shape[1] * t.shape[2], hs if t.shape[1] > 1 else t.shape[2], t.shape[1], _dtype_of(t))
+
+    def _run(self, where, call):
+        rc = _on_device(self.device, call)
+        if rc != 0:
+            raise HawkError(rc, where)
+
+    def append(self, k, v, row_start, n_past, q=None, rot=None, halves: bool = False, pos=None, q_gain=None, k_gain=None,
+               eps: float = 1e-5, q_out=None, layer: int = 0):
+        """hawk_paged_append: k, v [rows, n_heads, head_dim] become entries of layer `layer`, q [rows, q heads, head_dim] (or None)
+        comes back normalised and rotated in the cache's type (q_out: where, q itself allowed; None: a new tensor, whose
+        rows of no sequence are not written).  rot: a table [n_pos, rot_dim // 2, 2] (rotary_table) or None;
+        halves: pairs (j, j + rot_dim / 2) instead of (2 j, 2 j + 1); pos [rows] int32: positions other than the entries' own;
+        q_gain, k_gain [head_dim] fp32: RMS norm per head with eps."""
+        where, c = "hawk_paged_append", self._c
+        rows = k.shape[0]
+        hk, hv = self._heads(where, k, c.n_heads), self._heads(where, v, c.n_heads)
+        r = self._rows(where, rows, row_start, n_past)
+        hq = hqo = None
+        if q is not None:
+            import torch  # device memory and stream only
+            hq = self._heads(where, q)
+            if q_out is None:
+                q_out = torch.empty(q.shape, dtype=self.k.dtype, device=self.device)
+            hqo = self._heads(where, q_out, q.shape[1])
+            if q_out.shape[0] != rows:
+                raise HawkError(-1, where, "q_out must have q's shape")
+        f32 = _float32()
+        if v.shape[0] != rows or (q is not None and q.shape[0] != rows) or (q is None and q_out is not None):
+            raise HawkError(-1, where, "q, k and v must have the same rows")
+        for g in (q_gain, k_gain):
+            if g is not None and not (_dev_ok(g, f32, (c.head_dim,)) and g.device == self.device):
+                raise HawkError(-1, where, "gains must be fp32 tensors [head_dim] on the cache's device")
+        if rot is not None and not (_dev_ok(rot, f32) and rot.dim() == 3 and rot.shape[2] == 2 and rot.device == self.device):
+            raise HawkError(-1, where, "rot must be a contiguous fp32 tensor [n_pos, rot_dim / 2, 2] on the cache's device")
+        if pos is not None and not (_dev_ok(pos, _int32(), (rows,)) and pos.device == self.device):
+            raise HawkError(-1, where, "pos must be a contiguous int32 tensor [rows] on the cache's device")
+        self._run(where, lambda: self._L.hawk_paged_append(
+            self._ref, layer, C.byref(r), C.byref(hq) if hq is not None else None, C.byref(hk), C.byref(hv),
+            q_gain.data_ptr() if q_gain is not None else None, k_gain.data_ptr() if k_gain is not None else None, float(eps),
+            rot.data_ptr() if rot is not None else None, rot.shape[0] if rot is not None else 0,
+            2 * rot.shape[1] if rot is not None else 0, int(halves), pos.data_ptr() if pos is not None else None,
+            C.byref(hqo) if hqo is not None else None, _stream_of(self.k)))
+        return q_out
+
+    def attend(self, q, row_start, n_past, max_len: int = 0, scale: Optional[float] = None, tree=None, out=None, layer: int = 0):
+        """hawk_paged_attention: q [rows, q heads, head_dim] of the cache's type, the step's entries appended already.  max_len: the
+        longest n_past + rows of a sequence, if the caller knows it (it chooses the kernel, nothing else).  scale None:
+        1 / sqrt(head_dim).  tree [rows] int64: which of the first 64 rows of its sequence a row sees besides itself
+        (hawk_tree_layout's ancestors); None: those up to itself.  out: where the result goes, any of the three types (None: a new tensor of
+        q's type, whose rows of no sequence are not written)."""
+        import torch  # device memory and stream only
+        where, c = "hawk_paged_attention", self._c
+        hq = self._heads(where, q)
+        r = self._rows(where, q.shape[0], row_start, n_past)
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
+        ho = self._heads(where, out, q.shape[1])
+        if out.shape[0] != q.shape[0]:
+            raise HawkError(-1, where, "out must have q's shape")
+        if tree is not None and not (_dev_ok(tree, torch.int64, (q.shape[0],)) and tree.device == self.device):
+            raise HawkError(-1, where, "tree must be a contiguous int64 tensor [rows] on the cache's device")
+        nws = self._L.hawk_paged_attention_workspace_bytes(self._ref, q.shape[0], q.shape[1], max_len)
+        ws = torch.empty(nws, dtype=torch.uint8, device=self.device) if nws else None
+        self._run(where, lambda: self._L.hawk_paged_attention(
+            self._ref, layer, C.byref(r), C.byref(hq), tree.data_ptr() if tree is not None else None,
+            float(scale) if scale is not None else c.head_dim ** -0.5, max_len, C.byref(ho), ws.data_ptr() if nws else None, nws,
+            _stream_of(self.k)))
+        return out
+
+    def keep(self, n_past, path, n_keep):
+        """hawk_paged_keep: the accepted path of a tree step, path [n_seq, depth] int32 of node numbers of which the first n_keep
+        [n_seq] count, goes to the entries behind n_past's, in every layer."""
+        where, i32, n = "hawk_paged_keep", _int32(), self._c.n_seq
+        if not (_dev_ok(path, i32) and path.dim() == 2 and path.shape[0] == n and _dev_ok(n_past, i32, (n,)) and _dev_ok(n_keep, i32, (n,))
+                and path.device == self.device and n_past.device == self.device and n_keep.device == self.device):
+            raise HawkError(-1, where, "path [n_seq, depth], n_past and n_keep [n_seq] must be contiguous int32 tensors on the cache's device")
+        self._run(where, lambda: self._L.hawk_paged_keep(self._ref, n_past.data_ptr(), path.data_ptr(), n_keep.data_ptr(), path.shape[1],
+                                                         _stream_of(self.k)))
+
+    def entry(self, table_row, e: int, layer: int = 0) -> int:
+        """hawk_paged_entry: elements from k's (v's) start to entry e, head 0, of a sequence with the pages table_row (host); -1: none."""
+        t = _i32(table_row)
+        if t.shape != (self._c.max_pages,):
+            raise HawkError(-1, "hawk_paged_entry", "table_row must have max_pages entries")
+        return int(self._L.hawk_paged_entry(self._ref, _p(t), layer, e))
+
+
+def verify_chains(p_logits, q_logits, draft, u_acc, u_final, temperature: float, top_k: int, n_draft=None, p_start=None):
+    """hawk_verify_chains on device tensors: p_logits fp32 [p_rows, n] (rows may be strided), the k + 1 target rows of sequence s
+    from row p_start[s] (int32 [n_seq]; None: s * (k + 1)); q_logits fp32 [n_seq, k, n] (strided) or None (the drafts are
+    certain); draft [n_seq, k] int32; u_acc [n_seq, k], u_final [n_seq] fp32; n_draft None or int32 [n_seq].
+    Returns device tensors (accepted [n_seq], tokens [n_seq, k + 1]) int32."""
+    import torch  # device memory and stream only
+    where = "hawk_verify_chains"
+    n_seq, k = draft.shape
+    dev = p_logits.device
+    small = [(draft, torch.int32, (n_seq, k)), (u_acc, torch.float32, (n_seq, k)), (u_final, torch.float32, (n_seq,))]
+    small += [(t, torch.int32, (n_seq,)) for t in (n_draft, p_start) if t is not None]
+    if not (p_logits.is_cuda and p_logits.dim() == 2 and p_logits.dtype == torch.float32 and p_logits.stride(1) == 1
+            and all(t.device == dev and _dev_ok(t, dt, shape) for t, dt, shape in small)):
+        raise HawkError(-1, where, "arguments must be device tensors of the documented shapes and types")
+    p_rows, n = p_logits.shape
+    if q_logits is not None and not (q_logits.device == dev and q_logits.dtype == torch.float32 and tuple(q_logits.shape) == (n_seq, k, n)
+                                     and (q_logits.stride(2) == 1 or n == 1)):
+        raise HawkError(-1, where, "q_logits must be a device fp32 tensor [n_seq, k, n], the last axis contiguous")
+    if p_start is None and p_rows < n_seq * (k + 1):
+        raise HawkError(-1, where, "p_logits has fewer rows than n_seq * (k + 1)")
+    L = load_library()
+    nws = int(L.hawk_verify_chains_workspace_bytes(n_seq, k, n))
+    ws = torch.empty(max(nws, 16), dtype=torch.uint8, device=dev)
+    count = torch.empty(n_seq, dtype=torch.int32, device=dev)
+    toks = torch.empty((n_seq, k + 1), dtype=torch.int32, device=dev)
+    qs, qr = (0, n) if q_logits is None else (q_logits.stride(0) if n_seq > 1 else 0, q_logits.stride(1) if k > 1 else n)
+    rc = _on_device(dev, lambda: L.hawk_verify_chains(
+        p_logits.data_ptr(), p_logits.stride(0) if p_rows > 1 else n, p_start.data_ptr() if p_start is not None else None, p_rows,
+        q_logits.data_ptr() if q_logits is not None else None, qs, qr, draft.data_ptr(),
+        n_draft.data_ptr() if n_draft is not None else None, u_acc.data_ptr(), u_final.data_ptr(), n_seq, k, n, float(temperature),
+        int(top_k), count.data_ptr(), toks.data_ptr(), ws.data_ptr(), nws, _stream_of(p_logits)))
+    if rc != 0:
+        raise HawkError(rc, where)
+    return count, toks
 
 
 class Hawk:

@@ -1,0 +1,433 @@
+"""The calls over a paged cache against plain float64 arithmetic: appending with norms and rotation, attention of chains and
+trees, moving accepted paths - at lengths, pages, head shapes and masks where they can go wrong.
+
+Tolerances: a value rounded to a type is off by at most half a step, finfo(type).eps / 2 of it.  fp32 arithmetic of n terms
+is off by n 2^-24 of the terms' absolute sum at most; how much that is in a score or a weight is computed from the inputs."""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def H():
+    import torch
+    import paper_2510_25739_amd as H
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    return H
+
+
+def dt(name):
+    import torch
+    return {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}[name]
+
+
+def half_step(name):
+    import torch
+    return torch.finfo(dt(name)).eps / 2
+
+
+class Setup:
+    """A pool whose entries outside the sequences hold NaN, a scattered table, and the sequences' rows."""
+
+    def __init__(self, H, seed, cache, kv_heads, hd, page, rows, past, layers=1, order="heads", spare=0, extra=0):
+        import torch
+        self.g = torch.Generator().manual_seed(seed)
+        self.rows, self.past, self.page, self.hk, self.hd, self.cache_t = list(rows), list(past), page, kv_heads, hd, cache
+        per = [-(-(max(p, 0) + n + extra) // page) for p, n in zip(past, rows)]
+        self.n_pages = sum(per) + 2
+        perm = torch.randperm(self.n_pages, generator=self.g).tolist()
+        cols = max(per + [1]) + spare
+        table = np.full((len(rows), cols), -1, dtype=np.int32)      # places without a page
+        at = 0
+        for s, n in enumerate(per):
+            table[s, :n] = perm[at:at + n]
+            at += n
+        self.table_np = table
+        shape = {"heads": (layers, self.n_pages, kv_heads, page, hd), "entries": (layers, self.n_pages, page, kv_heads, hd)}[order]
+        self.order = order
+        def pool():
+            t = torch.full(shape, float("nan"), dtype=dt(cache), device=DEV)
+            return t if order == "heads" else t.permute(0, 1, 3, 2, 4)
+        self.k, self.v = pool(), pool()
+        self.table = torch.from_numpy(table).to(DEV)
+        start = np.concatenate([[0], np.cumsum(rows)]).astype(np.int32)
+        self.start_np = start
+        self.total = int(start[-1])
+        self.row_start = torch.from_numpy(start).to(DEV)
+        self.n_past = torch.tensor(past, dtype=torch.int32, device=DEV)
+        self.cache = H.PagedCache(self.k, self.v, self.table)
+
+    def randn(self, *shape, scale=1.0, t=None):
+        import torch
+        x = torch.randn(*shape, generator=self.g) * scale
+        return x.to(dt(t or self.cache_t))
+
+    def where(self, s, e):
+        return int(self.table_np[s, e // self.page]), e % self.page
+
+    def fill(self, layer=0, scale=1.0):
+        """Entries of every sequence (committed and the step's) in float64, and into the pool."""
+        self.K, self.V = [], []
+        for s, (n, p) in enumerate(zip(self.rows, self.past)):
+            L = p + n
+            k, v = self.randn(L, self.hk, self.hd, scale=scale), self.randn(L, self.hk, self.hd)
+            for e in range(L):
+                pg, sl = self.where(s, e)
+                if pg >= 0:
+                    self.k[layer, pg, :, sl], self.v[layer, pg, :, sl] = k[e].to(DEV), v[e].to(DEV)
+            self.K.append(k.double())
+            self.V.append(v.double())
+
+
+def attention_reference(su, q, seen, scale):
+    """out, and per element sum_e p |v| and the largest error of a score that fp32 sums can make; seen(s, i, e)."""
+    import torch
+    total, heads, hd = q.shape
+    q = q.double()
+    out, mag, err = torch.zeros(q.shape, dtype=torch.float64), torch.zeros(q.shape, dtype=torch.float64), torch.zeros(total, heads, 1, dtype=torch.float64)
+    group = heads // su.hk
+    for s in range(len(su.rows)):
+        for i in range(su.rows[s]):
+            r = int(su.start_np[s]) + i
+            es = [e for e in range(su.past[s] + su.rows[s]) if seen(s, i, e) and su.where(s, e)[0] >= 0]
+            if not es:
+                continue
+            k, v = su.K[s][es], su.V[s][es]
+            for h in range(heads):
+                z = (k[:, h // group] @ q[r, h]) * scale
+                w = torch.exp(z - z.max())
+                w = w / w.sum()
+                out[r, h] = w @ v[:, h // group]
+                mag[r, h] = w @ v[:, h // group].abs()
+                # hd products and their sum, the scale and its product with log2(e), the difference to the maximum
+                err[r, h] = ((hd + 6) * 2.0 ** -24 * (k[:, h // group].abs() @ q[r, h].abs()) * scale).max()
+    return out, mag, err
+
+
+def check_attention(su, got, want, out_type, weight_step, note=""):
+    out, mag, err = want
+    n = max(p + r for p, r in zip(su.past, su.rows)) + 64
+    # weights: both their numerator and their sum by the scores' error, the exponential (2^-21), the sums of n terms, and
+    # the rounding of the weights before the product
+    tol = half_step(out_type) * out.abs() + mag * (2 * err + 2.0 ** -21 + 2 * n * 2.0 ** -24 + weight_step) * 1.01 + 1e-30
+    if out_type == "fp16":
+        tol = tol + 2.0 ** -25
+    d = (got.double().cpu() - out).abs()
+    worst = float((d / tol).max()) if d.numel() else 0.0
+    print(f"{note} largest error / tolerance {worst:.3f}")
+    assert not bool(d.isnan().any()) and worst <= 1.0
+
+
+def weight_step(cache):
+    return {"fp32": 0.0, "bf16": 2.0 ** -16, "fp16": 2.0 ** -20}[cache]   # two roundings: 2^-8 squared, 2^-11 squared
+
+
+ATTEND = [
+    # cache, heads, kv_heads, hd, page, rows, past
+    ("fp32", 4, 4, 64, 16, [1], [0]),                      # a sequence's first token
+    ("bf16", 4, 4, 64, 16, [1], [15]),                     # the last place of a page
+    ("fp16", 4, 4, 64, 16, [1], [16]),                     # the first place of a page
+    ("fp16", 6, 6, 64, 16, [6, 6, 6], [0, 31, 100]),       # steps; nothing committed
+    ("bf16", 8, 2, 128, 32, [1, 3, 0, 5], [130, 0, 77, 64]),   # shared heads, a sequence without rows
+    ("bf16", 12, 1, 64, 24, [7, 2], [50, 3]),              # one cache head, pages no power of two
+    ("fp32", 6, 2, 96, 5, [3, 17, 1], [11, 40, 0]),        # pages that end inside groups of four, padded features
+    ("fp16", 3, 3, 80, 1, [2, 5], [9, 33]),                # one entry a page
+    ("bf16", 2, 2, 8, 7, [4], [13]),                       # the fewest features
+    ("fp16", 5, 5, 40, 12, [1, 1], [70, 1]),
+    ("bf16", 2, 1, 256, 16, [5, 1], [20, 90]),
+    ("fp32", 2, 2, 256, 16, [4], [60]),
+    ("fp16", 3, 1, 200, 8, [9], [14]),
+    ("fp32", 4, 4, 32, 64, [33], [0]),                     # a prompt
+    ("bf16", 4, 2, 64, 16, [70, 1, 40], [0, 200, 33]),     # pieces of prompts and a token
+    ("fp16", 8, 8, 128, 64, [50], [77]),
+    ("bf16", 16, 4, 128, 16, [1], [1500]),                 # a long axis
+    ("fp16", 4, 1, 64, 16, [2, 1], [1100, 2300]),          # parts of different numbers
+]
+
+
+@pytest.mark.parametrize("order", ["heads", "entries"])
+@pytest.mark.parametrize("cache,heads,kv_heads,hd,page,rows,past", ATTEND)
+def test_chains_attend(H, cache, heads, kv_heads, hd, page, rows, past, order):
+    import torch
+    su = Setup(H, hd * 7 + page + sum(rows), cache, kv_heads, hd, page, rows, past, order=order)
+    su.fill()
+    q = su.randn(su.total, heads, hd)
+    got = su.cache.attend(q.to(DEV), su.row_start, su.n_past, max_len=max(p + n for p, n in zip(past, rows)))
+    want = attention_reference(su, q, lambda s, i, e: e <= past[s] + i, hd ** -0.5)
+    check_attention(su, got, want, cache, weight_step(cache))
+    # the hint chooses the kernel, not the result's meaning; another type of result
+    got = su.cache.attend(q.to(DEV), su.row_start, su.n_past, out=torch.empty(q.shape, dtype=torch.float32, device=DEV))
+    check_attention(su, got, want, "fp32", weight_step(cache))
+    got = su.cache.attend(q.to(DEV), su.row_start, su.n_past, max_len=1, out=torch.empty(q.shape, dtype=torch.float32, device=DEV))
+    check_attention(su, got, want, "fp32", weight_step(cache))
+
+
+@pytest.mark.parametrize("cache,heads,kv_heads,hd,page,past,trees", [
+    ("bf16", 4, 2, 64, 16, [40, 0], [(3, 3), (2, 2, 1)]),
+    ("fp16", 2, 2, 128, 8, [100], [(5, 2)]),
+    ("fp32", 3, 3, 48, 6, [7, 30], [(1, 1, 1, 1), (63,)]),
+    ("bf16", 8, 1, 128, 32, [1200], [(4, 3)]),
+])
+def test_trees_attend(H, cache, heads, kv_heads, hd, page, past, trees):
+    import torch
+    layout = [H.tree_layout(t) for t in trees]
+    rows = [len(l[0]) for l in layout]
+    su = Setup(H, hd + page, cache, kv_heads, hd, page, rows, past)
+    su.fill()
+    anc = np.concatenate([l[3] for l in layout])
+    q = su.randn(su.total, heads, hd)
+    tree = torch.from_numpy(anc.view(np.int64)).to(DEV)
+
+    def seen(s, i, e):
+        return e < past[s] or e == past[s] + i or bool((int(anc[su.start_np[s] + i]) >> (e - past[s])) & 1)
+
+    got = su.cache.attend(q.to(DEV), su.row_start, su.n_past, tree=tree)
+    check_attention(su, got, attention_reference(su, q, seen, hd ** -0.5), cache, weight_step(cache))
+
+
+def test_a_row_that_sees_nothing_gives_zeros(H):
+    # a first node whose entry has no page, and nothing committed; its neighbours see their own
+    import torch
+    su = Setup(H, 2, "bf16", 2, 64, 1, [3, 2], [0, 0])
+    su.fill()
+    q = su.randn(5, 4, 64)
+    su.table_np[0, 0] = su.table_np[1, 1] = -1
+    su.table.copy_(torch.from_numpy(su.table_np))
+    tree = torch.zeros(5, dtype=torch.int64, device=DEV)
+    got = su.cache.attend(q.to(DEV), su.row_start, su.n_past, tree=tree)
+    check_attention(su, got, attention_reference(su, q, lambda s, i, e: e == i, 0.125), "bf16", weight_step("bf16"))
+    assert bool((got[[0, 4]] == 0).all()) and not bool((got[[1, 2, 3]] == 0).any())
+
+
+def test_tree_rows_past_the_sixty_fourth_see_the_first_sixty_four(H):
+    import torch
+    past, n = 10, 80
+    su = Setup(H, 3, "fp16", 2, 64, 16, [n], [past])
+    su.fill()
+    q = su.randn(n, 2, 64)
+    anc = np.array([(0x9E3779B97F4A7C15 * (i + 1)) & 0xFFFFFFFFFFFFFFFF for i in range(n)], dtype=np.uint64)
+    got = su.cache.attend(q.to(DEV), su.row_start, su.n_past, tree=torch.from_numpy(anc.view(np.int64)).to(DEV))
+    want = attention_reference(su, q, lambda s, i, e: e < past or e == past + i or (e - past < 64 and bool((int(anc[i]) >> (e - past)) & 1)), 64 ** -0.5)
+    check_attention(su, got, want, "fp16", weight_step("fp16"))
+
+
+@pytest.mark.parametrize("cache", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("page", [4, 16, 6])
+def test_values_a_row_does_not_see_have_no_part(H, cache, page):
+    # infinities and NaN in later rows' keys and values: rows before them are as if they were ordinary, rows that see one
+    # get what the formula gives
+    import torch
+    past, n, hd = 37, 9, 64
+    su = Setup(H, 5, cache, 2, hd, page, [n], [past])
+    su.fill()
+    q = su.randn(n, 4, hd)
+    want = attention_reference(su, q, lambda s, i, e: e <= past + i, hd ** -0.5)
+    bad = [(past + 4, 0, 3, float("inf")), (past + 6, 1, 60, float("nan")), (past + 7, 0, 17, float("-inf"))]
+    for e, h, f, x in bad:
+        pg, sl = su.where(0, e)
+        su.v[0, pg, h, sl, f] = x
+    pg, sl = su.where(0, past + 8)
+    su.k[0, pg, 1, sl] = float("nan")
+    out = su.cache.attend(q.to(DEV), su.row_start, su.n_past).double().cpu()
+    clean = torch.ones(n, 4, hd, dtype=torch.bool)
+    for e, h, f, x in bad:
+        clean[e - past:, 2 * h:2 * h + 2, f] = False
+        for i in range(e - past, n if h == 0 else 8):
+            got = out[i, 2 * h:2 * h + 2, f]
+            assert bool(got.isnan().all() if math.isnan(x) else (got == x).all()), (e, i, got)
+    clean[8, 2:] = False
+    assert bool(out[8, 2:].isnan().all())
+    o, m, er = want
+    keep = lambda t: torch.where(clean, t, torch.zeros((), dtype=torch.float64))
+    check_attention(su, keep(out), (keep(o), m, er), cache, weight_step(cache))
+
+
+def test_entries_without_a_page_are_not_attended(H):
+    import torch
+    past, n, hd = 90, 3, 64
+    su = Setup(H, 8, "bf16", 2, hd, 8, [n, n], [past, past], spare=3)
+    su.table_np[0, 2] = -1
+    su.table_np[1, 5] = su.n_pages          # behind the pool
+    su.table_np[1, 0] = 2 ** 31 - 1
+    su.table.copy_(torch.from_numpy(su.table_np))
+    su.table_np[1, 5] = su.table_np[1, 0] = -1     # for the reference
+    su.fill()
+    q = su.randn(2 * n, 2, hd)
+    got = su.cache.attend(q.to(DEV), su.row_start, su.n_past)
+    check_attention(su, got, attention_reference(su, q, lambda s, i, e: e <= past + i, hd ** -0.5), "bf16", weight_step("bf16"))
+    # lengths beyond the table: what exists is attended, rows whose own entry does not exist among them
+    su.n_past.fill_(2 ** 31 - 5)
+    got2 = su.cache.attend(q.to(DEV), su.row_start, su.n_past)
+    su.past = [su.table_np.shape[1] * 8 - n] * 2
+    su.K = [torch.cat([k, torch.zeros(su.past[0] + n - len(k), 2, hd, dtype=torch.float64)]) for k in su.K]
+    su.V = [torch.cat([k, torch.zeros(su.past[0] + n - len(k), 2, hd, dtype=torch.float64)]) for k in su.V]
+    last_page = -(-(past + n) // 8) * 8
+    su.k.nan_to_num_(0.0)
+    su.v.nan_to_num_(0.0)
+    got2 = su.cache.attend(q.to(DEV), su.row_start, su.n_past)
+    check_attention(su, got2, attention_reference(su, q, lambda s, i, e: e < last_page, hd ** -0.5), "bf16", weight_step("bf16"))
+    su.n_past.fill_(-1000)                  # nothing committed, no entry of the step's own
+    assert bool((su.cache.attend(q.to(DEV), su.row_start, su.n_past) == 0).all())
+
+
+def test_rows_of_no_sequence_and_other_rows_of_the_output_stay(H):
+    import torch
+    su = Setup(H, 9, "fp16", 2, 64, 16, [2, 0, 3], [20, 5, 700])
+    su.fill()
+    q = su.randn(su.total + 4, 2, 64)
+    out = torch.full((su.total + 4, 5, 64), 7.0, dtype=torch.float16, device=DEV)
+    su.cache.attend(q.to(DEV), su.row_start, su.n_past, out=out[:, 1:3])
+    want = attention_reference(su, q[:su.total], lambda s, i, e: e <= su.past[s] + i, 0.125)
+    check_attention(su, out[:su.total, 1:3], want, "fp16", weight_step("fp16"))
+    assert bool((out[su.total:] == 7).all()) and bool((out[:, 0] == 7).all()) and bool((out[:, 3:] == 7).all())
+
+
+def test_large_scores(H):
+    # scores of hundreds: the maximum moves from turn to turn, weights underflow
+    import torch
+    su = Setup(H, 10, "bf16", 2, 64, 16, [4], [300])
+    su.fill(scale=20.0)
+    q = su.randn(4, 2, 64, scale=4.0)
+    got = su.cache.attend(q.to(DEV), su.row_start, su.n_past, scale=0.25, out=torch.empty(4, 2, 64, device=DEV))
+    check_attention(su, got, attention_reference(su, q, lambda s, i, e: e <= 300 + i, 0.25), "fp32", weight_step("bf16"))
+
+
+def rotated_reference(x, gain, eps, table, rot, halves):
+    """float64, and the absolute sum of the two terms of every element"""
+    import torch
+    y = x.double()
+    if gain is not None:
+        y = y / torch.sqrt((y * y).mean(-1, keepdim=True) + eps) * gain.double()
+    mag = y.abs().clone()
+    if rot:
+        j = torch.arange(rot // 2)
+        a, b = (j, j + rot // 2) if halves else (2 * j, 2 * j + 1)
+        c, s = table[:, None, :, 0].double(), table[:, None, :, 1].double()
+        u, w = y[..., a].clone(), y[..., b].clone()
+        y[..., a], y[..., b] = u * c - w * s, u * s + w * c
+        mag[..., a], mag[..., b] = (u * c).abs() + (w * s).abs(), (u * s).abs() + (w * c).abs()
+    return y, mag
+
+
+APPEND = [
+    # x, cache, heads, kv_heads, hd, page, rows, past, rot, halves, norm
+    ("fp32", "fp32", 4, 4, 64, 16, [1], [0], 64, False, False),
+    ("bf16", "fp16", 6, 2, 64, 16, [3, 0, 5], [15, 9, 130], 64, True, True),
+    ("bf16", "bf16", 32, 8, 128, 32, [6, 6], [40, 0], 128, True, False),
+    ("fp16", "fp16", 5, 5, 80, 24, [2, 9], [23, 70], 40, True, True),
+    ("fp32", "bf16", 3, 1, 40, 7, [4], [12], 24, True, True),        # partners in pieces of four
+    ("fp32", "fp16", 2, 2, 256, 5, [7], [1], 128, False, True),
+    ("fp16", "fp32", 2, 2, 8, 1, [3], [4], 8, True, False),
+    ("bf16", "fp32", 7, 7, 96, 16, [1, 1, 1], [3, 4, 5], 0, False, True),
+    ("fp32", "fp16", 2, 1, 72, 16, [2], [3], 72, True, False),
+]
+
+
+@pytest.mark.parametrize("order", ["heads", "entries"])
+@pytest.mark.parametrize("x,cache,heads,kv_heads,hd,page,rows,past,rot,halves,norm", APPEND)
+def test_append(H, x, cache, heads, kv_heads, hd, page, rows, past, rot, halves, norm, order):
+    import torch
+    su = Setup(H, hd + page, cache, kv_heads, hd, page, rows, past, layers=2, order=order)
+    su.k.fill_(3.0)
+    su.v.fill_(4.0)
+    total, pad = su.total, 2
+    qkv = su.randn(total + pad, heads + 2 * kv_heads, hd, t=x)     # the columns of one projection
+    g = qkv.to(DEV)
+    q, k, v = g[:, :heads], g[:, heads:heads + kv_heads], g[:, heads + kv_heads:]
+    n_pos = max(p + n for p, n in zip(past, rows)) + 1
+    table = H.rotary_table(n_pos, rot, 10000.0) if rot else None
+    gains = [(1 + 0.3 * torch.randn(hd, generator=su.g)) for _ in range(2)] if norm else [None, None]
+    q_out = torch.full((total + pad, heads, hd), 9.0, dtype=dt(cache), device=DEV)
+    su.cache.append(k, v, su.row_start, su.n_past, q=q, rot=table, halves=halves, q_gain=None if not norm else gains[0].to(DEV),
+                    k_gain=None if not norm else gains[1].to(DEV), eps=1e-5, q_out=q_out, layer=1)
+    pos = torch.tensor([p + i for p, n in zip(past, rows) for i in range(n)])
+    tab = table.cpu()[pos] if rot else None
+    want_k, want_v = torch.full(su.k.shape, 3.0, dtype=torch.float64), torch.full(su.v.shape, 4.0, dtype=torch.float64)
+    qr, qm = rotated_reference(qkv[:total, :heads], gains[0], 1e-5, tab, rot, halves)
+    kr, km = rotated_reference(qkv[:total, heads:heads + kv_heads], gains[1], 1e-5, tab, rot, halves)
+    mag_k = torch.zeros_like(want_k)
+    r = 0
+    for s, (n, p) in enumerate(zip(rows, past)):
+        for i in range(n):
+            pg, sl = su.where(s, p + i)
+            want_k[1, pg, :, sl], mag_k[1, pg, :, sl], want_v[1, pg, :, sl] = kr[r], km[r], qkv[r, heads + kv_heads:].double()
+            r += 1
+    # the norm (hd + 4 roundings, half of the sum's error through the root), its two products, the rotation's three
+    rel = ((hd + 4) / 2 + 6 if norm else 3) * 2.0 ** -24
+    tiny = 2.0 ** -25 if cache == "fp16" else 1e-30
+    for got, ref, mag in ((q_out[:total].cpu().double(), qr, qm), (su.k.cpu().double(), want_k, mag_k)):
+        assert float(((got - ref).abs() / (half_step(cache) * ref.abs() + 1.01 * rel * mag + tiny)).max()) <= 1.0
+    assert torch.equal(su.v.cpu(), want_v.to(dt(cache)))
+    assert bool((q_out[total:] == 9).all())
+
+
+def test_append_in_place_and_positions_of_its_own(H):
+    import torch
+    su = Setup(H, 21, "bf16", 2, 128, 16, [3, 2], [10, 0])
+    x = su.randn(5, 6, 128)
+    k, v = su.randn(5, 2, 128), su.randn(5, 2, 128)
+    table = H.rotary_table(50, 128)
+    pos = torch.tensor([3, 3, 49, 0, 7], dtype=torch.int32)
+    a = x.to(DEV)
+    b = su.cache.append(k.to(DEV), v.to(DEV), su.row_start, su.n_past, q=a, rot=table, halves=True, pos=pos.to(DEV))
+    a2 = a.clone()
+    same = su.cache.append(k.to(DEV), v.to(DEV), su.row_start, su.n_past, q=a2, rot=table, halves=True, pos=pos.to(DEV), q_out=a2)
+    assert same is a2 and torch.equal(a2, b)
+    ref, mag = rotated_reference(x, None, 0, table.cpu()[pos.long()], 128, True)
+    assert float(((b.cpu().double() - ref).abs() / (half_step("bf16") * ref.abs() + 1.01 * 3 * 2.0 ** -24 * mag + 1e-30)).max()) <= 1.0
+    # a position outside the table leaves its row out altogether
+    su.k.fill_(1.0)
+    pos[1] = 50
+    pos[4] = -1
+    out = torch.full_like(b, 5.0)
+    su.cache.append(k.to(DEV), v.to(DEV), su.row_start, su.n_past, q=a, rot=table, halves=True, pos=pos.to(DEV), q_out=out)
+    assert torch.equal(out[[0, 2, 3]], b[[0, 2, 3]]) and bool((out[[1, 4]] == 5).all())
+    written = [su.where(0, 10), su.where(0, 12), su.where(1, 0)]
+    left = [su.where(0, 11), su.where(1, 1)]
+    assert all(not bool((su.k[0, p, :, e] == 1).all()) for p, e in written) and all(bool((su.k[0, p, :, e] == 1).all()) for p, e in left)
+
+
+def test_append_where_entries_do_not_exist_writes_the_queries_only(H):
+    import torch
+    su = Setup(H, 22, "fp16", 2, 64, 4, [4, 3], [2, 1])
+    su.k.fill_(1.0)
+    su.v.fill_(1.0)
+    su.table.fill_(su.n_pages)
+    k = su.randn(7, 2, 64).to(DEV)
+    for past in (su.n_past.clone(), torch.full_like(su.n_past, 2 ** 31 - 3), torch.full_like(su.n_past, -(2 ** 31))):
+        out = su.cache.append(k, k, su.row_start, past, q=k)
+        assert torch.equal(out, k) and bool((su.k == 1).all()) and bool((su.v == 1).all())
+
+
+@pytest.mark.parametrize("cache,hd,page,layers,heads", [("bf16", 64, 16, 3, 5), ("fp32", 256, 3, 2, 2), ("fp16", 8, 1, 1, 1), ("fp32", 72, 8, 2, 3)])
+@pytest.mark.parametrize("depth", [1, 3, 9, 64])
+def test_keep(H, cache, hd, page, layers, heads, depth):
+    import torch
+    past = [0, 13, 40, 7]
+    su = Setup(H, depth + hd, cache, heads, hd, page, [0] * 4, past, layers=layers, extra=2 * depth + 8)
+    su.k.copy_(su.randn(*su.k.shape))
+    su.v.copy_(su.randn(*su.v.shape))
+    rng = np.random.RandomState(depth)
+    path = np.sort(np.stack([rng.choice(2 * depth + 4, depth, replace=False) + 1 for _ in past]), axis=1).astype(np.int32)
+    keep = np.array([depth, 0, depth + 5, -3], dtype=np.int32)
+    keep[1] = rng.randint(0, depth + 1)
+    path[2, 0] = -5                                   # never on a path: skipped
+    if depth > 2:
+        path[2, 1] = 2 ** 31 - 1
+        path[0, 1] = path[0, 2]                       # one node twice
+    wk, wv = su.k.clone(), su.v.clone()
+    for s, p in enumerate(past):
+        for j in range(min(max(int(keep[s]), 0), depth)):
+            if path[s, j] < j + 1 or p + int(path[s, j]) >= su.table_np.shape[1] * page:
+                continue
+            (a, b), (c, d) = su.where(s, p + int(path[s, j])), su.where(s, p + j + 1)
+            if a < 0 or c < 0:
+                continue
+            wk[:, c, :, d], wv[:, c, :, d] = wk[:, a, :, b].clone(), wv[:, a, :, b].clone()
+    su.cache.keep(su.n_past, torch.from_numpy(path).to(DEV), torch.from_numpy(keep).to(DEV))
+    assert torch.equal(su.k.view(torch.uint8), wk.view(torch.uint8)) and torch.equal(su.v.view(torch.uint8), wv.view(torch.uint8))
