@@ -124,6 +124,10 @@ __device__ __forceinline__ void load8(const char* base, int64_t at, int dtype, f
         for (int i = 0; i < 4; ++i) widen2(w[i], dtype, x[2 * i], x[2 * i + 1]);
     }
 }
+__device__ __forceinline__ void store4(char* base, int64_t at, int dtype, const float* x) {
+    if (dtype == HAWK_FP32) *reinterpret_cast<float4*>(base + at * 4) = make_float4(x[0], x[1], x[2], x[3]);
+    else *reinterpret_cast<v2u*>(base + at * 2) = (v2u){narrow2(x[0], x[1], dtype), narrow2(x[2], x[3], dtype)};
+}
 __device__ __forceinline__ void store8(char* base, int64_t at, int dtype, const float* x) {
     if (dtype == HAWK_FP32) {
         float4* d = reinterpret_cast<float4*>(base + at * 4);

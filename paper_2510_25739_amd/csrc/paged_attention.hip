@@ -13,11 +13,11 @@ namespace hawk {
 namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 
-constexpr int kTile = 16;      // rows of a tile
-constexpr int kKeys = 32;      // entries of one turn of a wave
+constexpr int kTile = 16, kWide = 128;   // rows of a tile where a sequence has few, many
 
 struct AttnArgs {
     PagedView c;
@@ -25,27 +25,28 @@ struct AttnArgs {
     HeadsView q, out;
     const uint64_t* tree;
     float scale2;              // scale * log2(e)
-    int group, tiles;          // query heads of a cache head; tiles of the launch
+    int group, tile, tiles;    // query heads of a cache head; rows of a tile, tiles of the launch
     int splits, split_keys;    // parts of a long axis, entries of a part (the last one has the rest)
     float *part, *part_ml;     // [split][row][head][hd], [split][row][head][2]
 };
 
 // Which entries the rows of a tile are about.
 struct Span {
-    int s, r0, n;              // sequence, its first row, its rows
+    int s, first;              // sequence; the tile's first row * group + head
+    int r0, n;                 // the sequence's first row, its rows
     int past;                  // committed entries (clamped to what an entry number can be)
-    int end;                   // entries behind this one are seen by no row of the tile
+    int end;                   // entries from this one on are seen by no row of the tile
     int all;                   // entries before this one are seen by every row of the tile
 };
-__device__ __forceinline__ Span span_of(const AttnArgs& a, int s, int first) {   // first: the tile's first row * group + head
+__device__ __forceinline__ Span span_of(const AttnArgs& a, int s, int first, int start, int stop, int past) {
     Span t;
     t.s = s;
-    const int b = min(max(a.r.row_start[s], 0), a.r.rows), e = min(max(a.r.row_start[s + 1], 0), a.r.rows);
-    t.r0 = b;
-    t.n = max(e - b, 0);
-    t.past = min(max(a.r.n_past[s], -(1 << 30)), 1 << 30);
+    t.first = first;
+    t.r0 = min(max(start, 0), a.r.rows);
+    t.n = max(min(max(stop, 0), a.r.rows) - t.r0, 0);
+    t.past = min(max(past, -(1 << 30)), 1 << 30);
     const int cap = a.c.max_pages * a.c.page_size;
-    const int lo = first / a.group, hi = min((first + kTile - 1) / a.group, t.n - 1);
+    const int lo = first / a.group, hi = min((first + a.tile - 1) / a.group, t.n - 1);
     if (a.tree) {
         t.end = t.past + max(min(t.n, 64), hi + 1);
         t.all = t.past;
@@ -56,11 +57,40 @@ __device__ __forceinline__ Span span_of(const AttnArgs& a, int s, int first) {  
     t.end = max(min(t.end, cap), 0);
     return t;
 }
-// Tiles are counted so that a sequence's first tile follows from its first row alone: base(s) = row_start[s] * group / 16 + s,
+// Tiles are counted so that a sequence's first tile follows from its first row alone: base(s) = row_start[s] * group / tile + s,
 // which leaves every sequence room for its tiles and at most one unused number per sequence.
-__device__ __forceinline__ int tile_base(const AttnArgs& a, int s) {
-    const int64_t b = min(max(a.r.row_start[s], 0), a.r.rows);
-    return (int)(b * a.group / kTile) + s;
+__device__ __forceinline__ int tile_base(const AttnArgs& a, int s, int start) {
+    const int64_t b = min(max(start, 0), a.r.rows);
+    return (int)(b * a.group / a.tile) + s;
+}
+// The sequence of a tile and its span; false: the tile is one of the unused numbers.  Up to 64 sequences every lane has one
+// sequence's words, and the answer is there after one latency.
+__device__ __forceinline__ bool find_tile(const AttnArgs& a, int lane, int tile, Span& t) {
+    int s, start, stop, past;
+    if (a.c.n_seq <= 64) {
+        const int i = min(lane, a.c.n_seq - 1);
+        const int b = a.r.row_start[i], e = a.r.row_start[i + 1], p = a.r.n_past[i];
+        const int c = __popcll(__ballot(lane < a.c.n_seq && tile_base(a, i, b) <= tile));
+        if (c == 0) return false;
+        s = c - 1;
+        start = __builtin_amdgcn_readlane(b, s);
+        stop = __builtin_amdgcn_readlane(e, s);
+        past = __builtin_amdgcn_readlane(p, s);
+    } else {
+        s = __builtin_amdgcn_readfirstlane(last_not_above(a.c.n_seq, lane, tile, [&](int i) { return (int64_t)tile_base(a, i, a.r.row_start[i]); }));
+        if (s < 0) return false;
+        start = a.r.row_start[s];
+        stop = a.r.row_start[s + 1];
+        past = a.r.n_past[s];
+    }
+    t = span_of(a, s, (tile - tile_base(a, s, start)) * a.tile, start, stop, past);
+    return t.first < t.n * a.group;
+}
+// (Without branches a lane: with them a row's score of an entry that it does not see was once left as it was.)
+__device__ __forceinline__ bool sees(const AttnArgs& a, const Span& t, int own, unsigned long long bits, int e) {
+    const int j = e - t.past;
+    const bool chain = e <= own, node = (int)(j < 0) | (int)(e == own) | ((int)(j < 64) & (int)((bits >> (j & 63)) & 1ull));
+    return a.tree ? node : chain;
 }
 __device__ __forceinline__ int used_splits(const AttnArgs& a, int end) {
     return min(a.splits, max(1, (end + a.split_keys - 1) / a.split_keys));
@@ -119,32 +149,56 @@ template <> struct Of<HAWK_FP32> {
     static __device__ __forceinline__ unsigned clear(unsigned w) { return odd(w) ? 0u : w; }
 };
 
-// Tile of 16 rows, NW waves that share the entries of its part in turns of 32.  Keys and values go from the pages straight into the
-// operands' registers: a lane's 16 bytes of a key are its features of one product, and its piece of eight keys' values
-// - the same few features of each - become the transposed operand by pairing words of two keys.
+// Infinities and NaN among the values of entries that only some rows of a tile see would make NaN of the others' weights of zero:
+// they are zeros in the products, and come to the rows that see them at the end: N features from f on of a row's result.
+template <int TYPE, int N>
+__device__ void add_odd(const AttnArgs& a, const Span& t, const char* vh, int own, unsigned long long bits, int from, int to, int f, float* x) {
+    const int32_t* pages = a.c.table + (int64_t)t.s * a.c.table_stride;
+    for (int e = max(from, 0); e < to; ++e) {
+        const int64_t at = entry_at(a.c, pages, e);
+        if (at < 0 || !sees(a, t, own, bits, e)) continue;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            float v;
+            if constexpr (TYPE == HAWK_FP32) v = *reinterpret_cast<const float*>(vh + (at + f + j) * 4);
+            else v = Of<TYPE>::widen(*reinterpret_cast<const unsigned short*>(vh + (at + f + j) * 2));
+            if (!(fabsf(v) <= 3.4028235e38f)) x[j] += v;
+        }
+    }
+}
+
+// Tile of 16 rows, NW waves that share the entries of its part in turns of 32 (16 of fp32).  Keys and values go from the pages straight
+// into the operands' registers: a lane's 16 bytes of a key are its features of one product, and its piece of eight keys' values
+// - the same few features of each - become the transposed operand by pairing words of two keys.  A turn's keys are requested as soon
+// as the turn before has used its own, its values likewise.
 template <int TYPE, int DP, bool PAD, int NW>
-__global__ __launch_bounds__(64 * NW) void paged_rows_kernel(AttnArgs a) {
+__global__ __launch_bounds__(64 * NW, DP <= 128 ? 8 / NW : 1) void paged_rows_kernel(AttnArgs a) {
     using T = Of<TYPE>;
     constexpr int ES = T::kBytes, VEC = 16 / ES, STEP = 4 * VEC, NS = DP / STEP;   // features of a lane's piece, of a product; products
     constexpr int VD = DP / 16, VC = VD < VEC ? VD : VEC, NC = VD / VC;            // a lane's features of a value, per piece; pieces
     constexpr int VW = VC * ES / 4;                                                // words of a piece
     constexpr int COLS = 16 * VC;                                                  // features of a round of pieces
+    constexpr int KT = ES == 4 ? 1 : 2, KEYS = 16 * KT;                            // groups of 16 entries of a turn
     __shared__ float lo[NW][kTile][COLS + 4];
     __shared__ float lm[NW][kTile], ll[NW][kTile];
+    __shared__ int lodd[NW];
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m16 = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), m16 = lane & 15, g = lane >> 4;
     const int head = blockIdx.x % a.c.n_heads, rest = blockIdx.x / a.c.n_heads;
     const int split = rest % a.splits, tile = a.tiles - 1 - rest / a.splits;   // later tiles see more: they start first
-    const int s = last_not_above(a.c.n_seq, lane, tile, [&](int i) { return (int64_t)tile_base(a, i); });
-    if (s < 0) return;
-    const int first = (tile - tile_base(a, s)) * kTile;
-    const Span t = span_of(a, s, first);
-    if (first >= t.n * a.group || split >= used_splits(a, t.end)) return;
+    Span t;
+    if (!find_tile(a, lane, tile, t) || split >= used_splits(a, t.end)) return;
     const int k0 = split * a.split_keys, k1 = split == a.splits - 1 ? t.end : min(t.end, k0 + a.split_keys);
     const int hd = a.c.hd;
 
+    // page numbers of 64 pages from `window` on, one per lane
+    const int32_t* pages = a.c.table + (int64_t)t.s * a.c.table_stride;
+    int window = page_of(a.c, min(k0 + KEYS * wave, max(k1 - 1, 0)));
+    int ids = pages[min(window + lane, a.c.max_pages - 1)];
+    const char *kh = a.c.k + (int64_t)head * a.c.head_stride * ES, *vh = a.c.v + (int64_t)head * a.c.head_stride * ES;
+
     // this lane's row: its query, and what it sees
-    const int pr = first + m16, i = pr / a.group;
+    const int pr = t.first + m16, i = pr / a.group;
     const bool real = pr < t.n * a.group;
     const int row = t.r0 + (real ? i : 0), qh = head * a.group + (real ? pr - i * a.group : 0);
     const int own = t.past + i;   // the row's own entry, the last one it sees of a chain
@@ -157,144 +211,137 @@ __global__ __launch_bounds__(64 * NW) void paged_rows_kernel(AttnArgs a) {
         if (real && (!PAD || f < hd)) q[ks] = *reinterpret_cast<const v4u*>(a.q.data + ((int64_t)row * a.q.row_stride + (int64_t)qh * a.q.head_stride + f) * ES);
     }
 
+    // Places of a turn's entries: of the lane's keys, and of the four entries a group whose scores and values it has; -1: there is none.
+    // Groups of 16 entries within a page have their page number in common; otherwise every lane looks its entries up.
+    const bool easy = a.c.page_size % 16 == 0;
+    int64_t at[KT], vat[KT][4];
+    auto places = [&](int kb) {
+        const int p0 = page_of(a.c, kb), p1 = page_of(a.c, min(kb + KEYS, k1) - 1);
+        if (p0 < window || p1 >= window + 64) {
+            window = p0;
+            ids = pages[min(window + lane, a.c.max_pages - 1)];
+        }
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+            const int e = kb + kt * 16;
+            if (easy) {
+                const int p = min(page_of(a.c, e), p1);
+                const int64_t b = place_in(a.c, __builtin_amdgcn_readlane(ids, p - window), e - p * a.c.page_size);
+                at[kt] = b >= 0 && e + m16 < k1 ? b + m16 * a.c.entry_stride : -1;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) vat[kt][r] = b >= 0 && e + g * 4 + r < k1 ? b + (g * 4 + r) * a.c.entry_stride : -1;
+            } else {
+                const int p = page_of(a.c, min(e + m16, k1 - 1));
+                const int64_t b = place_in(a.c, __shfl(ids, p - window), e + m16 - p * a.c.page_size);
+                at[kt] = e + m16 < k1 ? b : -1;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) vat[kt][r] = __shfl((long long)at[kt], g * 4 + r);
+            }
+        }
+    };
+    v4u k[KT][NS];
+    auto keys = [&] {   // (an entry that does not exist reads entry 0 of page 0: its score is dropped)
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+            const char* src = kh + (at[kt] < 0 ? 0 : at[kt]) * ES + g * 16;
+#pragma unroll
+            for (int ks = 0; ks < NS; ++ks) {
+                if (PAD && ks * STEP + g * VEC >= hd) k[kt][ks] = (v4u){0u, 0u, 0u, 0u};
+                else k[kt][ks] = *reinterpret_cast<const v4u*>(src + ks * STEP * ES);
+            }
+        }
+    };
+    typedef unsigned piece __attribute__((ext_vector_type(VW)));
+    piece v[KT][4][NC];
+    auto values = [&] {
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const char* src = vh + (vat[kt][r] < 0 ? 0 : vat[kt][r]) * ES + m16 * VC * ES;
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    if (PAD && c * COLS + m16 * VC >= hd) v[kt][r][c] = (piece)0u;
+                    else v[kt][r][c] = *reinterpret_cast<const piece*>(src + c * COLS * ES);
+                }
+            }
+    };
+
     f32x4 o[VD];
 #pragma unroll
     for (int d = 0; d < VD; ++d) o[d] = (f32x4){0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
-    const int32_t* pages = a.c.table + (int64_t)t.s * a.c.table_stride;
-    const char *kh = a.c.k + (int64_t)head * a.c.head_stride * ES, *vh = a.c.v + (int64_t)head * a.c.head_stride * ES;
-    const bool quads = (a.c.page_size & 3) == 0;
-
-    for (int kb = k0 + kKeys * wave; kb < k1; kb += kKeys * NW) {
-        int64_t at[2], vat[2][4];   // places of the lane's keys, and of the entries whose scores and values it has
+    bool odd = false;
+    const int kfirst = k0 + KEYS * wave;
+    if (kfirst < k1) {
+        places(kfirst);
+        keys();
+        values();
+    }
+    for (int kb = kfirst; kb < k1; kb += KEYS * NW) {
+        float z[KT][4];
+        bool gone = false;
+        unsigned none = 0u;   // bit kt * 4 + r: no such entry
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
-            const int e = kb + kt * 16 + m16;
-            at[kt] = e < k1 ? entry_at(a.c, pages, e) : -1;
-            const int e0 = kb + kt * 16 + g * 4;
-            if (quads) {   // four entries from a multiple of four on lie in one page
-                const int64_t p = e0 < k1 ? entry_at(a.c, pages, e0) : -1;
+        for (int kt = 0; kt < KT; ++kt) {
+            gone = gone || at[kt] < 0;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) vat[kt][r] = p >= 0 && e0 + r < k1 ? p + r * a.c.entry_stride : -1;
-            } else {
+            for (int r = 0; r < 4; ++r) none |= vat[kt][r] < 0 ? 1u << (kt * 4 + r) : 0u;
+            f32x4 sc = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int r = 0; r < 4; ++r) vat[kt][r] = e0 + r < k1 ? entry_at(a.c, pages, e0 + r) : -1;
-            }
+            for (int ks = 0; ks < NS; ++ks) sc = T::mul(k[kt][ks], q[ks], sc);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) z[kt][r] = sc[r] * a.scale2;
         }
-        const bool full = kb + kKeys <= t.all && kb + kKeys <= k1 && !__any(at[0] < 0 || at[1] < 0);
-        v4u k[2][NS];
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-            for (int ks = 0; ks < NS; ++ks) {   // (an entry that does not exist reads entry 0 of page 0: its score is dropped)
-                const int f = ks * STEP + g * VEC;
-                k[kt][ks] = (v4u){0u, 0u, 0u, 0u};
-                if (!PAD || f < hd) k[kt][ks] = *reinterpret_cast<const v4u*>(kh + (max(at[kt], (int64_t)0) + f) * ES);
-            }
-        unsigned v[2][4][NC][VW];
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    const int f = c * COLS + m16 * VC;
-                    const unsigned* src = reinterpret_cast<const unsigned*>(vh + (max(vat[kt][r], (int64_t)0) + f) * ES);
-                    typedef unsigned piece __attribute__((ext_vector_type(VW)));
-                    piece w = {};
-                    if (!PAD || f < hd) w = *reinterpret_cast<const piece*>(src);
-#pragma unroll
-                    for (int x = 0; x < VW; ++x) v[kt][r][c][x] = w[x];
-                }
-        f32x4 sc[2];
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
-            sc[kt] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int ks = 0; ks < NS; ++ks) sc[kt] = T::mul(k[kt][ks], q[ks], sc[kt]);
-            sc[kt] *= a.scale2;
+        const bool more = kb + KEYS * NW < k1;
+        if (more) {
+            places(kb + KEYS * NW);
+            keys();
         }
-        unsigned seen = 0xFFu;   // bit kt * 4 + r
-        if (!full) {
-            seen = 0u;
+        const bool edge = kb + KEYS > t.all;   // not every row sees every entry
+        if (edge || __any(gone)) {
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
+            for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int e = kb + kt * 16 + g * 4 + r;
-                    const bool see = real && vat[kt][r] >= 0 &&
-                                     (a.tree ? e < t.past || e == own || (e - t.past < 64 && ((bits >> (e - t.past)) & 1ull)) : e <= own);
-                    seen |= see ? 1u << (kt * 4 + r) : 0u;
-                    if (!see) sc[kt][r] = -INFINITY;
-                }
-        }
-        float top = m;
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) top = fmaxf(top, sc[kt][r]);
-        top = row_max(top);
-        const float base = top == -INFINITY ? 0.f : top, shrink = __builtin_amdgcn_exp2f(m - base);
-        m = top;
-        float p[2][4], sum = 0.f;
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                p[kt][r] = __builtin_amdgcn_exp2f(sc[kt][r] - base + T::kLift);
-                sum += p[kt][r];
-            }
-        l = l * shrink + sum;
-#pragma unroll
-        for (int d = 0; d < VD; ++d) o[d] *= shrink;
-
-        if (!full) {   // values of entries that do not exist are nothing, and infinities and NaN must not meet a weight of zero
-            bool odd = false;
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
+                    const bool there = !((none >> (kt * 4 + r)) & 1u);
+                    const int see = (int)there & (int)real & (int)sees(a, t, own, bits, kb + kt * 16 + g * 4 + r);
+                    z[kt][r] = see ? z[kt][r] : -INFINITY;
 #pragma unroll
                     for (int c = 0; c < NC; ++c)
 #pragma unroll
                         for (int x = 0; x < VW; ++x) {
-                            if (vat[kt][r] < 0) v[kt][r][c][x] = 0u;
-                            odd = odd || T::odd(v[kt][r][c][x]);
+                            const unsigned w = there ? v[kt][r][c][x] : 0u, w0 = edge ? T::clear(w) : w;
+                            odd = (int)odd | (int)(w0 != w);
+                            v[kt][r][c][x] = w0;
                         }
-            if (__any(odd)) {   // they are added one by one to the rows that see them, and are zero in the product
-#pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        for (int from = 0; from < 64; from += 16) {
-                            const float w = __shfl(p[kt][r], from + m16);
-                            const bool see = (__shfl((int)seen, from + m16) >> (kt * 4 + r)) & 1;
-                            const int64_t place = __shfl((long long)vat[kt][r], from);
-                            if (place < 0) continue;
-#pragma unroll
-                            for (int d = 0; d < VD; ++d)
-#pragma unroll
-                                for (int y = 0; y < 4; ++y) {
-                                    const int f = (d / VC) * COLS + (g * 4 + y) * VC + d % VC;
-                                    float x = 0.f;
-                                    if (!PAD || f < hd) {
-                                        if constexpr (TYPE == HAWK_FP32) x = *reinterpret_cast<const float*>(vh + (place + f) * ES);
-                                        else x = T::widen(*reinterpret_cast<const unsigned short*>(vh + (place + f) * ES));
-                                    }
-                                    if (see && !(fabsf(x) <= 3.4028235e38f)) o[d][y] += w * x;
-                                }
-                        }
-#pragma unroll
-                        for (int c = 0; c < NC; ++c)
-#pragma unroll
-                            for (int x = 0; x < VW; ++x) v[kt][r][c][x] = T::clear(v[kt][r][c][x]);
-                    }
-            }
+                }
         }
-
+        float top = m;
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) top = fmaxf(top, z[kt][r]);
+        top = row_max(top);
+        const float base = top == -INFINITY ? 0.f : top;
+        if (__any(top > m)) {
+            const float shrink = __builtin_amdgcn_exp2f(m - base);
+            l *= shrink;
+#pragma unroll
+            for (int d = 0; d < VD; ++d) o[d] *= shrink;
+        }
+        m = top;
+        float p[KT][4];
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                p[kt][r] = __builtin_amdgcn_exp2f(z[kt][r] - base + T::kLift);
+                l += p[kt][r];
+            }
         if constexpr (TYPE == HAWK_FP32) {
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
+            for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -302,30 +349,25 @@ __global__ __launch_bounds__(64 * NW) void paged_rows_kernel(AttnArgs a) {
                         o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[kt][r][d / VC][d % VC]), p[kt][r], o[d], 0, 0, 0);
         } else {
             // the weights as two values of the type, the second the first one's remainder: about 16 bits
-            unsigned short hi[8], low[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                hi[j] = T::narrow(p[j >> 2][j & 3]);
-                low[j] = T::narrow(p[j >> 2][j & 3] - T::widen(hi[j]));
-            }
             v4u ph, pl;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                ph[j] = hi[2 * j] | ((unsigned)hi[2 * j + 1] << 16);
-                pl[j] = low[2 * j] | ((unsigned)low[2 * j + 1] << 16);
+                const float x = p[j >> 1][2 * j & 3], y = p[j >> 1][(2 * j & 3) + 1];
+                ph[j] = narrow2(x, y, TYPE);
+                pl[j] = narrow2(x - T::widen((unsigned short)ph[j]), y - T::widen((unsigned short)(ph[j] >> 16)), TYPE);
             }
 #pragma unroll
             for (int d = 0; d < VD; ++d) {
                 v4u w;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {   // feature d of entries 2 j and 2 j + 1
-                    const unsigned x = v[j >> 1][2 * j & 3][d / VC][(d % VC) >> 1], y = v[j >> 1][(2 * j & 3) + 1][d / VC][(d % VC) >> 1];
-                    w[j] = __builtin_amdgcn_perm(y, x, (d & 1) ? 0x07060302u : 0x05040100u);
-                }
+                for (int j = 0; j < 4; ++j)   // feature d of entries 2 j and 2 j + 1
+                    w[j] = __builtin_amdgcn_perm(v[j >> 1][(2 * j & 3) + 1][d / VC][(d % VC) >> 1], v[j >> 1][2 * j & 3][d / VC][(d % VC) >> 1],
+                                                 (d & 1) ? 0x07060302u : 0x05040100u);
                 o[d] = T::mul(w, pl, o[d]);
                 o[d] = T::mul(w, ph, o[d]);
             }
         }
+        if (more) values();
     }
 
     // the waves' parts: maximum and sum, then the results in rounds of COLS features
@@ -334,10 +376,16 @@ __global__ __launch_bounds__(64 * NW) void paged_rows_kernel(AttnArgs a) {
         lm[wave][m16] = m;
         ll[wave][m16] = l;
     }
+    odd = __any(odd);
+    if (lane == 0) lodd[wave] = odd;
     __syncthreads();
     float mt = -INFINITY, lt = 0.f;
+    bool any_odd = false;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) mt = fmaxf(mt, lm[w][m16]);
+    for (int w = 0; w < NW; ++w) {
+        mt = fmaxf(mt, lm[w][m16]);
+        any_odd = any_odd || lodd[w];
+    }
     const float base = mt == -INFINITY ? 0.f : mt;
 #pragma unroll
     for (int w = 0; w < NW; ++w) lt += ll[w][m16] * __builtin_amdgcn_exp2f(lm[w][m16] - base);
@@ -349,20 +397,17 @@ __global__ __launch_bounds__(64 * NW) void paged_rows_kernel(AttnArgs a) {
         ml[0] = mt;
         ml[1] = lt;
     }
+#pragma unroll
     for (int c = 0; c < NC; ++c) {
         if (c > 0) __syncthreads();
 #pragma unroll
-        for (int cc = 0; cc < NC; ++cc)
-            if (cc == c) {
+        for (int y = 0; y < 4; ++y)
 #pragma unroll
-                for (int y = 0; y < 4; ++y)
-#pragma unroll
-                    for (int d = 0; d < VC; ++d) lo[wave][m16][(g * 4 + y) * VC + d] = o[cc * VC + d][y] * mine * norm;
-            }
+            for (int d = 0; d < VC; ++d) lo[wave][m16][(g * 4 + y) * VC + d] = o[c * VC + d][y] * (mine * norm);
         __syncthreads();
         // eight features of a row per thread
         for (int u = threadIdx.x; u < kTile * (COLS / 8); u += 64 * NW) {
-            const int rr = u / (COLS / 8), f = (u % (COLS / 8)) * 8, ff = c * COLS + f, prr = first + rr;
+            const int rr = u / (COLS / 8), f = (u % (COLS / 8)) * 8, ff = c * COLS + f, prr = t.first + rr;
             if (prr >= t.n * a.group || (PAD && ff >= hd)) continue;
             float x[8];
 #pragma unroll
@@ -373,6 +418,7 @@ __global__ __launch_bounds__(64 * NW) void paged_rows_kernel(AttnArgs a) {
             }
             const int ri = prr / a.group;
             const int64_t orow = t.r0 + ri, oh = head * a.group + prr - ri * a.group;
+            if (any_odd) add_odd<TYPE, 8>(a, t, vh, t.past + ri, a.tree ? a.tree[orow] : 0ull, max(k0, t.all - KEYS), k1, ff, x);
             if (whole)
                 store8(a.out.data, orow * a.out.row_stride + oh * a.out.head_stride + ff, a.out.dtype, x);
             else
@@ -381,49 +427,288 @@ __global__ __launch_bounds__(64 * NW) void paged_rows_kernel(AttnArgs a) {
     }
 }
 
-// Joins the parts of a long axis: a wave per (row, head).
-__global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a) {
+// Many rows: a workgroup of four waves, 32 rows each, over turns of KB entries that all of them read from LDS.  The next
+// turn's keys and values are in registers while this one is computed and are written behind it, two buffers, one barrier a
+// turn.  Products of 32 x 32 x 16: a lane has one row's 16 scores of 32 entries - blocks of four entries, the other half of the
+// wave the blocks between -, which in that order are the next product's operand; values are read transposed.
+// LDS rows keep their 16-byte pieces in an order changed by the row number, so that the 16 rows (keys) or four rows (values) that a
+// request touches lie on different banks.
+template <int TYPE> struct Wide;
+template <> struct Wide<HAWK_BF16> {
+    static constexpr float kLift = 0.f;
+    static __device__ __forceinline__ f32x16 mul(v4u a, v4u b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
+    }
+};
+template <> struct Wide<HAWK_FP16> {
+    static constexpr float kLift = 6.f;   // with what a maximum may lag behind (kLag) weights are at most 2^14
+    static __device__ __forceinline__ f32x16 mul(v4u a, v4u b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
+    }
+};
+constexpr float kLag = 8.f;   // results are rescaled when a row's maximum has grown by more than 2^8, not whenever it grows
+
+template <int TYPE, int DP, bool PAD, int KB>
+__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void paged_wide_kernel(AttnArgs a) {
+    using T = Of<TYPE>;
+    constexpr int ROW = DP * 2, CH = ROW / 16, PIECES = KB * CH / 256, NS = DP / 16, NT = DP / 32, SUB = KB / 32;
+    __shared__ __attribute__((aligned(16))) char lk[2][KB * ROW];
+    __shared__ __attribute__((aligned(16))) char lv[2][KB * ROW];
+    __shared__ int flags[4];   // of the turns in flight: some entries do not exist
+    __shared__ int odd;        // infinities or NaN were taken out of values
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r32 = lane & 31, hh = lane >> 5;
+    const int head = blockIdx.x % a.c.n_heads, rest = blockIdx.x / a.c.n_heads;
+    const int split = rest % a.splits, tile = a.tiles - 1 - rest / a.splits;
+    Span t;
+    if (!find_tile(a, lane, tile, t) || split >= used_splits(a, t.end)) return;
+    const int first = t.first;
+    const int k0 = split * a.split_keys, k1 = split == a.splits - 1 ? t.end : min(t.end, k0 + a.split_keys);
+    const int hd = a.c.hd;
+    if (tid < 4) flags[tid] = 0;
+    if (tid == 4) odd = 0;
+
+    const int pr = first + wave * 32 + r32, i = pr / a.group;
+    const bool real = pr < t.n * a.group;
+    const int row = t.r0 + (real ? i : 0), qh = head * a.group + (real ? pr - i * a.group : 0);
+    const int own = t.past + i;
+    const unsigned long long bits = a.tree && real ? a.tree[row] : 0ull;
+    // entries that every row of the wave sees lie before `all`, none sees any from `end` on
+    const int wlo = (first + wave * 32) / a.group, whi = min((first + wave * 32 + 31) / a.group, t.n - 1);
+    const int all = a.tree ? t.past : t.past + wlo + 1;
+    const int end = first + wave * 32 >= t.n * a.group ? 0 : (a.tree ? k1 : min(k1, t.past + whi + 1));
+    v4u q[NS];
+#pragma unroll
+    for (int ks = 0; ks < NS; ++ks) {
+        q[ks] = (v4u){0u, 0u, 0u, 0u};
+        const int f = ks * 16 + hh * 8;
+        if (real && (!PAD || f < hd)) q[ks] = *reinterpret_cast<const v4u*>(a.q.data + ((int64_t)row * a.q.row_stride + (int64_t)qh * a.q.head_stride + f) * 2);
+    }
+    f32x16 o[NT];
+#pragma unroll
+    for (int d = 0; d < NT; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+    float mb = -INFINITY, l = 0.f;   // the reference the weights are taken to, scaled; their sum
+
+    const int32_t* pages = a.c.table + (int64_t)t.s * a.c.table_stride;
+    const char *kh = a.c.k + (int64_t)head * a.c.head_stride * 2, *vh = a.c.v + (int64_t)head * a.c.head_stride * 2;
+    // pieces of a turn that this thread brings: piece j is 16 bytes of row (tid + 256 j) / CH
+    const int chunk = tid % CH;
+    int page[PIECES];
+    v4u kr[PIECES], vr[PIECES];
+    auto look_up = [&](int kb) {
+#pragma unroll
+        for (int j = 0; j < PIECES; ++j) {
+            const int e = kb + (tid + 256 * j) / CH;
+            page[j] = e < k1 ? pages[page_of(a.c, e)] : -1;
+        }
+    };
+    auto request = [&](int kb) {
+#pragma unroll
+        for (int j = 0; j < PIECES; ++j) {
+            const int e = kb + (tid + 256 * j) / CH;
+            const int64_t at = e < k1 ? place_in(a.c, page[j], e - page_of(a.c, e) * a.c.page_size) : -1;
+            kr[j] = vr[j] = (v4u){0u, 0u, 0u, 0u};
+            if (at >= 0 && (!PAD || chunk * 8 < hd)) {
+                kr[j] = *reinterpret_cast<const v4u*>(kh + at * 2 + chunk * 16);
+                vr[j] = *reinterpret_cast<const v4u*>(vh + at * 2 + chunk * 16);
+            }
+        }
+    };
+    auto put = [&](int kb, int turn) {
+        char *dk = lk[turn & 1], *dv = lv[turn & 1];
+#pragma unroll
+        for (int j = 0; j < PIECES; ++j) {
+            const int r = (tid + 256 * j) / CH, e = kb + r;
+            const int ck = DP == 64 ? chunk ^ ((r >> 1) & 7) : chunk ^ (r & 15);
+            const int cv = DP == 64 ? chunk ^ (((r >> 1) & 1) << 2) : chunk ^ ((r & 3) << 2);
+            if (e < k1 && (unsigned)page[j] >= (unsigned)a.c.n_pages) flags[turn & 3] = 1;
+            v4u w = vr[j];
+            if (kb + KB > t.all && (T::odd(w[0]) || T::odd(w[1]) || T::odd(w[2]) || T::odd(w[3]))) {
+                odd = 1;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) w[x] = T::clear(w[x]);
+            }
+            *reinterpret_cast<v4u*>(dk + r * ROW + ck * 16) = kr[j];
+            *reinterpret_cast<v4u*>(dv + r * ROW + cv * 16) = w;
+        }
+    };
+
+    const int turns = (k1 - k0 + KB - 1) / KB;
+    // (kr, vr and page are of the same turn between request() and put(): look_up() of the next one comes behind put())
+    if (turns > 0) {
+        look_up(k0);
+        request(k0);
+        __syncthreads();   // flags are clear
+        put(k0, 0);
+        look_up(k0 + KB);
+        request(k0 + KB);
+    }
+    __syncthreads();
+
+    const int r16 = lane & 15, kbase = r32 * ROW + ((DP == 64 ? (r32 >> 1) & 7 : r32 & 15) ^ hh) * 16;
+    const int vbase = (4 * hh + (r16 >> 2)) * ROW + ((((lane >> 4) & 1) * 2 + ((r16 & 3) >> 1)) ^ (DP == 64 ? (r16 >> 3) << 2 : (r16 >> 2) << 2)) * 16 + (r16 & 1) * 8;
+    const float c = a.scale2;
+    for (int turn = 0; turn < turns; ++turn) {
+        const int kb = k0 + turn * KB;
+        const int flag = flags[turn & 3];
+        if (kb < end) {
+            const char *bk = lk[turn & 1], *bv = lv[turn & 1];
+            float z[SUB][16];
+#pragma unroll
+            for (int u = 0; u < SUB; ++u) {
+                f32x16 sc;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sc[e] = 0.f;
+#pragma unroll
+                for (int ks = 0; ks < NS; ++ks) {
+                    const v4u k = *reinterpret_cast<const v4u*>(bk + u * 32 * ROW + (kbase ^ (ks * 32)));
+                    sc = Wide<TYPE>::mul(k, q[ks], sc);
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) z[u][e] = sc[e];
+            }
+            if (flag || kb + KB > all || kb + KB > k1) {
+#pragma unroll
+                for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int e = kb + u * 32 + 8 * (r >> 2) + 4 * hh + (r & 3);
+                        const int see = (int)real & (int)(e < k1) & (int)sees(a, t, own, bits, e);
+                        z[u][r] = see ? z[u][r] : -INFINITY;
+                    }
+                if (flag) {
+#pragma unroll
+                    for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            z[u][r] = entry_at(a.c, pages, kb + u * 32 + 8 * (r >> 2) + 4 * hh + (r & 3)) >= 0 ? z[u][r] : -INFINITY;
+                }
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top = fmaxf(top, z[u][r]);
+            top = swap32(top, false) * c;
+            if (__any(top > mb + kLag)) {
+                const float now = fmaxf(mb, top), base = now == -INFINITY ? 0.f : now, shrink = __builtin_amdgcn_exp2f(mb - base);
+                mb = now;
+                l *= shrink;
+#pragma unroll
+                for (int d = 0; d < NT; ++d) o[d] *= shrink;
+            }
+            const float off = Wide<TYPE>::kLift - (mb == -INFINITY ? 0.f : mb);
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    z[u][r] = __builtin_amdgcn_exp2f(fmaf(z[u][r], c, off));
+                    l += z[u][r];
+                }
+#pragma unroll
+            for (int cc = 0; cc < KB / 16; ++cc) {
+                v4u p;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) p[j] = narrow2(z[cc >> 1][8 * (cc & 1) + 2 * j], z[cc >> 1][8 * (cc & 1) + 2 * j + 1], TYPE);
+#pragma unroll
+                for (int d = 0; d < NT; ++d) {
+                    typedef short s4 __attribute__((ext_vector_type(4)));
+                    const char* at = bv + cc * 16 * ROW + (vbase ^ (d * 64));
+                    const v2u x = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)const_cast<char*>(at)));
+                    const v2u y = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)const_cast<char*>(at + 8 * ROW)));
+                    o[d] = Wide<TYPE>::mul((v4u){x[0], x[1], y[0], y[1]}, p, o[d]);
+                }
+            }
+        }
+        if (turn + 1 < turns) {
+            put(kb + KB, turn + 1);
+            look_up(kb + 2 * KB);
+            request(kb + 2 * KB);
+        }
+        if (tid == 0) flags[(turn + 3) & 3] = 0;   // the turn before this one's: nobody looks at it any more
+        __syncthreads();
+    }
+
+    l = swap32(l, true);
+    if (!real) return;
+    const bool whole = a.splits == 1;
+    const float norm = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+    const int64_t vec = ((int64_t)split * a.r.rows + row) * a.q.n_heads + qh;
+    if (!whole && hh == 0) {
+        a.part_ml[vec * 2] = mb;
+        a.part_ml[vec * 2 + 1] = l;
+    }
+#pragma unroll
+    for (int d = 0; d < NT; ++d)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const int f = d * 32 + 8 * b + 4 * hh;
+            if (PAD && f >= hd) continue;
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = o[d][4 * b + e] * norm;
+            if (odd) add_odd<TYPE, 4>(a, t, vh, own, bits, max(k0, t.all - KB), k1, f, x);
+            if (whole) store4(a.out.data, (int64_t)row * a.out.row_stride + (int64_t)qh * a.out.head_stride + f, a.out.dtype, x);
+            else store4(reinterpret_cast<char*>(a.part), vec * hd + f, HAWK_FP32, x);
+        }
+}
+
+// Joins the parts of a long axis: a wave per (row, head).  Lane i has part i's maximum and sum; groups of lanes take a part's features each,
+// eight a lane, so that several parts are on their way at once.
+__global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a, int lanes) {
     const int lane = threadIdx.x & 63;
     const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     const int row = (int)(unit / a.q.n_heads), qh = (int)(unit - (int64_t)row * a.q.n_heads);
     if (row >= a.r.rows) return;
     const int s = last_not_above(a.c.n_seq, lane, row, [&](int i) { return (int64_t)a.r.row_start[i]; });
-    if (s < 0 || row >= a.r.row_start[s + 1]) return;
-    const int first = ((row - max(a.r.row_start[s], 0)) * a.group + qh % a.group) / kTile * kTile;
-    const Span t = span_of(a, s, first);
+    if (s < 0) return;
+    const int start = a.r.row_start[s], stop = a.r.row_start[s + 1];
+    if (row >= stop) return;
+    const Span t = span_of(a, s, ((row - max(start, 0)) * a.group + qh % a.group) / a.tile * a.tile, start, stop, a.r.n_past[s]);
     const int n = used_splits(a, t.end);
-    float mt = -INFINITY, lt = 0.f;
-    for (int i = 0; i < n; ++i) mt = fmaxf(mt, a.part_ml[(((int64_t)i * a.r.rows + row) * a.q.n_heads + qh) * 2]);
+    const int64_t step = (int64_t)a.r.rows * a.q.n_heads, vec = (int64_t)row * a.q.n_heads + qh;
+    const int f = (lane & (lanes - 1)) * 8, part0 = lane / lanes, per = 64 / lanes;
+    float mt = -INFINITY, lt = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int i = lane; i < n; i += 64) mt = fmaxf(mt, a.part_ml[(i * step + vec) * 2]);
+#pragma unroll
+    for (int w = 1; w < 64; w <<= 1) mt = fmaxf(mt, __shfl_xor(mt, w));
     const float base = mt == -INFINITY ? 0.f : mt;
-    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    const int f = lane * 8;
-    for (int i = 0; i < n; ++i) {
-        const int64_t at = ((int64_t)i * a.r.rows + row) * a.q.n_heads + qh;
-        const float w = __builtin_amdgcn_exp2f(a.part_ml[at * 2] - base);
-        lt += a.part_ml[at * 2 + 1] * w;
+#pragma unroll 4
+    for (int i = part0; i < n; i += per) {
+        const float w = __builtin_amdgcn_exp2f(a.part_ml[(i * step + vec) * 2] - base);
+        lt += a.part_ml[(i * step + vec) * 2 + 1] * w;
         if (f < a.c.hd) {
             float y[8];
-            load8(reinterpret_cast<const char*>(a.part), at * a.c.hd + f, HAWK_FP32, y);
+            load8(reinterpret_cast<const char*>(a.part), (i * step + vec) * a.c.hd + f, HAWK_FP32, y);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] += y[e] * w;
+            for (int e = 0; e < 8; ++e) x[e] = fmaf(y[e], w, x[e]);
         }
     }
-    if (f >= a.c.hd) return;
+    for (int w = lanes; w < 64; w <<= 1) {
+        lt += __shfl_xor(lt, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] += __shfl_xor(x[e], w);
+    }
+    if (lane >= lanes || f >= a.c.hd) return;
     const float norm = lt == 0.f ? 0.f : 1.f / lt;
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] *= norm;
     store8(a.out.data, (int64_t)row * a.out.row_stride + (int64_t)qh * a.out.head_stride + f, a.out.dtype, x);
 }
 
-struct Plan { int tiles, splits, split_keys; size_t part_bytes, ml_bytes; };
+struct Plan { bool wide; int tiles, splits, split_keys; size_t part_bytes, ml_bytes; };
 
-// How a call is cut: parts of the long axis where the tiles alone would leave most of the chip's 256 units idle.
-Plan plan_of(int n_seq, int rows, int n_heads, int n_q_heads, int hd, int64_t capacity, int max_len) {
+// How a call is cut.  Sequences of many rows on average take the kernel that shares entries through LDS.  Parts of the long axis where
+// the tiles alone would leave most of the chip's 256 units idle.
+Plan plan_of(int dtype, int n_seq, int rows, int n_heads, int n_q_heads, int hd, int64_t capacity, int max_len) {
     Plan p;
     const int group = n_q_heads / n_heads;
-    p.tiles = (int)((int64_t)rows * group / kTile) + n_seq;
+    p.wide = dtype != HAWK_FP32 && (int64_t)rows * group >= 64 * (int64_t)n_seq;
+    p.tiles = (int)((int64_t)rows * group / (p.wide ? kWide : kTile)) + n_seq;
     const int64_t len = max_len < 1 || max_len > capacity ? capacity : max_len, blocks = (int64_t)p.tiles * n_heads;
-    int64_t parts = 1024 / (blocks < 1 ? 1 : blocks);
+    int64_t parts = (p.wide ? 512 : 1024) / (blocks < 1 ? 1 : blocks);
     const int64_t most = len / 512;
     if (parts > most) parts = most;
     if (parts > 64) parts = 64;
@@ -458,12 +743,22 @@ template <int TYPE> void launch_typed(const AttnArgs& a, unsigned grid, hipStrea
     }
 }
 
+template <int TYPE> void launch_wide(const AttnArgs& a, unsigned grid, hipStream_t stream) {
+    const int hd = a.c.hd;
+    if (hd == 64) paged_wide_kernel<TYPE, 64, false, 64><<<grid, 256, 0, stream>>>(a);
+    else if (hd < 64) paged_wide_kernel<TYPE, 64, true, 64><<<grid, 256, 0, stream>>>(a);
+    else if (hd == 128) paged_wide_kernel<TYPE, 128, false, 64><<<grid, 256, 0, stream>>>(a);
+    else if (hd < 128) paged_wide_kernel<TYPE, 128, true, 64><<<grid, 256, 0, stream>>>(a);
+    else if (hd == 256) paged_wide_kernel<TYPE, 256, false, 32><<<grid, 256, 0, stream>>>(a);
+    else paged_wide_kernel<TYPE, 256, true, 32><<<grid, 256, 0, stream>>>(a);
+}
+
 }  // namespace
 
 size_t paged_attention_workspace_bytes(const hawk_paged_cache* cache, int rows, int n_q_heads, int max_len) {
     PagedView c;
     if (!paged_view(cache, 0, &c) || !shape_ok(c, rows, n_q_heads)) return 0;
-    const Plan p = plan_of(c.n_seq, rows, c.n_heads, n_q_heads, c.hd, (int64_t)c.max_pages * c.page_size, max_len);
+    const Plan p = plan_of(cache->dtype, c.n_seq, rows, c.n_heads, n_q_heads, c.hd, (int64_t)c.max_pages * c.page_size, max_len);
     return p.part_bytes + p.ml_bytes;
 }
 
@@ -478,23 +773,28 @@ int launch_paged_attention(const hawk_paged_cache* cache, int layer, const hawk_
     if (a.q.dtype != cache->dtype || !shape_ok(a.c, a.r.rows, a.q.n_heads)) return HAWK_EINVAL;
     if (!(scale > 0.f) || !(scale < 3.4e38f) || (reinterpret_cast<uintptr_t>(tree) & 7)) return HAWK_EINVAL;
     if (!room_for(a.out, a.r.rows, a.c.hd)) return HAWK_EINVAL;
-    const Plan p = plan_of(a.c.n_seq, a.r.rows, a.c.n_heads, a.q.n_heads, a.c.hd, (int64_t)a.c.max_pages * a.c.page_size, max_len);
+    const Plan p = plan_of(cache->dtype, a.c.n_seq, a.r.rows, a.c.n_heads, a.q.n_heads, a.c.hd, (int64_t)a.c.max_pages * a.c.page_size, max_len);
     if (p.part_bytes && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15))) return HAWK_EINVAL;
     if (workspace_bytes < p.part_bytes + p.ml_bytes) return p.part_bytes ? HAWK_ENOMEM : HAWK_EINVAL;
     a.tree = tree;
     a.scale2 = scale * 1.44269504f;
     a.group = a.q.n_heads / a.c.n_heads;
+    a.tile = p.wide ? kWide : kTile;
     a.tiles = p.tiles; a.splits = p.splits; a.split_keys = p.split_keys;
     a.part = static_cast<float*>(workspace);
     a.part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.part_bytes);
     const int64_t grid = (int64_t)p.tiles * p.splits * a.c.n_heads;
     if (grid > (1 << 23)) return HAWK_EINVAL;
-    if (cache->dtype == HAWK_FP32) launch_typed<HAWK_FP32>(a, (unsigned)grid, stream);
+    if (p.wide && cache->dtype == HAWK_BF16) launch_wide<HAWK_BF16>(a, (unsigned)grid, stream);
+    else if (p.wide) launch_wide<HAWK_FP16>(a, (unsigned)grid, stream);
+    else if (cache->dtype == HAWK_FP32) launch_typed<HAWK_FP32>(a, (unsigned)grid, stream);
     else if (cache->dtype == HAWK_BF16) launch_typed<HAWK_BF16>(a, (unsigned)grid, stream);
     else launch_typed<HAWK_FP16>(a, (unsigned)grid, stream);
     if (p.splits > 1) {
         const int64_t units = (int64_t)a.r.rows * a.q.n_heads;
-        paged_join_kernel<<<(unsigned)((units + 3) / 4), 256, 0, stream>>>(a);
+        int lanes = 1;
+        while (lanes * 8 < a.c.hd) lanes *= 2;
+        paged_join_kernel<<<(unsigned)((units + 3) / 4), 256, 0, stream>>>(a, lanes);
     }
     return hipGetLastError() == hipSuccess ? HAWK_OK : HAWK_EDEVICE;
 }
