@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional
 
 import numpy as np
@@ -243,9 +244,19 @@ def _int32():
     return torch.int32
 
 
+def _int64():
+    import torch
+    return torch.int64
+
+
 def _float32():
     import torch
     return torch.float32
+
+
+def _uint8():
+    import torch
+    return torch.uint8
 
 
 def _stream_of(t):
@@ -352,6 +363,8 @@ def sample_rows(logits, u, temperature: float, top_k: int, skip=None):
     return out
 
 _DTYPES = None   # torch dtype -> HAWK_*
+_PACK_HEADS = struct.Struct("@Pqqii").pack     # HawkHeads, HawkPagedRows as bytes: a third of a structure object's cost
+_PACK_ROWS = struct.Struct("@PPi4x").pack
 
 
 def _dtype_of(t):
@@ -362,20 +375,22 @@ def _dtype_of(t):
     return _DTYPES.get(t.dtype, -1)
 
 
-def _on_device(device, call):
-    """`call` with `device` current: launches go to the current device, whatever stream they are given."""
+def _call_on(index, fn, *args):
+    """fn(*args, stream) with device `index` current - launches go to the current device, whatever stream they are given - on
+    torch's current stream of that device."""
     import torch  # device memory and stream only
-    if device.index is None or device.index == torch.cuda.current_device():
-        return call()
-    with torch.cuda.device(device):
-        return call()
+    stream = torch._C._cuda_getCurrentRawStream(index)
+    if torch._C._cuda_getDevice() == index:
+        return fn(*args, stream)
+    with torch.cuda.device(index):
+        return fn(*args, stream)
 
 
 def rotary_table(n_pos: int, rot_dim: int, theta: float = 10000.0, device: str = "cuda:0"):
     """hawk_rotary_table: fp32 device tensor [n_pos, rot_dim // 2, 2] of cos and sin of position * theta^(-2 j / rot_dim)."""
     import torch  # device memory and stream only
     out = torch.empty((n_pos, rot_dim // 2, 2), dtype=torch.float32, device=device)
-    rc = _on_device(out.device, lambda: load_library().hawk_rotary_table(out.data_ptr(), n_pos, rot_dim, float(theta), _stream_of(out)))
+    rc = _call_on(out.get_device(), load_library().hawk_rotary_table, out.data_ptr(), n_pos, rot_dim, float(theta))
     if rc != 0:
         raise HawkError(rc, "hawk_rotary_table")
     return out
@@ -409,6 +424,8 @@ class PagedCache:
                                  entry_stride=(se + 7) // 8 * 8 if page_size == 1 else se, dtype=_dtype_of(k), n_layers=n_layers,
                                  n_pages=n_pages, page_size=page_size, n_heads=n_heads, head_dim=head_dim)
         self._ref = C.byref(self._c)
+        self._dev, self._type, self._hd, self._kv = k.get_device(), _dtype_of(k), head_dim, n_heads
+        self._room = {}     # workspace of an attention by (rows, q heads, max_len)
         self.table = table
 
     @property
@@ -422,25 +439,29 @@ class PagedCache:
         self._table = t
         self._c.table, self._c.table_stride = t.data_ptr(), max(t.shape[1], 1)
         self._c.n_seq, self._c.max_pages = t.shape
+        self._n_seq = t.shape[0]
+        self._room.clear()
 
     def _rows(self, where, rows, row_start, n_past):
-        n, i32 = self._c.n_seq, _int32()
-        if not (row_start.dtype == i32 and n_past.dtype == i32 and row_start.device == self.device and n_past.device == self.device
+        n, i32, dev = self._n_seq, _int32(), self._dev
+        if not (row_start.dtype is i32 and n_past.dtype is i32 and row_start.get_device() == dev and n_past.get_device() == dev
                 and row_start.shape == (n + 1,) and n_past.shape == (n,) and row_start.is_contiguous() and n_past.is_contiguous()):
             raise HawkError(-1, where, "row_start [n_seq + 1] and n_past [n_seq] must be contiguous int32 tensors on the cache's device")
-        return HawkPagedRows(row_start.data_ptr(), n_past.data_ptr(), rows)
+        return _PACK_ROWS(row_start.data_ptr(), n_past.data_ptr(), rows)
 
-    def _heads(self, where, t, heads=None):
-        if not (t.dim() == 3 and t.device == self.device and t.shape[2] == self._c.head_dim and (t.stride(2) == 1 or t.numel() == 0)
-                and (heads is None or t.shape[1] == heads) and t.shape[1] > 0 and _dtype_of(t) >= 0):
-            raise HawkError(-1, where, "vectors must be tensors [rows, heads, head_dim] of a supported type on the cache's device, the last axis contiguous")
-        rs, hs = t.stride(0), t.stride(1)
-        return HawkHeads(t.data_ptr(), rs if t.shape[0] > 1 else t.shape[1] * t.shape[2], hs if t.shape[1] > 1 else t.shape[2], t.shape[1], _dtype_of(t))
+    def _heads(self, where, t, rows=None, heads=None):
+        """HawkHeads of a tensor [rows, heads, head_dim] (strides of axes of one are not used), its rows and heads."""
+        if t.dim() == 3 and t.get_device() == self._dev:
+            r, h, d = t.shape
+            rs, hs, es = t.stride()
+            if d == self._hd and (es == 1 or r == 0) and h > 0 and (rows is None or r == rows) and (heads is None or h == heads):
+                return _PACK_HEADS(t.data_ptr(), rs if r > 1 else h * d, hs if h > 1 else d, h, _dtype_of(t)), r, h
+        raise HawkError(-1, where, "vectors must be tensors [rows, heads, head_dim] on the cache's device, the last axis contiguous, of the same rows "
+                                   "(keys and values: of the cache's heads; results: of the queries')")
 
-    def _run(self, where, call):
-        rc = _on_device(self.device, call)
-        if rc != 0:
-            raise HawkError(rc, where)
+    def _fits(self, where, what, t, dtype, shape):
+        if not (t.dtype is dtype and t.get_device() == self._dev and t.shape == shape and t.is_contiguous()):
+            raise HawkError(-1, where, what)
 
     def append(self, k, v, row_start, n_past, q=None, rot=None, halves: bool = False, pos=None, q_gain=None, k_gain=None,
                eps: float = 1e-5, q_out=None, layer: int = 0):
@@ -449,35 +470,40 @@ class PagedCache:
         rows of no sequence are not written).  rot: a table [n_pos, rot_dim // 2, 2] (rotary_table) or None;
         halves: pairs (j, j + rot_dim / 2) instead of (2 j, 2 j + 1); pos [rows] int32: positions other than the entries' own;
         q_gain, k_gain [head_dim] fp32: RMS norm per head with eps."""
-        where, c = "hawk_paged_append", self._c
-        rows = k.shape[0]
-        hk, hv = self._heads(where, k, c.n_heads), self._heads(where, v, c.n_heads)
+        where = "hawk_paged_append"
+        hk, rows, _ = self._heads(where, k, heads=self._kv)
+        hv, _, _ = self._heads(where, v, rows, self._kv)
         r = self._rows(where, rows, row_start, n_past)
-        hq = hqo = None
+        hq = ho = None
         if q is not None:
-            import torch  # device memory and stream only
-            hq = self._heads(where, q)
+            hq, _, n_heads = self._heads(where, q, rows)
             if q_out is None:
-                q_out = torch.empty(q.shape, dtype=self.k.dtype, device=self.device)
-            hqo = self._heads(where, q_out, q.shape[1])
-            if q_out.shape[0] != rows:
-                raise HawkError(-1, where, "q_out must have q's shape")
-        f32 = _float32()
-        if v.shape[0] != rows or (q is not None and q.shape[0] != rows) or (q is None and q_out is not None):
-            raise HawkError(-1, where, "q, k and v must have the same rows")
-        for g in (q_gain, k_gain):
-            if g is not None and not (_dev_ok(g, f32, (c.head_dim,)) and g.device == self.device):
-                raise HawkError(-1, where, "gains must be fp32 tensors [head_dim] on the cache's device")
-        if rot is not None and not (_dev_ok(rot, f32) and rot.dim() == 3 and rot.shape[2] == 2 and rot.device == self.device):
-            raise HawkError(-1, where, "rot must be a contiguous fp32 tensor [n_pos, rot_dim / 2, 2] on the cache's device")
-        if pos is not None and not (_dev_ok(pos, _int32(), (rows,)) and pos.device == self.device):
-            raise HawkError(-1, where, "pos must be a contiguous int32 tensor [rows] on the cache's device")
-        self._run(where, lambda: self._L.hawk_paged_append(
-            self._ref, layer, C.byref(r), C.byref(hq) if hq is not None else None, C.byref(hk), C.byref(hv),
-            q_gain.data_ptr() if q_gain is not None else None, k_gain.data_ptr() if k_gain is not None else None, float(eps),
-            rot.data_ptr() if rot is not None else None, rot.shape[0] if rot is not None else 0,
-            2 * rot.shape[1] if rot is not None else 0, int(halves), pos.data_ptr() if pos is not None else None,
-            C.byref(hqo) if hqo is not None else None, _stream_of(self.k)))
+                q_out = q.new_empty((rows, n_heads, self._hd), dtype=self.k.dtype)
+            ho, _, _ = self._heads(where, q_out, rows, n_heads)
+        elif q_out is not None:
+            raise HawkError(-1, where, "q_out without q")
+        gq = gk = table = at = None
+        n_pos = rot_dim = 0
+        if q_gain is not None:
+            self._fits(where, "gains must be fp32 tensors [head_dim] on the cache's device", q_gain, _float32(), (self._hd,))
+            gq = q_gain.data_ptr()
+        if k_gain is not None:
+            self._fits(where, "gains must be fp32 tensors [head_dim] on the cache's device", k_gain, _float32(), (self._hd,))
+            gk = k_gain.data_ptr()
+        if rot is not None:
+            if rot.dim() != 3:
+                raise HawkError(-1, where, "rot must be a tensor [n_pos, rot_dim / 2, 2]")
+            n_pos, half, _ = rot.shape
+            rot_dim = 2 * half
+            self._fits(where, "rot must be a contiguous fp32 tensor [n_pos, rot_dim / 2, 2] on the cache's device", rot, _float32(), (n_pos, half, 2))
+            table = rot.data_ptr()
+        if pos is not None:
+            self._fits(where, "pos must be a contiguous int32 tensor [rows] on the cache's device", pos, _int32(), (rows,))
+            at = pos.data_ptr()
+        rc = _call_on(self._dev, self._L.hawk_paged_append, self._ref, layer, r, hq, hk, hv, gq, gk, eps, table, n_pos, rot_dim, 1 if halves else 0,
+                      at, ho)
+        if rc != 0:
+            raise HawkError(rc, where)
         return q_out
 
     def attend(self, q, row_start, n_past, max_len: int = 0, scale: Optional[float] = None, tree=None, out=None, layer: int = 0):
@@ -486,34 +512,41 @@ class PagedCache:
         1 / sqrt(head_dim).  tree [rows] int64: which of the first 64 rows of its sequence a row sees besides itself
         (hawk_tree_layout's ancestors); None: those up to itself.  out: where the result goes, any of the three types (None: a new tensor of
         q's type, whose rows of no sequence are not written)."""
-        import torch  # device memory and stream only
-        where, c = "hawk_paged_attention", self._c
-        hq = self._heads(where, q)
-        r = self._rows(where, q.shape[0], row_start, n_past)
+        where = "hawk_paged_attention"
+        hq, rows, heads = self._heads(where, q)
+        r = self._rows(where, rows, row_start, n_past)
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
-        ho = self._heads(where, out, q.shape[1])
-        if out.shape[0] != q.shape[0]:
-            raise HawkError(-1, where, "out must have q's shape")
-        if tree is not None and not (_dev_ok(tree, torch.int64, (q.shape[0],)) and tree.device == self.device):
-            raise HawkError(-1, where, "tree must be a contiguous int64 tensor [rows] on the cache's device")
-        nws = self._L.hawk_paged_attention_workspace_bytes(self._ref, q.shape[0], q.shape[1], max_len)
-        ws = torch.empty(nws, dtype=torch.uint8, device=self.device) if nws else None
-        self._run(where, lambda: self._L.hawk_paged_attention(
-            self._ref, layer, C.byref(r), C.byref(hq), tree.data_ptr() if tree is not None else None,
-            float(scale) if scale is not None else c.head_dim ** -0.5, max_len, C.byref(ho), ws.data_ptr() if nws else None, nws,
-            _stream_of(self.k)))
+            out = q.new_empty((rows, heads, self._hd))
+        ho, _, _ = self._heads(where, out, rows, heads)
+        bits = None
+        if tree is not None:
+            self._fits(where, "tree must be a contiguous int64 tensor [rows] on the cache's device", tree, _int64(), (rows,))
+            bits = tree.data_ptr()
+        key = (rows, heads, max_len)
+        nws = self._room.get(key)
+        if nws is None:
+            if len(self._room) > 4096:
+                self._room.clear()
+            nws = self._room[key] = self._L.hawk_paged_attention_workspace_bytes(self._ref, rows, heads, max_len)
+        ws = q.new_empty((nws,), dtype=_uint8()) if nws else None
+        rc = _call_on(self._dev, self._L.hawk_paged_attention, self._ref, layer, r, hq, bits, scale if scale is not None else self._hd ** -0.5, max_len,
+                      ho, ws.data_ptr() if nws else None, nws)
+        if rc != 0:
+            raise HawkError(rc, where)
         return out
 
     def keep(self, n_past, path, n_keep):
         """hawk_paged_keep: the accepted path of a tree step, path [n_seq, depth] int32 of node numbers of which the first n_keep
         [n_seq] count, goes to the entries behind n_past's, in every layer."""
-        where, i32, n = "hawk_paged_keep", _int32(), self._c.n_seq
-        if not (_dev_ok(path, i32) and path.dim() == 2 and path.shape[0] == n and _dev_ok(n_past, i32, (n,)) and _dev_ok(n_keep, i32, (n,))
-                and path.device == self.device and n_past.device == self.device and n_keep.device == self.device):
-            raise HawkError(-1, where, "path [n_seq, depth], n_past and n_keep [n_seq] must be contiguous int32 tensors on the cache's device")
-        self._run(where, lambda: self._L.hawk_paged_keep(self._ref, n_past.data_ptr(), path.data_ptr(), n_keep.data_ptr(), path.shape[1],
-                                                         _stream_of(self.k)))
+        where, i32, n = "hawk_paged_keep", _int32(), self._n_seq
+        what = "path [n_seq, depth], n_past and n_keep [n_seq] must be contiguous int32 tensors on the cache's device"
+        self._fits(where, what, n_past, i32, (n,))
+        self._fits(where, what, n_keep, i32, (n,))
+        depth = path.shape[1] if path.dim() == 2 else 0
+        self._fits(where, what, path, i32, (n, depth))
+        rc = _call_on(self._dev, self._L.hawk_paged_keep, self._ref, n_past.data_ptr(), path.data_ptr(), n_keep.data_ptr(), depth)
+        if rc != 0:
+            raise HawkError(rc, where)
 
     def entry(self, table_row, e: int, layer: int = 0) -> int:
         """hawk_paged_entry: elements from k's (v's) start to entry e, head 0, of a sequence with the pages table_row (host); -1: none."""
@@ -523,37 +556,48 @@ class PagedCache:
         return int(self._L.hawk_paged_entry(self._ref, _p(t), layer, e))
 
 
+_CHAIN_ROOM = {}     # workspace of verify_chains by (n_seq, k, n)
+
+
 def verify_chains(p_logits, q_logits, draft, u_acc, u_final, temperature: float, top_k: int, n_draft=None, p_start=None):
     """hawk_verify_chains on device tensors: p_logits fp32 [p_rows, n] (rows may be strided), the k + 1 target rows of sequence s
     from row p_start[s] (int32 [n_seq]; None: s * (k + 1)); q_logits fp32 [n_seq, k, n] (strided) or None (the drafts are
     certain); draft [n_seq, k] int32; u_acc [n_seq, k], u_final [n_seq] fp32; n_draft None or int32 [n_seq].
     Returns device tensors (accepted [n_seq], tokens [n_seq, k + 1]) int32."""
-    import torch  # device memory and stream only
-    where = "hawk_verify_chains"
+    where, f32, i32 = "hawk_verify_chains", _float32(), _int32()
+    dev = p_logits.get_device()
     n_seq, k = draft.shape
-    dev = p_logits.device
-    small = [(draft, torch.int32, (n_seq, k)), (u_acc, torch.float32, (n_seq, k)), (u_final, torch.float32, (n_seq,))]
-    small += [(t, torch.int32, (n_seq,)) for t in (n_draft, p_start) if t is not None]
-    if not (p_logits.is_cuda and p_logits.dim() == 2 and p_logits.dtype == torch.float32 and p_logits.stride(1) == 1
-            and all(t.device == dev and _dev_ok(t, dt, shape) for t, dt, shape in small)):
+    small = [(draft, i32, (n_seq, k)), (u_acc, f32, (n_seq, k)), (u_final, f32, (n_seq,))]
+    if n_draft is not None:
+        small.append((n_draft, i32, (n_seq,)))
+    if p_start is not None:
+        small.append((p_start, i32, (n_seq,)))
+    if dev < 0 or p_logits.dim() != 2 or p_logits.dtype is not f32 or any(
+            t.dtype is not dt or t.get_device() != dev or t.shape != shape or not t.is_contiguous() for t, dt, shape in small):
         raise HawkError(-1, where, "arguments must be device tensors of the documented shapes and types")
     p_rows, n = p_logits.shape
-    if q_logits is not None and not (q_logits.device == dev and q_logits.dtype == torch.float32 and tuple(q_logits.shape) == (n_seq, k, n)
-                                     and (q_logits.stride(2) == 1 or n == 1)):
-        raise HawkError(-1, where, "q_logits must be a device fp32 tensor [n_seq, k, n], the last axis contiguous")
+    ps, es = p_logits.stride()
+    if es != 1 and n > 1:
+        raise HawkError(-1, where, "the last axis of p_logits must be contiguous")
+    q, qs, qr = None, 0, n
+    if q_logits is not None:
+        if q_logits.dtype is not f32 or q_logits.get_device() != dev or q_logits.shape != (n_seq, k, n) or (q_logits.stride(2) != 1 and n > 1):
+            raise HawkError(-1, where, "q_logits must be a device fp32 tensor [n_seq, k, n], the last axis contiguous")
+        q, qs, qr = q_logits.data_ptr(), q_logits.stride(0) if n_seq > 1 else 0, q_logits.stride(1) if k > 1 else n
     if p_start is None and p_rows < n_seq * (k + 1):
         raise HawkError(-1, where, "p_logits has fewer rows than n_seq * (k + 1)")
     L = load_library()
-    nws = int(L.hawk_verify_chains_workspace_bytes(n_seq, k, n))
-    ws = torch.empty(max(nws, 16), dtype=torch.uint8, device=dev)
-    count = torch.empty(n_seq, dtype=torch.int32, device=dev)
-    toks = torch.empty((n_seq, k + 1), dtype=torch.int32, device=dev)
-    qs, qr = (0, n) if q_logits is None else (q_logits.stride(0) if n_seq > 1 else 0, q_logits.stride(1) if k > 1 else n)
-    rc = _on_device(dev, lambda: L.hawk_verify_chains(
-        p_logits.data_ptr(), p_logits.stride(0) if p_rows > 1 else n, p_start.data_ptr() if p_start is not None else None, p_rows,
-        q_logits.data_ptr() if q_logits is not None else None, qs, qr, draft.data_ptr(),
-        n_draft.data_ptr() if n_draft is not None else None, u_acc.data_ptr(), u_final.data_ptr(), n_seq, k, n, float(temperature),
-        int(top_k), count.data_ptr(), toks.data_ptr(), ws.data_ptr(), nws, _stream_of(p_logits)))
+    nws = _CHAIN_ROOM.get((n_seq, k, n))
+    if nws is None:
+        if len(_CHAIN_ROOM) > 4096:
+            _CHAIN_ROOM.clear()
+        nws = _CHAIN_ROOM[n_seq, k, n] = L.hawk_verify_chains_workspace_bytes(n_seq, k, n)
+    ws = p_logits.new_empty((max(nws, 16),), dtype=_uint8())
+    out = p_logits.new_empty((n_seq * (k + 2),), dtype=i32)
+    count, toks = out[:n_seq], out[n_seq:].view(n_seq, k + 1)
+    rc = _call_on(dev, L.hawk_verify_chains, p_logits.data_ptr(), ps if p_rows > 1 else n, p_start.data_ptr() if p_start is not None else None, p_rows,
+                  q, qs, qr, draft.data_ptr(), n_draft.data_ptr() if n_draft is not None else None, u_acc.data_ptr(), u_final.data_ptr(),
+                  n_seq, k, n, temperature, top_k, count.data_ptr(), toks.data_ptr(), ws.data_ptr(), nws)
     if rc != 0:
         raise HawkError(rc, where)
     return count, toks
