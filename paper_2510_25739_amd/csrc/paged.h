@@ -6,35 +6,42 @@
 
 namespace hawk {
 
+// n / d for n below 2^31 and a d of the host's: with s = ceil(log2 d) and M = ceil(2^(31 + s) / d) < 2^32 the product n M / 2^(31 + s) is
+// above n / d by less than 1 / d.
+struct Divisor { unsigned magic; int shift, d; };   // shift < 0: d is one
+inline Divisor divisor(int d) {
+    int s = 0;
+    while ((1ll << s) < d) ++s;
+    return {(unsigned)(((1ull << (31 + s)) + d - 1) / d), s - 1, d};
+}
+__host__ __device__ inline int operator/(int n, const Divisor& d) {
+    if (d.shift < 0) return n;
+#if defined(__HIP_DEVICE_COMPILE__)
+    return (int)(__umulhi((unsigned)n, d.magic) >> d.shift);
+#else
+    return (int)((((uint64_t)(unsigned)n * d.magic) >> 32) >> d.shift);
+#endif
+}
+
 // One layer of a hawk_paged_cache as the kernels see it.
 struct PagedView {
     char *k, *v;                 // of the layer
     int64_t page_stride, head_stride, entry_stride;   // elements
     const int32_t* table;
     int64_t table_stride;
-    int n_pages, page_size, n_heads, hd, n_seq, max_pages;
-    unsigned magic;              // entry / page_size = umulhi(entry, magic) >> shift, shift < 0: entry itself
-    int shift;
+    int n_pages, page_size, n_heads, hd, n_seq, max_pages, capacity;   // capacity: entries of a sequence's pages
+    Divisor page;                // page_size
 };
 struct RowsView { const int32_t *row_start, *n_past; int rows; };
 struct HeadsView { char* data; int64_t row_stride, head_stride; int n_heads, dtype; };
 
-// entry / page_size for entries below 2^31: with s = ceil(log2 d) and M = ceil(2^(31 + s) / d) < 2^32 the product
-// e M / 2^(31 + s) is above e / d by less than 1 / d.
-__host__ __device__ inline int page_of(const PagedView& c, int e) {
-    if (c.shift < 0) return e;
-#if defined(__HIP_DEVICE_COMPILE__)
-    return (int)(__umulhi((unsigned)e, c.magic) >> c.shift);
-#else
-    return (int)((((uint64_t)(unsigned)e * c.magic) >> 32) >> c.shift);
-#endif
-}
+__host__ __device__ inline int page_of(const PagedView& c, int e) { return e / c.page; }
 // Elements from the layer's start to entry e (head 0), given its page; -1 if there is no such page.
 __host__ __device__ inline int64_t place_in(const PagedView& c, int page, int slot) {
     return page >= 0 && page < c.n_pages ? page * c.page_stride + slot * c.entry_stride : -1;
 }
 __host__ __device__ inline int64_t entry_at(const PagedView& c, const int32_t* table_row, int64_t e) {
-    if (e < 0 || e >= (int64_t)c.max_pages * c.page_size) return -1;
+    if (e < 0 || e >= c.capacity) return -1;
     const int p = page_of(c, (int)e);
     return place_in(c, table_row[p], (int)e - p * c.page_size);
 }

@@ -158,10 +158,8 @@ bool paged_view(const hawk_paged_cache* c, int layer, PagedView* out) {
     out->table = c->table; out->table_stride = c->table_stride;
     out->n_pages = c->n_pages; out->page_size = c->page_size; out->n_heads = c->n_heads; out->hd = c->head_dim;
     out->n_seq = c->n_seq; out->max_pages = c->max_pages;
-    int s = 0;
-    while ((1 << s) < c->page_size) ++s;
-    out->shift = s - 1;
-    out->magic = (unsigned)(((1ull << (31 + s)) + c->page_size - 1) / c->page_size);
+    out->capacity = c->max_pages * c->page_size;
+    out->page = divisor(c->page_size);
     return true;
 }
 

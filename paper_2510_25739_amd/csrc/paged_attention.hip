@@ -25,8 +25,9 @@ struct AttnArgs {
     HeadsView q, out;
     const uint64_t* tree;
     float scale2;              // scale * log2(e)
-    int group, tile, tiles;    // query heads of a cache head; rows of a tile, tiles of the launch
-    int splits, split_keys;    // parts of a long axis, entries of a part (the last one has the rest)
+    Divisor group, heads, splits;   // query heads of a cache head; cache heads; parts of a long axis
+    int tile, tiles;           // rows of a tile (2^tile), tiles of the launch
+    int split_keys;            // entries of a part (the last one has the rest)
     float *part, *part_ml;     // [split][row][head][hd], [split][row][head][2]
 };
 
@@ -45,8 +46,7 @@ __device__ __forceinline__ Span span_of(const AttnArgs& a, int s, int first, int
     t.r0 = min(max(start, 0), a.r.rows);
     t.n = max(min(max(stop, 0), a.r.rows) - t.r0, 0);
     t.past = min(max(past, -(1 << 30)), 1 << 30);
-    const int cap = a.c.max_pages * a.c.page_size;
-    const int lo = first / a.group, hi = min((first + a.tile - 1) / a.group, t.n - 1);
+    const int lo = first / a.group, hi = min((first + (1 << a.tile) - 1) / a.group, t.n - 1);
     if (a.tree) {
         t.end = t.past + max(min(t.n, 64), hi + 1);
         t.all = t.past;
@@ -54,14 +54,13 @@ __device__ __forceinline__ Span span_of(const AttnArgs& a, int s, int first, int
         t.end = t.past + hi + 1;
         t.all = t.past + lo + 1;
     }
-    t.end = max(min(t.end, cap), 0);
+    t.end = max(min(t.end, a.c.capacity), 0);
     return t;
 }
 // Tiles are counted so that a sequence's first tile follows from its first row alone: base(s) = row_start[s] * group / tile + s,
 // which leaves every sequence room for its tiles and at most one unused number per sequence.
 __device__ __forceinline__ int tile_base(const AttnArgs& a, int s, int start) {
-    const int64_t b = min(max(start, 0), a.r.rows);
-    return (int)(b * a.group / a.tile) + s;
+    return (min(max(start, 0), a.r.rows) * a.group.d >> a.tile) + s;   // (rows * group is below 2^30)
 }
 // The sequence of a tile and its span; false: the tile is one of the unused numbers.  Up to 64 sequences every lane has one
 // sequence's words, and the answer is there after one latency.
@@ -83,17 +82,16 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& a, int lane, int tile,
         stop = a.r.row_start[s + 1];
         past = a.r.n_past[s];
     }
-    t = span_of(a, s, (tile - tile_base(a, s, start)) * a.tile, start, stop, past);
-    return t.first < t.n * a.group;
+    t = span_of(a, s, (tile - tile_base(a, s, start)) << a.tile, start, stop, past);
+    return t.first < t.n * a.group.d;
 }
-// (Without branches a lane: with them a row's score of an entry that it does not see was once left as it was.)
-__device__ __forceinline__ bool sees(const AttnArgs& a, const Span& t, int own, unsigned long long bits, int e) {
+// What a row of a tree sees; a row of a chain sees the entries up to its own.
+__device__ __forceinline__ bool node_sees(const Span& t, int own, unsigned long long bits, int e) {
     const int j = e - t.past;
-    const bool chain = e <= own, node = (int)(j < 0) | (int)(e == own) | ((int)(j < 64) & (int)((bits >> (j & 63)) & 1ull));
-    return a.tree ? node : chain;
+    return (int)(j < 0) | (int)(e == own) | ((int)(j < 64) & (int)((bits >> (j & 63)) & 1ull));
 }
 __device__ __forceinline__ int used_splits(const AttnArgs& a, int end) {
-    return min(a.splits, max(1, (end + a.split_keys - 1) / a.split_keys));
+    return a.splits.shift < 0 ? 1 : min(a.splits.d, max(1, (end + a.split_keys - 1) / a.split_keys));
 }
 
 __device__ __forceinline__ float swap16(float v, bool add) {
@@ -109,7 +107,11 @@ __device__ __forceinline__ float swap32(float v, bool add) {
 __device__ __forceinline__ float row_max(float v) { return swap32(swap16(v, false), false); }   // over the four lanes of a row
 __device__ __forceinline__ float row_sum(float v) { return swap32(swap16(v, true), true); }
 
+// Values of a type as words: the products, and which words hold an infinity or NaN (any sign bit of carry(w) set) and as which
+// they are taken out.
 template <int TYPE> struct Of;
+template <class T> __device__ __forceinline__ unsigned carry(unsigned w) { return (w & T::kExp) + T::kCarry; }
+template <class T> __device__ __forceinline__ bool odd(unsigned carries) { return (carries & (T::kExp ^ (T::kExp << 1)) & 0x80008000u) != 0u; }
 template <> struct Of<HAWK_BF16> {
     static constexpr int kBytes = 2;
     static constexpr float kLift = 0.f;
@@ -118,7 +120,7 @@ template <> struct Of<HAWK_BF16> {
     }
     static __device__ __forceinline__ unsigned short narrow(float x) { return __builtin_bit_cast(unsigned short, (__bf16)x); }
     static __device__ __forceinline__ float widen(unsigned short b) { return __uint_as_float((unsigned)b << 16); }
-    static __device__ __forceinline__ bool odd(unsigned w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
+    static constexpr unsigned kExp = 0x7F807F80u, kCarry = 0x00800080u;   // an exponent of ones carries into the sign's place
     static __device__ __forceinline__ unsigned clear(unsigned w) {
         return ((w & 0x7F80u) == 0x7F80u ? 0u : w & 0xFFFFu) | ((w & 0x7F800000u) == 0x7F800000u ? 0u : w & 0xFFFF0000u);
     }
@@ -131,7 +133,7 @@ template <> struct Of<HAWK_FP16> {
     }
     static __device__ __forceinline__ unsigned short narrow(float x) { return __builtin_bit_cast(unsigned short, (_Float16)x); }
     static __device__ __forceinline__ float widen(unsigned short b) { return half_up(b); }
-    static __device__ __forceinline__ bool odd(unsigned w) { return (w & 0x7C00u) == 0x7C00u || (w & 0x7C000000u) == 0x7C000000u; }
+    static constexpr unsigned kExp = 0x7C007C00u, kCarry = 0x04000400u;
     static __device__ __forceinline__ unsigned clear(unsigned w) {
         return ((w & 0x7C00u) == 0x7C00u ? 0u : w & 0xFFFFu) | ((w & 0x7C000000u) == 0x7C000000u ? 0u : w & 0xFFFF0000u);
     }
@@ -145,8 +147,8 @@ template <> struct Of<HAWK_FP32> {
         for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[i]), __uint_as_float(b[i]), c, 0, 0, 0);
         return c;
     }
-    static __device__ __forceinline__ bool odd(unsigned w) { return (w & 0x7F800000u) == 0x7F800000u; }
-    static __device__ __forceinline__ unsigned clear(unsigned w) { return odd(w) ? 0u : w; }
+    static constexpr unsigned kExp = 0x7F800000u, kCarry = 0x00800000u;
+    static __device__ __forceinline__ unsigned clear(unsigned w) { return (w & kExp) == kExp ? 0u : w; }
 };
 
 // Infinities and NaN among the values of entries that only some rows of a tile see would make NaN of the others' weights of zero:
@@ -156,7 +158,7 @@ __device__ void add_odd(const AttnArgs& a, const Span& t, const char* vh, int ow
     const int32_t* pages = a.c.table + (int64_t)t.s * a.c.table_stride;
     for (int e = max(from, 0); e < to; ++e) {
         const int64_t at = entry_at(a.c, pages, e);
-        if (at < 0 || !sees(a, t, own, bits, e)) continue;
+        if (at < 0 || !(a.tree ? node_sees(t, own, bits, e) : e <= own)) continue;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             float v;
@@ -169,10 +171,12 @@ __device__ void add_odd(const AttnArgs& a, const Span& t, const char* vh, int ow
 
 // Tile of 16 rows, NW waves that share the entries of its part in turns of 32 (16 of fp32).  Keys and values go from the pages straight
 // into the operands' registers: a lane's 16 bytes of a key are its features of one product, and its piece of eight keys' values
-// - the same few features of each - become the transposed operand by pairing words of two keys.  A turn's keys are requested as soon
-// as the turn before has used its own, its values likewise.
-template <int TYPE, int DP, bool PAD, int NW>
-__global__ __launch_bounds__(64 * NW, DP <= 128 ? 8 / NW : 1) void paged_rows_kernel(AttnArgs a) {
+// - the same few features of each - become the transposed operand by pairing words of two keys.  The next turn's keys and values
+// are requested as soon as this turn's scores are there.
+// EASY: groups of 16 entries lie within a page, so that their page number is one for the wave; otherwise every lane looks its
+// entries up (16 sequences of six rows, 20 heads of 64, pages of 64 or of 60 entries: MEASURE).
+template <int TYPE, int DP, bool PAD, bool EASY, int NW>
+__global__ __launch_bounds__(64 * NW, DP == 64 ? (NW == 4 ? 3 : (TYPE == HAWK_FP32 ? 2 : 4)) : (DP == 128 ? 2 : 1)) void paged_rows_kernel(AttnArgs a) {
     using T = Of<TYPE>;
     constexpr int ES = T::kBytes, VEC = 16 / ES, STEP = 4 * VEC, NS = DP / STEP;   // features of a lane's piece, of a product; products
     constexpr int VD = DP / 16, VC = VD < VEC ? VD : VEC, NC = VD / VC;            // a lane's features of a value, per piece; pieces
@@ -184,11 +188,11 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 8 / NW : 1) void paged_rows_ke
     __shared__ int lodd[NW];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), m16 = lane & 15, g = lane >> 4;
-    const int head = blockIdx.x % a.c.n_heads, rest = blockIdx.x / a.c.n_heads;
-    const int split = rest % a.splits, tile = a.tiles - 1 - rest / a.splits;   // later tiles see more: they start first
+    const int rest = (int)blockIdx.x / a.heads, head = blockIdx.x - rest * a.heads.d, turned = rest / a.splits;
+    const int split = rest - turned * a.splits.d, tile = a.tiles - 1 - turned;   // later tiles see more: they start first
     Span t;
     if (!find_tile(a, lane, tile, t) || split >= used_splits(a, t.end)) return;
-    const int k0 = split * a.split_keys, k1 = split == a.splits - 1 ? t.end : min(t.end, k0 + a.split_keys);
+    const int k0 = split * a.split_keys, k1 = split == a.splits.d - 1 ? t.end : min(t.end, k0 + a.split_keys);
     const int hd = a.c.hd;
 
     // page numbers of 64 pages from `window` on, one per lane
@@ -199,8 +203,8 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 8 / NW : 1) void paged_rows_ke
 
     // this lane's row: its query, and what it sees
     const int pr = t.first + m16, i = pr / a.group;
-    const bool real = pr < t.n * a.group;
-    const int row = t.r0 + (real ? i : 0), qh = head * a.group + (real ? pr - i * a.group : 0);
+    const bool real = pr < t.n * a.group.d;
+    const int row = t.r0 + (real ? i : 0), qh = head * a.group.d + (real ? pr - i * a.group.d : 0);
     const int own = t.past + i;   // the row's own entry, the last one it sees of a chain
     const unsigned long long bits = a.tree && real ? a.tree[row] : 0ull;
     v4u q[NS];
@@ -211,10 +215,12 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 8 / NW : 1) void paged_rows_ke
         if (real && (!PAD || f < hd)) q[ks] = *reinterpret_cast<const v4u*>(a.q.data + ((int64_t)row * a.q.row_stride + (int64_t)qh * a.q.head_stride + f) * ES);
     }
 
-    // Places of a turn's entries: of the lane's keys, and of the four entries a group whose scores and values it has; -1: there is none.
-    // Groups of 16 entries within a page have their page number in common; otherwise every lane looks its entries up.
-    const bool easy = a.c.page_size % 16 == 0;
-    int64_t at[KT], vat[KT][4];
+    // Bytes from a head's start to a turn's groups of entries (EASY: of the group, in the wave's registers; otherwise of the lane's own
+    // entry) and which entries there are.  Ones that do not exist read the pool's first entry: their scores are dropped.
+    const int64_t es = a.c.entry_stride * ES;
+    const int64_t klane = (EASY ? m16 * es : 0) + g * 16, vlane = (EASY ? g * 4 * es : 0) + m16 * VC * ES;
+    int64_t at[KT];
+    bool there[KT];                     // (EASY: of the page; the turn's end counts apart)
     auto places = [&](int kb) {
         const int p0 = page_of(a.c, kb), p1 = page_of(a.c, min(kb + KEYS, k1) - 1);
         if (p0 < window || p1 >= window + 64) {
@@ -223,42 +229,37 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 8 / NW : 1) void paged_rows_ke
         }
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
-            const int e = kb + kt * 16;
-            if (easy) {
-                const int p = min(page_of(a.c, e), p1);
-                const int64_t b = place_in(a.c, __builtin_amdgcn_readlane(ids, p - window), e - p * a.c.page_size);
-                at[kt] = b >= 0 && e + m16 < k1 ? b + m16 * a.c.entry_stride : -1;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) vat[kt][r] = b >= 0 && e + g * 4 + r < k1 ? b + (g * 4 + r) * a.c.entry_stride : -1;
-            } else {
-                const int p = page_of(a.c, min(e + m16, k1 - 1));
-                const int64_t b = place_in(a.c, __shfl(ids, p - window), e + m16 - p * a.c.page_size);
-                at[kt] = e + m16 < k1 ? b : -1;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) vat[kt][r] = __shfl((long long)at[kt], g * 4 + r);
-            }
+            const int e = EASY ? kb + kt * 16 : min(kb + kt * 16 + m16, k1 - 1);
+            const int p = min(page_of(a.c, e), p1);   // (a group behind the end: any page)
+            const int id = EASY ? __builtin_amdgcn_readlane(ids, p - window) : __shfl(ids, p - window);
+            const int64_t x = place_in(a.c, id, e - p * a.c.page_size);
+            // a group's first entry at or behind the end, or a lane's own entry there: the pool's first one
+            there[kt] = x >= 0 && (EASY ? e < k1 : kb + kt * 16 + m16 < k1);
+            at[kt] = there[kt] ? x * ES : 0;
         }
     };
+    // EASY groups are read whole, past the end of the sequence too: the rest of the page is there, and dropped like any entry
+    // that does not exist.
     v4u k[KT][NS];
-    auto keys = [&] {   // (an entry that does not exist reads entry 0 of page 0: its score is dropped)
+    typedef unsigned piece __attribute__((ext_vector_type(VW)));
+    typedef piece pieces[KT][4][NC];
+    auto request = [&](pieces& v) {
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
-            const char* src = kh + (at[kt] < 0 ? 0 : at[kt]) * ES + g * 16;
+            const char* src = kh + at[kt] + (EASY && !there[kt] ? (int64_t)g * 16 : klane);
 #pragma unroll
             for (int ks = 0; ks < NS; ++ks) {
                 if (PAD && ks * STEP + g * VEC >= hd) k[kt][ks] = (v4u){0u, 0u, 0u, 0u};
                 else k[kt][ks] = *reinterpret_cast<const v4u*>(src + ks * STEP * ES);
             }
         }
-    };
-    typedef unsigned piece __attribute__((ext_vector_type(VW)));
-    piece v[KT][4][NC];
-    auto values = [&] {
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const char* src = vh + (vat[kt][r] < 0 ? 0 : vat[kt][r]) * ES + m16 * VC * ES;
+                const char* src;
+                if (EASY) src = vh + at[kt] + (there[kt] ? vlane + r * es : (int64_t)m16 * VC * ES);
+                else src = vh + __shfl((long long)at[kt], g * 4 + r) + vlane;
 #pragma unroll
                 for (int c = 0; c < NC; ++c) {
                     if (PAD && c * COLS + m16 * VC >= hd) v[kt][r][c] = (piece)0u;
@@ -271,51 +272,76 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 8 / NW : 1) void paged_rows_ke
 #pragma unroll
     for (int d = 0; d < VD; ++d) o[d] = (f32x4){0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
-    bool odd = false;
-    const int kfirst = k0 + KEYS * wave;
-    if (kfirst < k1) {
-        places(kfirst);
-        keys();
-        values();
-    }
-    for (int kb = kfirst; kb < k1; kb += KEYS * NW) {
+    bool found = false;   // values were taken out
+    auto turn = [&](int kb, pieces& v, pieces& vn) {
         float z[KT][4];
+        unsigned have = 0u;   // bit kt * 4 + r: entry g * 4 + r of group kt exists
         bool gone = false;
-        unsigned none = 0u;   // bit kt * 4 + r: no such entry
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
-            gone = gone || at[kt] < 0;
+            gone = gone || !there[kt];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) none |= vat[kt][r] < 0 ? 1u << (kt * 4 + r) : 0u;
+            for (int r = 0; r < 4; ++r) {
+                const int ok = EASY ? (int)there[kt] & (int)(kb + kt * 16 + g * 4 + r < k1) : __shfl((int)there[kt], g * 4 + r);
+                have |= ok ? 1u << (kt * 4 + r) : 0u;
+            }
             f32x4 sc = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int ks = 0; ks < NS; ++ks) sc = T::mul(k[kt][ks], q[ks], sc);
 #pragma unroll
             for (int r = 0; r < 4; ++r) z[kt][r] = sc[r] * a.scale2;
         }
-        const bool more = kb + KEYS * NW < k1;
-        if (more) {
+        if (kb + KEYS * NW < k1) {
             places(kb + KEYS * NW);
-            keys();
+            request(vn);
         }
         const bool edge = kb + KEYS > t.all;   // not every row sees every entry
-        if (edge || __any(gone)) {
+        if (edge || kb + KEYS > k1 || __any(gone)) {
+            const int e0 = kb + g * 4, last = real ? min(own, k1 - 1) : -1;
+            if (!a.tree) {
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) z[kt][r] = e0 + kt * 16 + r <= last ? z[kt][r] : -INFINITY;
+            } else {
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int e = e0 + kt * 16 + r, see = (int)real & (int)(e < k1) & (int)node_sees(t, own, bits, e);
+                        z[kt][r] = see ? z[kt][r] : -INFINITY;
+                    }
+            }
+            if (__any(gone)) {
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) z[kt][r] = (have >> (kt * 4 + r)) & 1u ? z[kt][r] : -INFINITY;
+            }
+            // Weights of zero do not meet infinities and NaN: those of entries behind the end or without a page are dropped, others wait
+            // for the rows that see them (add_odd).
+            unsigned any = 0u;
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const bool there = !((none >> (kt * 4 + r)) & 1u);
-                    const int see = (int)there & (int)real & (int)sees(a, t, own, bits, kb + kt * 16 + g * 4 + r);
-                    z[kt][r] = see ? z[kt][r] : -INFINITY;
+                for (int r = 0; r < 4; ++r)
 #pragma unroll
                     for (int c = 0; c < NC; ++c)
 #pragma unroll
-                        for (int x = 0; x < VW; ++x) {
-                            const unsigned w = there ? v[kt][r][c][x] : 0u, w0 = edge ? T::clear(w) : w;
-                            odd = (int)odd | (int)(w0 != w);
-                            v[kt][r][c][x] = w0;
-                        }
-                }
+                        for (int x = 0; x < VW; ++x) any |= carry<T>(v[kt][r][c][x]);
+            if (__any(odd<T>(any))) {
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const bool ok = (have >> (kt * 4 + r)) & 1u;
+#pragma unroll
+                        for (int c = 0; c < NC; ++c)
+#pragma unroll
+                            for (int x = 0; x < VW; ++x) v[kt][r][c][x] = ok && !edge ? v[kt][r][c][x] : T::clear(v[kt][r][c][x]);
+                    }
+                found = found || edge;
+            }
         }
         float top = m;
 #pragma unroll
@@ -367,7 +393,16 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 8 / NW : 1) void paged_rows_ke
                 o[d] = T::mul(w, ph, o[d]);
             }
         }
-        if (more) values();
+    };
+    int kb = k0 + KEYS * wave;
+    pieces va, vb;
+    if (kb < k1) {
+        places(kb);
+        request(va);
+    }
+    for (; kb < k1; kb += 2 * KEYS * NW) {
+        turn(kb, va, vb);
+        if (kb + KEYS * NW < k1) turn(kb + KEYS * NW, vb, va);
     }
 
     // the waves' parts: maximum and sum, then the results in rounds of COLS features
@@ -376,8 +411,7 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 8 / NW : 1) void paged_rows_ke
         lm[wave][m16] = m;
         ll[wave][m16] = l;
     }
-    odd = __any(odd);
-    if (lane == 0) lodd[wave] = odd;
+    if (lane == 0) lodd[wave] = found;
     __syncthreads();
     float mt = -INFINITY, lt = 0.f;
     bool any_odd = false;
@@ -390,7 +424,7 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 8 / NW : 1) void paged_rows_ke
 #pragma unroll
     for (int w = 0; w < NW; ++w) lt += ll[w][m16] * __builtin_amdgcn_exp2f(lm[w][m16] - base);
     const float mine = __builtin_amdgcn_exp2f(m - base);
-    const bool whole = a.splits == 1;
+    const bool whole = a.splits.d == 1;
     const float norm = whole ? (lt == 0.f ? 0.f : 1.f / lt) : 1.f;
     if (!whole && real && wave == 0 && g == 0) {
         float* ml = a.part_ml + (((int64_t)split * a.r.rows + row) * a.q.n_heads + qh) * 2;
@@ -408,7 +442,7 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 8 / NW : 1) void paged_rows_ke
         // eight features of a row per thread
         for (int u = threadIdx.x; u < kTile * (COLS / 8); u += 64 * NW) {
             const int rr = u / (COLS / 8), f = (u % (COLS / 8)) * 8, ff = c * COLS + f, prr = t.first + rr;
-            if (prr >= t.n * a.group || (PAD && ff >= hd)) continue;
+            if (prr >= t.n * a.group.d || (PAD && ff >= hd)) continue;
             float x[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -417,7 +451,7 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 8 / NW : 1) void paged_rows_ke
                 for (int w = 0; w < NW; ++w) x[e] += lo[w][rr][f + e];
             }
             const int ri = prr / a.group;
-            const int64_t orow = t.r0 + ri, oh = head * a.group + prr - ri * a.group;
+            const int64_t orow = t.r0 + ri, oh = head * a.group.d + prr - ri * a.group.d;
             if (any_odd) add_odd<TYPE, 8>(a, t, vh, t.past + ri, a.tree ? a.tree[orow] : 0ull, max(k0, t.all - KEYS), k1, ff, x);
             if (whole)
                 store8(a.out.data, orow * a.out.row_stride + oh * a.out.head_stride + ff, a.out.dtype, x);
@@ -455,28 +489,28 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void paged_wide_kernel(Attn
     __shared__ __attribute__((aligned(16))) char lk[2][KB * ROW];
     __shared__ __attribute__((aligned(16))) char lv[2][KB * ROW];
     __shared__ int flags[4];   // of the turns in flight: some entries do not exist
-    __shared__ int odd;        // infinities or NaN were taken out of values
+    __shared__ int found;      // infinities or NaN were taken out of values
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r32 = lane & 31, hh = lane >> 5;
-    const int head = blockIdx.x % a.c.n_heads, rest = blockIdx.x / a.c.n_heads;
-    const int split = rest % a.splits, tile = a.tiles - 1 - rest / a.splits;
+    const int rest = (int)blockIdx.x / a.heads, head = blockIdx.x - rest * a.heads.d, turned = rest / a.splits;
+    const int split = rest - turned * a.splits.d, tile = a.tiles - 1 - turned;
     Span t;
     if (!find_tile(a, lane, tile, t) || split >= used_splits(a, t.end)) return;
     const int first = t.first;
-    const int k0 = split * a.split_keys, k1 = split == a.splits - 1 ? t.end : min(t.end, k0 + a.split_keys);
+    const int k0 = split * a.split_keys, k1 = split == a.splits.d - 1 ? t.end : min(t.end, k0 + a.split_keys);
     const int hd = a.c.hd;
     if (tid < 4) flags[tid] = 0;
-    if (tid == 4) odd = 0;
+    if (tid == 4) found = 0;
 
     const int pr = first + wave * 32 + r32, i = pr / a.group;
-    const bool real = pr < t.n * a.group;
-    const int row = t.r0 + (real ? i : 0), qh = head * a.group + (real ? pr - i * a.group : 0);
+    const bool real = pr < t.n * a.group.d;
+    const int row = t.r0 + (real ? i : 0), qh = head * a.group.d + (real ? pr - i * a.group.d : 0);
     const int own = t.past + i;
     const unsigned long long bits = a.tree && real ? a.tree[row] : 0ull;
     // entries that every row of the wave sees lie before `all`, none sees any from `end` on
     const int wlo = (first + wave * 32) / a.group, whi = min((first + wave * 32 + 31) / a.group, t.n - 1);
     const int all = a.tree ? t.past : t.past + wlo + 1;
-    const int end = first + wave * 32 >= t.n * a.group ? 0 : (a.tree ? k1 : min(k1, t.past + whi + 1));
+    const int end = first + wave * 32 >= t.n * a.group.d ? 0 : (a.tree ? k1 : min(k1, t.past + whi + 1));
     v4u q[NS];
 #pragma unroll
     for (int ks = 0; ks < NS; ++ks) {
@@ -525,8 +559,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void paged_wide_kernel(Attn
             const int cv = DP == 64 ? chunk ^ (((r >> 1) & 1) << 2) : chunk ^ ((r & 3) << 2);
             if (e < k1 && (unsigned)page[j] >= (unsigned)a.c.n_pages) flags[turn & 3] = 1;
             v4u w = vr[j];
-            if (kb + KB > t.all && (T::odd(w[0]) || T::odd(w[1]) || T::odd(w[2]) || T::odd(w[3]))) {
-                odd = 1;
+            if (kb + KB > t.all && odd<T>(carry<T>(w[0]) | carry<T>(w[1]) | carry<T>(w[2]) | carry<T>(w[3]))) {
+                found = 1;
 #pragma unroll
                 for (int x = 0; x < 4; ++x) w[x] = T::clear(w[x]);
             }
@@ -570,14 +604,21 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void paged_wide_kernel(Attn
                 for (int e = 0; e < 16; ++e) z[u][e] = sc[e];
             }
             if (flag || kb + KB > all || kb + KB > k1) {
+                const int e0 = kb + 4 * hh, last = real ? min(own, k1 - 1) : -1;
+                if (!a.tree) {
 #pragma unroll
-                for (int u = 0; u < SUB; ++u)
+                    for (int u = 0; u < SUB; ++u)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int e = kb + u * 32 + 8 * (r >> 2) + 4 * hh + (r & 3);
-                        const int see = (int)real & (int)(e < k1) & (int)sees(a, t, own, bits, e);
-                        z[u][r] = see ? z[u][r] : -INFINITY;
-                    }
+                        for (int r = 0; r < 16; ++r) z[u][r] = e0 + u * 32 + 8 * (r >> 2) + (r & 3) <= last ? z[u][r] : -INFINITY;
+                } else {
+#pragma unroll
+                    for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const int e = e0 + u * 32 + 8 * (r >> 2) + (r & 3), see = (int)real & (int)(e < k1) & (int)node_sees(t, own, bits, e);
+                            z[u][r] = see ? z[u][r] : -INFINITY;
+                        }
+                }
                 if (flag) {
 #pragma unroll
                     for (int u = 0; u < SUB; ++u)
@@ -633,7 +674,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void paged_wide_kernel(Attn
 
     l = swap32(l, true);
     if (!real) return;
-    const bool whole = a.splits == 1;
+    const bool whole = a.splits.d == 1;
     const float norm = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
     const int64_t vec = ((int64_t)split * a.r.rows + row) * a.q.n_heads + qh;
     if (!whole && hh == 0) {
@@ -649,7 +690,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void paged_wide_kernel(Attn
             float x[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = o[d][4 * b + e] * norm;
-            if (odd) add_odd<TYPE, 4>(a, t, vh, own, bits, max(k0, t.all - KB), k1, f, x);
+            if (found) add_odd<TYPE, 4>(a, t, vh, own, bits, max(k0, t.all - KB), k1, f, x);
             if (whole) store4(a.out.data, (int64_t)row * a.out.row_stride + (int64_t)qh * a.out.head_stride + f, a.out.dtype, x);
             else store4(reinterpret_cast<char*>(a.part), vec * hd + f, HAWK_FP32, x);
         }
@@ -666,7 +707,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a, int lanes) 
     if (s < 0) return;
     const int start = a.r.row_start[s], stop = a.r.row_start[s + 1];
     if (row >= stop) return;
-    const Span t = span_of(a, s, ((row - max(start, 0)) * a.group + qh % a.group) / a.tile * a.tile, start, stop, a.r.n_past[s]);
+    const Span t = span_of(a, s, ((row - max(start, 0)) * a.group.d + (qh - qh / a.group * a.group.d)) >> a.tile << a.tile, start, stop, a.r.n_past[s]);
     const int n = used_splits(a, t.end);
     const int64_t step = (int64_t)a.r.rows * a.q.n_heads, vec = (int64_t)row * a.q.n_heads + qh;
     const int f = (lane & (lanes - 1)) * 8, part0 = lane / lanes, per = 64 / lanes;
@@ -698,7 +739,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a, int lanes) 
     store8(a.out.data, (int64_t)row * a.out.row_stride + (int64_t)qh * a.out.head_stride + f, a.out.dtype, x);
 }
 
-struct Plan { bool wide; int tiles, splits, split_keys; size_t part_bytes, ml_bytes; };
+struct Plan { bool wide; int waves, tiles, splits, split_keys; size_t part_bytes, ml_bytes; };
 
 // How a call is cut.  Sequences of many rows on average take the kernel that shares entries through LDS.  Parts of the long axis where
 // the tiles alone would leave most of the chip's 256 units idle.
@@ -707,8 +748,10 @@ Plan plan_of(int dtype, int n_seq, int rows, int n_heads, int n_q_heads, int hd,
     const int group = n_q_heads / n_heads;
     p.wide = dtype != HAWK_FP32 && (int64_t)rows * group >= 64 * (int64_t)n_seq;
     p.tiles = (int)((int64_t)rows * group / (p.wide ? kWide : kTile)) + n_seq;
-    const int64_t len = max_len < 1 || max_len > capacity ? capacity : max_len, blocks = (int64_t)p.tiles * n_heads;
-    int64_t parts = (p.wide ? 512 : 1024) / (blocks < 1 ? 1 : blocks);
+    // workgroups if the sequences are alike; the numbers that no tile has end at once
+    const int size = p.wide ? kWide : kTile, each = n_seq > 0 ? (int)(((int64_t)rows * group + n_seq - 1) / n_seq) : 0;
+    const int64_t len = max_len < 1 || max_len > capacity ? capacity : max_len, blocks = (int64_t)((each + size - 1) / size) * n_seq * n_heads;
+    int64_t parts = (p.wide || len <= 2048 ? 512 : 1024) / (blocks < 1 ? 1 : blocks);
     const int64_t most = len / 512;
     if (parts > most) parts = most;
     if (parts > 64) parts = 64;
@@ -718,6 +761,7 @@ Plan plan_of(int dtype, int n_seq, int rows, int n_heads, int n_q_heads, int hd,
     p.splits = (int)((len + keys - 1) / keys);
     if (p.splits < 1) p.splits = 1;
     p.split_keys = (int)keys;
+    p.waves = blocks * p.splits <= (hd <= 64 ? 512 : 256) ? 8 : 4;
     const size_t vectors = p.splits > 1 ? (size_t)p.splits * rows * n_q_heads : 0;
     p.part_bytes = (vectors * hd * sizeof(float) + 15) / 16 * 16;
     p.ml_bytes = (vectors * 2 * sizeof(float) + 15) / 16 * 16;
@@ -729,18 +773,17 @@ bool shape_ok(const PagedView& c, int rows, int n_q_heads) {
            ((int64_t)rows * (n_q_heads / c.n_heads) / kTile + c.n_seq) * c.n_heads <= (1 << 23);
 }
 
-template <int TYPE> void launch_typed(const AttnArgs& a, unsigned grid, hipStream_t stream) {
+template <int TYPE, int DP, int NW> void launch_rows(const AttnArgs& a, unsigned grid, hipStream_t stream) {
+    const bool easy = a.c.page_size % 16 == 0, exact = a.c.hd == DP;
+    auto kern = !easy ? paged_rows_kernel<TYPE, DP, true, false, NW>
+                      : (exact ? paged_rows_kernel<TYPE, DP, false, true, NW> : paged_rows_kernel<TYPE, DP, true, true, NW>);
+    kern<<<grid, 64 * NW, 0, stream>>>(a);
+}
+template <int TYPE> void launch_typed(const AttnArgs& a, int waves, unsigned grid, hipStream_t stream) {
     const int hd = a.c.hd;
-    if (hd <= 64) {
-        if (hd == 64) paged_rows_kernel<TYPE, 64, false, 4><<<grid, 256, 0, stream>>>(a);
-        else paged_rows_kernel<TYPE, 64, true, 4><<<grid, 256, 0, stream>>>(a);
-    } else if (hd <= 128) {
-        if (hd == 128) paged_rows_kernel<TYPE, 128, false, 4><<<grid, 256, 0, stream>>>(a);
-        else paged_rows_kernel<TYPE, 128, true, 4><<<grid, 256, 0, stream>>>(a);
-    } else {
-        if (hd == 256) paged_rows_kernel<TYPE, 256, false, 4><<<grid, 256, 0, stream>>>(a);
-        else paged_rows_kernel<TYPE, 256, true, 4><<<grid, 256, 0, stream>>>(a);
-    }
+    if (hd > 128) launch_rows<TYPE, 256, 4>(a, grid, stream);
+    else if (hd > 64) waves == 8 ? launch_rows<TYPE, 128, 8>(a, grid, stream) : launch_rows<TYPE, 128, 4>(a, grid, stream);
+    else waves == 8 ? launch_rows<TYPE, 64, 8>(a, grid, stream) : launch_rows<TYPE, 64, 4>(a, grid, stream);
 }
 
 template <int TYPE> void launch_wide(const AttnArgs& a, unsigned grid, hipStream_t stream) {
@@ -778,18 +821,20 @@ int launch_paged_attention(const hawk_paged_cache* cache, int layer, const hawk_
     if (workspace_bytes < p.part_bytes + p.ml_bytes) return p.part_bytes ? HAWK_ENOMEM : HAWK_EINVAL;
     a.tree = tree;
     a.scale2 = scale * 1.44269504f;
-    a.group = a.q.n_heads / a.c.n_heads;
-    a.tile = p.wide ? kWide : kTile;
-    a.tiles = p.tiles; a.splits = p.splits; a.split_keys = p.split_keys;
+    a.group = divisor(a.q.n_heads / a.c.n_heads);
+    a.heads = divisor(a.c.n_heads);
+    a.splits = divisor(p.splits);
+    a.tile = p.wide ? 7 : 4;
+    a.tiles = p.tiles; a.split_keys = p.split_keys;
     a.part = static_cast<float*>(workspace);
     a.part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.part_bytes);
     const int64_t grid = (int64_t)p.tiles * p.splits * a.c.n_heads;
     if (grid > (1 << 23)) return HAWK_EINVAL;
     if (p.wide && cache->dtype == HAWK_BF16) launch_wide<HAWK_BF16>(a, (unsigned)grid, stream);
     else if (p.wide) launch_wide<HAWK_FP16>(a, (unsigned)grid, stream);
-    else if (cache->dtype == HAWK_FP32) launch_typed<HAWK_FP32>(a, (unsigned)grid, stream);
-    else if (cache->dtype == HAWK_BF16) launch_typed<HAWK_BF16>(a, (unsigned)grid, stream);
-    else launch_typed<HAWK_FP16>(a, (unsigned)grid, stream);
+    else if (cache->dtype == HAWK_FP32) launch_typed<HAWK_FP32>(a, p.waves, (unsigned)grid, stream);
+    else if (cache->dtype == HAWK_BF16) launch_typed<HAWK_BF16>(a, p.waves, (unsigned)grid, stream);
+    else launch_typed<HAWK_FP16>(a, p.waves, (unsigned)grid, stream);
     if (p.splits > 1) {
         const int64_t units = (int64_t)a.r.rows * a.q.n_heads;
         int lanes = 1;
