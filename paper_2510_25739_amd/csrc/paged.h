@@ -107,9 +107,11 @@ __device__ __forceinline__ void widen2(unsigned w, int dtype, float& a, float& b
     }
 }
 __device__ __forceinline__ unsigned narrow2(float a, float b, int dtype) {   // to nearest, ties to even
-    if (dtype == HAWK_BF16)
-        return (unsigned)__builtin_bit_cast(unsigned short, (__bf16)a) | ((unsigned)__builtin_bit_cast(unsigned short, (__bf16)b) << 16);
-    return (unsigned)__builtin_bit_cast(unsigned short, (_Float16)a) | ((unsigned)__builtin_bit_cast(unsigned short, (_Float16)b) << 16);
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    const f2 v = {a, b};
+    return dtype == HAWK_BF16 ? __builtin_bit_cast(unsigned, __builtin_convertvector(v, b2)) : __builtin_bit_cast(unsigned, __builtin_convertvector(v, h2));
 }
 __device__ __forceinline__ void load4(const char* base, int64_t at, int dtype, float* x) {
     if (dtype == HAWK_FP32) {

@@ -55,6 +55,7 @@ __device__ __forceinline__ Span span_of(const AttnArgs& a, int s, int first, int
         t.all = t.past + lo + 1;
     }
     t.end = max(min(t.end, a.c.capacity), 0);
+    t.all = min(t.all, t.end);
     return t;
 }
 // Tiles are counted so that a sequence's first tile follows from its first row alone: base(s) = row_start[s] * group / tile + s,
@@ -89,6 +90,25 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& a, int lane, int tile,
 __device__ __forceinline__ bool node_sees(const Span& t, int own, unsigned long long bits, int e) {
     const int j = e - t.past;
     return (int)(j < 0) | (int)(e == own) | ((int)(j < 64) & (int)((bits >> (j & 63)) & 1ull));
+}
+// Which of the 64 entries from e0 on a row sees, as bits: those before k1, of a chain up to its own, of a tree also by its ancestors' bits.
+// One word a turn, so that a score costs a constant shift and a merge.
+__device__ __forceinline__ unsigned long long first_bits(int n) { return n <= 0 ? 0ull : (n >= 64 ? ~0ull : (1ull << n) - 1ull); }
+__device__ __forceinline__ unsigned long long seen_from(const AttnArgs& a, const Span& t, bool real, int own, unsigned long long bits, int e0, int k1) {
+    unsigned long long w;
+    if (a.tree) {
+        const int j = e0 - t.past, m = own - e0;
+        w = j >= 0 ? (j < 64 ? bits >> j : 0ull) : (j > -64 ? bits << -j : 0ull) | first_bits(-j);
+        w |= m >= 0 && m < 64 ? 1ull << m : 0ull;
+    } else {
+        w = first_bits(own - e0 + 1);
+    }
+    return real ? w & first_bits(k1 - e0) : 0ull;
+}
+// z where bit c of the word is set, else minus infinity
+__device__ __forceinline__ float if_seen(unsigned long long w, int c, float z) {
+    const unsigned on = (unsigned)(((int)((unsigned)(w >> (c & 32)) << (31 - (c & 31)))) >> 31);
+    return __uint_as_float((on & __float_as_uint(z)) | (~on & 0xFF800000u));
 }
 __device__ __forceinline__ int used_splits(const AttnArgs& a, int end) {
     return a.splits.shift < 0 ? 1 : min(a.splits.d, max(1, (end + a.split_keys - 1) / a.split_keys));
@@ -152,19 +172,28 @@ template <> struct Of<HAWK_FP32> {
 };
 
 // Infinities and NaN among the values of entries that only some rows of a tile see would make NaN of the others' weights of zero:
-// they are zeros in the products, and come to the rows that see them at the end: N features from f on of a row's result.
+// they are zeros in the products, and are added, behind everything else, to results of rows that see them, where these have been
+// stored: N features from f on of a row, at dst.
 template <int TYPE, int N>
-__device__ void add_odd(const AttnArgs& a, const Span& t, const char* vh, int own, unsigned long long bits, int from, int to, int f, float* x) {
+__device__ void add_odd(const AttnArgs& a, const Span& t, const char* vh, int own, unsigned long long bits, int from, int to, int f, char* dst,
+                        int64_t at, int dtype) {
     const int32_t* pages = a.c.table + (int64_t)t.s * a.c.table_stride;
     for (int e = max(from, 0); e < to; ++e) {
-        const int64_t at = entry_at(a.c, pages, e);
-        if (at < 0 || !(a.tree ? node_sees(t, own, bits, e) : e <= own)) continue;
-#pragma unroll
+        const int64_t place = entry_at(a.c, pages, e);
+        if (place < 0 || !(a.tree ? node_sees(t, own, bits, e) : e <= own)) continue;
         for (int j = 0; j < N; ++j) {
             float v;
-            if constexpr (TYPE == HAWK_FP32) v = *reinterpret_cast<const float*>(vh + (at + f + j) * 4);
-            else v = Of<TYPE>::widen(*reinterpret_cast<const unsigned short*>(vh + (at + f + j) * 2));
-            if (!(fabsf(v) <= 3.4028235e38f)) x[j] += v;
+            if constexpr (TYPE == HAWK_FP32) v = *reinterpret_cast<const float*>(vh + (place + f + j) * 4);
+            else v = Of<TYPE>::widen(*reinterpret_cast<const unsigned short*>(vh + (place + f + j) * 2));
+            if (fabsf(v) <= 3.4028235e38f) continue;
+            if (dtype == HAWK_FP32) {
+                *reinterpret_cast<float*>(dst + (at + j) * 4) += v;
+            } else {
+                unsigned short* p = reinterpret_cast<unsigned short*>(dst + (at + j) * 2);
+                float x, y;
+                widen2(*p, dtype, x, y);
+                *p = (unsigned short)narrow2(x + v, 0.f, dtype);
+            }
         }
     }
 }
@@ -297,21 +326,11 @@ __global__ __launch_bounds__(64 * NW, DP == 64 ? (NW == 4 ? 3 : (TYPE == HAWK_FP
         }
         const bool edge = kb + KEYS > t.all;   // not every row sees every entry
         if (edge || kb + KEYS > k1 || __any(gone)) {
-            const int e0 = kb + g * 4, last = real ? min(own, k1 - 1) : -1;
-            if (!a.tree) {
+            const unsigned long long w = seen_from(a, t, real, own, bits, kb + g * 4, k1);
 #pragma unroll
-                for (int kt = 0; kt < KT; ++kt)
+            for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) z[kt][r] = e0 + kt * 16 + r <= last ? z[kt][r] : -INFINITY;
-            } else {
-#pragma unroll
-                for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int e = e0 + kt * 16 + r, see = (int)real & (int)(e < k1) & (int)node_sees(t, own, bits, e);
-                        z[kt][r] = see ? z[kt][r] : -INFINITY;
-                    }
-            }
+                for (int r = 0; r < 4; ++r) z[kt][r] = if_seen(w, kt * 16 + r, z[kt][r]);
             if (__any(gone)) {
 #pragma unroll
                 for (int kt = 0; kt < KT; ++kt)
@@ -452,11 +471,11 @@ __global__ __launch_bounds__(64 * NW, DP == 64 ? (NW == 4 ? 3 : (TYPE == HAWK_FP
             }
             const int ri = prr / a.group;
             const int64_t orow = t.r0 + ri, oh = head * a.group.d + prr - ri * a.group.d;
-            if (any_odd) add_odd<TYPE, 8>(a, t, vh, t.past + ri, a.tree ? a.tree[orow] : 0ull, max(k0, t.all - KEYS), k1, ff, x);
-            if (whole)
-                store8(a.out.data, orow * a.out.row_stride + oh * a.out.head_stride + ff, a.out.dtype, x);
-            else
-                store8(reinterpret_cast<char*>(a.part), (((int64_t)split * a.r.rows + orow) * a.q.n_heads + oh) * hd + ff, HAWK_FP32, x);
+            char* dst = whole ? a.out.data : reinterpret_cast<char*>(a.part);
+            const int64_t at = whole ? orow * a.out.row_stride + oh * a.out.head_stride + ff : (((int64_t)split * a.r.rows + orow) * a.q.n_heads + oh) * hd + ff;
+            const int type = whole ? a.out.dtype : HAWK_FP32;
+            store8(dst, at, type, x);
+            if (any_odd) add_odd<TYPE, 8>(a, t, vh, t.past + ri, a.tree ? a.tree[orow] : 0ull, max(k0, t.all - KEYS), k1, ff, dst, at, type);
         }
     }
 }
@@ -482,16 +501,18 @@ template <> struct Wide<HAWK_FP16> {
 };
 constexpr float kLag = 8.f;   // results are rescaled when a row's maximum has grown by more than 2^8, not whenever it grows
 
-template <int TYPE, int DP, bool PAD, int KB>
-__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void paged_wide_kernel(AttnArgs a) {
+// EASY as above: a wave's part of a turn's rows lies in one group of 16, whose place is found once for the wave and added to by the
+// requests themselves.
+template <int TYPE, int DP, bool PAD, bool EASY, int KB, int NW>
+__global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void paged_wide_kernel(AttnArgs a) {
     using T = Of<TYPE>;
-    constexpr int ROW = DP * 2, CH = ROW / 16, PIECES = KB * CH / 256, NS = DP / 16, NT = DP / 32, SUB = KB / 32;
+    constexpr int ROW = DP * 2, CH = ROW / 16, TH = 64 * NW, PIECES = KB * CH / TH, NS = DP / 16, NT = DP / 32, SUB = KB / 32;
     __shared__ __attribute__((aligned(16))) char lk[2][KB * ROW];
     __shared__ __attribute__((aligned(16))) char lv[2][KB * ROW];
-    __shared__ int flags[4];   // of the turns in flight: some entries do not exist
+    __shared__ unsigned gone[4][SUB];   // of the turns in flight: which entries do not exist
     __shared__ int found;      // infinities or NaN were taken out of values
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r32 = lane & 31, hh = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r32 = lane & 31, hh = lane >> 5;
     const int rest = (int)blockIdx.x / a.heads, head = blockIdx.x - rest * a.heads.d, turned = rest / a.splits;
     const int split = rest - turned * a.splits.d, tile = a.tiles - 1 - turned;
     Span t;
@@ -499,8 +520,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void paged_wide_kernel(Attn
     const int first = t.first;
     const int k0 = split * a.split_keys, k1 = split == a.splits.d - 1 ? t.end : min(t.end, k0 + a.split_keys);
     const int hd = a.c.hd;
-    if (tid < 4) flags[tid] = 0;
-    if (tid == 4) found = 0;
+    if (tid < 4 * SUB) gone[0][tid] = 0u;
+    if (tid == 0) found = 0;
 
     const int pr = first + wave * 32 + r32, i = pr / a.group;
     const bool real = pr < t.n * a.group.d;
@@ -527,45 +548,71 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void paged_wide_kernel(Attn
 
     const int32_t* pages = a.c.table + (int64_t)t.s * a.c.table_stride;
     const char *kh = a.c.k + (int64_t)head * a.c.head_stride * 2, *vh = a.c.v + (int64_t)head * a.c.head_stride * 2;
-    // pieces of a turn that this thread brings: piece j is 16 bytes of row (tid + 256 j) / CH
+    // pieces of a turn that this thread brings: piece j is 16 bytes of row (tid + TH j) / CH
     const int chunk = tid % CH;
-    int page[PIECES];
+    const bool inside = !PAD || chunk * 8 < hd;
+    int page[PIECES];           // EASY: of the wave's group; -1: behind the end
     v4u kr[PIECES], vr[PIECES];
     auto look_up = [&](int kb) {
 #pragma unroll
         for (int j = 0; j < PIECES; ++j) {
-            const int e = kb + (tid + 256 * j) / CH;
+            const int e = kb + (EASY ? (wave * 64 + TH * j) / CH & ~15 : (tid + TH * j) / CH);
             page[j] = e < k1 ? pages[page_of(a.c, e)] : -1;
+            if (EASY) page[j] = __builtin_amdgcn_readfirstlane(page[j]);
         }
     };
     auto request = [&](int kb) {
 #pragma unroll
         for (int j = 0; j < PIECES; ++j) {
-            const int e = kb + (tid + 256 * j) / CH;
-            const int64_t at = e < k1 ? place_in(a.c, page[j], e - page_of(a.c, e) * a.c.page_size) : -1;
             kr[j] = vr[j] = (v4u){0u, 0u, 0u, 0u};
-            if (at >= 0 && (!PAD || chunk * 8 < hd)) {
-                kr[j] = *reinterpret_cast<const v4u*>(kh + at * 2 + chunk * 16);
-                vr[j] = *reinterpret_cast<const v4u*>(vh + at * 2 + chunk * 16);
+            if (EASY) {
+                const int e = kb + ((wave * 64 + TH * j) / CH & ~15);
+                const int64_t at = place_in(a.c, page[j], e - page_of(a.c, e) * a.c.page_size) * 2;
+                if (at >= 0) {
+                    const unsigned off = (unsigned)((tid + TH * j) / CH & 15) * (unsigned)(a.c.entry_stride * 2) + chunk * 16;
+                    if (inside) {
+                        kr[j] = *reinterpret_cast<const v4u*>(kh + at + off);
+                        vr[j] = *reinterpret_cast<const v4u*>(vh + at + off);
+                    }
+                }
+            } else {
+                const int e = kb + (tid + TH * j) / CH;
+                const int64_t at = e < k1 ? place_in(a.c, page[j], e - page_of(a.c, e) * a.c.page_size) : -1;
+                if (at >= 0 && inside) {
+                    kr[j] = *reinterpret_cast<const v4u*>(kh + at * 2 + chunk * 16);
+                    vr[j] = *reinterpret_cast<const v4u*>(vh + at * 2 + chunk * 16);
+                }
             }
         }
     };
     auto put = [&](int kb, int turn) {
-        char *dk = lk[turn & 1], *dv = lv[turn & 1];
+        const int buffer = (turn & 1) * (KB * ROW);
 #pragma unroll
         for (int j = 0; j < PIECES; ++j) {
-            const int r = (tid + 256 * j) / CH, e = kb + r;
-            const int ck = DP == 64 ? chunk ^ ((r >> 1) & 7) : chunk ^ (r & 15);
-            const int cv = DP == 64 ? chunk ^ (((r >> 1) & 1) << 2) : chunk ^ ((r & 3) << 2);
-            if (e < k1 && (unsigned)page[j] >= (unsigned)a.c.n_pages) flags[turn & 3] = 1;
-            v4u w = vr[j];
-            if (kb + KB > t.all && odd<T>(carry<T>(w[0]) | carry<T>(w[1]) | carry<T>(w[2]) | carry<T>(w[3]))) {
+            const int r = EASY ? (wave * 64 + TH * j) / CH & ~15 : (tid + TH * j) / CH;
+            if (kb + r < k1 && (unsigned)page[j] >= (unsigned)a.c.n_pages) atomicOr(&gone[turn & 3][r >> 5], (EASY ? 0xFFFFu : 1u) << (r & 31));
+        }
+        if (kb + KB > t.all) {   // not every row sees every entry
+            unsigned any = 0u;
+#pragma unroll
+            for (int j = 0; j < PIECES; ++j)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) any |= carry<T>(vr[j][x]);
+            if (odd<T>(any)) {
                 found = 1;
 #pragma unroll
-                for (int x = 0; x < 4; ++x) w[x] = T::clear(w[x]);
+                for (int j = 0; j < PIECES; ++j)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) vr[j][x] = T::clear(vr[j][x]);
             }
-            *reinterpret_cast<v4u*>(dk + r * ROW + ck * 16) = kr[j];
-            *reinterpret_cast<v4u*>(dv + r * ROW + cv * 16) = w;
+        }
+#pragma unroll
+        for (int j = 0; j < PIECES; ++j) {
+            const int r = (tid + TH * j) / CH;
+            const int ck = DP == 64 ? chunk ^ ((r >> 1) & 7) : chunk ^ (r & 15);
+            const int cv = DP == 64 ? chunk ^ (((r >> 1) & 1) << 2) : chunk ^ ((r & 3) << 2);
+            *reinterpret_cast<v4u*>(lk[0] + buffer + r * ROW + ck * 16) = kr[j];
+            *reinterpret_cast<v4u*>(lv[0] + buffer + r * ROW + cv * 16) = vr[j];
         }
     };
 
@@ -574,7 +621,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void paged_wide_kernel(Attn
     if (turns > 0) {
         look_up(k0);
         request(k0);
-        __syncthreads();   // flags are clear
+        __syncthreads();   // gone is clear
         put(k0, 0);
         look_up(k0 + KB);
         request(k0 + KB);
@@ -586,9 +633,11 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void paged_wide_kernel(Attn
     const float c = a.scale2;
     for (int turn = 0; turn < turns; ++turn) {
         const int kb = k0 + turn * KB;
-        const int flag = flags[turn & 3];
+        unsigned none[SUB], some = 0u;
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) some |= none[u] = gone[turn & 3][u];
         if (kb < end) {
-            const char *bk = lk[turn & 1], *bv = lv[turn & 1];
+            const char *bk = lk[0] + (turn & 1) * (KB * ROW), *bv = lv[0] + (turn & 1) * (KB * ROW);
             float z[SUB][16];
 #pragma unroll
             for (int u = 0; u < SUB; ++u) {
@@ -603,29 +652,13 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void paged_wide_kernel(Attn
 #pragma unroll
                 for (int e = 0; e < 16; ++e) z[u][e] = sc[e];
             }
-            if (flag || kb + KB > all || kb + KB > k1) {
-                const int e0 = kb + 4 * hh, last = real ? min(own, k1 - 1) : -1;
-                if (!a.tree) {
+            if (some || kb + KB > all || kb + KB > k1) {
+                unsigned long long w = seen_from(a, t, real, own, bits, kb + 4 * hh, k1);
+                w &= ~(((unsigned long long)none[0] | (SUB > 1 ? (unsigned long long)none[SUB - 1] << 32 : 0ull)) >> (4 * hh));
 #pragma unroll
-                    for (int u = 0; u < SUB; ++u)
+                for (int u = 0; u < SUB; ++u)
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) z[u][r] = e0 + u * 32 + 8 * (r >> 2) + (r & 3) <= last ? z[u][r] : -INFINITY;
-                } else {
-#pragma unroll
-                    for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            const int e = e0 + u * 32 + 8 * (r >> 2) + (r & 3), see = (int)real & (int)(e < k1) & (int)node_sees(t, own, bits, e);
-                            z[u][r] = see ? z[u][r] : -INFINITY;
-                        }
-                }
-                if (flag) {
-#pragma unroll
-                    for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            z[u][r] = entry_at(a.c, pages, kb + u * 32 + 8 * (r >> 2) + 4 * hh + (r & 3)) >= 0 ? z[u][r] : -INFINITY;
-                }
+                    for (int r = 0; r < 16; ++r) z[u][r] = if_seen(w, u * 32 + 8 * (r >> 2) + (r & 3), z[u][r]);
             }
             float top = -INFINITY;
 #pragma unroll
@@ -668,7 +701,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void paged_wide_kernel(Attn
             look_up(kb + 2 * KB);
             request(kb + 2 * KB);
         }
-        if (tid == 0) flags[(turn + 3) & 3] = 0;   // the turn before this one's: nobody looks at it any more
+        if (tid < SUB) gone[(turn + 3) & 3][tid] = 0u;   // the turn before this one's: nobody looks at it any more
         __syncthreads();
     }
 
@@ -681,6 +714,9 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void paged_wide_kernel(Attn
         a.part_ml[vec * 2] = mb;
         a.part_ml[vec * 2 + 1] = l;
     }
+    char* dst = whole ? a.out.data : reinterpret_cast<char*>(a.part);
+    const int64_t at = whole ? (int64_t)row * a.out.row_stride + (int64_t)qh * a.out.head_stride : vec * hd;
+    const int type = whole ? a.out.dtype : HAWK_FP32;
 #pragma unroll
     for (int d = 0; d < NT; ++d)
 #pragma unroll
@@ -690,10 +726,10 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void paged_wide_kernel(Attn
             float x[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = o[d][4 * b + e] * norm;
-            if (found) add_odd<TYPE, 4>(a, t, vh, own, bits, max(k0, t.all - KB), k1, f, x);
-            if (whole) store4(a.out.data, (int64_t)row * a.out.row_stride + (int64_t)qh * a.out.head_stride + f, a.out.dtype, x);
-            else store4(reinterpret_cast<char*>(a.part), vec * hd + f, HAWK_FP32, x);
+            store4(dst, at + f, type, x);
         }
+    if (found)
+        for (int f = 4 * hh; f < hd; f += 8) add_odd<TYPE, 4>(a, t, vh, own, bits, max(k0, t.all - KB), k1, f, dst, at + f, type);
 }
 
 // Joins the parts of a long axis: a wave per (row, head).  Lane i has part i's maximum and sum; groups of lanes take a part's features each,
@@ -786,14 +822,16 @@ template <int TYPE> void launch_typed(const AttnArgs& a, int waves, unsigned gri
     else waves == 8 ? launch_rows<TYPE, 64, 8>(a, grid, stream) : launch_rows<TYPE, 64, 4>(a, grid, stream);
 }
 
+template <int TYPE, int DP, int KB, int NW> void launch_wide_of(const AttnArgs& a, unsigned grid, hipStream_t stream) {
+    const bool easy = a.c.page_size % 16 == 0 && a.c.entry_stride <= (1 << 24), exact = a.c.hd == DP;
+    auto kern = !easy ? paged_wide_kernel<TYPE, DP, true, false, KB, NW>
+                      : (exact ? paged_wide_kernel<TYPE, DP, false, true, KB, NW> : paged_wide_kernel<TYPE, DP, true, true, KB, NW>);
+    kern<<<grid, 64 * NW, 0, stream>>>(a);
+}
 template <int TYPE> void launch_wide(const AttnArgs& a, unsigned grid, hipStream_t stream) {
-    const int hd = a.c.hd;
-    if (hd == 64) paged_wide_kernel<TYPE, 64, false, 64><<<grid, 256, 0, stream>>>(a);
-    else if (hd < 64) paged_wide_kernel<TYPE, 64, true, 64><<<grid, 256, 0, stream>>>(a);
-    else if (hd == 128) paged_wide_kernel<TYPE, 128, false, 64><<<grid, 256, 0, stream>>>(a);
-    else if (hd < 128) paged_wide_kernel<TYPE, 128, true, 64><<<grid, 256, 0, stream>>>(a);
-    else if (hd == 256) paged_wide_kernel<TYPE, 256, false, 32><<<grid, 256, 0, stream>>>(a);
-    else paged_wide_kernel<TYPE, 256, true, 32><<<grid, 256, 0, stream>>>(a);
+    if (a.c.hd > 128) launch_wide_of<TYPE, 256, 32, 4>(a, grid, stream);
+    else if (a.c.hd > 64) launch_wide_of<TYPE, 128, 64, 4>(a, grid, stream);
+    else launch_wide_of<TYPE, 64, 64, 4>(a, grid, stream);
 }
 
 }  // namespace
