@@ -775,7 +775,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a, int lanes) 
     store8(a.out.data, (int64_t)row * a.out.row_stride + (int64_t)qh * a.out.head_stride + f, a.out.dtype, x);
 }
 
-struct Plan { bool wide; int waves, tiles, splits, split_keys; size_t part_bytes, ml_bytes; };
+struct Plan { bool wide; int tile, waves, tiles, splits, split_keys; size_t part_bytes, ml_bytes; };
 
 // How a call is cut.  Sequences of many rows on average take the kernel that shares entries through LDS.  Parts of the long axis where
 // the tiles alone would leave most of the chip's 256 units idle.
@@ -783,9 +783,10 @@ Plan plan_of(int dtype, int n_seq, int rows, int n_heads, int n_q_heads, int hd,
     Plan p;
     const int group = n_q_heads / n_heads;
     p.wide = dtype != HAWK_FP32 && (int64_t)rows * group >= 64 * (int64_t)n_seq;
-    p.tiles = (int)((int64_t)rows * group / (p.wide ? kWide : kTile)) + n_seq;
+    p.tile = !p.wide ? 4 : ((int64_t)rows * group >= 512 * (int64_t)n_seq && hd <= 128 ? 8 : 7);
+    p.tiles = (int)((int64_t)rows * group >> p.tile) + n_seq;
     // workgroups if the sequences are alike; the numbers that no tile has end at once
-    const int size = p.wide ? kWide : kTile, each = n_seq > 0 ? (int)(((int64_t)rows * group + n_seq - 1) / n_seq) : 0;
+    const int size = 1 << p.tile, each = n_seq > 0 ? (int)(((int64_t)rows * group + n_seq - 1) / n_seq) : 0;
     const int64_t len = max_len < 1 || max_len > capacity ? capacity : max_len, blocks = (int64_t)((each + size - 1) / size) * n_seq * n_heads;
     int64_t parts = (p.wide || len <= 2048 ? 512 : 1024) / (blocks < 1 ? 1 : blocks);
     const int64_t most = len / 512;
@@ -830,8 +831,8 @@ template <int TYPE, int DP, int KB, int NW> void launch_wide_of(const AttnArgs& 
 }
 template <int TYPE> void launch_wide(const AttnArgs& a, unsigned grid, hipStream_t stream) {
     if (a.c.hd > 128) launch_wide_of<TYPE, 256, 32, 4>(a, grid, stream);
-    else if (a.c.hd > 64) launch_wide_of<TYPE, 128, 64, 4>(a, grid, stream);
-    else launch_wide_of<TYPE, 64, 64, 4>(a, grid, stream);
+    else if (a.c.hd > 64) a.tile == 8 ? launch_wide_of<TYPE, 128, 64, 8>(a, grid, stream) : launch_wide_of<TYPE, 128, 64, 4>(a, grid, stream);
+    else a.tile == 8 ? launch_wide_of<TYPE, 64, 64, 8>(a, grid, stream) : launch_wide_of<TYPE, 64, 64, 4>(a, grid, stream);
 }
 
 }  // namespace
@@ -862,7 +863,7 @@ int launch_paged_attention(const hawk_paged_cache* cache, int layer, const hawk_
     a.group = divisor(a.q.n_heads / a.c.n_heads);
     a.heads = divisor(a.c.n_heads);
     a.splits = divisor(p.splits);
-    a.tile = p.wide ? 7 : 4;
+    a.tile = p.tile;
     a.tiles = p.tiles; a.split_keys = p.split_keys;
     a.part = static_cast<float*>(workspace);
     a.part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.part_bytes);
