@@ -497,7 +497,8 @@ int hawk_paged_append(const hawk_paged_cache* cache, int layer, const hawk_paged
  * ancestors of hawk_tree_layout) and its own.  A row that sees nothing (or whose every score is minus infinity) gives zeros.  What
  * a row does not see has no part in its result, whatever values it holds.
  * q of the cache's type; out of any of the three types, not overlapping q.  Scores, maximum, sums and results in
- * fp32; the weights reach the products with about 16 bits for rows of few, with the type's own for many (see below).
+ * fp32; the weights reach the products of 16-bit types with about 16 bits where sequences have few rows, rounded to the type
+ * where they have many (64 rows times group and more, behind long sequences).
  * scale > 0.  max_len (host): the longest n_past + rows of a sequence, for the choice of the kernel only: any value
  * gives the right results (at most max_pages * page_size is assumed).
  * workspace (may be NULL where the size function says 0; 16-byte aligned): hawk_paged_attention_workspace_bytes

@@ -17,7 +17,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 
-constexpr int kTile = 16, kWide = 128;   // rows of a tile where a sequence has few, many
+constexpr int kTile = 16;      // rows of a tile where a sequence has few (many: 128 or 256)
 
 struct AttnArgs {
     PagedView c;
@@ -480,7 +480,7 @@ __global__ __launch_bounds__(64 * NW, DP == 64 ? (NW == 4 ? 3 : (TYPE == HAWK_FP
     }
 }
 
-// Many rows: a workgroup of four waves, 32 rows each, over turns of KB entries that all of them read from LDS.  The next
+// Many rows: a workgroup of four or eight waves, 32 rows each, over turns of KB entries that all of them read from LDS.  The next
 // turn's keys and values are in registers while this one is computed and are written behind it, two buffers, one barrier a
 // turn.  Products of 32 x 32 x 16: a lane has one row's 16 scores of 32 entries - blocks of four entries, the other half of the
 // wave the blocks between -, which in that order are the next product's operand; values are read transposed.
@@ -777,17 +777,24 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a, int lanes) 
 
 struct Plan { bool wide; int tile, waves, tiles, splits, split_keys; size_t part_bytes, ml_bytes; };
 
-// How a call is cut.  Sequences of many rows on average take the kernel that shares entries through LDS.  Parts of the long axis where
-// the tiles alone would leave most of the chip's 256 units idle.
+// How a call is cut.
+// Tiles of 16 rows read a sequence's entries once for every 16 rows, but are there after 8 us; tiles of 128 through LDS want 64 rows a
+// sequence (rows times query heads of a cache head) and some work.  16-row tiles times entries, 8 sequences, us for tiles of
+// 16 / 128 rows: 32 heads of 128 on 8, 64 rows behind 300 entries (154 thousand) 12.7 / 18.3, 128 rows (307 thousand) 23.5 / 18.7, 32 behind
+// 2000 (1 million) 44.6 / 44.2, 64 (2 million) 88.4 / 54.1; 20 heads of 64, 64 rows behind 300 (192 thousand) 12.8 / 12.3, behind 2000 49.4 / 39.2.
+// Tiles of 256 rows halve what is brought and put, but eight waves meet at every barrier: 4001 rows x 4 behind 2048 292 us, in
+// tiles of 128 337; 8 sequences of 512 rows x 4 behind 2000 199 / 223, of 256 rows x 4 142 / 110.
+// Parts of the long axis where the tiles alone would leave most of the chip's 256 units idle.
 Plan plan_of(int dtype, int n_seq, int rows, int n_heads, int n_q_heads, int hd, int64_t capacity, int max_len) {
     Plan p;
-    const int group = n_q_heads / n_heads;
-    p.wide = dtype != HAWK_FP32 && (int64_t)rows * group >= 64 * (int64_t)n_seq;
-    p.tile = !p.wide ? 4 : ((int64_t)rows * group >= 512 * (int64_t)n_seq && hd <= 128 ? 8 : 7);
+    const int group = n_q_heads / n_heads, each = n_seq > 0 ? (int)(((int64_t)rows * group + n_seq - 1) / n_seq) : 0;
+    const int64_t len = max_len < 1 || max_len > capacity ? capacity : max_len;
+    p.wide = dtype != HAWK_FP32 && each >= 64 && (int64_t)((each + kTile - 1) / kTile) * n_seq * n_heads * len >= 300000;
+    p.tile = !p.wide ? 4 : (each >= 2048 && hd <= 128 ? 8 : 7);
     p.tiles = (int)((int64_t)rows * group >> p.tile) + n_seq;
     // workgroups if the sequences are alike; the numbers that no tile has end at once
-    const int size = 1 << p.tile, each = n_seq > 0 ? (int)(((int64_t)rows * group + n_seq - 1) / n_seq) : 0;
-    const int64_t len = max_len < 1 || max_len > capacity ? capacity : max_len, blocks = (int64_t)((each + size - 1) / size) * n_seq * n_heads;
+    const int size = 1 << p.tile;
+    const int64_t blocks = (int64_t)((each + size - 1) / size) * n_seq * n_heads;
     int64_t parts = (p.wide || len <= 2048 ? 512 : 1024) / (blocks < 1 ? 1 : blocks);
     const int64_t most = len / 512;
     if (parts > most) parts = most;
@@ -836,6 +843,12 @@ template <int TYPE> void launch_wide(const AttnArgs& a, unsigned grid, hipStream
 }
 
 }  // namespace
+
+// log2 of a tile's rows * 10000 + waves of a workgroup * 100 + parts: the dispatch's rules, for the tests as well.
+extern "C" int hawk_paged_attention_plan(int dtype, int n_seq, int rows, int n_heads, int n_q_heads, int hd, int capacity, int max_len) {
+    const Plan p = plan_of(dtype, n_seq, rows, n_heads, n_q_heads, hd, capacity, max_len);
+    return p.tile * 10000 + (p.wide ? (p.tile == 8 ? 8 : 4) : (hd > 128 ? 4 : p.waves)) * 100 + p.splits;
+}
 
 size_t paged_attention_workspace_bytes(const hawk_paged_cache* cache, int rows, int n_q_heads, int max_len) {
     PagedView c;

@@ -91,22 +91,28 @@ def attention_reference(su, q, seen, scale):
     q = q.double()
     out, mag, err = torch.zeros(q.shape, dtype=torch.float64), torch.zeros(q.shape, dtype=torch.float64), torch.zeros(total, heads, 1, dtype=torch.float64)
     group = heads // su.hk
-    for s in range(len(su.rows)):
-        for i in range(su.rows[s]):
-            r = int(su.start_np[s]) + i
-            es = [e for e in range(su.past[s] + su.rows[s]) if seen(s, i, e) and su.where(s, e)[0] >= 0]
-            if not es:
-                continue
-            k, v = su.K[s][es], su.V[s][es]
-            for h in range(heads):
-                z = (k[:, h // group] @ q[r, h]) * scale
-                w = torch.exp(z - z.max())
-                w = w / w.sum()
-                out[r, h] = w @ v[:, h // group]
-                mag[r, h] = w @ v[:, h // group].abs()
-                # hd products and their sum, the scale and its product with log2(e), the difference to the maximum
-                err[r, h] = ((hd + 6) * 2.0 ** -24 * (k[:, h // group].abs() @ q[r, h].abs()) * scale).max()
+    for s, n in enumerate(su.rows):
+        if n == 0:
+            continue
+        there = [su.where(s, e)[0] >= 0 for e in range(su.past[s] + n)]
+        see = torch.tensor([[ok and bool(seen(s, i, e)) for e, ok in enumerate(there)] for i in range(n)])
+        some = see.any(1)
+        r = slice(int(su.start_np[s]), int(su.start_np[s]) + n)
+        for h in range(heads):
+            k, v, x = su.K[s][:, h // group], su.V[s][:, h // group], q[r, h]
+            z = (x @ k.T * scale).masked_fill(~see, float("-inf"))
+            w = torch.softmax(z.masked_fill(~some[:, None], 0.0), -1) * some[:, None]
+            out[r, h], mag[r, h] = w @ v, w @ v.abs()
+            # hd products and their sum, the scale and its product with log2(e), the difference to the maximum
+            err[r, h, 0] = ((hd + 6) * 2.0 ** -24 * scale * (x.abs() @ k.abs().T) * see).amax(-1)
     return out, mag, err
+
+
+def plan(H, su, heads, max_len=0):
+    """(rows of a tile, waves, parts) of an attention of the setup's rows."""
+    t = H.load_library().hawk_paged_attention_plan({"fp32": 0, "bf16": 1, "fp16": 2}[su.cache_t], len(su.rows), su.total, su.hk, heads, su.hd,
+                                                   su.table_np.shape[1] * su.page, max_len)
+    return 1 << (t // 10000), t // 100 % 100, t % 100
 
 
 def check_attention(su, got, want, out_type, weight_step, note=""):
@@ -126,10 +132,10 @@ def check_attention(su, got, want, out_type, weight_step, note=""):
     assert fine, worst
 
 
-def weight_step(cache, rows=0, sequences=1):
-    """Rounding of the weights: with 64 rows and query heads of a cache head or more a sequence once, otherwise twice - half steps
-    of 2^-8 and 2^-11, squared (2^-20: the remainder of a half is subnormal at times)."""
-    if cache != "fp32" and rows >= 64 * sequences:
+def weight_step(cache, tile=16):
+    """Rounding of the weights: once in tiles of more than 16 rows, otherwise twice - half steps of 2^-8 and 2^-11, squared (2^-20:
+    the remainder of a half is subnormal at times)."""
+    if tile > 16:
         return half_step(cache)
     return {"fp32": 0.0, "bf16": 2.0 ** -16, "fp16": 2.0 ** -20}[cache]
 
@@ -167,19 +173,37 @@ ATTEND = [
 @pytest.mark.parametrize("order", ["heads", "entries"])
 @pytest.mark.parametrize("cache,heads,kv_heads,hd,page,rows,past", ATTEND)
 def test_chains_attend(H, cache, heads, kv_heads, hd, page, rows, past, order):
+    # a table with room for many more entries: without a hint the kernel is the one for long sequences, where that is another
     import torch
-    su = Setup(H, hd * 7 + page + sum(rows), cache, kv_heads, hd, page, rows, past, order=order)
+    su = Setup(H, hd * 7 + page + sum(rows), cache, kv_heads, hd, page, rows, past, order=order, spare=400000 // page + 1)
     su.fill()
     q = su.randn(su.total, heads, hd)
-    got = su.cache.attend(q.to(DEV), su.row_start, su.n_past, max_len=max(p + n for p, n in zip(past, rows)))
     want = attention_reference(su, q, lambda s, i, e: e <= past[s] + i, hd ** -0.5)
-    step = weight_step(cache, su.total * heads // kv_heads, len(rows))
-    check_attention(su, got, want, cache, step)
-    # the hint chooses the kernel, not the result's meaning; another type of result
-    got = su.cache.attend(q.to(DEV), su.row_start, su.n_past, out=torch.empty(q.shape, dtype=torch.float32, device=DEV))
-    check_attention(su, got, want, "fp32", step)
-    got = su.cache.attend(q.to(DEV), su.row_start, su.n_past, max_len=1, out=torch.empty(q.shape, dtype=torch.float32, device=DEV))
-    check_attention(su, got, want, "fp32", step)
+    most = max(p + n for p, n in zip(past, rows))
+    for max_len, out_type in ((most, cache), (0, "fp32"), (1, "fp32")):      # the hint chooses the kernel, nothing else
+        got = su.cache.attend(q.to(DEV), su.row_start, su.n_past, max_len=max_len, out=torch.full(q.shape, 9.0, dtype=dt(out_type), device=DEV))
+        check_attention(su, got, want, out_type, weight_step(cache, plan(H, su, heads, max_len)[0]), str(plan(H, su, heads, max_len)))
+
+
+WHOLE = [   # many sequences of many rows: tiles of 128 and 256 rows whose entries are not in parts
+    ("bf16", 8, 8, 64, 16, [70, 64, 90, 100] * 9, [300, 3, 0, 77] * 9, 128),
+    ("fp16", 32, 8, 128, 32, [40, 33, 16, 20] * 9, [100, 330, 0, 31] * 9, 128),
+    ("bf16", 8, 8, 96, 7, [70, 64, 90, 100] * 9, [300, 3, 0, 77] * 9, 128),
+    ("fp16", 8, 8, 200, 16, [70, 64, 90, 100] * 9, [300, 3, 0, 77] * 9, 128),
+    ("fp16", 16, 1, 64, 16, [150, 131] * 10, [40, 0] * 10, 256),
+    ("bf16", 32, 2, 128, 24, [150, 131] * 7, [40, 0] * 7, 256),
+    ("bf16", 32, 2, 80, 16, [150, 131] * 7, [40, 0] * 7, 256),
+]
+
+
+@pytest.mark.parametrize("cache,heads,kv_heads,hd,page,rows,past,tile", WHOLE)
+def test_many_rows_of_many_sequences_attend(H, cache, heads, kv_heads, hd, page, rows, past, tile):
+    su = Setup(H, hd + page, cache, kv_heads, hd, page, rows, past, spare=3000 // page)
+    su.fill()
+    q = su.randn(su.total, heads, hd)
+    assert plan(H, su, heads)[0] == tile and (plan(H, su, heads)[2] == 1 or tile == 256)
+    got = su.cache.attend(q.to(DEV), su.row_start, su.n_past)
+    check_attention(su, got, attention_reference(su, q, lambda s, i, e: e <= past[s] + i, hd ** -0.5), cache, weight_step(cache, tile))
 
 
 @pytest.mark.parametrize("cache,heads,kv_heads,hd,page,past,trees", [
@@ -187,12 +211,13 @@ def test_chains_attend(H, cache, heads, kv_heads, hd, page, rows, past, order):
     ("fp16", 2, 2, 128, 8, [100], [(5, 2)]),
     ("fp32", 3, 3, 48, 6, [7, 30], [(1, 1, 1, 1), (63,)]),
     ("bf16", 8, 1, 128, 32, [1200], [(4, 3)]),
+    ("fp16", 8, 1, 64, 16, [45, 0, 130], [(63,), (5, 5), (3, 3, 3)]),
 ])
 def test_trees_attend(H, cache, heads, kv_heads, hd, page, past, trees):
     import torch
     layout = [H.tree_layout(t) for t in trees]
     rows = [len(l[0]) for l in layout]
-    su = Setup(H, hd + page, cache, kv_heads, hd, page, rows, past)
+    su = Setup(H, hd + page, cache, kv_heads, hd, page, rows, past, spare=400000 // page)
     su.fill()
     anc = np.concatenate([l[3] for l in layout])
     q = su.randn(su.total, heads, hd)
@@ -201,8 +226,10 @@ def test_trees_attend(H, cache, heads, kv_heads, hd, page, past, trees):
     def seen(s, i, e):
         return e < past[s] or e == past[s] + i or bool((int(anc[su.start_np[s] + i]) >> (e - past[s])) & 1)
 
-    got = su.cache.attend(q.to(DEV), su.row_start, su.n_past, tree=tree)
-    check_attention(su, got, attention_reference(su, q, seen, hd ** -0.5), cache, weight_step(cache, su.total * heads // kv_heads, len(rows)))
+    want = attention_reference(su, q, seen, hd ** -0.5)
+    for max_len in (0, max(p + n for p, n in zip(past, rows))):
+        got = su.cache.attend(q.to(DEV), su.row_start, su.n_past, tree=tree, max_len=max_len)
+        check_attention(su, got, want, cache, weight_step(cache, plan(H, su, heads, max_len)[0]), str(plan(H, su, heads, max_len)))
 
 
 def test_a_row_that_sees_nothing_gives_zeros(H):
@@ -222,13 +249,16 @@ def test_a_row_that_sees_nothing_gives_zeros(H):
 def test_tree_rows_past_the_sixty_fourth_see_the_first_sixty_four(H):
     import torch
     past, n = 10, 80
-    su = Setup(H, 3, "fp16", 2, 64, 16, [n], [past])
+    su = Setup(H, 3, "fp16", 2, 64, 16, [n], [past], spare=20000)
     su.fill()
     q = su.randn(n, 2, 64)
     anc = np.array([(0x9E3779B97F4A7C15 * (i + 1)) & 0xFFFFFFFFFFFFFFFF for i in range(n)], dtype=np.uint64)
-    got = su.cache.attend(q.to(DEV), su.row_start, su.n_past, tree=torch.from_numpy(anc.view(np.int64)).to(DEV))
+    tree = torch.from_numpy(anc.view(np.int64)).to(DEV)
     want = attention_reference(su, q, lambda s, i, e: e < past or e == past + i or (e - past < 64 and bool((int(anc[i]) >> (e - past)) & 1)), 64 ** -0.5)
-    check_attention(su, got, want, "fp16", weight_step("fp16", n))
+    assert plan(H, su, 2)[0] == 128
+    for max_len in (0, past + n):
+        got = su.cache.attend(q.to(DEV), su.row_start, su.n_past, tree=tree, max_len=max_len)
+        check_attention(su, got, want, "fp16", weight_step("fp16", plan(H, su, 2, max_len)[0]))
 
 
 @pytest.mark.parametrize("cache", ["bf16", "fp16", "fp32"])
@@ -239,7 +269,8 @@ def test_values_a_row_does_not_see_have_no_part(H, cache, page, heads):
     # get what the formula gives
     import torch
     past, n, hd, group = 37, 9, 64, heads // 2      # 24 heads: nine rows are 108 of a cache head
-    su = Setup(H, 5, cache, 2, hd, page, [n], [past])
+    su = Setup(H, 5, cache, 2, hd, page, [n], [past], spare=200000)
+    assert plan(H, su, heads)[0] == (128 if heads == 24 and cache != "fp32" else 16)
     su.fill()
     q = su.randn(n, heads, hd)
     want = attention_reference(su, q, lambda s, i, e: e <= past + i, hd ** -0.5)
@@ -260,33 +291,35 @@ def test_values_a_row_does_not_see_have_no_part(H, cache, page, heads):
     assert bool(out[8, group:].isnan().all())
     o, m, er = want
     keep = lambda t: torch.where(clean, t, torch.zeros((), dtype=torch.float64))
-    check_attention(su, keep(out), (keep(o), m, er), cache, weight_step(cache, n * group))
+    check_attention(su, keep(out), (keep(o), m, er), cache, weight_step(cache, plan(H, su, heads)[0]))
 
 
-def test_entries_without_a_page_are_not_attended(H):
+@pytest.mark.parametrize("page,heads", [(8, 2), (16, 2), (8, 64), (16, 64)])
+def test_entries_without_a_page_are_not_attended(H, page, heads):
     import torch
-    past, n, hd = 90, 3, 64
-    su = Setup(H, 8, "bf16", 2, hd, 8, [n, n], [past, past], spare=3)
+    past, n, hd = 11 * page + 2, 3, 64
+    su = Setup(H, 8, "bf16", 2, hd, page, [n, n], [past, past], spare=60000)
+    assert plan(H, su, heads)[0] == (128 if heads == 64 else 16)
+    step = weight_step("bf16", plan(H, su, heads)[0])
     su.table_np[0, 2] = -1
     su.table_np[1, 5] = su.n_pages          # behind the pool
     su.table_np[1, 0] = 2 ** 31 - 1
     su.table.copy_(torch.from_numpy(su.table_np))
     su.table_np[1, 5] = su.table_np[1, 0] = -1     # for the reference
     su.fill()
-    q = su.randn(2 * n, 2, hd)
+    q = su.randn(2 * n, heads, hd)
     got = su.cache.attend(q.to(DEV), su.row_start, su.n_past)
-    check_attention(su, got, attention_reference(su, q, lambda s, i, e: e <= past + i, hd ** -0.5), "bf16", weight_step("bf16"))
+    check_attention(su, got, attention_reference(su, q, lambda s, i, e: e <= past + i, hd ** -0.5), "bf16", step)
     # lengths beyond the table: what exists is attended, rows whose own entry does not exist among them
     su.n_past.fill_(2 ** 31 - 5)
-    got2 = su.cache.attend(q.to(DEV), su.row_start, su.n_past)
-    su.past = [su.table_np.shape[1] * 8 - n] * 2
-    su.K = [torch.cat([k, torch.zeros(su.past[0] + n - len(k), 2, hd, dtype=torch.float64)]) for k in su.K]
-    su.V = [torch.cat([k, torch.zeros(su.past[0] + n - len(k), 2, hd, dtype=torch.float64)]) for k in su.V]
-    last_page = -(-(past + n) // 8) * 8
+    exist = -(-(past + n) // page) * page
+    su.past = [exist - n] * 2
+    su.K = [torch.cat([k, torch.zeros(exist - len(k), 2, hd, dtype=torch.float64)]) for k in su.K]
+    su.V = [torch.cat([k, torch.zeros(exist - len(k), 2, hd, dtype=torch.float64)]) for k in su.V]
     su.k.nan_to_num_(0.0)
     su.v.nan_to_num_(0.0)
-    got2 = su.cache.attend(q.to(DEV), su.row_start, su.n_past)
-    check_attention(su, got2, attention_reference(su, q, lambda s, i, e: e < last_page, hd ** -0.5), "bf16", weight_step("bf16"))
+    got = su.cache.attend(q.to(DEV), su.row_start, su.n_past)
+    check_attention(su, got, attention_reference(su, q, lambda s, i, e: True, hd ** -0.5), "bf16", step)
     su.n_past.fill_(-1000)                  # nothing committed, no entry of the step's own
     assert bool((su.cache.attend(q.to(DEV), su.row_start, su.n_past) == 0).all())
 
