@@ -21,90 +21,152 @@ struct AppendArgs {
     HeadsView q, k, v, q_out;
     const float *q_gain, *k_gain, *rot;
     const int32_t* pos;
-    float eps;
+    float eps, inv_hd;
     int n_pos, rot_dim, pairs;
-    int lanes, per_block, blocks;   // lanes of a vector (a power of two), vectors of a workgroup, workgroups of a row
+    int lanes, per_block;           // lanes of a vector (2^lanes), vectors that a workgroup's lanes take side by side
+    Divisor blocks;                 // workgroups of a row
 };
 
-// Block (part of a row's vectors, row); a vector - one head of q, k or v - belongs to `lanes` neighbouring lanes of one wave,
-// eight elements each, so that its sum of squares is a few lane swaps and its bytes are one request.  Every lane reads
-// its elements' partners of the rotation itself where they are half a vector away: they are in the same lines.
+template <int TYPE> struct Bytes { static constexpr int n = TYPE == HAWK_FP32 ? 4 : 2; };
+
+// Sum over 2^n neighbouring lanes, the same value in each: quad permutes and mirrors inside a row of 16, a swap beyond it.
+template <int CTRL> __device__ __forceinline__ float moved(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float sum_of_lanes(float v, int n) {
+    if (n > 0) v += moved<0xB1>(v);    // quad_perm [1,0,3,2]
+    if (n > 1) v += moved<0x4E>(v);    // quad_perm [2,3,0,1]
+    if (n > 2) v += moved<0x141>(v);   // row_half_mirror
+    if (n > 3) v += moved<0x140>(v);   // row_mirror
+    if (n > 4) v += __shfl_xor(v, 16);
+    return v;
+}
+
+// Block (vectors of a row, U rows); a vector - one head of q, k or v - belongs to 2^lanes neighbouring lanes of one wave, eight elements
+// each, so that its sum of squares is a few lane moves and its bytes are one request.  Every lane reads its elements' partners
+// of the rotation itself where they are half a vector away: they are in the same lines.  Three dependent latencies (row
+// starts, lengths, table and rotation) stand against a few hundred bytes, and what a lane works out about its vector - where it comes
+// from and goes to, its gains - holds for every row, so a lane of a large call takes U of them.  4048 rows of 32 + 16 heads of 128,
+// norms and rotation: MEASURE us (MEASURE TB/s of what is read and written), with one row a lane MEASURE.
+template <int U, int FROM, int TO>   // rows a lane; types
 __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
-    const int row = blockIdx.x / a.blocks, part = blockIdx.x - row * a.blocks;
-    const int lane = threadIdx.x & 63, e0 = (threadIdx.x & (a.lanes - 1)) * 8, hd = a.c.hd;
-    const int vec = part * a.per_block + (int)threadIdx.x / a.lanes;
-    const int nq = a.q.n_heads, nk = a.c.n_heads;
-    const int what = vec < nq ? 0 : (vec < nq + nk ? 1 : 2), head = vec - (what == 0 ? 0 : (what == 1 ? nq : nq + nk));
-    const bool mine = vec < nq + 2 * nk && e0 < hd;
-    const HeadsView& src = what == 0 ? a.q : (what == 1 ? a.k : a.v);
-    const int64_t at = (int64_t)row * src.row_stride + (int64_t)head * src.head_stride;
-    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (mine) load8(src.data, at + e0, src.dtype, x);
-
-    const int s = last_not_above(a.c.n_seq, lane, row, [&](int i) { return (int64_t)a.r.row_start[i]; });
-    if (s < 0 || row >= a.r.row_start[s + 1]) return;   // in no sequence
-    const int64_t entry = (int64_t)a.r.n_past[s] + (row - a.r.row_start[s]);
-    const float2* cs = nullptr;
-    if (a.rot) {
-        const int64_t p = a.pos ? (int64_t)a.pos[row] : entry;
-        if (p < 0 || p >= a.n_pos) return;
-        cs = reinterpret_cast<const float2*>(a.rot) + p * (a.rot_dim >> 1);
-    }
-    const int64_t place = entry_at(a.c, a.c.table + s * a.c.table_stride, entry);
-
-    const float* gain = what == 0 ? a.q_gain : (what == 1 ? a.k_gain : nullptr);
-    float rs = 1.f;
-    if (gain) {
-        float ss = 0.f;
+    const int group = (int)blockIdx.x / a.blocks, part = blockIdx.x - group * a.blocks.d, row0 = group * U;
+    const int lane = threadIdx.x & 63, e0 = (threadIdx.x & ((1 << a.lanes) - 1)) * 8, hd = a.c.hd;
+    const int nq = a.q.n_heads, nk = a.c.n_heads, half = a.rot_dim >> 1;   // half: a multiple of four, so four elements' partners are four in a row
+    const int vec = part * a.per_block + ((int)threadIdx.x >> a.lanes), what = vec < nq ? 0 : (vec < nq + nk ? 1 : 2);
+    const int head = vec - (what == 0 ? 0 : (what == 1 ? nq : nq + nk));
+    const bool mine = vec < nq + 2 * nk && e0 < hd, turned = a.rot && what < 2 && e0 < a.rot_dim, apart = turned && a.pairs;
+    int other[2] = {e0, e0 + 4}, at_table[2] = {e0 >> 1, (e0 >> 1) + 2};   // partners' elements; rows of the table (pairs side by side: one piece)
+    float sign[2] = {1.f, 1.f};
+    if (apart) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
-        for (int m = 1; m < a.lanes; m <<= 1) ss += __shfl_xor(ss, m);
-        rs = 1.f / sqrtf(ss / (float)hd + a.eps);
-        if (mine) {
-            float g[8];
-            load8(reinterpret_cast<const char*>(gain), e0, HAWK_FP32, g);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = x[i] * rs * g[i];
+        for (int g = 0; g < 2; ++g) {
+            const bool low = e0 + 4 * g < half;
+            other[g] += low ? half : -half;
+            at_table[g] = low ? e0 + 4 * g : other[g];
+            sign[g] = low ? -1.f : 1.f;
         }
     }
-    if (cs && what < 2 && mine && e0 < a.rot_dim) {
-        if (a.pairs == 0) {
+    const HeadsView& src = what == 0 ? a.q : (what == 1 ? a.k : a.v);
+    const char* from = src.data + (int64_t)head * src.head_stride * Bytes<FROM>::n;
+    const int64_t from_step = src.row_stride * Bytes<FROM>::n;
+    char* to = what == 0 ? a.q_out.data + (int64_t)head * a.q_out.head_stride * Bytes<TO>::n
+                         : (what == 1 ? a.c.k : a.c.v) + (int64_t)head * a.c.head_stride * Bytes<TO>::n;
+    float x[U][8], y[U][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[u][i] = y[u][i] = 0.f;
+        if (mine && row0 + u < a.r.rows) {
+            const char* p = from + (row0 + u) * from_step;
+            load8(p, e0, FROM, x[u]);
+            if (apart) {
+                load4(p, other[0], FROM, y[u]);
+                load4(p, other[1], FROM, y[u] + 4);
+            }
+        }
+    }
+    const float* gain = what == 0 ? a.q_gain : (what == 1 ? a.k_gain : nullptr);
+    float g[8], gp[8];   // the elements' gains and, signed as the rotation has them, their partners'
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { g[i] = 1.f; gp[i] = sign[i >> 2]; }
+    if (gain && mine) {
+        load8(reinterpret_cast<const char*>(gain), e0, HAWK_FP32, g);
+        if (apart) {
+            load4(reinterpret_cast<const char*>(gain), other[0], HAWK_FP32, gp);
+            load4(reinterpret_cast<const char*>(gain), other[1], HAWK_FP32, gp + 4);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) gp[i] *= sign[i >> 2];
+        }
+    }
+
+    // the rows' sequences; up to 64 of them every lane has one sequence's words, and one look answers for all
+    const bool few = a.c.n_seq <= 64;
+    const int mine_s = min(lane, a.c.n_seq - 1);
+    int starts = 0, stops = 0, pasts = 0;
+    if (few) {
+        starts = a.r.row_start[mine_s];
+        stops = a.r.row_start[mine_s + 1];
+        pasts = a.r.n_past[mine_s];
+    }
+    bool there[U];
+    int64_t place[U];
+    float2 f[U][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int row = row0 + u;
+        int s, start, stop, past;
+        if (few) {
+            s = __popcll(__ballot(lane < a.c.n_seq && starts <= row)) - 1;
+            start = __builtin_amdgcn_readlane(starts, max(s, 0));
+            stop = __builtin_amdgcn_readlane(stops, max(s, 0));
+            past = __builtin_amdgcn_readlane(pasts, max(s, 0));
+        } else {
+            s = __builtin_amdgcn_readfirstlane(last_not_above(a.c.n_seq, lane, row, [&](int i) { return (int64_t)a.r.row_start[i]; }));
+            start = a.r.row_start[max(s, 0)];
+            stop = a.r.row_start[max(s, 0) + 1];
+            past = a.r.n_past[max(s, 0)];
+        }
+        there[u] = row < a.r.rows && s >= 0 && row < stop;   // else in no sequence
+        const int64_t entry = (int64_t)past + (row - start);
+        int64_t p = entry;
+        if (a.pos && there[u]) p = a.pos[row];
+        if (a.rot) there[u] = there[u] && p >= 0 && p < a.n_pos;
+        place[u] = there[u] ? entry_at(a.c, a.c.table + s * a.c.table_stride, entry) : -1;
+        if (turned && there[u]) {
+            const float2* cs = reinterpret_cast<const float2*>(a.rot) + p * half;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (a.pairs || i < 4) f[u][i] = cs[at_table[i >> 2] + (i & 3)];
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        float rs = 1.f;
+        if (a.q_gain || a.k_gain) {   // (every lane takes part in the sum)
+            float ss = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) ss = fmaf(x[u][i], x[u][i], ss);
+            ss = sum_of_lanes(ss, a.lanes);
+            if (gain) rs = rsqrtf(ss * a.inv_hd + a.eps);
+        }
+        if (!there[u]) continue;
+        if (apart) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[u][i] = rs * fmaf(y[u][i], gp[i] * f[u][i].y, x[u][i] * (g[i] * f[u][i].x));
+        } else if (turned) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float2 t = cs[(e0 >> 1) + i];
-                const float u = x[2 * i], w = x[2 * i + 1];
-                x[2 * i] = u * t.x - w * t.y;
-                x[2 * i + 1] = u * t.y + w * t.x;
+                const float v = x[u][2 * i] * g[2 * i], w = x[u][2 * i + 1] * g[2 * i + 1];
+                x[u][2 * i] = rs * fmaf(-w, f[u][i].y, v * f[u][i].x);
+                x[u][2 * i + 1] = rs * fmaf(w, f[u][i].x, v * f[u][i].y);
             }
-        } else {
-            const int half = a.rot_dim >> 1;   // a multiple of four: four elements' partners are four in a row
+        } else if (gain) {
 #pragma unroll
-            for (int g4 = 0; g4 < 2; ++g4) {
-                const int e = e0 + 4 * g4;
-                const bool low = e < half;
-                const int other = low ? e + half : e - half, j = low ? e : e - half;
-                float y[4];
-                load4(src.data, at + other, src.dtype, y);
-                if (gain) {
-                    float g[4];
-                    load4(reinterpret_cast<const char*>(gain), other, HAWK_FP32, g);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) y[i] = y[i] * rs * g[i];
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float2 t = cs[j + i];
-                    float& v = x[4 * g4 + i];
-                    v = low ? v * t.x - y[i] * t.y : y[i] * t.y + v * t.x;
-                }
-            }
+            for (int i = 0; i < 8; ++i) x[u][i] = rs * (x[u][i] * g[i]);
         }
+        if (mine && (what == 0 || place[u] >= 0)) store8(to, (what == 0 ? (row0 + u) * a.q_out.row_stride : place[u]) + e0, TO, x[u]);
     }
-    if (!mine) return;
-    if (what == 0)
-        store8(a.q_out.data, (int64_t)row * a.q_out.row_stride + (int64_t)head * a.q_out.head_stride + e0, a.q_out.dtype, x);
-    else if (place >= 0)
-        store8(what == 1 ? a.c.k : a.c.v, place + (int64_t)head * a.c.head_stride + e0, a.q_out.dtype, x);
 }
 
 // A wave moves one head's keys or values of one sequence and layer.  Nodes lie at or behind the places they go to, so an
@@ -136,6 +198,17 @@ __global__ __launch_bounds__(256) void paged_keep_kernel(PagedView c, const int3
         if (move) w = *reinterpret_cast<const v4u*>(pool + from * esz + piece * 16);
         if (move) *reinterpret_cast<v4u*>(pool + to * esz + piece * 16) = w;
     }
+}
+
+template <int U, int FROM> void launch_append_from(const AppendArgs& a, int to, unsigned grid, hipStream_t stream) {
+    auto kern = to == HAWK_FP32 ? paged_append_kernel<U, FROM, HAWK_FP32>
+                                : (to == HAWK_BF16 ? paged_append_kernel<U, FROM, HAWK_BF16> : paged_append_kernel<U, FROM, HAWK_FP16>);
+    kern<<<grid, 256, 0, stream>>>(a);
+}
+template <int U> void launch_append(const AppendArgs& a, int to, unsigned grid, hipStream_t stream) {
+    if (a.k.dtype == HAWK_FP32) launch_append_from<U, HAWK_FP32>(a, to, grid, stream);
+    else if (a.k.dtype == HAWK_BF16) launch_append_from<U, HAWK_BF16>(a, to, grid, stream);
+    else launch_append_from<U, HAWK_FP16>(a, to, grid, stream);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -207,14 +280,17 @@ int launch_paged_append(const hawk_paged_cache* cache, int layer, const hawk_pag
     } else if (pos) {
         return HAWK_EINVAL;
     }
+    a.inv_hd = 1.f / (float)hd;
     a.q_gain = q_gain; a.k_gain = k_gain; a.eps = eps; a.rot = rot; a.n_pos = n_pos; a.rot_dim = rot ? rot_dim : 0; a.pairs = pairs; a.pos = pos;
-    a.lanes = 1;
-    while (a.lanes * 8 < hd) a.lanes *= 2;
-    a.per_block = 256 / a.lanes;
-    a.blocks = (a.q.n_heads + 2 * a.c.n_heads + a.per_block - 1) / a.per_block;
-    const int64_t grid = (int64_t)a.r.rows * a.blocks;
+    while ((8 << a.lanes) < hd) ++a.lanes;
+    a.per_block = 256 >> a.lanes;
+    const int vectors = a.q.n_heads + 2 * a.c.n_heads;
+    const bool large = (int64_t)a.r.rows * vectors >= 4096 * (int64_t)a.per_block;
+    a.blocks = divisor((vectors + a.per_block - 1) / a.per_block);
+    const int64_t grid = (int64_t)(large ? (a.r.rows + 1) / 2 : a.r.rows) * a.blocks.d;
     if (grid > (1 << 23)) return HAWK_EINVAL;   // a launch has fewer than 2^32 threads
-    paged_append_kernel<<<(unsigned)grid, 256, 0, stream>>>(a);
+    if (large) launch_append<2>(a, cache->dtype, (unsigned)grid, stream);
+    else launch_append<1>(a, cache->dtype, (unsigned)grid, stream);
     return status();
 }
 
