@@ -2,9 +2,9 @@
 // sequence the acceptance tests and one draw from the first rejected position's residual or the row behind the last draft.
 //
 // Rows whose kept entries fit a list (top-k up to 2048, slices up to 16384) and short slices are one workgroup a row and one a
-// sequence.  Other slices are cut into 16 parts: a row of 65536 entries takes one compute unit 15 us for its exponentials
+// sequence.  Other slices are cut into up to 16 parts: a row of 65536 entries takes one compute unit 15 us for its exponentials
 // alone, and a sequence's draw three passes over two of them.  Where every entry is kept, a part's statistics are its maximum and
-// sum, and whoever needs a row's joins 16 of them; where top-k cuts a long slice, a workgroup finds a row's threshold.  Then a
+// sum, and whoever needs a row's joins them; where top-k cuts a long slice, a workgroup finds a row's threshold.  Then a
 // workgroup per sequence and part makes the tests (all of them the same ones) and sums its part of the residual, and one per sequence
 // picks the part and the entry.
 #include "sample_rows.h"
@@ -21,7 +21,7 @@ struct ChainArgs {
     int64_t p_stride, q_seq, q_stride;
     const int32_t *p_start, *draft, *n_draft;
     const float *u_acc, *u_final;
-    int p_rows, n_seq, k, n, top_k, greedy;
+    int p_rows, n_seq, k, n, top_k, greedy, n_parts;
     float inv_t;
     WarpStat* stat;            // [n_seq][2 k + 1]: the target's k + 1 rows, then the proposals'
     int32_t *llen, *lidx;      // lists of the target's rows, [n_seq][k + 1]
@@ -183,8 +183,11 @@ __global__ __launch_bounds__(NT) void chain_stats_kernel(ChainArgs a) {
 }
 
 // ---- slices in parts ----
-constexpr int kParts = 16, kPT = 256;   // parts of a slice, threads of a part's workgroup
-__device__ __forceinline__ int part_entries(int n) { return ((n + kParts - 1) / kParts + 3) / 4 * 4; }
+// A part is 4096 entries, 16 a thread, as far as 16 parts go; with 16 parts for every slice 48 chains over 5000 entries took 41 us,
+// over 16384 49 us.
+constexpr int kParts = 16, kPT = 256;   // parts of a slice at most, threads of a part's workgroup
+inline int parts_of(int n) { return n > kParts * 16 * kPT ? kParts : (n + 16 * kPT - 1) / (16 * kPT); }
+__device__ __forceinline__ int part_entries(const ChainArgs& a) { return ((a.n + a.n_parts - 1) / a.n_parts + 3) / 4 * 4; }
 // exp(x), x <= 0, by Tang's table-driven method (ACM TOMS 15, 1989): x = (64 m + i) ln2 / 64 + r, exp(x) = 2^m 2^(i / 64) exp(r), |r| < 0.0055, so
 // that the series to r^5 is exact to 4e-17.  18 instructions where the library's has 48, which is what sums over whole slices are bound by;
 // far below (minus infinity, and for NaN) the result is 0.  48 chains over 65536 entries: chain_part_kernel 31 us with the library's, 24 us.
@@ -231,11 +234,11 @@ __global__ __launch_bounds__(kPT) void chain_part_kernel(ChainArgs a) {
     __shared__ double ssum[kPT / 64];
     __shared__ float smax[kPT / 64];
     __shared__ int sarg[kPT / 64];
-    const int per = a.q ? 2 * a.k + 1 : a.k + 1, part = blockIdx.x % kParts, u = blockIdx.x / kParts, s = u / per, r = u - s * per;
+    const int per = a.q ? 2 * a.k + 1 : a.k + 1, u = blockIdx.x / a.n_parts, part = blockIdx.x - u * a.n_parts, s = u / per, r = u - s * per;
     int64_t row0;
     const int nd = chain_of(a, s, row0);
     if (!row_needed(a, r, nd)) return;
-    const int len = part_entries(a.n), j0 = min(part * len, a.n), cnt = min(len, a.n - j0);
+    const int len = part_entries(a), j0 = min(part * len, a.n), cnt = min(len, a.n - j0);
     const float* l = chain_row(a, s, row0, r) + j0;
     float top = -INFINITY;
     int arg = 0x7FFFFFFF;
@@ -323,7 +326,7 @@ __global__ __launch_bounds__(kPT) void chain_residual_kernel(ChainArgs a) {
     __shared__ WarpStat stat[2 * kMaxK + 1];
     __shared__ double steps[kSteps];
     __shared__ double sr[kPT / 64], sp[kPT / 64];
-    const int groups = a.greedy ? 1 : kParts, s = blockIdx.x / groups, part = blockIdx.x - s * groups;
+    const int groups = a.greedy ? 1 : a.n_parts, s = blockIdx.x / groups, part = blockIdx.x - s * groups;
     int64_t row0;
     const int nd = chain_of(a, s, row0);
     if (nd < 0) {
@@ -338,7 +341,7 @@ __global__ __launch_bounds__(kPT) void chain_residual_kernel(ChainArgs a) {
             const int r = r0 + (int)threadIdx.x / kParts;
             const bool mine = r < rows && row_needed(a, r, nd);
             PartStat p = {0.0, -INFINITY, 0x7FFFFFFF};
-            if (mine) p = a.parts[(first + r) * kParts + (threadIdx.x & (kParts - 1))];
+            if (mine && (int)(threadIdx.x & (kParts - 1)) < a.n_parts) p = a.parts[(first + r) * kParts + (threadIdx.x & (kParts - 1))];
             float top = p.top;
 #pragma unroll
             for (int w = 1; w < kParts; w <<= 1) top = fmaxf(top, __shfl_xor(top, w));
@@ -369,7 +372,7 @@ __global__ __launch_bounds__(kPT) void chain_residual_kernel(ChainArgs a) {
     const WarpStat ps = stat[acc], qs = ended && a.q ? stat[a.k + 1 + acc] : ps;
     const float *prow = chain_row(a, s, row0, acc), *qrow = ended && a.q ? chain_row(a, s, row0, a.k + 1 + acc) : nullptr;
     const int d = ended ? a.draft[(int64_t)s * a.k + acc] : -1;
-    const int len = part_entries(a.n), j0 = min(part * len, a.n), cnt = min(len, a.n - j0);
+    const int len = part_entries(a), j0 = min(part * len, a.n), cnt = min(len, a.n - j0);
     const bool whole = a.parts != nullptr;   // every entry above minus infinity is kept
     const double ip = 1.0 / ps.total, iq = 1.0 / qs.total;
     double r = 0.0, p = 0.0;
@@ -423,17 +426,17 @@ __global__ __launch_bounds__(NT) void chain_draw_kernel(ChainArgs a) {
     const ChainEnd e = a.end[s];
     const double* mass = a.mass + (size_t)s * 2 * kParts;
     double total = 0.0;
-    for (int i = 0; i < kParts; ++i) total += mass[i];
+    for (int i = 0; i < a.n_parts; ++i) total += mass[i];
     const bool resid = e.ended && total > 0.0;
     if (!resid) {
         mass += kParts;
         total = 0.0;
-        for (int i = 0; i < kParts; ++i) total += mass[i];
+        for (int i = 0; i < a.n_parts; ++i) total += mass[i];
     }
     const double target = (double)a.u_final[s] * total;
     int part = -1, last = 0;
     double before = 0.0, base = 0.0;
-    for (int i = 0; i < kParts; ++i) {
+    for (int i = 0; i < a.n_parts; ++i) {
         if (mass[i] > 0.0) last = i;
         if (part < 0 && before + mass[i] > target) {
             part = i;
@@ -447,7 +450,7 @@ __global__ __launch_bounds__(NT) void chain_draw_kernel(ChainArgs a) {
         for (int i = 0; i < last; ++i) base += mass[i];
     }
     const float *prow = chain_row(a, s, row0, e.acc), *qrow = resid && a.q ? chain_row(a, s, row0, a.k + 1 + e.acc) : nullptr;
-    const int len = part_entries(a.n), j0 = min(part * len, a.n), j1 = min(j0 + len, a.n);
+    const int len = part_entries(a), j0 = min(part * len, a.n), j1 = min(j0 + len, a.n);
     const bool whole = a.parts != nullptr;
     const double ip = 1.0 / e.ps.total, iq = 1.0 / e.qs.total;
     int tok = -1;
@@ -487,8 +490,9 @@ __global__ __launch_bounds__(NT) void chain_draw_kernel(ChainArgs a) {
     put_tokens(a, s, e.acc, tok);
 }
 
-// ---- one workgroup a sequence: lists, and slices short enough for passes over all of them ----
-constexpr int kShort = 4 * NT;
+// ---- one workgroup a sequence: lists, and slices short enough for passes over all of them (2048 entries 17 us, 4096 entries 25
+// us; in parts 20) ----
+constexpr int kShort = 2 * NT;
 __global__ __launch_bounds__(NT) void chain_accept_kernel(ChainArgs a) {
     __shared__ Slots sl;
     __shared__ Shared sh;
@@ -601,16 +605,17 @@ int launch_verify_chains(const float* p_logits, int64_t p_stride, const int32_t*
         chain_accept_kernel<<<n_seq, NT, 0, stream>>>(a);
     } else {
         char* more = w + z.stat;
+        a.n_parts = parts_of(n);
         a.mass = reinterpret_cast<double*>(more + z.parts);
         a.end = reinterpret_cast<ChainEnd*>(more + z.parts + z.mass);
         if (a.greedy || a.top_k == n) {
             a.parts = reinterpret_cast<PartStat*>(more);
-            chain_part_kernel<<<rows * kParts, kPT, 0, stream>>>(a);
+            chain_part_kernel<<<rows * a.n_parts, kPT, 0, stream>>>(a);
         } else {
-            auto stats = E == 8 ? chain_stats_kernel<8> : (E == 16 ? chain_stats_kernel<16> : chain_stats_kernel<0>);
+            auto stats = E == 4 ? chain_stats_kernel<4> : (E == 8 ? chain_stats_kernel<8> : (E == 16 ? chain_stats_kernel<16> : chain_stats_kernel<0>));
             stats<<<rows, NT, 0, stream>>>(a);
         }
-        chain_residual_kernel<<<n_seq * (a.greedy ? 1 : kParts), kPT, 0, stream>>>(a);
+        chain_residual_kernel<<<n_seq * (a.greedy ? 1 : a.n_parts), kPT, 0, stream>>>(a);
         if (!a.greedy) chain_draw_kernel<<<n_seq, NT, 0, stream>>>(a);
     }
     return hipGetLastError() == hipSuccess ? HAWK_OK : HAWK_EDEVICE;
