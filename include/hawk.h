@@ -512,7 +512,8 @@ int hawk_paged_attention(const hawk_paged_cache* cache, int layer, const hawk_pa
 /* After a tree step: the entries of the accepted path move to their positions, in every layer.  For sequence s and
  * j = 0 .. n_keep[s] - 1 (n_keep clamped to 0..depth): entry n_past[s] + path[s * depth + j] goes to
  * n_past[s] + j + 1 (path: node numbers as in hawk_tree_layout, the root's own entry stays).  Nodes below j + 1, which
- * a path never has, and entries that do not exist are skipped.  depth 1..64. */
+ * a path never has, and entries that do not exist are skipped.  depth 1..64; layers apart from one another (layer_stride
+ * not below head_dim). */
 int hawk_paged_keep(const hawk_paged_cache* cache, const int32_t* n_past, const int32_t* path, const int32_t* n_keep,
                     int depth, void* stream);
 

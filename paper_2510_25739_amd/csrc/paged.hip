@@ -245,7 +245,7 @@ bool heads_view(const hawk_heads* h, HeadsView* out) {
 }
 
 int launch_rotary_table(float* table, int n_pos, int rot_dim, double theta, hipStream_t stream) {
-    if (!table || n_pos < 0 || rot_dim < 2 || rot_dim % 2 || !(theta > 0.0) || (reinterpret_cast<uintptr_t>(table) & 7)) return HAWK_EINVAL;
+    if ((!table && n_pos > 0) || n_pos < 0 || rot_dim < 2 || rot_dim % 2 || !(theta > 0.0) || (reinterpret_cast<uintptr_t>(table) & 7)) return HAWK_EINVAL;
     if (n_pos == 0) return HAWK_OK;
     const int64_t total = (int64_t)n_pos * (rot_dim / 2), blocks = (total + 255) / 256;
     if (blocks > (1 << 23)) return HAWK_EINVAL;
@@ -297,8 +297,10 @@ int launch_paged_append(const hawk_paged_cache* cache, int layer, const hawk_pag
 int launch_paged_keep(const hawk_paged_cache* cache, const int32_t* n_past, const int32_t* path, const int32_t* n_keep,
                       int depth, hipStream_t stream) {
     PagedView c;
-    if (!paged_view(cache, 0, &c) || !n_past || !path || !n_keep || depth < 1 || depth > 64) return HAWK_EINVAL;
+    if (!paged_view(cache, 0, &c) || depth < 1 || depth > 64) return HAWK_EINVAL;
+    if (cache->n_layers > 1 && cache->layer_stride < c.hd) return HAWK_EINVAL;   // layers in one another's place
     if (c.n_seq == 0) return HAWK_OK;
+    if (!n_past || !path || !n_keep) return HAWK_EINVAL;
     const int esz = (int)type_bytes(cache->dtype), pieces = c.hd * esz / 16;
     int lanes = 1;
     while (lanes < pieces) lanes *= 2;

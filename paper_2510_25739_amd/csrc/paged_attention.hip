@@ -846,6 +846,7 @@ template <int TYPE> void launch_wide(const AttnArgs& a, unsigned grid, hipStream
 
 // log2 of a tile's rows * 10000 + waves of a workgroup * 100 + parts: the dispatch's rules, for the tests as well.
 extern "C" int hawk_paged_attention_plan(int dtype, int n_seq, int rows, int n_heads, int n_q_heads, int hd, int capacity, int max_len) {
+    if (n_seq < 0 || rows < 0 || n_heads < 1 || n_q_heads < n_heads || capacity < 1) return 0;
     const Plan p = plan_of(dtype, n_seq, rows, n_heads, n_q_heads, hd, capacity, max_len);
     return p.tile * 10000 + (p.wide ? (p.tile == 8 ? 8 : 4) : (hd > 128 ? 4 : p.waves)) * 100 + p.splits;
 }

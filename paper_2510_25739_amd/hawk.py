@@ -389,7 +389,9 @@ def _call_on(index, fn, *args):
 def rotary_table(n_pos: int, rot_dim: int, theta: float = 10000.0, device: str = "cuda:0"):
     """hawk_rotary_table: fp32 device tensor [n_pos, rot_dim // 2, 2] of cos and sin of position * theta^(-2 j / rot_dim)."""
     import torch  # device memory and stream only
-    out = torch.empty((n_pos, rot_dim // 2, 2), dtype=torch.float32, device=device)
+    out = torch.empty((max(n_pos, 0), max(rot_dim, 0) // 2, 2), dtype=torch.float32, device=device)
+    if not out.is_cuda:
+        raise HawkError(-1, "hawk_rotary_table", "the table is a device tensor")
     rc = _call_on(out.get_device(), load_library().hawk_rotary_table, out.data_ptr(), n_pos, rot_dim, float(theta))
     if rc != 0:
         raise HawkError(rc, "hawk_rotary_table")
@@ -402,7 +404,7 @@ class PagedCache:
     k, v: device tensors [n_layers, n_pages, n_heads, page_size, head_dim] (or without the first axis) of the same strides,
     fp32, bf16 or fp16, the last axis contiguous - any other order of the axes is a permuted view.  table [n_seq, max_pages]
     int32: the pages of every sequence.  The tensors stay the caller's: their contents may change between calls (new pages
-    in the table), and `table` may be replaced by another tensor.
+    in the table), and `table` may be replaced by another tensor (a captured graph keeps the one it was captured with).
     Calls launch on torch's current stream of the cache's device.  `row_start` [n_seq + 1] and `n_past` [n_seq] are int32 device
     tensors: rows row_start[s] .. row_start[s + 1] - 1 of a call belong to sequence s, which has n_past[s] committed entries."""
 
@@ -566,7 +568,7 @@ def verify_chains(p_logits, q_logits, draft, u_acc, u_final, temperature: float,
     Returns device tensors (accepted [n_seq], tokens [n_seq, k + 1]) int32."""
     where, f32, i32 = "hawk_verify_chains", _float32(), _int32()
     dev = p_logits.get_device()
-    n_seq, k = draft.shape
+    n_seq, k = draft.shape if draft.dim() == 2 else (-1, -1)
     small = [(draft, i32, (n_seq, k)), (u_acc, f32, (n_seq, k)), (u_final, f32, (n_seq,))]
     if n_draft is not None:
         small.append((n_draft, i32, (n_seq,)))

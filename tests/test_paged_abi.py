@@ -127,7 +127,7 @@ def test_bad_keeps_are_refused(H):
     assert L.hawk_paged_keep(C.byref(cache(n_seq=0)), ONE, ONE, ONE, 3, None) == 0
     assert L.hawk_rotary_table(None, 4, 8, 1e4, None) == -1 and L.hawk_rotary_table(ONE, 4, 7, 1e4, None) == -1
     assert L.hawk_rotary_table(ONE, 4, 8, 0.0, None) == -1 and L.hawk_rotary_table(ONE, -1, 8, 1e4, None) == -1
-    assert L.hawk_rotary_table(ONE, 0, 8, 1e4, None) == 0
+    assert L.hawk_rotary_table(ONE, 0, 8, 1e4, None) == 0 and L.hawk_rotary_table(None, 0, 8, 1e4, None) == 0
 
 
 def test_bad_chains_are_refused(H):
@@ -144,3 +144,36 @@ def test_bad_chains_are_refused(H):
     assert call(n_seq=0, p=None, d=None, ws=None) == 0
     for a in ((0, 2, 100), (3, -1, 100), (3, 64, 100), (3, 2, 0), (3, 2, (1 << 20) + 1)):
         assert L.hawk_verify_chains_workspace_bytes(*a) == 0
+
+
+def test_a_keep_of_no_sequences_needs_no_buffers(H):
+    L = H.load_library()
+    assert L.hawk_paged_keep(C.byref(cache(n_seq=0, table=None)), None, None, None, 3, None) == 0
+    assert L.hawk_paged_keep(C.byref(cache(n_seq=0)), None, None, None, 0, None) == -1
+
+
+def test_a_keep_in_layers_that_share_memory_is_refused(H):
+    """With no stride between layers every layer would move the same entries, one over the other's."""
+    L = H.load_library()
+    for stride in (0, 56):
+        assert L.hawk_paged_keep(C.byref(cache(layer_stride=stride)), ONE, ONE, ONE, 3, None) == -1
+    assert L.hawk_paged_keep(C.byref(cache(layer_stride=0, n_layers=1, n_seq=0)), None, None, None, 3, None) == 0
+
+
+def test_host_tensors_are_refused(H):
+    import torch
+    with pytest.raises(hawk.HawkError):
+        H.rotary_table(4, 8, device="cpu")
+    f, i = torch.float32, torch.int32
+    with pytest.raises(hawk.HawkError):
+        H.verify_chains(torch.zeros(3, 9), None, torch.zeros(1, 2, dtype=i), torch.zeros(1, 2), torch.zeros(1), 1.0, 5)
+    with pytest.raises(hawk.HawkError):
+        H.verify_chains(torch.zeros(3, 9), None, torch.zeros(2, dtype=i), torch.zeros(1, 2), torch.zeros(1), 1.0, 5)
+    with pytest.raises(hawk.HawkError):
+        H.PagedCache(torch.zeros(2, 2, 2, 4, 8, dtype=f), torch.zeros(2, 2, 2, 4, 8, dtype=f), torch.zeros(1, 2, dtype=i))
+
+
+def test_the_rule_of_the_cut_takes_any_sizes(H):
+    L = H.load_library()
+    for a in ((1, 3, 5, 0, 4, 64, 100, 0), (1, 3, 5, 2, 1, 64, 100, 0), (1, 0, 5, 2, 4, 64, 100, 0), (1, 3, -1, 2, 4, 64, 100, 0), (1, 3, 5, 2, 4, 64, 0, 0)):
+        assert L.hawk_paged_attention_plan(*a) >= 0
