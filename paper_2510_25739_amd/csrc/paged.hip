@@ -3,6 +3,8 @@
 // paged_attention.hip reads it.
 #include "paged.h"
 
+#include <algorithm>
+
 namespace hawk {
 
 namespace {
@@ -25,9 +27,34 @@ struct AppendArgs {
     int n_pos, rot_dim, pairs;
     int lanes, per_block;           // lanes of a vector (2^lanes), vectors that a workgroup's lanes take side by side
     Divisor blocks;                 // workgroups of a row
+    int step;                       // rows between a workgroup's rows
 };
 
 template <int TYPE> struct Bytes { static constexpr int n = TYPE == HAWK_FP32 ? 4 : 2; };
+
+// N values of a type as they lie in memory: requested in one place, used in another.
+template <int TYPE, int N> struct Piece {
+    static constexpr int kWords = N * Bytes<TYPE>::n / 4;
+    typedef unsigned part __attribute__((ext_vector_type(kWords < 4 ? kWords : 4)));
+    static constexpr int kParts = kWords < 4 ? 1 : kWords / 4;
+    part w[kParts];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) w[i] = (part)0u;
+    }
+    __device__ __forceinline__ void load(const char* base, int at) {
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) w[i] = reinterpret_cast<const part*>(base + at * Bytes<TYPE>::n)[i];
+    }
+    __device__ __forceinline__ void widen(float* x) const {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+            const unsigned v = w[i / 4][i % 4];
+            if (TYPE == HAWK_FP32) x[i] = __uint_as_float(v);
+            else widen2(v, TYPE, x[2 * i], x[2 * i + 1]);
+        }
+    }
+};
 
 // Sum over 2^n neighbouring lanes, the same value in each: quad permutes and mirrors inside a row of 16, a swap beyond it.
 template <int CTRL> __device__ __forceinline__ float moved(float v) {
@@ -42,15 +69,18 @@ __device__ __forceinline__ float sum_of_lanes(float v, int n) {
     return v;
 }
 
-// Block (vectors of a row, U rows); a vector - one head of q, k or v - belongs to 2^lanes neighbouring lanes of one wave, eight elements
-// each, so that its sum of squares is a few lane moves and its bytes are one request.  Every lane reads its elements' partners
-// of the rotation itself where they are half a vector away: they are in the same lines.  Three dependent latencies (row
-// starts, lengths, table and rotation) stand against a few hundred bytes, and what a lane works out about its vector - where it comes
-// from and goes to, its gains - holds for every row, so a lane of a large call takes U of them.  4048 rows of 32 + 16 heads of 128,
-// norms and rotation: 34.4 us (2.9 TB/s of what is read and written; a copy of as much takes 21), with one row a lane 37.3.
-template <int U, int FROM, int TO>   // rows a lane; types
-__global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
-    const int group = (int)blockIdx.x / a.blocks, part = blockIdx.x - group * a.blocks.d, row0 = group * U;
+// A workgroup has some vectors - a vector is one head of q, k or v - of every step-th row; a vector belongs to 2^lanes neighbouring lanes
+// of one wave, eight elements each, so that its sum of squares is a few lane moves and its bytes are one request.  Every
+// lane reads its elements' partners of the rotation itself where they are half a vector away: they are in the same lines.
+// Dependent latencies (row starts and lengths, then table and rotation) stand against a few hundred bytes, so a workgroup stays for as
+// many rows as make the chip full of workgroups once, holds what is the same for all of them - where its vectors come from and go
+// to, their gains, the sequences - and has the next row's requests under way while it works on a row's.  4048 rows of 32 + 16 heads of
+// 128, norms and rotation of halves: 28 us (3.6 TB/s of what is read and written; a copy of as much takes 21), with a workgroup for
+// every two rows 34.4, for every row 37.3; 16000 rows of 16 + 4 heads of 256 99 us, with a workgroup for two rows 139.
+constexpr int kResident = 1024;     // workgroups that are on the chip at a time: four to a unit
+template <int FROM, int TO>   // types
+__global__ __launch_bounds__(256, 4) void paged_append_kernel(AppendArgs a) {
+    const int row0 = (int)blockIdx.x / a.blocks, part = blockIdx.x - row0 * a.blocks.d;
     const int lane = threadIdx.x & 63, e0 = (threadIdx.x & ((1 << a.lanes) - 1)) * 8, hd = a.c.hd;
     const int nq = a.q.n_heads, nk = a.c.n_heads, half = a.rot_dim >> 1;   // half: a multiple of four, so four elements' partners are four in a row
     const int vec = part * a.per_block + ((int)threadIdx.x >> a.lanes), what = vec < nq ? 0 : (vec < nq + nk ? 1 : 2);
@@ -72,35 +102,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
     const int64_t from_step = src.row_stride * Bytes<FROM>::n;
     char* to = what == 0 ? a.q_out.data + (int64_t)head * a.q_out.head_stride * Bytes<TO>::n
                          : (what == 1 ? a.c.k : a.c.v) + (int64_t)head * a.c.head_stride * Bytes<TO>::n;
-    float x[U][8], y[U][8];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[u][i] = y[u][i] = 0.f;
-        if (mine && row0 + u < a.r.rows) {
-            const char* p = from + (row0 + u) * from_step;
-            load8(p, e0, FROM, x[u]);
-            if (apart) {
-                load4(p, other[0], FROM, y[u]);
-                load4(p, other[1], FROM, y[u] + 4);
-            }
-        }
-    }
-    const float* gain = what == 0 ? a.q_gain : (what == 1 ? a.k_gain : nullptr);
-    float g[8], gp[8];   // the elements' gains and, signed as the rotation has them, their partners'
-#pragma unroll
-    for (int i = 0; i < 8; ++i) { g[i] = 1.f; gp[i] = sign[i >> 2]; }
-    if (gain && mine) {
-        load8(reinterpret_cast<const char*>(gain), e0, HAWK_FP32, g);
-        if (apart) {
-            load4(reinterpret_cast<const char*>(gain), other[0], HAWK_FP32, gp);
-            load4(reinterpret_cast<const char*>(gain), other[1], HAWK_FP32, gp + 4);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) gp[i] *= sign[i >> 2];
-        }
-    }
-
-    // the rows' sequences; up to 64 of them every lane has one sequence's words, and one look answers for all
+    // the sequences; up to 64 of them every lane has one sequence's words, and one look answers for a row
     const bool few = a.c.n_seq <= 64;
     const int mine_s = min(lane, a.c.n_seq - 1);
     int starts = 0, stops = 0, pasts = 0;
@@ -109,12 +111,27 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
         stops = a.r.row_start[mine_s + 1];
         pasts = a.r.n_past[mine_s];
     }
-    bool there[U];
-    int64_t place[U];
-    float2 f[U][8];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int row = row0 + u;
+    struct Row {            // of one row, as requested
+        Piece<FROM, 8> x;
+        Piece<FROM, 4> y[2];
+        float2 f[8];
+        int page, slot;     // of the entry
+        bool there;
+    };
+    auto request_x = [&](int row, Row& r) {
+        r.x.clear();
+        r.y[0].clear();
+        r.y[1].clear();
+        if (mine && row < a.r.rows) {
+            const char* p = from + row * from_step;
+            r.x.load(p, e0);
+            if (apart) {
+                r.y[0].load(p, other[0]);
+                r.y[1].load(p, other[1]);
+            }
+        }
+    };
+    auto request_place = [&](int row, Row& r) {
         int s, start, stop, past;
         if (few) {
             s = __popcll(__ballot(lane < a.c.n_seq && starts <= row)) - 1;
@@ -127,45 +144,86 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
             stop = a.r.row_start[max(s, 0) + 1];
             past = a.r.n_past[max(s, 0)];
         }
-        there[u] = row < a.r.rows && s >= 0 && row < stop;   // else in no sequence
+        r.there = row < a.r.rows && s >= 0 && row < stop;   // else in no sequence
         const int64_t entry = (int64_t)past + (row - start);
         int64_t p = entry;
-        if (a.pos && there[u]) p = a.pos[row];
-        if (a.rot) there[u] = there[u] && p >= 0 && p < a.n_pos;
-        place[u] = there[u] ? entry_at(a.c, a.c.table + s * a.c.table_stride, entry) : -1;
-        if (turned && there[u]) {
+        if (a.pos && r.there) p = a.pos[row];
+        if (a.rot) r.there = r.there && p >= 0 && p < a.n_pos;
+        r.page = -1;
+        r.slot = 0;
+        if (r.there && entry >= 0 && entry < a.c.capacity) {
+            const int n = page_of(a.c, (int)entry);
+            r.page = a.c.table[s * a.c.table_stride + n];
+            r.slot = (int)entry - n * a.c.page_size;
+        }
+        if (turned && r.there) {
             const float2* cs = reinterpret_cast<const float2*>(a.rot) + p * half;
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (a.pairs || i < 4) f[u][i] = cs[at_table[i >> 2] + (i & 3)];
+                if (a.pairs || i < 4) r.f[i] = cs[at_table[i >> 2] + (i & 3)];
         }
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        float rs = 1.f;
+    };
+    const float* gain = what == 0 ? a.q_gain : (what == 1 ? a.k_gain : nullptr);
+    float g[8], gp[8];   // the elements' gains and, signed as the rotation has them, their partners'
+    auto append = [&](int row, const Row& r) {
+        float x[8], y[8], rs = 1.f;
+        r.x.widen(x);
         if (a.q_gain || a.k_gain) {   // (every lane takes part in the sum)
             float ss = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) ss = fmaf(x[u][i], x[u][i], ss);
+            for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
             ss = sum_of_lanes(ss, a.lanes);
             if (gain) rs = rsqrtf(ss * a.inv_hd + a.eps);
         }
-        if (!there[u]) continue;
+        if (!r.there) return;
         if (apart) {
+            r.y[0].widen(y);
+            r.y[1].widen(y + 4);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[u][i] = rs * fmaf(y[u][i], gp[i] * f[u][i].y, x[u][i] * (g[i] * f[u][i].x));
+            for (int i = 0; i < 8; ++i) x[i] = rs * fmaf(y[i], gp[i] * r.f[i].y, x[i] * (g[i] * r.f[i].x));
         } else if (turned) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float v = x[u][2 * i] * g[2 * i], w = x[u][2 * i + 1] * g[2 * i + 1];
-                x[u][2 * i] = rs * fmaf(-w, f[u][i].y, v * f[u][i].x);
-                x[u][2 * i + 1] = rs * fmaf(w, f[u][i].x, v * f[u][i].y);
+                const float v = x[2 * i] * g[2 * i], w = x[2 * i + 1] * g[2 * i + 1];
+                x[2 * i] = rs * fmaf(-w, r.f[i].y, v * r.f[i].x);
+                x[2 * i + 1] = rs * fmaf(w, r.f[i].x, v * r.f[i].y);
             }
         } else if (gain) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[u][i] = rs * (x[u][i] * g[i]);
+            for (int i = 0; i < 8; ++i) x[i] = rs * (x[i] * g[i]);
         }
-        if (mine && (what == 0 || place[u] >= 0)) store8(to, (what == 0 ? (row0 + u) * a.q_out.row_stride : place[u]) + e0, TO, x[u]);
+        const int64_t place = place_in(a.c, r.page, r.slot);
+        if (mine && (what == 0 || place >= 0)) store8(to, (what == 0 ? row * a.q_out.row_stride : place) + e0, TO, x);
+    };
+
+    Row r0, r1;
+    request_x(row0, r0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { g[i] = 1.f; gp[i] = sign[i >> 2]; }
+    if (gain && mine) {
+        load8(reinterpret_cast<const char*>(gain), e0, HAWK_FP32, g);
+        if (apart) {
+            load4(reinterpret_cast<const char*>(gain), other[0], HAWK_FP32, gp);
+            load4(reinterpret_cast<const char*>(gain), other[1], HAWK_FP32, gp + 4);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) gp[i] *= sign[i >> 2];
+        }
+    }
+    request_place(row0, r0);
+    for (int row = row0;; row += 2 * a.step) {
+        const bool second = row + a.step < a.r.rows, third = row + 2 * a.step < a.r.rows;
+        if (second) {
+            request_x(row + a.step, r1);
+            request_place(row + a.step, r1);
+        }
+        append(row, r0);
+        if (!second) break;
+        if (third) {
+            request_x(row + 2 * a.step, r0);
+            request_place(row + 2 * a.step, r0);
+        }
+        append(row + a.step, r1);
+        if (!third) break;
     }
 }
 
@@ -200,15 +258,10 @@ __global__ __launch_bounds__(256) void paged_keep_kernel(PagedView c, const int3
     }
 }
 
-template <int U, int FROM> void launch_append_from(const AppendArgs& a, int to, unsigned grid, hipStream_t stream) {
-    auto kern = to == HAWK_FP32 ? paged_append_kernel<U, FROM, HAWK_FP32>
-                                : (to == HAWK_BF16 ? paged_append_kernel<U, FROM, HAWK_BF16> : paged_append_kernel<U, FROM, HAWK_FP16>);
+template <int FROM> void launch_append_from(const AppendArgs& a, int to, unsigned grid, hipStream_t stream) {
+    auto kern = to == HAWK_FP32 ? paged_append_kernel<FROM, HAWK_FP32>
+                                : (to == HAWK_BF16 ? paged_append_kernel<FROM, HAWK_BF16> : paged_append_kernel<FROM, HAWK_FP16>);
     kern<<<grid, 256, 0, stream>>>(a);
-}
-template <int U> void launch_append(const AppendArgs& a, int to, unsigned grid, hipStream_t stream) {
-    if (a.k.dtype == HAWK_FP32) launch_append_from<U, HAWK_FP32>(a, to, grid, stream);
-    else if (a.k.dtype == HAWK_BF16) launch_append_from<U, HAWK_BF16>(a, to, grid, stream);
-    else launch_append_from<U, HAWK_FP16>(a, to, grid, stream);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -285,12 +338,13 @@ int launch_paged_append(const hawk_paged_cache* cache, int layer, const hawk_pag
     while ((8 << a.lanes) < hd) ++a.lanes;
     a.per_block = 256 >> a.lanes;
     const int vectors = a.q.n_heads + 2 * a.c.n_heads;
-    const bool large = (int64_t)a.r.rows * vectors >= 4096 * (int64_t)a.per_block;
     a.blocks = divisor((vectors + a.per_block - 1) / a.per_block);
-    if ((int64_t)a.r.rows * a.blocks.d > (1 << 23)) return HAWK_EINVAL;   // a launch has fewer than 2^32 threads
-    const int64_t grid = (int64_t)(large ? (a.r.rows + 1) / 2 : a.r.rows) * a.blocks.d;
-    if (large) launch_append<2>(a, cache->dtype, (unsigned)grid, stream);
-    else launch_append<1>(a, cache->dtype, (unsigned)grid, stream);
+    if ((int64_t)a.r.rows * a.blocks.d > (1 << 23)) return HAWK_EINVAL;   // as other steps too large for one launch
+    a.step = std::min(a.r.rows, std::max(1, kResident / a.blocks.d));
+    const unsigned grid = (unsigned)(a.step * a.blocks.d);
+    if (a.k.dtype == HAWK_FP32) launch_append_from<HAWK_FP32>(a, cache->dtype, grid, stream);
+    else if (a.k.dtype == HAWK_BF16) launch_append_from<HAWK_BF16>(a, cache->dtype, grid, stream);
+    else launch_append_from<HAWK_FP16>(a, cache->dtype, grid, stream);
     return status();
 }
 
