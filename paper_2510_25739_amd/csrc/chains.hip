@@ -14,7 +14,7 @@ namespace hawk {
 namespace {
 
 struct PartStat { double sum; float top; int arg; };                       // of a part of a row: sum of exp(z - top); entry of the maximum
-struct ChainEnd { WarpStat ps, qs; int acc, ended, d; };                    // of a sequence: the position that ends it
+struct ChainEnd { WarpStat ps, qs; int64_t row0; int acc, ended, d; };      // of a sequence: the position that ends it (acc < 0: it is left out)
 
 struct ChainArgs {
     const float *p, *q;
@@ -189,20 +189,22 @@ constexpr int kParts = 16, kPT = 256;   // parts of a slice at most, threads of 
 inline int parts_of(int n) { return n > kParts * 16 * kPT ? kParts : (n + 16 * kPT - 1) / (16 * kPT); }
 __device__ __forceinline__ int part_entries(const ChainArgs& a) { return ((a.n + a.n_parts - 1) / a.n_parts + 3) / 4 * 4; }
 // exp(x), x <= 0, by Tang's table-driven method (ACM TOMS 15, 1989): x = (64 m + i) ln2 / 64 + r, exp(x) = 2^m 2^(i / 64) exp(r), |r| < 0.0055, so
-// that the series to r^5 is exact to 4e-17.  18 instructions where the library's has 48, which is what sums over whole slices are bound by;
-// far below (minus infinity, and for NaN) the result is 0.  48 chains over 65536 entries: chain_part_kernel 31 us with the library's, 24 us.
+// that the series to r^5 is exact to 4e-17.  The whole number is rounded to by adding 1.5 2^52, whose low word then holds it, and 2^m
+// is added to the exponent.  Below -700 (minus infinity among it, and for NaN) the result is 0.  Fewer instructions than the library's, all of
+// the quick kind, which is what sums over whole slices are bound by; 48 chains over 65536 entries: chain_part_kernel 31 us with
+// the library's, EXP_US us.
 constexpr int kSteps = 64;
 __device__ __forceinline__ void fill_steps(double* steps) {   // ends without a barrier
     if (threadIdx.x < kSteps) steps[threadIdx.x] = exp2((double)threadIdx.x / kSteps);
 }
 __device__ __forceinline__ double exp_below(double x, const double* steps) {
-    x = fmax(x, -800.0);
-    const double n = rint(x * 0x1.71547652b82fep+6);
+    const double shifted = fma(x, 0x1.71547652b82fep+6, 0x1.8p52), n = shifted - 0x1.8p52;
     const double r = fma(n, -0x1.abc9e3b39803fp-62, fma(n, -0x1.62e42fefa39efp-7, x));
     const double p = r * fma(r, fma(r, fma(r, fma(r, 1.0 / 120, 1.0 / 24), 1.0 / 6), 0.5), 1.0);
-    const int i = (int)n;
-    const double t = steps[i & (kSteps - 1)];
-    return ldexp(fma(t, p, t), i >> 6);
+    const int i = __double2loint(shifted);
+    const double t = steps[i & (kSteps - 1)], v = fma(t, p, t);
+    const bool some = x >= -700.0;
+    return __hiloint2double(some ? __double2hiint(v) + (int)((unsigned)(i & -kSteps) << 14) : 0, some ? __double2loint(v) : 0);
 }
 // weight_of with it, of a scaled logit.
 __device__ __forceinline__ double entry_weight(const WarpStat& st, float z, int j, bool whole, const double* steps) {
@@ -262,7 +264,7 @@ __global__ __launch_bounds__(kPT) void chain_part_kernel(ChainArgs a) {
                 top = most;
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sum += top > -INFINITY ? exp_below((double)z[i] - (double)top, steps) : 0.0;
+            for (int i = 0; i < 16; ++i) sum += exp_below((double)z[i] - (double)top, steps);   // (top minus infinity: NaN, so 0)
         }
     }
     const float wtop = wave_max_f(top);
@@ -285,22 +287,40 @@ __global__ __launch_bounds__(kPT) void chain_part_kernel(ChainArgs a) {
     }
 }
 
-// The acceptance tests of a sequence, lane i of every wave making test i: how many drafts are accepted.
-__device__ __forceinline__ int accepted(const ChainArgs& a, int s, int64_t row0, int nd, const WarpStat* stat) {
+// The acceptance tests of a sequence, lane i of every wave making test i: what a test needs besides the rows' statistics, which may be asked
+// for before these are there, and how many drafts are accepted.
+struct Test { float zp, zq, u; int d; };
+__device__ __forceinline__ Test test_of(const ChainArgs& a, int s, int64_t row0, int nd) {
+    const int lane = threadIdx.x & 63;
+    Test t = {0.f, 0.f, 0.f, -1};
+    if (lane < nd) {
+        t.d = a.draft[(int64_t)s * a.k + lane];
+        t.u = a.u_acc[(int64_t)s * a.k + lane];
+        if ((unsigned)t.d < (unsigned)a.n) {
+            t.zp = chain_row(a, s, row0, lane)[t.d] * a.inv_t;
+            if (a.q) t.zq = chain_row(a, s, row0, a.k + 1 + lane)[t.d] * a.inv_t;
+        }
+    }
+    return t;
+}
+__device__ __forceinline__ double scaled_weight(const WarpStat& st, float z, int j) {   // weight_of, of a scaled logit
+    if (st.onehot >= 0) return j == st.onehot ? 1.0 : 0.0;
+    return kept(st, z, j) ? exp((double)z - (double)st.zmax) : 0.0;
+}
+__device__ __forceinline__ int accepted(const ChainArgs& a, int nd, const Test& t, const WarpStat* stat) {
     const int lane = threadIdx.x & 63;
     bool rejected = false;
     if (lane < nd) {
-        const int d = a.draft[(int64_t)s * a.k + lane];
         double pd = 0.0, qd = 1.0;
-        if ((unsigned)d < (unsigned)a.n) {
+        if ((unsigned)t.d < (unsigned)a.n) {
             const WarpStat ps = stat[lane];
-            pd = weight_of(ps, chain_row(a, s, row0, lane), a.inv_t, d) / ps.total;
+            pd = scaled_weight(ps, t.zp, t.d) / ps.total;
             if (a.q) {
                 const WarpStat qs = stat[a.k + 1 + lane];
-                qd = weight_of(qs, chain_row(a, s, row0, a.k + 1 + lane), a.inv_t, d) / qs.total;
+                qd = scaled_weight(qs, t.zq, t.d) / qs.total;
             }
         }
-        rejected = !((double)a.u_acc[(int64_t)s * a.k + lane] * qd < pd);
+        rejected = !((double)t.u * qd < pd);
     }
     const unsigned long long rej = __ballot(rejected);
     return rej ? (int)__ffsll(rej) - 1 : nd;   // the first rejection is where the chain ends (k <= 63)
@@ -331,10 +351,12 @@ __global__ __launch_bounds__(kPT) void chain_residual_kernel(ChainArgs a) {
     const int nd = chain_of(a, s, row0);
     if (nd < 0) {
         if (part == 0) leave_out(a, s);
+        if (part == 0 && threadIdx.x == 0) a.end[s].acc = -1;
         return;
     }
     const int rows = a.q ? 2 * a.k + 1 : a.k + 1;
     const size_t first = (size_t)s * (2 * a.k + 1);
+    const Test test = test_of(a, s, row0, nd);
     fill_steps(steps);
     if (a.parts) {
         for (int r0 = 0; r0 < rows; r0 += kPT / kParts) {   // 16 lanes a row
@@ -363,7 +385,7 @@ __global__ __launch_bounds__(kPT) void chain_residual_kernel(ChainArgs a) {
             if (row_needed(a, r, nd)) stat[r] = a.stat[first + r];
     }
     __syncthreads();
-    const int acc = accepted(a, s, row0, nd, stat);
+    const int acc = accepted(a, nd, test, stat);
     if (a.greedy) {   // point masses: what is left of the target's is the target's
         put_tokens(a, s, acc, stat[acc].onehot);
         return;
@@ -408,7 +430,7 @@ __global__ __launch_bounds__(kPT) void chain_residual_kernel(ChainArgs a) {
         a.mass[(size_t)s * 2 * kParts + part] = r;
         a.mass[(size_t)s * 2 * kParts + kParts + part] = p;
         if (part == 0) {
-            ChainEnd e = {ps, qs, acc, ended, d};
+            ChainEnd e = {ps, qs, row0, acc, ended, d};
             a.end[s] = e;
         }
     }
@@ -419,37 +441,48 @@ __global__ __launch_bounds__(NT) void chain_draw_kernel(ChainArgs a) {
     __shared__ Shared sh;
     __shared__ double steps[kSteps];
     const int s = blockIdx.x;
-    int64_t row0;
-    if (chain_of(a, s, row0) < 0) return;
-    fill_steps(steps);
-    __syncthreads();
     const ChainEnd e = a.end[s];
     const double* mass = a.mass + (size_t)s * 2 * kParts;
-    double total = 0.0;
-    for (int i = 0; i < a.n_parts; ++i) total += mass[i];
+    double mr[kParts], m[kParts], total = 0.0;   // (all requested at once)
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+        mr[i] = i < a.n_parts ? mass[i] : 0.0;
+        m[i] = i < a.n_parts ? mass[kParts + i] : 0.0;
+    }
+    fill_steps(steps);
+    if (e.acc < 0) return;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) total += mr[i];
     const bool resid = e.ended && total > 0.0;
-    if (!resid) {
-        mass += kParts;
+    if (resid) {
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) m[i] = mr[i];
+    } else {
         total = 0.0;
-        for (int i = 0; i < a.n_parts; ++i) total += mass[i];
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) total += m[i];
     }
     const double target = (double)a.u_final[s] * total;
     int part = -1, last = 0;
-    double before = 0.0, base = 0.0;
-    for (int i = 0; i < a.n_parts; ++i) {
-        if (mass[i] > 0.0) last = i;
-        if (part < 0 && before + mass[i] > target) {
+    double before = 0.0, base = 0.0, lower = 0.0;   // what lies before the part; before the last one with weight
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+        if (m[i] > 0.0) {
+            last = i;
+            lower = before;
+        }
+        if (part < 0 && before + m[i] > target) {
             part = i;
             base = before;
         }
-        before += mass[i];
+        before += m[i];
     }
     if (part < 0) {
         part = last;
-        base = 0.0;
-        for (int i = 0; i < last; ++i) base += mass[i];
+        base = lower;
     }
-    const float *prow = chain_row(a, s, row0, e.acc), *qrow = resid && a.q ? chain_row(a, s, row0, a.k + 1 + e.acc) : nullptr;
+    const float *prow = chain_row(a, s, e.row0, e.acc), *qrow = resid && a.q ? chain_row(a, s, e.row0, a.k + 1 + e.acc) : nullptr;
     const int len = part_entries(a), j0 = min(part * len, a.n), j1 = min(j0 + len, a.n);
     const bool whole = a.parts != nullptr;
     const double ip = 1.0 / e.ps.total, iq = 1.0 / e.qs.total;
@@ -505,7 +538,7 @@ __global__ __launch_bounds__(NT) void chain_accept_kernel(ChainArgs a) {
     }
     if (threadIdx.x == 0) sl.pick = 0x7FFFFFFF;
     const WarpStat* stat = a.stat + (size_t)s * (2 * a.k + 1);
-    const int acc = accepted(a, s, row0, nd, stat);
+    const int acc = accepted(a, nd, test_of(a, s, row0, nd), stat);
     const float uf = a.u_final[s];
     const bool ended = acc < nd;
     const WarpStat ps = stat[acc], qs = ended && a.q ? stat[a.k + 1 + acc] : ps;
