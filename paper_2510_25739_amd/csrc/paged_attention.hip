@@ -784,7 +784,12 @@ struct Plan { bool wide; int tile, waves, tiles, splits, split_keys; size_t part
 // 2000 (1 million) 44.6 / 44.2, 64 (2 million) 88.4 / 54.1; 20 heads of 64, 64 rows behind 300 (192 thousand) 12.8 / 12.3, behind 2000 49.4 / 39.2.
 // Tiles of 256 rows halve what is brought and put, but eight waves meet at every barrier: 4001 rows x 4 behind 2048 292 us, in
 // tiles of 128 337; 8 sequences of 512 rows x 4 behind 2000 199 / 223, of 256 rows x 4 142 / 110.
-// Parts of the long axis where the tiles alone would leave most of the chip's 256 units idle.
+// Parts of the long axis where the tiles alone would leave many of the chip's 256 units idle: joining them is a launch of its own of 4 to
+// 5 us, and a workgroup of 16 rows reads 35 to 70 KB a us, so 400 KB are worth parts, of 128 KB then (us whole / in two / in more: one
+// row behind 1500 entries, 32 heads of 128 on 8, 18.3 / 16.5 / 13.5; four rows behind 9000 22.1 in 8, 18 in more; 4 x 6 rows behind 1100, 20
+// heads of 64, 11.3 / 14.2 / 15.1).  Where every other unit has a tile, parts only even sequences out and have to be larger: 8 trees
+// of 13 rows behind 64 to 1080, 32 heads of 128, 19.6 / 27.3; 16 x 1 behind 300 to 1500, 32 heads on 8, 20 in one, 25 in four; behind 100 to
+// 8000 97 in one, 77 in three, 65 in eight; 32 x 1 behind 100 to 16000 231 in one, 200 in three, 233 in four.
 Plan plan_of(int dtype, int n_seq, int rows, int n_heads, int n_q_heads, int hd, int64_t capacity, int max_len) {
     Plan p;
     const int group = n_q_heads / n_heads, each = n_seq > 0 ? (int)(((int64_t)rows * group + n_seq - 1) / n_seq) : 0;
@@ -795,8 +800,11 @@ Plan plan_of(int dtype, int n_seq, int rows, int n_heads, int n_q_heads, int hd,
     // workgroups if the sequences are alike; the numbers that no tile has end at once
     const int size = 1 << p.tile;
     const int64_t blocks = (int64_t)((each + size - 1) / size) * n_seq * n_heads;
-    int64_t parts = (p.wide || len <= 2048 ? 512 : 1024) / (blocks < 1 ? 1 : blocks);
-    const int64_t most = len / 512;
+    int64_t parts = (p.wide || len <= 2048 ? 512 : 1024) / (blocks < 1 ? 1 : blocks), most = len / 512;
+    if (!p.wide) {
+        const int64_t kb = len * 2 * hd * (int64_t)type_bytes(dtype) >> 10;   // what a workgroup would read one piece after the other
+        most = blocks >= 256 ? kb / 2048 : (blocks >= 128 ? kb / 1024 : (kb < 400 ? 1 : kb / 128));
+    }
     if (parts > most) parts = most;
     if (parts > 64) parts = 64;
     if (parts < 1) parts = 1;

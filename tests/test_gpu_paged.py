@@ -169,6 +169,10 @@ ATTEND = [
     ("bf16", 4, 4, 64, 64, [70], [1300]),
     ("fp16", 4, 2, 64, 16, [1, 2, 0, 3] * 40, [5, 0, 17, 40] * 40),    # more sequences than a wave has lanes
     ("bf16", 8, 1, 64, 32, [9, 0, 11] * 30, [3, 2, 50] * 30),
+    ("fp32", 4, 1, 64, 24, [3, 1], [1900, 40]),            # parts whose borders lie inside pages; a sequence that has one part
+    ("fp32", 2, 2, 256, 16, [2], [700]),
+    ("bf16", 2, 1, 200, 7, [5], [1500]),
+    ("fp16", 12, 4, 80, 16, [30, 1], [2600, 5]),
 ]
 
 
