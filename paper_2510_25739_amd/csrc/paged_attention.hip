@@ -790,6 +790,8 @@ struct Plan { bool wide; int tile, waves, tiles, splits, split_keys; size_t part
 // heads of 64, 11.3 / 14.2 / 15.1).  Where every other unit has a tile, parts only even sequences out and have to be larger: 8 trees
 // of 13 rows behind 64 to 1080, 32 heads of 128, 19.6 / 27.3; 16 x 1 behind 300 to 1500, 32 heads on 8, 20 in one, 25 in four; behind 100 to
 // 8000 97 in one, 77 in three, 65 in eight; 32 x 1 behind 100 to 16000 231 in one, 200 in three, 233 in four.
+// As many parts as make one workgroup of eight waves a unit, two for heads of up to 64 (us with one / two / four of four waves a unit: 4 x 1
+// behind 70001 to 100000, 32 heads of 128 on 8, 228 / 236 / 258; 1 x 5 behind 16000 22.9 / 26.1 / 32; 6 x 6 behind 2500, 20 heads of 64, 27.0 / 21.7 / 21.6).
 Plan plan_of(int dtype, int n_seq, int rows, int n_heads, int n_q_heads, int hd, int64_t capacity, int max_len) {
     Plan p;
     const int group = n_q_heads / n_heads, each = n_seq > 0 ? (int)(((int64_t)rows * group + n_seq - 1) / n_seq) : 0;
@@ -800,11 +802,13 @@ Plan plan_of(int dtype, int n_seq, int rows, int n_heads, int n_q_heads, int hd,
     // workgroups if the sequences are alike; the numbers that no tile has end at once
     const int size = 1 << p.tile;
     const int64_t blocks = (int64_t)((each + size - 1) / size) * n_seq * n_heads;
-    int64_t parts = (p.wide || len <= 2048 ? 512 : 1024) / (blocks < 1 ? 1 : blocks), most = len / 512;
+    int64_t room = 512, most = len / 512;   // workgroups; parts
     if (!p.wide) {
+        room = blocks >= 128 && len > 2048 ? 1024 : (hd <= 64 ? 512 : 256);
         const int64_t kb = len * 2 * hd * (int64_t)type_bytes(dtype) >> 10;   // what a workgroup would read one piece after the other
         most = blocks >= 256 ? kb / 2048 : (blocks >= 128 ? kb / 1024 : (kb < 400 ? 1 : kb / 128));
     }
+    int64_t parts = room / (blocks < 1 ? 1 : blocks);
     if (parts > most) parts = most;
     if (parts > 64) parts = 64;
     if (parts < 1) parts = 1;
