@@ -53,7 +53,10 @@ typedef unsigned v4u __attribute__((ext_vector_type(4)));
 
 constexpr int kCW = 4, kNIO = 4;                 // compute / IO waves per workgroup
 constexpr int kThreads = (kCW + kNIO) * 64, kIOThreads = kNIO * 64;
-constexpr int kXcd = 8, kPer = kNWG / kXcd;      // workgroup i runs on XCD i % 8 (checked by every workgroup)
+// Workgroups go round the XCDs in order, but a hardware queue has its own first one, and in a process that has used several streams a stream
+// may be on another queue from launch to launch: a workgroup is of the XCD that it finds itself on and unit i / 8 there.  If the
+// order were another, some unit would have no workgroup and the waits for it would run out: fail, never hang.
+constexpr int kXcd = 8, kPer = kNWG / kXcd;
 constexpr unsigned kSpinLimit = 1u << 20;
 constexpr int kNIT = 4;                          // cache positions per lane group and register buffer
 constexpr int kPaceGap = 0, kPaceTiles = 6;   // weight requests go out six tiles per wave at a time (see issue_paced); XL shape 780 us a
@@ -1497,8 +1500,7 @@ __global__ __launch_bounds__(kThreads, 1) void verify_xcd_kernel(const XP* __res
     if (threadIdx.x == 0) { *s.join = 0u; *s.go = 0u; *s.sent = 0u; }
     __syncthreads();
     Ctx c;
-    c.x = blockIdx.x % kXcd; c.j = blockIdx.x / kXcd; c.epoch0 = epoch0; c.par = par; c.par_lm = par_lm; c.dead = false; c.err = p.err; c.dbg = dbg;
-    if (xcc_id() != c.x) give_up(c);   // the dispatch order this layout relies on does not hold: fail, never hang
+    c.x = xcc_id() % kXcd; c.j = blockIdx.x / kXcd; c.epoch0 = epoch0; c.par = par; c.par_lm = par_lm; c.dead = false; c.err = p.err; c.dbg = dbg;
     // The two kinds of waves run separate code (and cross the same workgroup barriers), so that neither
     // carries the other's registers: compute waves the weights in flight, IO waves the attention's keys
     // and values and the partial sums of a reduce job.
@@ -1525,8 +1527,7 @@ __global__ __launch_bounds__(kThreads, 1) void verify_xcd_stream_kernel(const XP
     if (threadIdx.x == 0) { *s.join = 0u; *s.go = 0u; *s.sent = 0u; }
     __syncthreads();
     Ctx c;
-    c.x = blockIdx.x % kXcd; c.j = blockIdx.x / kXcd; c.epoch0 = epoch0; c.par = par; c.par_lm = par_lm; c.dead = false; c.err = p.err; c.dbg = dbg;
-    if (xcc_id() != c.x) give_up(c);
+    c.x = xcc_id() % kXcd; c.j = blockIdx.x / kXcd; c.epoch0 = epoch0; c.par = par; c.par_lm = par_lm; c.dead = false; c.err = p.err; c.dbg = dbg;
     if ((threadIdx.x >> 6) >= kCW) io_main<RPJ, HD, false>(p, c, s);
     else compute_main_stream<NA, NC, ND, NE, KE, NL>(p, c, s);
 }
