@@ -375,14 +375,20 @@ def _dtype_of(t):
     return _DTYPES.get(t.dtype, -1)
 
 
+_torch = None
+
+
 def _call_on(index, fn, *args):
     """fn(*args, stream) with device `index` current - launches go to the current device, whatever stream they are given - on
     torch's current stream of that device."""
-    import torch  # device memory and stream only
-    stream = torch._C._cuda_getCurrentRawStream(index)
-    if torch._C._cuda_getDevice() == index:
+    global _torch
+    if _torch is None:
+        import torch  # device memory and stream only
+        _torch = torch
+    stream = _torch._C._cuda_getCurrentRawStream(index)
+    if _torch._C._cuda_getDevice() == index:
         return fn(*args, stream)
-    with torch.cuda.device(index):
+    with _torch.cuda.device(index):
         return fn(*args, stream)
 
 
@@ -426,7 +432,8 @@ class PagedCache:
                                  entry_stride=(se + 7) // 8 * 8 if page_size == 1 else se, dtype=_dtype_of(k), n_layers=n_layers,
                                  n_pages=n_pages, page_size=page_size, n_heads=n_heads, head_dim=head_dim)
         self._ref = C.byref(self._c)
-        self._dev, self._type, self._hd, self._kv = k.get_device(), _dtype_of(k), head_dim, n_heads
+        self._dev, self._hd, self._kv = k.get_device(), head_dim, n_heads
+        self._dtype, self._f32, self._i32, self._i64 = k.dtype, _float32(), _int32(), _int64()
         self._room = {}     # workspace of an attention by (rows, q heads, max_len)
         self.table = table
 
@@ -442,12 +449,13 @@ class PagedCache:
         self._c.table, self._c.table_stride = t.data_ptr(), max(t.shape[1], 1)
         self._c.n_seq, self._c.max_pages = t.shape
         self._n_seq = t.shape[0]
+        self._past_shape, self._start_shape = (self._n_seq,), (self._n_seq + 1,)
         self._room.clear()
 
     def _rows(self, where, rows, row_start, n_past):
-        n, i32, dev = self._n_seq, _int32(), self._dev
+        i32, dev = self._i32, self._dev
         if not (row_start.dtype is i32 and n_past.dtype is i32 and row_start.get_device() == dev and n_past.get_device() == dev
-                and row_start.shape == (n + 1,) and n_past.shape == (n,) and row_start.is_contiguous() and n_past.is_contiguous()):
+                and row_start.shape == self._start_shape and n_past.shape == self._past_shape and row_start.is_contiguous() and n_past.is_contiguous()):
             raise HawkError(-1, where, "row_start [n_seq + 1] and n_past [n_seq] must be contiguous int32 tensors on the cache's device")
         return _PACK_ROWS(row_start.data_ptr(), n_past.data_ptr(), rows)
 
@@ -457,9 +465,14 @@ class PagedCache:
             r, h, d = t.shape
             rs, hs, es = t.stride()
             if d == self._hd and (es == 1 or r == 0) and h > 0 and (rows is None or r == rows) and (heads is None or h == heads):
-                return _PACK_HEADS(t.data_ptr(), rs if r > 1 else h * d, hs if h > 1 else d, h, _dtype_of(t)), r, h
+                return _PACK_HEADS(t.data_ptr(), rs if r > 1 else h * d, hs if h > 1 else d, h, _DTYPES.get(t.dtype, -1)), r, h
         raise HawkError(-1, where, "vectors must be tensors [rows, heads, head_dim] on the cache's device, the last axis contiguous, of the same rows "
                                    "(keys and values: of the cache's heads; results: of the queries')")
+
+    def _result(self, like, rows, heads, dtype):
+        """A new tensor [rows, heads, head_dim] and its HawkHeads."""
+        t = like.new_empty((rows, heads, self._hd), dtype=dtype)
+        return t, _PACK_HEADS(t.data_ptr(), heads * self._hd, self._hd, heads, _DTYPES[dtype])
 
     def _fits(self, where, what, t, dtype, shape):
         if not (t.dtype is dtype and t.get_device() == self._dev and t.shape == shape and t.is_contiguous()):
@@ -473,34 +486,35 @@ class PagedCache:
         halves: pairs (j, j + rot_dim / 2) instead of (2 j, 2 j + 1); pos [rows] int32: positions other than the entries' own;
         q_gain, k_gain [head_dim] fp32: RMS norm per head with eps."""
         where = "hawk_paged_append"
-        hk, rows, _ = self._heads(where, k, heads=self._kv)
+        hk, rows, _ = self._heads(where, k, None, self._kv)
         hv, _, _ = self._heads(where, v, rows, self._kv)
         r = self._rows(where, rows, row_start, n_past)
         hq = ho = None
         if q is not None:
             hq, _, n_heads = self._heads(where, q, rows)
             if q_out is None:
-                q_out = q.new_empty((rows, n_heads, self._hd), dtype=self.k.dtype)
-            ho, _, _ = self._heads(where, q_out, rows, n_heads)
+                q_out, ho = self._result(q, rows, n_heads, self._dtype)
+            else:
+                ho, _, _ = self._heads(where, q_out, rows, n_heads)
         elif q_out is not None:
             raise HawkError(-1, where, "q_out without q")
         gq = gk = table = at = None
         n_pos = rot_dim = 0
         if q_gain is not None:
-            self._fits(where, "gains must be fp32 tensors [head_dim] on the cache's device", q_gain, _float32(), (self._hd,))
+            self._fits(where, "gains must be fp32 tensors [head_dim] on the cache's device", q_gain, self._f32, (self._hd,))
             gq = q_gain.data_ptr()
         if k_gain is not None:
-            self._fits(where, "gains must be fp32 tensors [head_dim] on the cache's device", k_gain, _float32(), (self._hd,))
+            self._fits(where, "gains must be fp32 tensors [head_dim] on the cache's device", k_gain, self._f32, (self._hd,))
             gk = k_gain.data_ptr()
         if rot is not None:
             if rot.dim() != 3:
                 raise HawkError(-1, where, "rot must be a tensor [n_pos, rot_dim / 2, 2]")
             n_pos, half, _ = rot.shape
             rot_dim = 2 * half
-            self._fits(where, "rot must be a contiguous fp32 tensor [n_pos, rot_dim / 2, 2] on the cache's device", rot, _float32(), (n_pos, half, 2))
+            self._fits(where, "rot must be a contiguous fp32 tensor [n_pos, rot_dim / 2, 2] on the cache's device", rot, self._f32, (n_pos, half, 2))
             table = rot.data_ptr()
         if pos is not None:
-            self._fits(where, "pos must be a contiguous int32 tensor [rows] on the cache's device", pos, _int32(), (rows,))
+            self._fits(where, "pos must be a contiguous int32 tensor [rows] on the cache's device", pos, self._i32, (rows,))
             at = pos.data_ptr()
         rc = _call_on(self._dev, self._L.hawk_paged_append, self._ref, layer, r, hq, hk, hv, gq, gk, eps, table, n_pos, rot_dim, 1 if halves else 0,
                       at, ho)
@@ -518,11 +532,12 @@ class PagedCache:
         hq, rows, heads = self._heads(where, q)
         r = self._rows(where, rows, row_start, n_past)
         if out is None:
-            out = q.new_empty((rows, heads, self._hd))
-        ho, _, _ = self._heads(where, out, rows, heads)
+            out, ho = self._result(q, rows, heads, self._dtype)
+        else:
+            ho, _, _ = self._heads(where, out, rows, heads)
         bits = None
         if tree is not None:
-            self._fits(where, "tree must be a contiguous int64 tensor [rows] on the cache's device", tree, _int64(), (rows,))
+            self._fits(where, "tree must be a contiguous int64 tensor [rows] on the cache's device", tree, self._i64, (rows,))
             bits = tree.data_ptr()
         key = (rows, heads, max_len)
         nws = self._room.get(key)
@@ -540,7 +555,7 @@ class PagedCache:
     def keep(self, n_past, path, n_keep):
         """hawk_paged_keep: the accepted path of a tree step, path [n_seq, depth] int32 of node numbers of which the first n_keep
         [n_seq] count, goes to the entries behind n_past's, in every layer."""
-        where, i32, n = "hawk_paged_keep", _int32(), self._n_seq
+        where, i32, n = "hawk_paged_keep", self._i32, self._n_seq
         what = "path [n_seq, depth], n_past and n_keep [n_seq] must be contiguous int32 tensors on the cache's device"
         self._fits(where, what, n_past, i32, (n,))
         self._fits(where, what, n_keep, i32, (n,))
@@ -595,8 +610,7 @@ def verify_chains(p_logits, q_logits, draft, u_acc, u_final, temperature: float,
             _CHAIN_ROOM.clear()
         nws = _CHAIN_ROOM[n_seq, k, n] = L.hawk_verify_chains_workspace_bytes(n_seq, k, n)
     ws = p_logits.new_empty((max(nws, 16),), dtype=_uint8())
-    out = p_logits.new_empty((n_seq * (k + 2),), dtype=i32)
-    count, toks = out[:n_seq], out[n_seq:].view(n_seq, k + 1)
+    count, toks = draft.new_empty((n_seq,)), draft.new_empty((n_seq, k + 1))
     rc = _call_on(dev, L.hawk_verify_chains, p_logits.data_ptr(), ps if p_rows > 1 else n, p_start.data_ptr() if p_start is not None else None, p_rows,
                   q, qs, qr, draft.data_ptr(), n_draft.data_ptr() if n_draft is not None else None, u_acc.data_ptr(), u_final.data_ptr(),
                   n_seq, k, n, temperature, top_k, count.data_ptr(), toks.data_ptr(), ws.data_ptr(), nws)
