@@ -75,7 +75,7 @@ __device__ __forceinline__ float sum_of_lanes(float v, int n) {
 // Dependent latencies (row starts and lengths, then table and rotation) stand against a few hundred bytes, so a workgroup stays for as
 // many rows as make the chip full of workgroups once, holds what is the same for all of them - where its vectors come from and go
 // to, their gains, the sequences - and has the next row's requests under way while it works on a row's.  4048 rows of 32 + 16 heads of
-// 128, norms and rotation of halves: 28 us (3.6 TB/s of what is read and written; a copy of as much takes 21), with a workgroup for
+// 128, norms and rotation of halves: 25.9 us (3.9 TB/s of what is read and written; a copy of as much takes 21), with a workgroup for
 // every two rows 34.4, for every row 37.3; 16000 rows of 16 + 4 heads of 256 99 us, with a workgroup for two rows 139.
 constexpr int kResident = 1024;     // workgroups that are on the chip at a time: four to a unit
 template <int FROM, int TO>   // types
