@@ -73,6 +73,9 @@ size_t paged_attention_workspace_bytes(const hawk_paged_cache* cache, int rows, 
 int launch_paged_attention(const hawk_paged_cache* cache, int layer, const hawk_paged_rows* rows, const hawk_heads* q,
                            const uint64_t* tree, float scale, int max_len, const hawk_heads* out, void* workspace,
                            size_t workspace_bytes, hipStream_t stream);
+// rules of the dispatch and of the kernels, for the tests as well
+extern "C" int hawk_paged_attention_plan(int dtype, int n_seq, int rows, int n_heads, int n_q_heads, int hd, int capacity, int max_len);
+extern "C" int hawk_paged_attention_row(const int32_t* row_start, int n_past, int s, int rows, int group, int capacity, int tile_log2, int tile, int r);
 
 #if defined(__HIPCC__)
 namespace {

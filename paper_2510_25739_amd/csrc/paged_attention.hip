@@ -39,7 +39,7 @@ struct Span {
     int end;                   // entries from this one on are seen by no row of the tile
     int all;                   // entries before this one are seen by every row of the tile
 };
-__device__ __forceinline__ Span span_of(const AttnArgs& a, int s, int first, int start, int stop, int past) {
+__host__ __device__ inline Span span_of(const AttnArgs& a, int s, int first, int start, int stop, int past) {
     Span t;
     t.s = s;
     t.first = first;
@@ -60,8 +60,14 @@ __device__ __forceinline__ Span span_of(const AttnArgs& a, int s, int first, int
 }
 // Tiles are counted so that a sequence's first tile follows from its first row alone: base(s) = row_start[s] * group / tile + s,
 // which leaves every sequence room for its tiles and at most one unused number per sequence.
-__device__ __forceinline__ int tile_base(const AttnArgs& a, int s, int start) {
+__host__ __device__ inline int tile_base(const AttnArgs& a, int s, int start) {
     return (min(max(start, 0), a.r.rows) * a.group.d >> a.tile) + s;   // (rows * group is below 2^30)
+}
+// Tile `tile` as one of sequence s; false: it is none of its.  Where row starts do not ascend the search below may end at any
+// sequence, one whose tiles lie behind this one (first below 0) among them.
+__host__ __device__ inline bool tile_of(const AttnArgs& a, int s, int tile, int start, int stop, int past, Span& t) {
+    t = span_of(a, s, (tile - tile_base(a, s, start)) * (1 << a.tile), start, stop, past);
+    return t.first >= 0 && t.first < t.n * a.group.d;
 }
 // The sequence of a tile and its span; false: the tile is one of the unused numbers.  Up to 64 sequences every lane has one
 // sequence's words, and the answer is there after one latency.
@@ -83,8 +89,7 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& a, int lane, int tile,
         stop = a.r.row_start[s + 1];
         past = a.r.n_past[s];
     }
-    t = span_of(a, s, (tile - tile_base(a, s, start)) << a.tile, start, stop, past);
-    return t.first < t.n * a.group.d;
+    return tile_of(a, s, tile, start, stop, past, t);
 }
 // What a row of a tree sees; a row of a chain sees the entries up to its own.
 __device__ __forceinline__ bool node_sees(const Span& t, int own, unsigned long long bits, int e) {
@@ -742,7 +747,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a, int lanes) 
     const int s = last_not_above(a.c.n_seq, lane, row, [&](int i) { return (int64_t)a.r.row_start[i]; });
     if (s < 0) return;
     const int start = a.r.row_start[s], stop = a.r.row_start[s + 1];
-    if (row >= stop) return;
+    if (row < start || row >= stop) return;   // (the first only where row starts do not ascend)
     const Span t = span_of(a, s, ((row - max(start, 0)) * a.group.d + (qh - qh / a.group * a.group.d)) >> a.tile << a.tile, start, stop, a.r.n_past[s]);
     const int n = used_splits(a, t.end);
     const int64_t step = (int64_t)a.r.rows * a.q.n_heads, vec = (int64_t)row * a.q.n_heads + qh;
@@ -861,6 +866,20 @@ extern "C" int hawk_paged_attention_plan(int dtype, int n_seq, int rows, int n_h
     if (n_seq < 0 || rows < 0 || n_heads < 1 || n_q_heads < n_heads || capacity < 1) return 0;
     const Plan p = plan_of(dtype, n_seq, rows, n_heads, n_q_heads, hd, capacity, max_len);
     return p.tile * 10000 + (p.wide ? (p.tile == 8 ? 8 : 4) : (hd > 128 ? 4 : p.waves)) * 100 + p.splits;
+}
+
+// The row of the buffers that row r of tile `tile` (of 2^tile_log2 rows) is, if the search for the tile ends at sequence s; -1: none. What the
+// kernels compute, for the tests.
+extern "C" int hawk_paged_attention_row(const int32_t* row_start, int n_past, int s, int rows, int group, int capacity, int tile_log2, int tile, int r) {
+    AttnArgs a = {};
+    a.r.rows = rows;
+    a.group = divisor(group);
+    a.c.capacity = capacity;
+    a.tile = tile_log2;
+    Span t;
+    if (!tile_of(a, s, tile, row_start[s], row_start[s + 1], n_past, t)) return -1;
+    const int pr = t.first + r;
+    return pr < t.n * a.group.d ? t.r0 + pr / a.group : -1;
 }
 
 size_t paged_attention_workspace_bytes(const hawk_paged_cache* cache, int rows, int n_q_heads, int max_len) {

@@ -177,3 +177,46 @@ def test_the_rule_of_the_cut_takes_any_sizes(H):
     L = H.load_library()
     for a in ((1, 3, 5, 0, 4, 64, 100, 0), (1, 3, 5, 2, 1, 64, 100, 0), (1, 0, 5, 2, 4, 64, 100, 0), (1, 3, -1, 2, 4, 64, 100, 0), (1, 3, 5, 2, 4, 64, 0, 0)):
         assert L.hawk_paged_attention_plan(*a) >= 0
+
+
+def bad_starts():
+    """Row starts as they must not be: descending, below 0, behind the rows, in any order; and one as it must."""
+    rng = np.random.RandomState(7)
+    far = [-2 ** 31, -1000, -1, 0, 5, 90, 99, 100, 101, 1000, 2 ** 31 - 1]
+    for n_seq in (1, 3, 4, 70, 130):
+        yield np.sort(rng.randint(0, 101, n_seq + 1))
+        yield np.sort(rng.randint(0, 101, n_seq + 1))[::-1]
+        for _ in range(3):
+            yield rng.randint(-50, 160, n_seq + 1)
+            yield rng.choice(far, n_seq + 1)
+    yield np.array([0, 90, 0, 5])
+
+
+@pytest.mark.parametrize("group,tile", [(1, 4), (4, 4), (3, 7), (8, 8)])
+def test_no_row_starts_lead_a_tile_outside_the_buffers(H, group, tile):
+    # Whichever sequence the search for a tile ends at, the rows of the tile are rows of that sequence and of the buffers.  (Of the last array,
+    # 100 rows in groups of four, tile 2 taken as sequence 1's had row 2^30.)
+    L, rows = H.load_library(), 100
+    for starts in bad_starts():
+        starts = np.ascontiguousarray(starts, dtype=np.int32)
+        p, n_seq = starts.ctypes.data_as(C.c_void_p), len(starts) - 1
+        tiles = (rows * group >> tile) + n_seq
+        for s in sorted({0, 1, 2, n_seq // 2, n_seq - 1} & set(range(n_seq))):
+            lo, hi = max(int(starts[s]), 0), min(int(starts[s + 1]), rows)
+            for t in range(tiles):
+                for r in {0, 1, group, (1 << tile) // 2, (1 << tile) - 1}:
+                    row = L.hawk_paged_attention_row(p, 10, s, rows, group, 4096, tile, t, r)
+                    assert row == -1 or lo <= row < hi, (starts, s, t, r, row)
+
+
+@pytest.mark.parametrize("group,tile", [(1, 4), (4, 4), (3, 7), (8, 8)])
+def test_tiles_hold_every_row_of_a_step_once(H, group, tile):
+    L, rows = H.load_library(), 100
+    starts = np.array([0, 0, 7, 8, 40, 40, 93], dtype=np.int32)
+    p, n_seq = starts.ctypes.data_as(C.c_void_p), len(starts) - 1
+    count = np.zeros(rows + 1, dtype=int)
+    for s in range(n_seq):
+        for t in range((rows * group >> tile) + n_seq):
+            for r in range(1 << tile):
+                count[L.hawk_paged_attention_row(p, 0, s, rows, group, 4096, tile, t, r)] += 1
+    assert (count[:93] == group).all() and (count[93:rows] == 0).all()
