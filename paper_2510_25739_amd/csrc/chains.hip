@@ -9,6 +9,10 @@
 // picks the part and the entry.
 #include "sample_rows.h"
 
+// Kernels here compute the same value more than once - an entry's bin in two passes, a weight where it is summed and where it is drawn - and
+// compare what comes out: every product is rounded by itself, whatever it is added to.
+#pragma clang fp contract(off)
+
 namespace hawk {
 
 namespace {
@@ -45,7 +49,8 @@ __device__ __forceinline__ const float* chain_row(const ChainArgs& a, int s, int
 __device__ __forceinline__ bool row_needed(const ChainArgs& a, int r, int nd) { return r <= a.k ? r <= nd : r - a.k - 1 < nd; }
 
 // The threshold of a long row's top_k largest: linear bins below the maximum (whatever lies more than kReach below shares the last one),
-// and an exact ranking of the entries of the threshold's bin.  Rows this does not thin out take the general form.
+// and an exact ranking of the entries of the threshold's bin.  Rows this does not thin out take the general form.  Both passes bin the rounded
+// z (a product fused with the difference to the maximum would put entries at a border into another bin than the second pass).
 constexpr float kReach = 32.f;
 constexpr int kRank = 1024;
 struct LongShared {
