@@ -496,7 +496,8 @@ int hawk_paged_append(const hawk_paged_cache* cache, int layer, const hawk_paged
  * over the entries e that exist and that the row sees: e <= n_past + i; or, with tree (uint64 [rows]), the
  * committed entries e < n_past, those of the step's rows j < 64 whose bit j is set in tree[row] (e = n_past + j; the
  * ancestors of hawk_tree_layout) and its own.  A row that sees nothing (or whose every score is minus infinity) gives zeros.  What
- * a row does not see has no part in its result, whatever values it holds.
+ * a row does not see has no part in its result, whatever values it holds.  An infinity among the values it sees is in its result, however
+ * small the weight (NaN where both signs meet, and where a score is NaN or plus infinity).
  * q of the cache's type; out of any of the three types, not overlapping q.  Scores, maximum, sums and results in
  * fp32; the weights reach the products of 16-bit types with about 16 bits where sequences have few rows, rounded to the type
  * where they have many (64 rows times group and more, behind long sequences).

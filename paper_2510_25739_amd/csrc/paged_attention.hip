@@ -176,30 +176,51 @@ template <> struct Of<HAWK_FP32> {
     static __device__ __forceinline__ unsigned clear(unsigned w) { return (w & kExp) == kExp ? 0u : w; }
 };
 
-// Infinities and NaN among the values of entries that only some rows of a tile see would make NaN of the others' weights of zero:
-// they are zeros in the products, and are added, behind everything else, to results of rows that see them, where these have been
-// stored: N features from f on of a row, at dst.
+// Infinities and NaN among the values, N features from f on of a row whose results are at dst.  An infinity that a row sees is in its result with
+// its sign, however small its weight.
+//   Of entries that only some rows of a tile see they would make NaN of the others' weights of zero: they are zeros in the products
+// (entries from .. to - 1), and are added here, behind everything else.
+//   Where every row sees an entry its values are multiplied as they are.  A weight's second part, which is zero or below it for every other
+// weight, or a weight or factor that is zero in 32 bits then makes NaN of an infinity.  So a feature that is NaN is what the infinities and NaN
+// among all values the row sees (entries begin .. to - 1) add up to; where there are none it stays.  (The row's sum of weights is a number above
+// zero: that is looked at before.)
 template <int TYPE, int N>
-__device__ void add_odd(const AttnArgs& a, const Span& t, const char* vh, int own, unsigned long long bits, int from, int to, int f, char* dst,
-                        int64_t at, int dtype) {
+__device__ void add_odd(const AttnArgs& a, const Span& t, const char* vh, int own, unsigned long long bits, int begin, int from, int to, int f,
+                        char* dst, int64_t at, int dtype) {
     const int32_t* pages = a.c.table + (int64_t)t.s * a.c.table_stride;
-    for (int e = max(from, 0); e < to; ++e) {
+    auto stored = [&](int j) {
+        float x, y;
+        if (dtype == HAWK_FP32) return *reinterpret_cast<const float*>(dst + (at + j) * 4);
+        widen2(*reinterpret_cast<const unsigned short*>(dst + (at + j) * 2), dtype, x, y);
+        return x;
+    };
+    float sum[N];
+    unsigned lost = 0u, some = 0u;   // features that are NaN; that have anything to add
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        sum[j] = 0.f;
+        lost |= isnan(stored(j)) ? 1u << j : 0u;
+    }
+    for (int e = max(lost ? begin : from, 0); e < to; ++e) {
         const int64_t place = entry_at(a.c, pages, e);
         if (place < 0 || !(a.tree ? node_sees(t, own, bits, e) : e <= own)) continue;
+        const unsigned take = e < from ? lost : ~0u;
+#pragma unroll
         for (int j = 0; j < N; ++j) {
             float v;
             if constexpr (TYPE == HAWK_FP32) v = *reinterpret_cast<const float*>(vh + (place + f + j) * 4);
             else v = Of<TYPE>::widen(*reinterpret_cast<const unsigned short*>(vh + (place + f + j) * 2));
-            if (fabsf(v) <= 3.4028235e38f) continue;
-            if (dtype == HAWK_FP32) {
-                *reinterpret_cast<float*>(dst + (at + j) * 4) += v;
-            } else {
-                unsigned short* p = reinterpret_cast<unsigned short*>(dst + (at + j) * 2);
-                float x, y;
-                widen2(*p, dtype, x, y);
-                *p = (unsigned short)narrow2(x + v, 0.f, dtype);
-            }
+            if (fabsf(v) <= 3.4028235e38f || !((take >> j) & 1u)) continue;
+            sum[j] += v;
+            some |= 1u << j;
         }
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        if (!((some >> j) & 1u)) continue;
+        const float x = (lost >> j) & 1u ? sum[j] : stored(j) + sum[j];
+        if (dtype == HAWK_FP32) *reinterpret_cast<float*>(dst + (at + j) * 4) = x;
+        else *reinterpret_cast<unsigned short*>(dst + (at + j) * 2) = (unsigned short)narrow2(x, 0.f, dtype);
     }
 }
 
@@ -455,6 +476,16 @@ __global__ __launch_bounds__(64 * NW, DP == 64 ? (NW == 4 ? 3 : (TYPE == HAWK_FP
         ml[0] = mt;
         ml[1] = lt;
     }
+    // eight features of a row per thread
+    const int type = whole ? a.out.dtype : HAWK_FP32;
+    char* dst = whole ? a.out.data : reinterpret_cast<char*>(a.part);
+    auto place_of = [&](int rr, int ff, int& ri) {
+        const int prr = t.first + rr;
+        ri = prr / a.group;
+        const int64_t orow = t.r0 + ri, oh = head * a.group.d + prr - ri * a.group.d;
+        return whole ? orow * a.out.row_stride + oh * a.out.head_stride + ff : (((int64_t)split * a.r.rows + orow) * a.q.n_heads + oh) * hd + ff;
+    };
+    bool lost = false;   // a result of this thread's is NaN
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
         if (c > 0) __syncthreads();
@@ -463,26 +494,36 @@ __global__ __launch_bounds__(64 * NW, DP == 64 ? (NW == 4 ? 3 : (TYPE == HAWK_FP
 #pragma unroll
             for (int d = 0; d < VC; ++d) lo[wave][m16][(g * 4 + y) * VC + d] = o[c * VC + d][y] * (mine * norm);
         __syncthreads();
-        // eight features of a row per thread
         for (int u = threadIdx.x; u < kTile * (COLS / 8); u += 64 * NW) {
-            const int rr = u / (COLS / 8), f = (u % (COLS / 8)) * 8, ff = c * COLS + f, prr = t.first + rr;
-            if (prr >= t.n * a.group.d || (PAD && ff >= hd)) continue;
+            const int rr = u / (COLS / 8), f = (u % (COLS / 8)) * 8, ff = c * COLS + f;
+            if (t.first + rr >= t.n * a.group.d || (PAD && ff >= hd)) continue;
             float x[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 x[e] = 0.f;
 #pragma unroll
                 for (int w = 0; w < NW; ++w) x[e] += lo[w][rr][f + e];
+                lost = lost || isnan(x[e]);
             }
-            const int ri = prr / a.group;
-            const int64_t orow = t.r0 + ri, oh = head * a.group.d + prr - ri * a.group.d;
-            char* dst = whole ? a.out.data : reinterpret_cast<char*>(a.part);
-            const int64_t at = whole ? orow * a.out.row_stride + oh * a.out.head_stride + ff : (((int64_t)split * a.r.rows + orow) * a.q.n_heads + oh) * hd + ff;
-            const int type = whole ? a.out.dtype : HAWK_FP32;
-            store8(dst, at, type, x);
-            if (any_odd) add_odd<TYPE, 8>(a, t, vh, t.past + ri, a.tree ? a.tree[orow] : 0ull, max(k0, t.all - KEYS), k1, ff, dst, at, type);
+            int ri;
+            store8(dst, place_of(rr, ff, ri), type, x);
         }
     }
+    if (!lost && !any_odd) return;
+    for (int c = 0; c < NC; ++c)
+        for (int u = threadIdx.x; u < kTile * (COLS / 8); u += 64 * NW) {
+            const int rr = u / (COLS / 8), ff = c * COLS + (u % (COLS / 8)) * 8;
+            if (t.first + rr >= t.n * a.group.d || (PAD && ff >= hd)) continue;
+            float sum = 0.f;   // of the row's weights: where it is NaN or zero, so is every feature
+#pragma unroll
+            for (int w = 0; w < NW; ++w) sum += ll[w][rr];
+            int ri;
+            const int64_t at = place_of(rr, ff, ri);
+            const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (sum == 0.f) store8(dst, at, type, none);
+            else if (!isnan(sum))
+                add_odd<TYPE, 8>(a, t, vh, t.past + ri, a.tree ? a.tree[t.r0 + ri] : 0ull, k0, max(k0, t.all - KEYS), k1, ff, dst, at, type);
+        }
 }
 
 // Many rows: a workgroup of four or eight waves, 32 rows each, over turns of KB entries that all of them read from LDS.  The next
@@ -722,6 +763,7 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void paged_wide_kernel(
     char* dst = whole ? a.out.data : reinterpret_cast<char*>(a.part);
     const int64_t at = whole ? (int64_t)row * a.out.row_stride + (int64_t)qh * a.out.head_stride : vec * hd;
     const int type = whole ? a.out.dtype : HAWK_FP32;
+    bool lost = false;
 #pragma unroll
     for (int d = 0; d < NT; ++d)
 #pragma unroll
@@ -730,11 +772,19 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void paged_wide_kernel(
             if (PAD && f >= hd) continue;
             float x[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = o[d][4 * b + e] * norm;
+            for (int e = 0; e < 4; ++e) {
+                x[e] = o[d][4 * b + e] * norm;
+                lost = lost || isnan(x[e]);
+            }
             store4(dst, at + f, type, x);
         }
-    if (found)
-        for (int f = 4 * hh; f < hd; f += 8) add_odd<TYPE, 4>(a, t, vh, own, bits, max(k0, t.all - KB), k1, f, dst, at + f, type);
+    if (lost || found) {
+        const float none[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int f = 4 * hh; f < hd; f += 8) {
+            if (l == 0.f) store4(dst, at + f, type, none);
+            else if (!isnan(l)) add_odd<TYPE, 4>(a, t, vh, own, bits, k0, max(k0, t.all - KB), k1, f, dst, at + f, type);
+        }
+    }
 }
 
 // Joins the parts of a long axis: a wave per (row, head).  Lane i has part i's maximum and sum; groups of lanes take a part's features each,
@@ -759,7 +809,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a, int lanes) 
     const float base = mt == -INFINITY ? 0.f : mt;
 #pragma unroll 4
     for (int i = part0; i < n; i += per) {
-        const float w = __builtin_amdgcn_exp2f(a.part_ml[(i * step + vec) * 2] - base);
+        const float w = fmaxf(__builtin_amdgcn_exp2f(a.part_ml[(i * step + vec) * 2] - base), 0x1p-126f);   // (not zero: infinities stay what they are)
         lt += a.part_ml[(i * step + vec) * 2 + 1] * w;
         if (f < a.c.hd) {
             float y[8];
