@@ -502,7 +502,8 @@ int hawk_paged_append(const hawk_paged_cache* cache, int layer, const hawk_paged
  * fp32; the weights reach the products of 16-bit types with about 16 bits where sequences have few rows, rounded to the type
  * where they have many (64 rows times group and more, behind long sequences).
  * scale > 0.  max_len (host): the longest n_past + rows of a sequence, for the choice of the kernel only: any value
- * gives the right results (at most max_pages * page_size is assumed).
+ * gives the right results (at most max_pages * page_size is assumed).  That choice is one for the whole call and goes by the average
+ * rows of a sequence: single tokens behind long histories and a large piece of a prompt are faster as two calls.
  * workspace (may be NULL where the size function says 0; 16-byte aligned): hawk_paged_attention_workspace_bytes
  * for the same cache, rows and max_len; nothing in it has to be cleared or is kept from call to call. */
 size_t hawk_paged_attention_workspace_bytes(const hawk_paged_cache* cache, int rows, int n_q_heads, int max_len);

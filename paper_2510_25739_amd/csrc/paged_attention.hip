@@ -530,6 +530,9 @@ __global__ __launch_bounds__(64 * NW, DP == 64 ? (NW == 4 ? 3 : (TYPE == HAWK_FP
 // turn's keys and values are in registers while this one is computed and are written behind it, two buffers, one barrier a
 // turn.  Products of 32 x 32 x 16: a lane has one row's 16 scores of 32 entries - blocks of four entries, the other half of the
 // wave the blocks between -, which in that order are the next product's operand; values are read transposed.
+// Weights are rounded to the type once before the product with the values (their sum is not): a second part as in the tiles of 16 rows would be
+// half of all products again, 374 us where this takes 291 (4001 rows x 4 behind 2048, heads of 128, bf16), and takes the relative error of
+// bf16 results, which their own rounding makes 1.66e-3, from 2.34e-3 to 1.66e-3.
 // LDS rows keep their 16-byte pieces in an order changed by the row number, so that the 16 rows (keys) or four rows (values) that a
 // request touches lie on different banks.
 template <int TYPE> struct Wide;

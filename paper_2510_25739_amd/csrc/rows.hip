@@ -107,8 +107,10 @@ __device__ __forceinline__ float ssq_share(const RowsGemm& g, int row, int lane,
     return v;
 }
 
-// A workgroup past a launch's own: brings its share of what the next launches read into the L2 it will be read from.  Their
-// workgroup i runs on XCD i % 8 and so do strip group i % 8, + 8, .. of its weights; so do the workgroups here.
+// A workgroup past a launch's own: brings its share of what the next launches read into the L2 it will be read from.  Workgroups
+// i, i + 8, .. of a launch run on one XCD, the same one from launch to launch as long as the stream stays on its hardware queue, and
+// so do strip groups i, i + 8, .. of their weights; so do the workgroups here.  (A process that uses several streams may find its
+// launches on another queue: then the weights lie in L2s that do not read them, and nothing else changes.)
 // (Kernels have an instance without this: the parameters and the look at them cost 0.2 us a launch.)
 __device__ __forceinline__ void bring_ahead(const Ahead& a, int wave, int waves, int lane) {
     const int x = blockIdx.x & 7, all = (a.extra >> 3) * waves, mine = (((int)blockIdx.x - a.grid) >> 3) * waves + wave;
@@ -191,7 +193,7 @@ __device__ __forceinline__ void rows_gemm(const RowsGemm& g) {
     __shared__ float rscale[16 * CT];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int r16 = lane & 15, kg = lane >> 4;
-    // workgroup i runs on XCD i % 8: the row groups of a strip group follow each other on the same XCD
+    // workgroups i, i + 8, .. run on one XCD: the row groups of a strip group follow each other on the same XCD
     const int strips = g.N / 16, tiles = (g.M + 15) / 16, groups = (tiles + CT - 1) / CT, i8 = blockIdx.x >> 3;
     const int s_first = ((i8 / groups) * 8 + (blockIdx.x & 7)) * SR, t_first = (i8 % groups) * CT;
     if (s_first >= strips) return;
@@ -333,7 +335,7 @@ __global__ __launch_bounds__(64 * WN * WM) void rows_gemm_staged_kernel(RowsGemm
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int r16 = lane & 15, kg = lane >> 4, wn = wave / WM, wm = wave - wn * WM;
     const int strips = g.N / 16, tiles = (g.M + 15) / 16, nk = g.K / 32;
-    // Workgroup i runs on XCD i % 8: an XCD takes a contiguous piece of the list (row groups outer, strip groups
+    // Workgroups i, i + 8, .. run on one XCD: an XCD takes a contiguous piece of the list (row groups outer, strip groups
     // inner), so that the row groups it works on at a time stay in its L2.
     const int sg = (strips + BS - 1) / BS, total = sg * ((tiles + BT - 1) / BT);
     const int per = (total + 7) / 8, id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);

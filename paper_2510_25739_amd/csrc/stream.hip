@@ -50,7 +50,7 @@ constexpr int kRing = 3;                        // exchange arenas used round ro
 constexpr int kPS = 68;                         // floats per attention partial row: 64 outputs, max, sum, pad
 constexpr int kNIT = 6;                         // iterations (of kCW*8 cache positions) per KV register buffer
 constexpr int kNCMax = 4;                       // chunks per (sequence, head)
-constexpr int kXcd = 8, kPerXcd = kNWG / kXcd;  // workgroup i is dispatched to XCD i % 8
+constexpr int kXcd = 8, kPerXcd = kNWG / kXcd;  // workgroups i, i + 8, .. run on one XCD (which one is the queue's)
 
 // ------------------------------------------------------------------------- kernel parameters
 
@@ -1318,7 +1318,7 @@ void build_plan(const hawk_ctx* c, StreamPlan* P) {
     std::vector<std::vector<int>> assign[K_NKIND];  // [kind][round][wg] -> strips
     for (int k = 0; k < K_NKIND; ++k) assign[k].assign((size_t)P->kind[k].rounds * kNWG, {});
     // Wo and W2: strip s of both belongs to workgroup s, which keeps that strip of the residual
-    // stream in registers for the whole launch (workgroup s runs on XCD s % 8).
+    // stream in registers for the whole launch (strips s, s + 8, .. on one XCD).
     if (nstrips[K_C] > kNWG || nstrips[K_E] != nstrips[K_C]) { P->ok = false; return; }
     std::vector<long> load(kNWG, 0);
     const int fE = P->kind[K_E].ksplit;

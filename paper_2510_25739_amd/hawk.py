@@ -410,7 +410,8 @@ class PagedCache:
     k, v: device tensors [n_layers, n_pages, n_heads, page_size, head_dim] (or without the first axis) of the same strides,
     fp32, bf16 or fp16, the last axis contiguous - any other order of the axes is a permuted view.  table [n_seq, max_pages]
     int32: the pages of every sequence.  The tensors stay the caller's: their contents may change between calls (new pages
-    in the table), and `table` may be replaced by another tensor (a captured graph keeps the one it was captured with).
+    in the table), and `table` may be replaced by another tensor (a captured graph goes on reading the one it was captured with,
+    which the caller then keeps).
     Calls launch on torch's current stream of the cache's device.  `row_start` [n_seq + 1] and `n_past` [n_seq] are int32 device
     tensors: rows row_start[s] .. row_start[s + 1] - 1 of a call belong to sequence s, which has n_past[s] committed entries."""
 
