@@ -8,6 +8,9 @@
 // same tile: row r of a tile is (row of the sequence r / group, head r % group).
 #include "paged.h"
 
+// A score and its row's maximum are rounded alike, so that their difference is never above zero: nothing is fused but where it says so.
+#pragma clang fp contract(off)
+
 namespace hawk {
 
 namespace {
@@ -549,6 +552,7 @@ template <> struct Wide<HAWK_FP16> {
     }
 };
 constexpr float kLag = 8.f;   // results are rescaled when a row's maximum has grown by more than 2^8, not whenever it grows
+constexpr float kFused = 0x1p20f;   // scaled scores up to this (half a step: 2^-5) are multiplied and added in one instruction
 
 // EASY as above: a wave's part of a turn's rows lies in one group of 16, whose place is found once for the wave and added to by the
 // requests themselves.
@@ -722,12 +726,23 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void paged_wide_kernel(
 #pragma unroll
                 for (int d = 0; d < NT; ++d) o[d] *= shrink;
             }
-            const float off = Wide<TYPE>::kLift - (mb == -INFINITY ? 0.f : mb);
+            const float ref = mb == -INFINITY ? 0.f : mb;
+            float by = c, off = Wide<TYPE>::kLift - ref;
+            // The reference is a rounded product: an entry's own, not rounded, may lie above it by half a step.  Where that is more than a
+            // small part of a power of two - a weight could leave the type, or every weight of a row be zero - both are rounded.
+            if (__any(fabsf(ref) > kFused)) {
+#pragma unroll
+                for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) z[u][r] = z[u][r] * c - ref;
+                by = 1.f;
+                off = Wide<TYPE>::kLift;
+            }
 #pragma unroll
             for (int u = 0; u < SUB; ++u)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    z[u][r] = __builtin_amdgcn_exp2f(fmaf(z[u][r], c, off));
+                    z[u][r] = __builtin_amdgcn_exp2f(fmaf(z[u][r], by, off));
                     l += z[u][r];
                 }
 #pragma unroll

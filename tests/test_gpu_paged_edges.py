@@ -149,3 +149,42 @@ def test_a_score_that_is_nan_or_plus_infinity_is_nan_whatever_the_values(H, cach
         assert bool(out[:, :heads // 2].isnan().all())
         other = out[:, heads // 2:]
         assert bool((other[0, :, 5] == float("inf")).all()) and bool(other[1:, :, 5].isnan().all()) and int(other.isnan().sum()) == 8 * (heads // 2)
+
+
+LARGE = [
+    # cache, heads, kv_heads, hd, page, rows, past, rows of a tile, log2 of the largest query and key
+    ("bf16", 2, 2, 64, 16, [9], [700], 16, 20, 18),
+    ("fp16", 2, 2, 128, 16, [9], [2100], 16, 15, 15),
+    ("fp32", 2, 2, 96, 6, [9], [700], 16, 20, 18),
+    ("bf16", 48, 2, 64, 16, [9], [1500], 128, 20, 18),
+    ("bf16", 48, 2, 128, 6, [9], [1500], 128, 26, 20),
+    ("fp16", 48, 2, 128, 16, [9], [1500], 128, 15, 15),
+    ("fp16", 48, 2, 200, 16, [9], [1500], 128, 13, 13),
+    ("bf16", 64, 8, 64, 16, [70, 64] * 5, [300, 90] * 5, 128, 18, 14),
+    ("fp16", 32, 2, 64, 16, [150, 131] * 10, [340, 300] * 10, 256, 15, 15),
+]
+
+
+@pytest.mark.parametrize("cache,heads,kv_heads,hd,page,rows,past,tile,q_log,k_log", LARGE)
+def test_scores_of_which_one_step_is_more_than_a_power_of_two(H, cache, heads, kv_heads, hd, page, rows, past, tile, q_log, k_log):
+    # One feature makes the score, so that it is exact, and two scores of a large query are equal or far apart: the weights are one (or a few
+    # equal ones) and zero.  Queries of ordinary size lie between them, in the same tile.
+    import torch
+    su = Setup(H, hd + tile, cache, kv_heads, hd, page, rows, past, spare=400000 // page)
+    su.fill()
+    assert plan(H, su, heads)[0] == tile
+    for s, K in enumerate(su.K):
+        K.zero_()
+        K[:, :, 5] = (torch.randn(len(K), kv_heads, generator=su.g) * 2.0 ** (k_log - 2)).clamp(-2.0 ** k_log, 2.0 ** k_log).to(dt(cache)).double()
+        e = torch.arange(len(K))
+        pg = torch.from_numpy(su.table_np[s].astype(np.int64))[e // page]
+        su.k[0].index_put_((pg.to(DEV)[:, None], torch.arange(kv_heads, device=DEV)[None], (e % page).to(DEV)[:, None]), K.to(dt(cache)).to(DEV))
+    q = su.randn(su.total, heads, hd)
+    large = torch.rand(su.total, heads, generator=su.g) < 0.6
+    sign = torch.where(torch.rand(su.total, heads, generator=su.g) < 0.5, -1.0, 1.0)
+    q[:, :, 5] = (sign * torch.where(large, 2.0 ** q_log, 2.0 ** (1 - k_log))).to(dt(cache))
+    o, m, er = attention_reference(su, q, lambda s, i, e: e <= past[s] + i, hd ** -0.5)
+    er = torch.where(large[..., None], torch.zeros((), dtype=torch.float64), er)
+    for max_len in (0, max(p + n for p, n in zip(past, rows))):
+        got = su.cache.attend(q.to(DEV), su.row_start, su.n_past, max_len=max_len)
+        check_attention(su, got, (o, m, er), cache, weight_step(cache, plan(H, su, heads, max_len)[0]))
