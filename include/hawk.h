@@ -523,6 +523,88 @@ int hawk_paged_keep(const hawk_paged_cache* cache, const int32_t* n_past, const 
  * the entry does not exist (host arithmetic only; the kernels use the same function). */
 int64_t hawk_paged_entry(const hawk_paged_cache* cache, const int32_t* table_row, int layer, int64_t e);
 
+/* Pages of many sequences.  Which page holds what is known from the cache's table, which these calls write, and from refs
+ * (int32 [n_pages]): how many places of the table have a page, 0: it is free.  A program starts with a table of -1 and refs of 0, gets its pages
+ * by hawk_paged_take before it appends, and keeps both in step by making all changes through these calls.  Several sequences may hold one
+ * page (images of one prompt): a page that more than one place has is never written, hawk_paged_take gives the writer one of its own first.
+ * Counts below 0 are free pages; what the arrays hold is checked as everywhere: no page outside the pool is read, written or counted.
+ *
+ * hawk_paged_fork: sequence dst[i] becomes a second holder of what sequence src[i] has committed (i < n, n <= n_seq): its row of the table gets
+ *   the pages of the first n_past[src[i]] entries, n_past[dst[i]] that length, and the pages it held until now are given back.  A pair
+ *   is left out if either number is no sequence, both are the same, an earlier pair has the same dst, or its src is the dst of any pair.
+ * hawk_paged_take: pages for entries n_past[s] .. n_past[s] + n_new[s] - 1 of every sequence with n_new[s] > 0 (those up to max_pages *
+ *   page_size that is; others are left alone).  A place without a page gets a free one; a place whose page has other holders gets a free one too,
+ *   with the entries before n_past[s] copied in all layers (every holder that writes in one call gets its own, the last one too).  Free
+ *   pages are taken in ascending order, sequences and places in ascending order; a sequence that needs more than are left, and every one behind
+ *   it that needs any, is left as it was.  short_by [n_seq]: 0, or for a sequence that was left how many pages it needs.
+ * hawk_paged_trim: the pages behind the first n_past[s] entries are given back (n_past[s] = 0: all of them; negative: the sequence is left alone).
+ * hawk_paged_compact: the pages in use (refs > 0), U of them, come to lie in pages 0 .. U - 1: those behind are moved, in all layers, in
+ *   ascending order into the free ones before, in ascending order.  table_out (row s table_out_stride places behind row s - 1) and refs_out
+ *   get the table and the counts as they are then, in place or elsewhere; places of pages that are not in use become -1.  n_used: U.
+ *   No entry that the old table leads to is overwritten.
+ * hawk_paged_copy: page src[i] of one pool goes to page dst[i] of another (or the same) of equal type, layers, heads, head_dim and page_size, all
+ *   layers, i < n, n <= 2^20; pairs with a page outside its pool are left out.  A page that is written twice, or written and read, holds either.
+ * workspace of take and compact (16-byte aligned): hawk_paged_pages_workspace_bytes; nothing in it has to be cleared or is kept.
+ * n_seq * max_pages <= 2^30, a page of one head at most 2^30 times 16 bytes, layers apart from one another. */
+size_t hawk_paged_pages_workspace_bytes(const hawk_paged_cache* cache);
+int hawk_paged_fork(const hawk_paged_cache* cache, int32_t* refs, int32_t* n_past, const int32_t* src, const int32_t* dst, int n, void* stream);
+int hawk_paged_take(const hawk_paged_cache* cache, int32_t* refs, const int32_t* n_past, const int32_t* n_new, int32_t* short_by,
+                    void* workspace, size_t workspace_bytes, void* stream);
+int hawk_paged_trim(const hawk_paged_cache* cache, int32_t* refs, const int32_t* n_past, void* stream);
+int hawk_paged_compact(const hawk_paged_cache* cache, const int32_t* refs, int32_t* table_out, int64_t table_out_stride, int32_t* refs_out,
+                       int32_t* n_used, void* workspace, size_t workspace_bytes, void* stream);
+int hawk_paged_copy(const hawk_paged_cache* from, const hawk_paged_cache* to, const int32_t* src, const int32_t* dst, int n, void* stream);
+
+/* Low-rank adapters of many requests beside a shared projection:
+ *   out[r] = base[r] + scale[i] * B_i (A_i x[r]),   i = adapter[s], s the sequence of row r,
+ * where base is the projection's result (NULL: zero; it may be out itself).  Rows of a sequence whose adapter is not one of
+ * 0 .. n_adapters - 1 (-1: none) get base alone; rows of no sequence are left as they are.
+ * hawk_adapter_plan lays out which rows have which adapter, once a step, for all projections of all layers: rows row_start[s] ..
+ * row_start[s + 1] - 1 of sequence s as in hawk_paged_rows, adapter [n_seq].  plan: hawk_adapter_plan_bytes(rows, n_adapters) bytes, 16-byte
+ * aligned, for calls with the same rows and n_adapters (rows <= 2^22, n_adapters <= 8192).
+ * hawk_adapter_apply: A_i is rank rows of d_in elements, element (j, k) at a + i * a_adapter_stride + j * a_row_stride + k; B_i d_out rows of rank
+ * elements, likewise.  scale fp32 [n_adapters] (NULL: 1).  rank, d_in, d_out multiples of 8, rank at most 128; strides multiples of 8
+ * elements, pointers 16-byte aligned.  x and the weights of one type, base and out of one (any) type; out overlaps nothing but base,
+ * and that only as a whole.  A x and B h are summed in fp32; A x enters the second product with 16 bits (bf16; 24 if out is fp32), 22 bits below
+ * a row's largest (fp16) or 24 (fp32); the sum is rounded once to out's type.  Weights are finite numbers; an infinity or NaN in a row of x
+ * stays in that row. */
+typedef struct {
+    const void *a, *b;
+    int64_t a_adapter_stride, a_row_stride, b_adapter_stride, b_row_stride;
+    const float* scale;
+    int32_t dtype, n_adapters, rank, d_in, d_out;
+} hawk_adapters;
+/* Rows of elements: row r starts r * row_stride elements behind data (16-byte aligned; row_stride a multiple of 8). */
+typedef struct {
+    void* data;
+    int64_t row_stride;
+    int32_t dtype;
+} hawk_matrix;
+size_t hawk_adapter_plan_bytes(int rows, int n_adapters);
+int hawk_adapter_plan(const int32_t* row_start, const int32_t* adapter, int n_seq, int rows, int n_adapters, void* plan, size_t plan_bytes,
+                      void* stream);
+int hawk_adapter_apply(const hawk_adapters* weights, const void* plan, size_t plan_bytes, int rows, const hawk_matrix* x, const hawk_matrix* base,
+                       const hawk_matrix* out, void* stream);
+
+/* One draw per row from logits that the caller has, each row with parameters of its own (arrays of rows values in device memory; NULL: the
+ * value in brackets): temperature [1], top_k [0], top_p [1], min_p [0].
+ *   z = l * (1 / temperature) in fp32, weights w = exp(z - the largest z); entries in the order of z, equal ones by index.  Of that order
+ *   is kept: the first top_k (all if below 1 or above n); of these the ones before which less than top_p of their mass lies (all if
+ *   top_p >= 1 or NaN; the first always); of these the ones with w >= min_p (all if min_p <= 0 or NaN; above 1 it is 1).
+ *   The token is the first in ascending index at which the sum of kept weights exceeds u times their whole, u in [0, 1).
+ * temperature 0 (or below, or NaN): the largest entry, lowest index first.  A NaN is never drawn, nor is minus infinity; entries of plus infinity
+ * are alike and everything else beside them is nothing.  A row with nothing to draw gives token -1.
+ * Weights are held as multiples of 2^-S of the largest, S = min(51, 62 - log2 n rounded up), and summed exactly.
+ * logits: n values of dtype (any of the three types), row r starting r * row_stride elements in, n 1..2^20, rows <= 2^22; skip (may be NULL) [rows]: a row
+ * with a negative entry is not read and gives token -1.  out_prob (may be NULL): the probability with which the token was drawn, kept weights
+ * alone; out_kept (may be NULL): how many entries were kept; both 0 where there is no token.
+ * workspace (16-byte aligned, may be NULL where the size function says 0): hawk_sample_filtered_workspace_bytes; nothing in it has to be cleared
+ * or is kept. */
+size_t hawk_sample_filtered_workspace_bytes(int rows, int n);
+int hawk_sample_filtered(const void* logits, int dtype, int64_t row_stride, const int32_t* skip, const float* u, const float* temperature,
+                         const int32_t* top_k, const float* top_p, const float* min_p, int rows, int n, int32_t* out_token, float* out_prob,
+                         int32_t* out_kept, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Verification of drafted chains (Preliminary, "Speculative Sampling"), the rule of hawk_verify for logits that
  * the caller has: sequence s has n_draft[s] drafts (NULL: k; clamped to k; negative: the sequence is
  * left out, count and tokens -1), draft[s * k + i] judged by row i of its k + 1 target rows.

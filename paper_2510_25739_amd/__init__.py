@@ -15,12 +15,14 @@ from .hawk import (  # noqa: F401
     multi_verify_workspace_bytes,
     plan_info,
     rotary_table,
+    sample_filtered,
     sample_rows,
     spatial_heads,
     spec_cache_bytes,
     spec_cache_slot,
     tree_layout,
     verify_chains,
+    AdapterPlan,
     PagedCache,
     SpecCache,
     workspace_bytes,

@@ -9,7 +9,9 @@
 #include <algorithm>
 #include <new>
 
+#include "adapters.h"
 #include "chain.h"
+#include "filtered.h"
 #include "paged.h"
 
 #include <vector>
@@ -603,6 +605,52 @@ int hawk_paged_attention(const hawk_paged_cache* cache, int layer, const hawk_pa
 int hawk_paged_keep(const hawk_paged_cache* cache, const int32_t* n_past, const int32_t* path, const int32_t* n_keep,
                     int depth, void* stream) {
     return hawk::launch_paged_keep(cache, n_past, path, n_keep, depth, static_cast<hipStream_t>(stream));
+}
+
+size_t hawk_paged_pages_workspace_bytes(const hawk_paged_cache* cache) { return hawk::paged_pages_workspace_bytes(cache); }
+
+int hawk_paged_fork(const hawk_paged_cache* cache, int32_t* refs, int32_t* n_past, const int32_t* src, const int32_t* dst, int n, void* stream) {
+    return hawk::launch_paged_fork(cache, refs, n_past, src, dst, n, static_cast<hipStream_t>(stream));
+}
+
+int hawk_paged_take(const hawk_paged_cache* cache, int32_t* refs, const int32_t* n_past, const int32_t* n_new, int32_t* short_by,
+                    void* workspace, size_t workspace_bytes, void* stream) {
+    return hawk::launch_paged_take(cache, refs, n_past, n_new, short_by, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+}
+
+int hawk_paged_trim(const hawk_paged_cache* cache, int32_t* refs, const int32_t* n_past, void* stream) {
+    return hawk::launch_paged_trim(cache, refs, n_past, static_cast<hipStream_t>(stream));
+}
+
+int hawk_paged_compact(const hawk_paged_cache* cache, const int32_t* refs, int32_t* table_out, int64_t table_out_stride, int32_t* refs_out,
+                       int32_t* n_used, void* workspace, size_t workspace_bytes, void* stream) {
+    return hawk::launch_paged_compact(cache, refs, table_out, table_out_stride, refs_out, n_used, workspace, workspace_bytes,
+                                      static_cast<hipStream_t>(stream));
+}
+
+int hawk_paged_copy(const hawk_paged_cache* from, const hawk_paged_cache* to, const int32_t* src, const int32_t* dst, int n, void* stream) {
+    return hawk::launch_paged_copy(from, to, src, dst, n, static_cast<hipStream_t>(stream));
+}
+
+size_t hawk_adapter_plan_bytes(int rows, int n_adapters) { return hawk::adapter_plan_bytes(rows, n_adapters); }
+
+int hawk_adapter_plan(const int32_t* row_start, const int32_t* adapter, int n_seq, int rows, int n_adapters, void* plan, size_t plan_bytes,
+                      void* stream) {
+    return hawk::launch_adapter_plan(row_start, adapter, n_seq, rows, n_adapters, plan, plan_bytes, static_cast<hipStream_t>(stream));
+}
+
+int hawk_adapter_apply(const hawk_adapters* weights, const void* plan, size_t plan_bytes, int rows, const hawk_matrix* x, const hawk_matrix* base,
+                       const hawk_matrix* out, void* stream) {
+    return hawk::launch_adapter_apply(weights, plan, plan_bytes, rows, x, base, out, static_cast<hipStream_t>(stream));
+}
+
+size_t hawk_sample_filtered_workspace_bytes(int rows, int n) { return hawk::sample_filtered_workspace_bytes(rows, n); }
+
+int hawk_sample_filtered(const void* logits, int dtype, int64_t row_stride, const int32_t* skip, const float* u, const float* temperature,
+                         const int32_t* top_k, const float* top_p, const float* min_p, int rows, int n, int32_t* out_token, float* out_prob,
+                         int32_t* out_kept, void* workspace, size_t workspace_bytes, void* stream) {
+    return hawk::launch_sample_filtered(logits, dtype, row_stride, skip, u, temperature, top_k, top_p, min_p, rows, n, out_token, out_prob, out_kept,
+                                        workspace, workspace_bytes, static_cast<hipStream_t>(stream));
 }
 
 int64_t hawk_paged_entry(const hawk_paged_cache* cache, const int32_t* table_row, int layer, int64_t e) {

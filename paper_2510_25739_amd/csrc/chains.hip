@@ -193,25 +193,7 @@ __global__ __launch_bounds__(NT) void chain_stats_kernel(ChainArgs a) {
 constexpr int kParts = 16, kPT = 256;   // parts of a slice at most, threads of a part's workgroup
 inline int parts_of(int n) { return n > kParts * 16 * kPT ? kParts : (n + 16 * kPT - 1) / (16 * kPT); }
 __device__ __forceinline__ int part_entries(const ChainArgs& a) { return ((a.n + a.n_parts - 1) / a.n_parts + 3) / 4 * 4; }
-// exp(x), x <= 0, by Tang's table-driven method (ACM TOMS 15, 1989): x = (64 m + i) ln2 / 64 + r, exp(x) = 2^m 2^(i / 64) exp(r), |r| < 0.0055, so
-// that the series to r^5 is exact to 4e-17.  The whole number is rounded to by adding 1.5 2^52, whose low word then holds it, and 2^m
-// is added to the exponent.  Below -700 (minus infinity among it, and for NaN) the result is 0.  Fewer instructions than the library's, all of
-// the quick kind, which is what sums over whole slices are bound by; 48 chains over 65536 entries: chain_part_kernel 31 us with
-// the library's, 24.5 us.
-constexpr int kSteps = 64;
-__device__ __forceinline__ void fill_steps(double* steps) {   // ends without a barrier
-    if (threadIdx.x < kSteps) steps[threadIdx.x] = exp2((double)threadIdx.x / kSteps);
-}
-__device__ __forceinline__ double exp_below(double x, const double* steps) {
-    const double shifted = fma(x, 0x1.71547652b82fep+6, 0x1.8p52), n = shifted - 0x1.8p52;
-    const double r = fma(n, -0x1.abc9e3b39803fp-62, fma(n, -0x1.62e42fefa39efp-7, x));
-    const double p = r * fma(r, fma(r, fma(r, fma(r, 1.0 / 120, 1.0 / 24), 1.0 / 6), 0.5), 1.0);
-    const int i = __double2loint(shifted);
-    const double t = steps[i & (kSteps - 1)], v = fma(t, p, t);
-    const bool some = x >= -700.0;
-    return __hiloint2double(some ? __double2hiint(v) + (int)((unsigned)(i & -kSteps) << 14) : 0, some ? __double2loint(v) : 0);
-}
-// weight_of with it, of a scaled logit.
+// weight_of by exp_below, of a scaled logit.
 __device__ __forceinline__ double entry_weight(const WarpStat& st, float z, int j, bool whole, const double* steps) {
     return whole || kept(st, z, j) ? exp_below((double)z - (double)st.zmax, steps) : 0.0;
 }

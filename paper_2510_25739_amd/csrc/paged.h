@@ -69,6 +69,14 @@ int launch_paged_append(const hawk_paged_cache* cache, int layer, const hawk_pag
                         hipStream_t stream);
 int launch_paged_keep(const hawk_paged_cache* cache, const int32_t* n_past, const int32_t* path, const int32_t* n_keep,
                       int depth, hipStream_t stream);
+size_t paged_pages_workspace_bytes(const hawk_paged_cache* cache);
+int launch_paged_fork(const hawk_paged_cache* cache, int32_t* refs, int32_t* n_past, const int32_t* src, const int32_t* dst, int n, hipStream_t stream);
+int launch_paged_take(const hawk_paged_cache* cache, int32_t* refs, const int32_t* n_past, const int32_t* n_new, int32_t* short_by, void* workspace,
+                      size_t workspace_bytes, hipStream_t stream);
+int launch_paged_trim(const hawk_paged_cache* cache, int32_t* refs, const int32_t* n_past, hipStream_t stream);
+int launch_paged_compact(const hawk_paged_cache* cache, const int32_t* refs, int32_t* table_out, int64_t table_out_stride, int32_t* refs_out,
+                         int32_t* n_used, void* workspace, size_t workspace_bytes, hipStream_t stream);
+int launch_paged_copy(const hawk_paged_cache* from, const hawk_paged_cache* to, const int32_t* src, const int32_t* dst, int n, hipStream_t stream);
 size_t paged_attention_workspace_bytes(const hawk_paged_cache* cache, int rows, int n_q_heads, int max_len);
 int launch_paged_attention(const hawk_paged_cache* cache, int layer, const hawk_paged_rows* rows, const hawk_heads* q,
                            const uint64_t* tree, float scale, int max_len, const hawk_heads* out, void* workspace,

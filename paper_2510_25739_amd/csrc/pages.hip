@@ -1,0 +1,404 @@
+// Pages of the cache of many sequences: which are taken, shared, given back and moved.  Everything is known from two arrays in device
+// memory, the table (which page a place of a sequence has) and the counts (how many places have a page; 0: free), so that a step
+// can be captured and replayed.  Lookups are one workgroup's work - they are a few thousand numbers, and what they cost is
+// latency -, the entries are moved by a second launch that fills the chip.
+#include "paged.h"
+
+#include <algorithm>
+
+namespace hawk {
+
+namespace {
+
+constexpr int kWide = 1024;         // threads of a workgroup that looks up
+constexpr int kEach = 16;           // neighbouring counts a thread looks at in one round
+
+// Exclusive prefix sum over the workgroup and the whole sum, the same in every thread.  `sums`: 17 words.  Ends with a barrier.
+__device__ __forceinline__ int block_before(int v, int* sums, int& all) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int x = v;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+    }
+    if (lane == 63) sums[wave] = x;
+    __syncthreads();
+    int before = 0;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < kWide / 64; ++w) {
+        const int s = sums[w];
+        before += w < wave ? s : 0;
+        all += s;
+    }
+    __syncthreads();
+    return before + x - v;
+}
+
+__device__ __forceinline__ int pages_for(int64_t entries, const PagedView& c) {   // places that so many entries of a sequence fill
+    if (entries <= 0) return 0;
+    return entries >= c.capacity ? c.max_pages : page_of(c, (int)entries - 1) + 1;
+}
+__device__ __forceinline__ bool in_pool(const PagedView& c, int page) { return page >= 0 && page < c.n_pages; }
+
+// A copy of the first n entries of a page, all layers and heads.
+struct Move { int from, to, n; };
+struct MoveList { int* count; Move* move; };
+
+// Pair i: the sequence dst[i] has from now on the pages that hold src[i]'s committed entries, and what it had is given back.  A workgroup
+// a pair.  Counts are sums of whole numbers: their order does not matter.
+__global__ __launch_bounds__(256) void paged_fork_kernel(PagedView c, int32_t* table, int32_t* refs, int32_t* n_past, const int32_t* src,
+                                                         const int32_t* dst, int n) {
+    const int i = blockIdx.x, from = src[i], to = dst[i];
+    if (from < 0 || from >= c.n_seq || to < 0 || to >= c.n_seq || from == to) return;
+    int lost = 0;
+    for (int j = threadIdx.x; j < n; j += 256) {
+        const int other = dst[j], base = src[j];
+        const bool real = other >= 0 && other < c.n_seq && base >= 0 && base < c.n_seq && base != other;
+        lost |= (other == to && j < i && real) || (other == from && real);   // a second pair for one sequence; a source that changes
+    }
+    if (__syncthreads_or(lost)) return;
+    const int past = n_past[from], there = pages_for(past, c);
+    const int32_t* a = table + from * c.table_stride;
+    int32_t* b = table + to * c.table_stride;
+    for (int p = threadIdx.x; p < c.max_pages; p += 256) {
+        const int old = b[p], page = p < there ? a[p] : -1;
+        if (in_pool(c, old)) atomicAdd(&refs[old], -1);
+        if (in_pool(c, page)) atomicAdd(&refs[page], 1);
+        b[p] = page;
+    }
+    if (threadIdx.x == 0) n_past[to] = past;
+}
+
+__global__ __launch_bounds__(256) void paged_trim_kernel(PagedView c, int32_t* table, int32_t* refs, const int32_t* n_past, Divisor blocks) {
+    const int s = (int)blockIdx.x / blocks, p = ((int)blockIdx.x - s * blocks.d) * 256 + (int)threadIdx.x, past = n_past[s];
+    if (p >= c.max_pages || past < 0 || p < pages_for(past, c)) return;
+    int32_t* at = table + s * c.table_stride + p;
+    const int page = *at;
+    if (in_pool(c, page)) atomicAdd(&refs[page], -1);
+    *at = -1;
+}
+
+struct TakeArgs {
+    PagedView c;
+    int32_t *table, *refs;
+    const int32_t *n_past, *n_new;
+    int32_t* short_by;              // [n_seq]
+    int *free, *old;                // [n_pages]: free pages, lowest first, as many as are wanted; the page that a taken one stands in for
+    MoveList moves;
+    int lanes;                      // neighbouring lanes of a sequence (2^lanes)
+};
+
+// The pages that are written next.  First what every sequence lacks: places among those of entries n_past .. n_past + n_new - 1 that have no
+// page or one that other places have too.  Then the free pages in ascending order, as many as are lacking.  Then they are handed
+// out, sequences and places in ascending order, a sequence that would need more than there are (and all behind it) left as it
+// was.  The counts that decide are those before the call: they are changed at the end.
+__global__ __launch_bounds__(kWide) void paged_take_kernel(TakeArgs a) {
+    __shared__ int sums[kWide / 64 + 1];
+    const PagedView& c = a.c;
+    const int tid = threadIdx.x, per = kWide >> a.lanes, width = 1 << a.lanes, l = tid & (width - 1), group = (tid & 63) & ~(width - 1);
+    const unsigned long long mine = width == 64 ? ~0ull : ((1ull << width) - 1ull) << group, before = mine & ((1ull << (tid & 63)) - 1ull);
+    struct Span { int first, stop, inside; };        // places that are written; entries of the first one that stay
+    auto span = [&](int s) {
+        Span t = {0, 0, 0};
+        if (s < c.n_seq) {
+            const int past = a.n_past[s], add = a.n_new[s];
+            if (past >= 0 && add > 0 && past < c.capacity) {
+                t.first = page_of(c, past);
+                t.stop = pages_for((int64_t)past + add, c);
+                t.inside = past - t.first * c.page_size;
+            }
+        }
+        return t;
+    };
+    auto lacks = [&](int s, int p, int& page) {
+        page = a.table[s * c.table_stride + p];
+        if (!in_pool(c, page)) { page = -1; return true; }
+        return a.refs[page] > 1;
+    };
+    int wanted = 0;                                  // of this thread's sequences
+    for (int s0 = 0; s0 < c.n_seq; s0 += per) {
+        const int s = s0 + (tid >> a.lanes);
+        const Span t = span(s);
+        int page;
+        for (int p = t.first + l; p < t.stop; p += width) wanted += lacks(s, p, page) ? 1 : 0;
+    }
+    int total, n_free = 0;
+    block_before(wanted, sums, total);
+    for (int p0 = 0; p0 < c.n_pages && n_free < total; p0 += kWide * kEach) {
+        const int at = p0 + tid * kEach;
+        unsigned bits = 0u;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) bits |= at + j < c.n_pages && a.refs[min(at + j, c.n_pages - 1)] == 0 ? 1u << j : 0u;
+        int all, k = n_free + block_before(__popc(bits), sums, all);
+        for (; bits && k < total; bits &= bits - 1u) a.free[k++] = at + __ffs(bits) - 1;
+        n_free += all;
+    }
+    __syncthreads();
+    int asked = 0, moves = 0, given = 0;             // of the sequences before this round's; given: of those that are served
+    for (int s0 = 0; s0 < c.n_seq; s0 += per) {
+        const int s = s0 + (tid >> a.lanes);
+        const Span t = span(s);
+        int page, need = 0;
+        for (int p = t.first + l; p < t.stop; p += width) need += lacks(s, p, page) ? 1 : 0;
+        for (int w = 1; w < width; w <<= 1) need += __shfl_xor(need, w);
+        int all, k = asked + block_before(l == 0 ? need : 0, sums, all);
+        k = __shfl(k, group);                        // (the group's first lane counts for it)
+        asked += all;
+        const bool served = k + need <= n_free;
+        const bool bring = served && t.inside > 0 && t.stop > t.first && lacks(s, t.first, page) && page >= 0;
+        int brought, m = moves + block_before(bring && l == 0 ? 1 : 0, sums, brought);
+        moves += brought;
+        int gave;
+        block_before(served && l == 0 ? need : 0, sums, gave);
+        given += gave;
+        if (s < c.n_seq && l == 0) a.short_by[s] = served ? 0 : need;
+        if (bring && l == 0) {
+            // (the first place is the first that lacks a page: the first page of the sequence's)
+            const Move mv = {page, a.free[k], t.inside};
+            a.moves.move[m] = mv;
+        }
+        if (served) {
+            for (int p0 = t.first; p0 < t.stop; p0 += width) {
+                const int p = p0 + l;
+                const bool take = p < t.stop && lacks(s, p, page);
+                const unsigned long long who = __ballot(take);
+                if (take) {
+                    const int at = k + __popcll(who & before), to = a.free[at];
+                    a.old[at] = page;
+                    a.table[s * c.table_stride + p] = to;
+                }
+                k += __popcll(who & mine);
+            }
+        }
+    }
+    if (tid == 0) *a.moves.count = moves;
+    __syncthreads();
+    for (int i = tid; i < given; i += kWide) {
+        a.refs[a.free[i]] = 1;
+        if (a.old[i] >= 0) atomicAdd(&a.refs[a.old[i]], -1);
+    }
+}
+
+// Of the pages in use those that lie behind as many places as there are pages in use, and the free ones before, are paired in ascending order.
+__global__ __launch_bounds__(kWide) void paged_holes_kernel(PagedView c, const int32_t* refs, int32_t* refs_out, int* to, int* src, int* dst, MoveList moves,
+                                                            int32_t* n_used) {
+    __shared__ int sums[kWide / 64 + 1];
+    const int tid = threadIdx.x;
+    auto used = [&](int p) { return p < c.n_pages && refs[min(p, c.n_pages - 1)] > 0; };
+    int n = 0;
+    for (int p = tid; p < c.n_pages; p += kWide) n += used(p) ? 1 : 0;
+    int total, holes = 0, behind = 0;
+    block_before(n, sums, total);
+    for (int p0 = 0; p0 < c.n_pages; p0 += kWide * kEach) {
+        const int at = p0 + tid * kEach;
+        unsigned bits = 0u;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) bits |= used(at + j) ? 1u << j : 0u;
+        const int real = min(max(c.n_pages - at, 0), kEach), front = min(max(total - at, 0), real);   // of the thread's pages; before the border
+        const unsigned low = (1u << front) - 1u, whole = (1u << real) - 1u;
+        unsigned h = ~bits & low, b = bits & whole & ~low;
+        int all;
+        int k = holes + block_before(__popc(h), sums, all);
+        holes += all;
+        for (; h; h &= h - 1u) dst[k++] = at + __ffs(h) - 1;
+        k = behind + block_before(__popc(b), sums, all);
+        behind += all;
+        for (; b; b &= b - 1u) src[k++] = at + __ffs(b) - 1;
+        for (int j = 0; j < real; ++j) to[at + j] = (bits >> j) & 1u ? at + j : -1;
+    }
+    __syncthreads();
+    if (refs_out != refs)
+        for (int p = tid; p < c.n_pages; p += kWide) refs_out[p] = max(refs[p], 0);
+    __syncthreads();
+    for (int i = tid; i < behind; i += kWide) {
+        const Move mv = {src[i], dst[i], c.page_size};
+        moves.move[i] = mv;
+        to[mv.from] = mv.to;
+        const int r = refs[mv.from];
+        refs_out[mv.to] = r;
+        refs_out[mv.from] = 0;
+    }
+    if (tid == 0) {
+        *moves.count = behind;
+        *n_used = total;
+    }
+}
+
+struct CopyArgs {
+    PagedView from, to;
+    int64_t from_layer, to_layer;   // bytes
+    const int32_t *src, *dst;       // pages of a list of the caller's (moves.count null)
+    MoveList moves;
+    int n, esz;
+    Divisor units, heads, pieces;   // of a page: layers times two pools times heads; heads; 16-byte pieces of an entry
+    // tables on the way
+    const int* map;                 // [n_pages]; null: none
+    int32_t* table_out;
+    int64_t table_out_stride, places;
+};
+
+// A wave moves one head's keys or values of one page and layer: up to 8 KB requested at once, then stored.  Waves stay for as many units as fill
+// the chip a few times.
+constexpr int kCopyWaves = 8192;
+__global__ __launch_bounds__(256) void paged_copy_kernel(CopyArgs a) {
+    const int lane = threadIdx.x & 63;
+    if (a.map) {
+        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.places; i += (int64_t)gridDim.x * 256) {
+            const int s = (int)(i / a.from.max_pages), p = (int)(i - (int64_t)s * a.from.max_pages), page = a.from.table[s * a.from.table_stride + p];
+            a.table_out[s * a.table_out_stride + p] = in_pool(a.from, page) ? a.map[page] : -1;
+        }
+    }
+    const int count = a.moves.count ? min(*a.moves.count, a.n) : a.n;
+    const int64_t units = (int64_t)count * a.units.d;
+    for (int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); u < units; u += (int64_t)gridDim.x * 4) {
+        const int m = __builtin_amdgcn_readfirstlane((int)(u / a.units.d)), rest = __builtin_amdgcn_readfirstlane((int)(u - (int64_t)m * a.units.d));
+        const int lk = rest / a.heads, head = rest - lk * a.heads.d;
+        Move mv = {-1, -1, a.from.page_size};
+        if (a.moves.count) mv = a.moves.move[m];
+        else { mv.from = a.src[m]; mv.to = a.dst[m]; }
+        if (!in_pool(a.from, mv.from) || !in_pool(a.to, mv.to)) continue;
+        const char* x = ((lk & 1) ? a.from.v : a.from.k) + (lk >> 1) * a.from_layer + (mv.from * a.from.page_stride + head * a.from.head_stride) * a.esz;
+        char* y = ((lk & 1) ? a.to.v : a.to.k) + (lk >> 1) * a.to_layer + (mv.to * a.to.page_stride + head * a.to.head_stride) * a.esz;
+        const int total = mv.n * a.pieces.d;
+        const int64_t xs = a.from.entry_stride * a.esz, ys = a.to.entry_stride * a.esz;
+        for (int i0 = lane; i0 < total; i0 += 512) {
+            v4u w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int i = i0 + 64 * j, e = i / a.pieces, p = i - e * a.pieces.d;
+                if (i < total) w[j] = *reinterpret_cast<const v4u*>(x + e * xs + p * 16);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int i = i0 + 64 * j, e = i / a.pieces, p = i - e * a.pieces.d;
+                if (i < total) *reinterpret_cast<v4u*>(y + e * ys + p * 16) = w[j];
+            }
+        }
+    }
+}
+
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+int status() { return hipGetLastError() == hipSuccess ? HAWK_OK : HAWK_EDEVICE; }
+size_t round16(size_t n) { return (n + 15) / 16 * 16; }
+
+// A cache whose pages can be copied in all layers.
+bool whole_view(const hawk_paged_cache* c, PagedView* v) {
+    return paged_view(c, 0, v) && !(c->n_layers > 1 && c->layer_stride < c->head_dim) && (int64_t)c->n_layers * 2 * c->n_heads <= (1 << 25) &&
+           (int64_t)c->page_size * (c->head_dim * (int)type_bytes(c->dtype) / 16) <= (1 << 30) && (int64_t)c->n_seq * c->max_pages <= (1 << 30);
+}
+void copy_sides(const hawk_paged_cache* from, const hawk_paged_cache* to, CopyArgs* a) {
+    a->esz = (int)type_bytes(from->dtype);
+    a->from_layer = from->layer_stride * a->esz;
+    a->to_layer = to->layer_stride * a->esz;
+    a->units = divisor(from->n_layers * 2 * from->n_heads);
+    a->heads = divisor(from->n_heads);
+    a->pieces = divisor(from->head_dim * a->esz / 16);
+}
+void launch_copy(const CopyArgs& a, int64_t most, hipStream_t stream) {   // most: units there can be
+    const int64_t waves = std::min<int64_t>(kCopyWaves, std::max<int64_t>(most, 1));
+    paged_copy_kernel<<<(unsigned)((waves + 3) / 4), 256, 0, stream>>>(a);
+}
+
+// The workspace: a count, the moves, two lists of pages and where each page goes.
+struct Room { int* count; Move* move; int *a, *b, *to; size_t bytes; };
+Room room_of(const hawk_paged_cache* c, void* at) {
+    Room r;
+    char* p = static_cast<char*>(at);
+    const size_t moves = round16(sizeof(Move) * (size_t)std::max(c->n_seq, c->n_pages / 2 + 1)), list = round16(sizeof(int) * (size_t)c->n_pages);
+    r.count = reinterpret_cast<int*>(p);
+    r.move = reinterpret_cast<Move*>(p + 16);
+    r.a = reinterpret_cast<int*>(p + 16 + moves);
+    r.b = reinterpret_cast<int*>(p + 16 + moves + list);
+    r.to = reinterpret_cast<int*>(p + 16 + moves + 2 * list);
+    r.bytes = 16 + moves + 3 * list;
+    return r;
+}
+
+}  // namespace
+
+size_t paged_pages_workspace_bytes(const hawk_paged_cache* cache) {
+    PagedView v;
+    return whole_view(cache, &v) ? room_of(cache, nullptr).bytes : 0;
+}
+
+int launch_paged_fork(const hawk_paged_cache* cache, int32_t* refs, int32_t* n_past, const int32_t* src, const int32_t* dst, int n, hipStream_t stream) {
+    PagedView c;
+    if (!paged_view(cache, 0, &c) || n < 0 || n > c.n_seq) return HAWK_EINVAL;
+    if (n == 0) return HAWK_OK;
+    if (!refs || !n_past || !src || !dst) return HAWK_EINVAL;
+    paged_fork_kernel<<<(unsigned)n, 256, 0, stream>>>(c, const_cast<int32_t*>(c.table), refs, n_past, src, dst, n);
+    return status();
+}
+
+int launch_paged_trim(const hawk_paged_cache* cache, int32_t* refs, const int32_t* n_past, hipStream_t stream) {
+    PagedView c;
+    if (!paged_view(cache, 0, &c)) return HAWK_EINVAL;
+    if (c.n_seq == 0) return HAWK_OK;
+    if (!refs || !n_past) return HAWK_EINVAL;
+    const int64_t blocks = (c.max_pages + 255) / 256;
+    if (blocks * c.n_seq > (1 << 23)) return HAWK_EINVAL;
+    paged_trim_kernel<<<(unsigned)(blocks * c.n_seq), 256, 0, stream>>>(c, const_cast<int32_t*>(c.table), refs, n_past, divisor((int)blocks));
+    return status();
+}
+
+int launch_paged_take(const hawk_paged_cache* cache, int32_t* refs, const int32_t* n_past, const int32_t* n_new, int32_t* short_by, void* workspace,
+                      size_t workspace_bytes, hipStream_t stream) {
+    TakeArgs a = {};
+    if (!whole_view(cache, &a.c)) return HAWK_EINVAL;
+    if (a.c.n_seq == 0) return HAWK_OK;
+    if (!refs || !n_past || !n_new || !short_by || !workspace || !aligned16(workspace)) return HAWK_EINVAL;
+    const Room r = room_of(cache, workspace);
+    if (workspace_bytes < r.bytes) return HAWK_ENOMEM;
+    a.table = const_cast<int32_t*>(a.c.table);
+    a.refs = refs; a.n_past = n_past; a.n_new = n_new; a.short_by = short_by;
+    a.free = r.a; a.old = r.b;
+    a.moves = {r.count, r.move};
+    while (a.lanes < 6 && (int64_t)a.c.n_seq << (a.lanes + 1) <= kWide) ++a.lanes;
+    paged_take_kernel<<<1, kWide, 0, stream>>>(a);
+    CopyArgs m = {};
+    m.from = m.to = a.c;
+    m.moves = a.moves;
+    m.n = a.c.n_seq;
+    copy_sides(cache, cache, &m);
+    launch_copy(m, (int64_t)m.n * m.units.d, stream);
+    return status();
+}
+
+int launch_paged_compact(const hawk_paged_cache* cache, const int32_t* refs, int32_t* table_out, int64_t table_out_stride, int32_t* refs_out,
+                         int32_t* n_used, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    CopyArgs m = {};
+    if (!whole_view(cache, &m.from) || !refs || !refs_out || !n_used || !workspace || !aligned16(workspace)) return HAWK_EINVAL;
+    if (m.from.n_seq > 0 && (!table_out || table_out_stride < m.from.max_pages)) return HAWK_EINVAL;
+    const Room r = room_of(cache, workspace);
+    if (workspace_bytes < r.bytes) return HAWK_ENOMEM;
+    m.to = m.from;
+    m.moves = {r.count, r.move};
+    m.n = m.from.n_pages / 2;
+    m.map = r.to;
+    m.table_out = table_out;
+    m.table_out_stride = table_out_stride;
+    m.places = (int64_t)m.from.n_seq * m.from.max_pages;
+    copy_sides(cache, cache, &m);
+    paged_holes_kernel<<<1, kWide, 0, stream>>>(m.from, refs, refs_out, r.to, r.a, r.b, m.moves, n_used);
+    launch_copy(m, std::max<int64_t>((int64_t)m.n * m.units.d, (m.places + 63) / 64), stream);
+    return status();
+}
+
+int launch_paged_copy(const hawk_paged_cache* from, const hawk_paged_cache* to, const int32_t* src, const int32_t* dst, int n, hipStream_t stream) {
+    CopyArgs m = {};
+    if (!whole_view(from, &m.from) || !whole_view(to, &m.to) || n < 0 || n > (1 << 20)) return HAWK_EINVAL;
+    if (from->dtype != to->dtype || from->n_layers != to->n_layers || from->page_size != to->page_size || from->n_heads != to->n_heads ||
+        from->head_dim != to->head_dim)
+        return HAWK_EINVAL;
+    if (n == 0) return HAWK_OK;
+    if (!src || !dst) return HAWK_EINVAL;
+    m.src = src; m.dst = dst; m.n = n;
+    copy_sides(from, to, &m);
+    launch_copy(m, (int64_t)n * m.units.d, stream);
+    return status();
+}
+
+}  // namespace hawk

