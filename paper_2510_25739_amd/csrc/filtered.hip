@@ -1,23 +1,27 @@
 // One draw a row from logits cut by top-k, top-p and min-p, each row with parameters of its own.
 //
-// z = l / T in 32 bits, w = exp(z - zmax).  Entries are ordered by z, equal ones by index; what is kept is a beginning of that order: the
-// top_k first, of these the ones before which less than top_p of their mass lies, of these the ones with w >= min_p.  The token is the first
-// in ascending index whose sum of kept weights exceeds u times the whole.
+// z = l / T in 32 bits, w = exp(z - reference).  Entries are ordered by z, equal ones by index; what is kept is a beginning of that order: the
+// top_k first, of these the ones before which less than top_p of their mass lies, of these the ones with w >= min_p times the largest.  The token
+// is the first in ascending index whose sum of kept weights exceeds u times the whole.
 //
-// Weights are whole multiples of 2^-S of the largest (S as large as n of them still sum up in 64 bits: 48 for 16384 entries),
-// rounded to nearest, so that a sum has one value whatever the order it is made in, and masses can be counted in bins by atomics.  What
-// that rounding moves is n 2^-(S + 1) of the largest weight at most, 2^-35 for 16384 entries; sums of random errors are a hundredth of it.
+// Weights are whole multiples of 2^-S of the reference's (S as large as n of them still sum up in 64 bits: 48 for 16384 entries), rounded to
+// nearest, so that a sum has one value whatever the order it is made in, and masses can be counted in bins by atomics.  What that
+// rounding moves is n 2^-(S + 1) at most, 2^-35 for 16384 entries; the sum of random errors is a hundredth of it.
 //
-// A workgroup of 1024 threads has a row, in registers up to 65536 entries, read again for every look at a longer one.  The border of a cut is
-// found by linear bins of z below the maximum; the entries of the border's bin are ranked against each other.  Bins of too many entries (ties,
-// far tails) are searched by the bits of z instead.
+// The border of a cut - its last entry - is found by bins: linear ones of z below the maximum first, then, while more than a few entries share the
+// border's bin, bins of the keys' bits in that range and, among equal ones, of the index.  The few are ranked against each other.
+//
+// Up to 16384 entries one workgroup of 1024 threads has a row in its registers (sample_filtered_kernel).  Longer rows are cut into parts, a
+// workgroup each, in three launches: the parts' bins (filter_bins_kernel); sums of what is kept for certain, and the entries of the bins
+// that a border may be in (filter_parts_kernel); the borders and the draw, a workgroup a row (filter_draw_kernel).  A row whose border bins hold
+// too many entries for that, or whose logits are beyond the bins' grid, is read again and again by that last workgroup alone.
 #include "filtered.h"
 #include "paged.h"
 #include "sample_rows.h"
 
 #include <algorithm>
 
-// z is a rounded product wherever it is compared, binned or subtracted from the maximum.
+// z is a rounded product wherever it is compared, binned or subtracted from the reference.
 #pragma clang fp contract(off)
 
 namespace hawk {
@@ -26,9 +30,11 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int kCutBins = 2048;
-constexpr float kCutReach = 32.f;       // bins reach so far below the maximum; what lies behind shares the last one
-constexpr int kList = 2048;          // entries of a border's bin that are ranked
+constexpr int kBinCount = 2048;
+constexpr float kPerUnit = 64.f;     // bins of a unit of z
+constexpr int kFew = 256;            // entries that are ranked against each other
+constexpr int kChunk = 256;          // entries that a wave has of four a lane: sums of kept weights are held for each
+constexpr int kChunks = 4096;        // of 2^20 entries
 
 struct FilterArgs {
     const char* logits;
@@ -38,54 +44,87 @@ struct FilterArgs {
     int dtype, n, unit;              // unit: S
     int32_t *out_token, *out_kept;
     float* out_prob;
+    // rows in parts
+    int parts;
+    char* room;
 };
 
-struct FilterShared {
-    u64 mass[kCutBins], list_mass[kList];
-    unsigned count[kCutBins], list_key[kList], ranked_key[kList];
-    int list_at[kList], ranked_at[kList];
+struct Border { unsigned key; int at; };     // entries are inside if their key is larger, or equal and their index not above `at`
+__device__ __forceinline__ bool inside(const Border& b, float z, int j) {
+    const unsigned k = fkey(z);
+    return k > b.key || (k == b.key && j <= b.at);
+}
+// An entry is before a cut if fewer than K entries and a mass below M lie before it, in order.
+struct Cut { u64 M; unsigned K; };
+// Where the border lies: entries and mass before, m entries with keys lo..hi, of equal keys with indices first..last.
+struct Range { u64 before; unsigned ahead, m, lo, hi; int first, last; };
+struct Found { Border border; u64 mass; };   // mass: of all entries up to the border
+
+struct Picked { int bin; unsigned m, ahead; u64 before; };   // a bin: its entries; entries and mass before it
+struct CutShared {
+    u64 mass[kBinCount], fine_mass[kBinCount];
+    unsigned count[kBinCount], fine[kBinCount];      // fine: zero between uses
+    u64 w[kFew], winner, within, base;
+    unsigned key[kFew];
+    int at[kFew], n, chunk;
+    Picked picked;
     double steps[kSteps];
     u64 sum[NW];
     int isum[NW];
     float fmax[NW];
-    u64 b_mass;                      // broadcasts
-    unsigned b_key;
-    int b_bin, b_count, b_at, n;
 };
 
-__device__ __forceinline__ u64 block_sum(u64 v, u64 (&slot)[NW]) {   // ends with a barrier
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
-    if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
-    __syncthreads();
-    u64 s = 0;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) s += slot[w];
-    __syncthreads();
-    return s;
+__device__ __forceinline__ u64 lane_u64(u64 v, int l) {
+    return ((u64)(unsigned)__builtin_amdgcn_readlane((int)(v >> 32), l) << 32) | (unsigned)__builtin_amdgcn_readlane((int)(unsigned)v, l);
 }
-template <class V> __device__ __forceinline__ V block_before(V v, V (&slot)[NW], V& all) {   // exclusive prefix; ends with a barrier
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    V x = v;
-    for (int d = 1; d < 64; d <<= 1) {
-        const V y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
-    if (lane == 63) slot[wave] = x;
-    __syncthreads();
-    V before = 0;
-    all = 0;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-        const V s = slot[w];
-        before += w < wave ? s : 0;
-        all += s;
-    }
-    __syncthreads();
-    return before + x - v;
+__device__ __forceinline__ u64 addu(u64 a, u64 b) { return a + b; }
+__device__ __forceinline__ int addi(int a, int b) { return a + b; }
+__device__ __forceinline__ u64 wave_sum_u64(u64 v) {
+    ROW_ALLREDUCE(v, addu, dpp_u64)
+    return (lane_u64(v, 0) + lane_u64(v, 16)) + (lane_u64(v, 32) + lane_u64(v, 48));
+}
+__device__ __forceinline__ int wave_sum_i(int v) {
+    ROW_ALLREDUCE(v, addi, dpp_i)
+    return (__builtin_amdgcn_readlane(v, 0) + __builtin_amdgcn_readlane(v, 16)) + (__builtin_amdgcn_readlane(v, 32) + __builtin_amdgcn_readlane(v, 48));
+}
+__device__ __forceinline__ u64 wave_incl_scan_u64(u64 v) {
+    v += dpp_u64<0x111>(v);
+    v += dpp_u64<0x112>(v);
+    v += dpp_u64<0x114>(v);
+    v += dpp_u64<0x118>(v);
+    const u64 r0 = lane_u64(v, 15), r1 = lane_u64(v, 31), r2 = lane_u64(v, 47);
+    const int row = (threadIdx.x & 63) >> 4;
+    return v + (row == 0 ? 0ull : row == 1 ? r0 : row == 2 ? r0 + r1 : r0 + r1 + r2);
 }
 
-// A row: groups of four neighbouring entries, group q of a thread starts at q * 4096 + 4 * thread.  Values are z, minus infinity where there is
-// nothing to draw (past the end, NaN).
+// A weight as a whole number of 2^-S: a sum with 2^(52 - S) has it in its last 52 bits.
+struct Weigh {
+    double ref, magic;
+    const double* steps;
+    __device__ __forceinline__ double real(float z) const { return exp_below((double)z - ref, steps); }
+    __device__ __forceinline__ u64 operator()(float z) const { return (u64)__double_as_longlong(real(z) + magic) & 0xFFFFFFFFFFFFFull; }
+};
+__device__ __forceinline__ double magic_of(int unit) { return __hiloint2double((1075 - unit) << 20, 0); }
+
+// ceil(p * mass), 0 < p < 1, exactly: p is a whole number of 24 bits times a power of two.
+__device__ __forceinline__ u64 share_of(float p, u64 mass) {
+    const unsigned b = __float_as_uint(p), e = b >> 23;
+    const u64 m = e ? (b & 0x7FFFFFu) | 0x800000u : b & 0x7FFFFFu;
+    const int s = 150 - (int)max(e, 1u);             // p = m / 2^s, s >= 24
+    const u64 lo = m * mass, hi = __umul64hi(m, mass);
+    if (s >= 128) return (lo | hi) ? 1ull : 0ull;
+    u64 q, rest;
+    if (s >= 64) {
+        q = s == 64 ? hi : hi >> (s - 64);
+        rest = lo | (s == 64 ? 0ull : hi << (128 - s));
+    } else {
+        q = (lo >> s) | (hi << (64 - s));
+        rest = lo << (64 - s);
+    }
+    return q + (rest ? 1ull : 0ull);
+}
+
+// A row's values: z, minus infinity where there is nothing to draw (past the end, NaN).
 struct Source {
     const char* l;
     int dtype, n;
@@ -113,336 +152,872 @@ struct Source {
         }
     }
 };
-template <int E> struct Row {
-    float z[E > 0 ? E : 1];
-    Source s;
-    __device__ __forceinline__ void load() {
-        if (E > 0) {
-#pragma unroll
-            for (int q = 0; q < E / 4; ++q) {
-                float v[4];
-                s.four(q * 4 * NT + 4 * (int)threadIdx.x, v);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) z[4 * q + i] = v[i];
-            }
-        }
-    }
-    __device__ __forceinline__ int groups() const { return E > 0 ? E / 4 : (s.n + 4 * NT - 1) / (4 * NT); }
-    template <class F> __device__ __forceinline__ void each_group(F f) const {   // f(group, first index, four values)
-        if (E > 0) {
-#pragma unroll
-            for (int q = 0; q < E / 4; ++q) {
-                const float v[4] = {z[4 * q], z[4 * q + 1], z[4 * q + 2], z[4 * q + 3]};
-                f(q, q * 4 * NT + 4 * (int)threadIdx.x, v);
-            }
-        } else {
-            for (int q = 0; q < groups(); ++q) {
-                float v[4];
-                s.four(q * 4 * NT + 4 * (int)threadIdx.x, v);
-                f(q, q * 4 * NT + 4 * (int)threadIdx.x, v);
-            }
-        }
-    }
-    template <class F> __device__ __forceinline__ void each(F f) const {         // f(index, z) of the entries there are
-        each_group([&](int, int j, const float (&v)[4]) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (v[i] > -INFINITY) f(j + i, v[i]);
-        });
-    }
+// What a row asks for.
+struct Asked {
+    float T, top_p, min_p;
+    unsigned k;
+    bool greedy, by_k, by_p;
 };
+__device__ __forceinline__ Asked asked_of(const FilterArgs& a, int r) {
+    Asked q;
+    q.T = a.temperature ? a.temperature[r] : 1.f;
+    q.greedy = !(q.T > 0.f);
+    const int k = a.top_k ? a.top_k[r] : 0;
+    q.by_k = k >= 1 && k < a.n;
+    q.k = q.by_k ? (unsigned)k : 0xFFFFFFFFu;
+    const float p = a.top_p ? a.top_p[r] : 1.f, m = a.min_p ? a.min_p[r] : 0.f;
+    q.by_p = p < 1.f;
+    q.top_p = fmaxf(p, 0.f);
+    q.min_p = m > 1.f ? 1.f : (m > 0.f ? m : 0.f);   // (NaN: none)
+    return q;
+}
+__device__ __forceinline__ Source source_of(const FilterArgs& a, int r, const Asked& q) {
+    Source s;
+    const int es = a.dtype == HAWK_FP32 ? 4 : 2;
+    s.dtype = a.dtype;
+    s.n = a.n;
+    s.l = a.logits + r * a.row_stride * es;
+    s.fours = (reinterpret_cast<uintptr_t>(s.l) & (4 * es - 1)) == 0;
+    s.inv_t = q.greedy ? 1.f : (float)(1.0 / (double)q.T);
+    s.infinite = false;
+    return s;
+}
+__device__ __forceinline__ void give(const FilterArgs& a, int r, int token, float prob, int kept) {
+    a.out_token[r] = token;
+    if (a.out_prob) a.out_prob[r] = prob;
+    if (a.out_kept) a.out_kept[r] = kept;
+}
+// The smallest weight that min_p keeps, top: the largest one's.
+__device__ __forceinline__ u64 least_of(const Asked& q, u64 top) { return q.min_p >= 1.f ? top : (q.min_p > 0.f ? share_of(q.min_p, top) : 0ull); }
 
-__device__ __forceinline__ int bin_of(float zmax, float z) { return (int)fminf((zmax - z) * (kCutBins / kCutReach), (float)(kCutBins - 1)); }
-
-// Entries are kept if z is above the border's key, or equal and not behind index `at`.
-struct Border { unsigned key; int at; };
-__device__ __forceinline__ bool inside(const Border& b, float z, int j) {
-    const unsigned k = fkey(z);
-    return k > b.key || (k == b.key && j <= b.at);
+// One wave: of NB bins the last one that is not empty and begins before the cut, with what it has
+// and what lies before it, the same in every lane; there is one.  A lane has neighbouring bins and reads them in an order in which lanes do
+// not meet.
+template <int NB> __device__ __forceinline__ Picked pick_bin(const unsigned* count, const u64* mass, const Cut& cut, unsigned ahead, u64 before) {
+    constexpr int PER = NB / 64;
+    const int lane = threadIdx.x & 63;
+    int c = 0;
+    u64 m = 0;
+#pragma unroll 8
+    for (int j = 0; j < PER; ++j) {
+        const int b = lane * PER + ((j + lane) & (PER - 1));
+        c += (int)count[b];
+        m += mass[b];
+    }
+    const int cb = wave_incl_scan_i(c) - c;
+    const u64 mb = wave_incl_scan_u64(m) - m;
+    u64 who = __ballot(c > 0 && before + mb < cut.M && ahead + (unsigned)cb < cut.K);
+    const int L = who ? 63 - __clzll((long long)who) : 0;
+    ahead += (unsigned)__builtin_amdgcn_readlane(cb, L);
+    before += lane_u64(mb, L);
+    const int b = L * PER + lane;
+    const int c1 = lane < PER ? (int)count[b] : 0;
+    const u64 m1 = lane < PER ? mass[b] : 0ull;
+    const unsigned a1 = ahead + (unsigned)(wave_incl_scan_i(c1) - c1);
+    const u64 b1 = before + (wave_incl_scan_u64(m1) - m1);
+    who = __ballot(c1 > 0 && b1 < cut.M && a1 < cut.K);
+    const int at = who ? 63 - __clzll((long long)who) : 0;
+    const Picked out = {L * PER + at, (unsigned)__builtin_amdgcn_readlane(c1, at), (unsigned)__builtin_amdgcn_readlane((int)a1, at), lane_u64(b1, at)};
+    return out;
+}
+// The same for a workgroup: the first wave looks, all threads have the result and find the words of a ranking cleared.  Ends with a barrier.
+__device__ __forceinline__ Picked pick_for_all(const unsigned* count, const u64* mass, const Cut& cut, unsigned ahead, u64 before, CutShared& sh) {
+    if (wave_id() == 0) {
+        const Picked p = pick_bin<kBinCount>(count, mass, cut, ahead, before);
+        if ((threadIdx.x & 63) == 0) {
+            sh.picked = p;
+            sh.n = 0;
+            sh.winner = 0ull;
+            sh.within = 0ull;
+        }
+    }
+    __syncthreads();
+    return sh.picked;
 }
 
-// What a cut looks for: the first entry, in order, before which there are K entries or a mass of M.  (The other one is then never reached.)
-struct Cut { u64 M; unsigned K; };
-
-// The border of a cut: the last entry before it; mass: of all entries up to it.  Every thread has the result.
-template <int E> __device__ Border find_border(const Row<E>& row, float zmax, const Cut& cut, int unit, FilterShared& sh, u64& mass) {
-    const int tid = threadIdx.x;
-    auto weight = [&](float z) { return (u64)__double_as_longlong(exp_below((double)z - (double)zmax, sh.steps) + __hiloint2double((1075 - unit) << 20, 0)) & 0xFFFFFFFFFFFFFull; };
-    // the bin in which the cut lies
-    {
-        u64 m0 = sh.mass[2 * tid], m1 = sh.mass[2 * tid + 1], all_m;
-        int c0 = (int)sh.count[2 * tid], c1 = (int)sh.count[2 * tid + 1], all_c;
-        const u64 bm = block_before(m0 + m1, sh.sum, all_m);
-        const int bc = block_before(c0 + c1, sh.isum, all_c);
-        // the last bin that begins before the cut and is not empty
-        const bool in0 = c0 > 0 && bm < cut.M && (unsigned)bc < cut.K, in1 = c1 > 0 && bm + m0 < cut.M && (unsigned)(bc + c0) < cut.K;
-        if (tid == 0) sh.n = 0;
-        if (in1 || in0) atomicMax(&sh.b_bin, in1 ? 2 * tid + 1 : 2 * tid);
-        __syncthreads();
-        const int b = sh.b_bin;
-        if (b >> 1 == tid) {
-            sh.b_mass = (b & 1) ? bm + m0 : bm;
-            sh.b_count = (b & 1) ? bc + c0 : bc;
-        }
-        __syncthreads();
-    }
-    const int bin = sh.b_bin, m = (int)sh.count[bin];
-    u64 before = sh.b_mass;
-    unsigned ahead = (unsigned)sh.b_count;
-    Border out;
-    if (m <= kList) {
-        row.each([&](int j, float z) {
-            if (bin_of(zmax, z) == bin) {
-                const int i = atomicAdd(&sh.n, 1);
-                sh.list_key[i] = fkey(z);
-                sh.list_at[i] = j;
-            }
-        });
-        __syncthreads();
-        for (int i = tid; i < m; i += NT) {
-            const unsigned k = sh.list_key[i];
-            const int at = sh.list_at[i];
-            int r = 0;
-            for (int x = 0; x < m; ++x) {
-                const unsigned other = sh.list_key[x];
-                r += other > k || (other == k && sh.list_at[x] < at) ? 1 : 0;
-            }
-            sh.ranked_key[r] = k;
-            sh.ranked_at[r] = at;
-        }
-        __syncthreads();
-        // two ranks a thread: sums of the masses before
-        u64 w[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) w[i] = 2 * tid + i < m ? weight(key_to_float(sh.ranked_key[2 * tid + i])) : 0;
-        u64 all, bm = before + block_before(w[0] + w[1], sh.sum, all);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int r = 2 * tid + i;
-            if (r < m && bm < cut.M && ahead + r < cut.K) atomicMax(&sh.b_at, r);   // the last one inside
-            bm += w[i];
-            if (r < m) sh.list_mass[r] = bm;
-        }
-        __syncthreads();
-        const int last = sh.b_at;
-        out.key = sh.ranked_key[last];
-        out.at = sh.ranked_at[last];
-        mass = sh.list_mass[last];
-        __syncthreads();
-        return out;
-    }
-    // by the key's bits, eight at a time: the key of the last entry inside, and how many of the entries that have it are
-    unsigned prefix = 0u, mask = 0u;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        __syncthreads();
-        if (tid < 256) { sh.list_key[tid] = 0u; sh.list_mass[tid] = 0ull; }
-        if (tid == 0) sh.b_at = -1;
-        __syncthreads();
-        row.each([&](int, float z) {
+// The border of a cut within a range.  each(f): f(index, z) of this thread's entries that may be in it.  masses: weights count.  All threads
+// call; sh.n, winner, within are zero; ends with a barrier.
+template <class Each>
+__device__ __forceinline__ Found find_border(const Each& each, const Weigh& weigh, bool masses, const Cut& cut, Range r, CutShared& sh) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
+    while (r.m > (unsigned)kFew) {
+        const bool by_key = r.lo < r.hi;
+        const unsigned span = by_key ? r.hi - r.lo : (unsigned)(r.last - r.first);
+        const int s = max(0, 32 - __clz((int)span) - 11);
+        each([&](int j, float z) {
             const unsigned k = fkey(z);
-            if (bin_of(zmax, z) == bin && (k & mask) == prefix) {
-                atomicAdd(&sh.list_key[(k >> shift) & 255u], 1u);
-                atomicAdd(&sh.list_mass[(k >> shift) & 255u], weight(z));
-            }
+            if (k < r.lo || k > r.hi || (!by_key && (j < r.first || j > r.last))) return;
+            const unsigned d = (by_key ? r.hi - k : (unsigned)(j - r.first)) >> s;
+            atomicAdd(&sh.fine[d], 1u);
+            if (masses) atomicAdd(&sh.fine_mass[d], weigh(z));
         });
         __syncthreads();
-        // descending: thread t has digit 255 - t
-        const int c = tid < 256 ? (int)sh.list_key[255 - tid] : 0;
-        const u64 w = tid < 256 ? sh.list_mass[255 - tid] : 0ull;
-        int all_c;
-        u64 all_w;
-        const int bc = block_before(c, sh.isum, all_c);
-        const u64 bw = block_before(w, sh.sum, all_w);
-        if (c > 0 && before + bw < cut.M && ahead + (unsigned)bc < cut.K) atomicMax(&sh.b_at, tid);
+        const Picked p = pick_for_all(sh.fine, sh.fine_mass, cut, r.ahead, r.before, sh);
+        const unsigned d = (unsigned)p.bin, up = ((d + 1u) << s) - 1u;
+        r.m = p.m;
+        r.ahead = p.ahead;
+        r.before = p.before;
+        if (by_key) {
+            const unsigned hi = r.hi;
+            r.lo = hi - min(hi - r.lo, up);
+            r.hi = hi - (d << s);
+        } else {
+            const int first = r.first;
+            r.first = first + (int)(d << s);
+            r.last = (int)min((unsigned)r.last, (unsigned)first + up);
+        }
+        for (int i = tid; i < kBinCount; i += NT) { sh.fine[i] = 0u; sh.fine_mass[i] = 0ull; }
         __syncthreads();
-        const int t = sh.b_at;
-        if (tid == t) { sh.b_mass = before + bw; sh.b_count = (int)ahead + bc; }
-        __syncthreads();
-        before = sh.b_mass;
-        ahead = (unsigned)sh.b_count;
-        prefix |= (unsigned)(255 - t) << shift;
-        mask |= 255u << shift;
-        if (shift == 0 && tid == 0) sh.n = (int)sh.list_key[255 - t];
     }
-    __syncthreads();
-    // of the equal ones entry i (from 0) is inside if before + i w < M and ahead + i < K
-    const int equal = sh.n;
-    const u64 w = weight(key_to_float(prefix));
-    u64 c = min((u64)equal, (u64)(cut.K - ahead));
-    if (w > 0) c = min(c, (cut.M - before + w - 1) / w);
-    mass = before + c * w;
-    int seen = 0;
-    out.key = prefix;
-    out.at = 0x7FFFFFFF;
-    __syncthreads();
-    if (tid == 0) sh.b_at = -1;
-    row.each_group([&](int, int j, const float (&v)[4]) {
-        int own = 0, all;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) own += v[i] > -INFINITY && fkey(v[i]) == prefix ? 1 : 0;
-        int k = seen + block_before(own, sh.isum, all);
-        seen += all;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (v[i] > -INFINITY && fkey(v[i]) == prefix && (u64)++k == c) sh.b_at = j + i;
+    each([&](int j, float z) {
+        const unsigned k = fkey(z);
+        if (k < r.lo || k > r.hi || (r.lo == r.hi && (j < r.first || j > r.last))) return;
+        const int i = atomicAdd(&sh.n, 1);
+        if (i >= kFew) return;       // (there are r.m of them)
+        sh.key[i] = k;
+        sh.at[i] = j;
+        sh.w[i] = masses ? weigh(z) : 0ull;
     });
     __syncthreads();
-    out.at = sh.b_at;
+    // a wave has every sixteenth entry, its lanes compare it with all others
+    const int m = (int)r.m;
+    unsigned k[kFew / 64];
+    int at[kFew / 64];
+    u64 w[kFew / 64];
+#pragma unroll
+    for (int c = 0; c < kFew / 64; ++c) {
+        const int i = c * 64 + lane;
+        k[c] = i < m ? sh.key[i] : 0u;
+        at[c] = i < m ? sh.at[i] : 0x7FFFFFFF;
+        w[c] = i < m ? sh.w[i] : 0ull;
+    }
+    u64 best = 0ull, within = 0ull;
+    for (int i = wave; i < m; i += NW) {
+        const unsigned mk = sh.key[i];
+        const int ma = sh.at[i];
+        int rank = 0;
+        u64 sum = 0ull;
+#pragma unroll
+        for (int c = 0; c < kFew / 64; ++c) {
+            if (c * 64 >= m) break;
+            const bool ahead = k[c] > mk || (k[c] == mk && at[c] < ma);
+            rank += __popcll(__ballot(ahead));
+            sum += ahead ? w[c] : 0ull;
+        }
+        if (masses) sum = wave_sum_u64(sum);
+        if (r.before + sum < cut.M && r.ahead + (unsigned)rank < cut.K) {
+            best = maxu64(best, ((u64)(unsigned)(rank + 1) << 32) | (unsigned)i);
+            within += sh.w[i];
+        }
+    }
+    if (lane == 0 && best) {
+        atomicMax(&sh.winner, best);
+        atomicAdd(&sh.within, within);
+    }
     __syncthreads();
+    const int i = (int)(unsigned)sh.winner;
+    const Found out = {{sh.key[i], sh.at[i]}, r.before + sh.within};
     return out;
 }
 
-template <int E>
-__global__ __launch_bounds__(NT) void sample_filtered_kernel(FilterArgs a) {
-    __shared__ FilterShared sh;
-    const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    auto give = [&](int token, double prob, int kept) {
-        if (tid == 0) {
-            a.out_token[r] = token;
-            if (a.out_prob) a.out_prob[r] = (float)prob;
-            if (a.out_kept) a.out_kept[r] = kept;
+// Which keys bin b of the linear ones has: z is between its ends but for the rounding of zmax - z.
+__device__ __forceinline__ int bin_of(float zmax, float z) { return (int)fminf((zmax - z) * kPerUnit, (float)(kBinCount - 1)); }
+__device__ __forceinline__ Range bin_range(float zmax, const Picked& p) {
+    Range r;
+    const int b = p.bin;
+    r.before = p.before;
+    r.ahead = p.ahead;
+    r.m = p.m;
+    const double top = (double)zmax - b / (double)kPerUnit * (1.0 - 0x1p-23), low = (double)zmax - (b + 1) / (double)kPerUnit * (1.0 + 0x1p-23);
+    r.hi = b == 0 ? fkey(zmax) : fkey((float)top) + 1u;
+    r.lo = b == kBinCount - 1 ? 0u : fkey((float)low) - 1u;
+    r.first = 0;
+    r.last = 0x7FFFFFFF;
+    return r;
+}
+
+// Four neighbouring entries of a lane, 256 of a wave: the one in which the sum of kept weights from `base` on first exceeds target.
+template <class Kept>
+__device__ __forceinline__ void draw_of_chunk(const FilterArgs& a, int r, int j, const float (&z)[4], const Kept& kept, const Weigh& weigh, u64 base, u64 target,
+                                              u64 total) {
+    u64 w[4], s = 0ull;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        w[i] = kept(z[i], j + i);
+        s += w[i];
+    }
+    u64 at = base + wave_incl_scan_u64(s) - s;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (at <= target && target < at + w[i]) {
+            a.out_token[r] = j + i;
+            if (a.out_prob) a.out_prob[r] = (float)(weigh.real(z[i]) * __hiloint2double((1023 + a.unit) << 20, 0) / (double)total);
+        }
+        at += w[i];
+    }
+}
+__device__ __forceinline__ u64 target_of(const FilterArgs& a, int r, u64 total) {   // the first sum above it
+    return min((u64)(fmax((double)a.u[r], 0.0) * (double)total), total - 1ull);
+}
+
+// Sums of chunks (in sums, n of them): finds the one in which the sum first exceeds u times the whole.  All threads call and have the result.
+__device__ __forceinline__ int pick_chunk(const FilterArgs& a, int r, const u64* sums, int n, CutShared& sh, u64& base, u64& target, u64& total) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
+    u64 s[kChunks / NT], own = 0ull;
+#pragma unroll
+    for (int i = 0; i < kChunks / NT; ++i) {
+        s[i] = tid * (kChunks / NT) + i < n ? sums[tid * (kChunks / NT) + i] : 0ull;
+        own += s[i];
+    }
+    const u64 upto = wave_incl_scan_u64(own);
+    if (lane == 63) sh.sum[wave] = upto;
+    if (tid == 0) { sh.chunk = 0; sh.base = 0ull; }
+    __syncthreads();
+    u64 before = 0ull;
+    total = 0ull;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        before += w < wave ? sh.sum[w] : 0ull;
+        total += sh.sum[w];
+    }
+    before += upto - own;
+    target = target_of(a, r, total);
+#pragma unroll
+    for (int i = 0; i < kChunks / NT; ++i) {
+        if (before <= target && target < before + s[i]) {
+            sh.chunk = tid * (kChunks / NT) + i;
+            sh.base = before;
+        }
+        before += s[i];
+    }
+    __syncthreads();
+    base = sh.base;
+    return sh.chunk;
+}
+
+// One workgroup, one row.  E entries a thread in registers: group q of four starts at q * 4096 + 4 * thread; E = 0: read again for every look.
+template <int E> __device__ __forceinline__ void whole_row(const FilterArgs& a, int r, CutShared& sh, u64* sums) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
+    const Asked q = asked_of(a, r);
+    Source src = source_of(a, r, q);
+    float z[E > 0 ? E : 1];
+    u64 weights[E > 0 ? E : 1];      // of the row's entries, where they are asked for by top-p
+    const int groups = E > 0 ? E / 4 : (a.n + 4 * NT - 1) / (4 * NT);
+    auto load = [&]() {
+        if constexpr (E > 0) {
+#pragma unroll
+            for (int g = 0; g < E / 4; ++g) {
+                float v[4];
+                src.four(g * 4 * NT + 4 * tid, v);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z[4 * g + i] = v[i];
+            }
         }
     };
-    if (a.skip && a.skip[r] < 0) { give(-1, 0.0, 0); return; }
-    const float T = a.temperature ? a.temperature[r] : 1.f;
-    const bool greedy = !(T > 0.f);
-    Row<E> row;
-    row.s.dtype = a.dtype;
-    row.s.n = a.n;
-    const int es = a.dtype == HAWK_FP32 ? 4 : 2;
-    row.s.l = a.logits + r * a.row_stride * es;
-    row.s.fours = (reinterpret_cast<uintptr_t>(row.s.l) & (4 * es - 1)) == 0;
-    row.s.inv_t = greedy ? 1.f : (float)(1.0 / (double)T);
-    row.s.infinite = false;
-    fill_steps(sh.steps);
-    for (int i = tid; i < kCutBins; i += NT) { sh.count[i] = 0u; sh.mass[i] = 0ull; }
-    if (tid == 0) { sh.b_bin = -1; sh.b_at = -1; sh.n = 0; }
-    row.load();
-
-    // the largest entry, lowest index first
-    u64 best = 0ull;
-    row.each([&](int j, float z) { best = maxu64(best, ((u64)fkey(z) << 32) | (0xFFFFFFFFu - (unsigned)j)); });
-    for (int d = 1; d < 64; d <<= 1) best = maxu64(best, __shfl_xor(best, d));
-    if (lane == 0) sh.sum[wave] = best;
-    __syncthreads();
+    auto each = [&](auto f) {        // f(index, z) of the entries there are
+        if constexpr (E > 0) {
+            const int th = this_thread();
 #pragma unroll
-    for (int w = 0; w < NW; ++w) best = maxu64(best, sh.sum[w]);
+            for (int e = 0; e < E; ++e) {
+                float v = z[e];
+                asm volatile("" : "+v"(v));      // (or the keys, bins and weights of all entries are kept for the next look: more than there are registers)
+                if (v > -INFINITY) f(entry<E>(e, th), v);
+            }
+        } else {
+            for (int g = 0; g < groups; ++g) {
+                float v[4];
+                const int j = g * 4 * NT + 4 * tid;
+                src.four(j, v);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (v[i] > -INFINITY) f(j + i, v[i]);
+            }
+        }
+    };
     __syncthreads();
-    if (best == 0ull) { give(-1, 0.0, 0); return; }
-    float zmax = key_to_float((unsigned)(best >> 32));
-    if (greedy) { give((int)(0xFFFFFFFFu - (unsigned)best), 1.0, 1); return; }
-    if (zmax == INFINITY) {
-        row.s.infinite = true;
-        zmax = 0.f;
-        row.load();
-    }
-    const int unit = a.unit;
-    const double magic = __hiloint2double((1075 - unit) << 20, 0);   // 2^(52 - S): a sum with it has round(w 2^S) in its last 52 bits
-    auto exact_weight = [&](float z) { return exp_below((double)z - (double)zmax, sh.steps); };
-    auto whole = [&](double w) { return (u64)__double_as_longlong(w + magic) & 0xFFFFFFFFFFFFFull; };
+    load();
+    fill_steps(sh.steps);
+    for (int i = tid; i < kBinCount; i += NT) { sh.count[i] = 0u; sh.mass[i] = 0ull; sh.fine[i] = 0u; sh.fine_mass[i] = 0ull; }
 
-    const int want = a.top_k ? a.top_k[r] : 0;
-    const float top_p = a.top_p ? a.top_p[r] : 1.f, asked = a.min_p ? a.min_p[r] : 0.f, min_p = asked > 1.f ? 1.f : asked;   // (NaN: none)
-    const bool by_k = want >= 1 && want < a.n, by_p = top_p < 1.f, by_m = min_p > 0.f;
+    if (q.greedy) {                  // the largest entry, lowest index first
+        u64 best = 0ull;
+        each([&](int j, float v) { best = maxu64(best, ((u64)fkey(v) << 32) | (0xFFFFFFFFu - (unsigned)j)); });
+        best = max1(best, sh.sum);
+        if (tid == 0) best == 0ull ? give(a, r, -1, 0.f, 0) : give(a, r, (int)(0xFFFFFFFFu - (unsigned)best), 1.f, 1);
+        return;
+    }
+    float zmax = -INFINITY;
+    each([&](int, float v) { zmax = fmaxf(zmax, v); });
+    zmax = wave_max_f(zmax);
+    if (lane == 0) sh.fmax[wave] = zmax;
+    __syncthreads();
+    zmax = sh.fmax[lane & 15];
+    ROW_ALLREDUCE(zmax, fmaxf, dpp_f)
+    zmax = lane_f(zmax, 0);
+    if (zmax == -INFINITY) {
+        if (tid == 0) give(a, r, -1, 0.f, 0);
+        return;
+    }
+    if (zmax == INFINITY) {
+        src.infinite = true;
+        zmax = 0.f;
+        load();
+    }
+    const Weigh weigh = {(double)zmax, magic_of(a.unit), sh.steps};
+
     Border border = {0u, 0x7FFFFFFF};
-    if (by_k || by_p) {
-        row.each([&](int, float z) {
-            const int b = bin_of(zmax, z);
-            atomicAdd(&sh.count[b], 1u);
-            if (by_p) atomicAdd(&sh.mass[b], whole(exact_weight(z)));
-        });
+    if (q.by_k || q.by_p) {
+        if constexpr (E > 0) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                weights[e] = 0ull;
+                if (z[e] > -INFINITY) {
+                    const int b = bin_of(zmax, z[e]);
+                    atomicAdd(&sh.count[b], 1u);
+                    if (q.by_p) atomicAdd(&sh.mass[b], weights[e] = weigh(z[e]));
+                }
+            }
+        } else {
+            each([&](int, float v) {
+                const int b = bin_of(zmax, v);
+                atomicAdd(&sh.count[b], 1u);
+                if (q.by_p) atomicAdd(&sh.mass[b], weigh(v));
+            });
+        }
         __syncthreads();
         u64 mass = 0ull;
-        if (by_k) {
-            const Cut cut = {1ull << 63, (unsigned)want};
-            border = find_border<E>(row, zmax, cut, unit, sh, mass);
+        auto cut_at = [&](const Cut& cut) {
+            const Picked p = pick_for_all(sh.count, sh.mass, cut, 0u, 0ull, sh);
+            const int b = p.bin;
+            const Range range = bin_range(zmax, p);
+            auto in_bin = [&](auto f) {
+                each([&](int j, float v) {
+                    if (bin_of(zmax, v) == b) f(j, v);
+                });
+            };
+            const Found found = find_border(in_bin, weigh, q.by_p, cut, range, sh);
+            border = found.border;
+            mass = found.mass;
+        };
+        if (q.by_k) {
+            const Cut cut = {1ull << 63, q.k};
+            cut_at(cut);
         } else {
-            mass = block_sum(sh.mass[2 * tid] + sh.mass[2 * tid + 1], sh.sum);
-        }
-        if (by_p) {
-            if (tid == 0) { sh.b_bin = -1; sh.b_at = -1; }
+            u64 own = sh.mass[tid] + sh.mass[tid + NT];
+            own = wave_sum_u64(own);
+            if (lane == 0) sh.sum[wave] = own;
             __syncthreads();
-            // an entry is inside if the mass before it is below top_p times the whole: of whole numbers, below that rounded up
-            const Cut cut = {max((u64)ceil(fmax((double)top_p * (double)mass, 0.0)), 1ull), by_k ? (unsigned)want : 0xFFFFFFFFu};
-            border = find_border<E>(row, zmax, cut, unit, sh, mass);
+#pragma unroll
+            for (int w = 0; w < NW; ++w) mass += sh.sum[w];
+        }
+        if (q.by_p) {
+            __syncthreads();
+            const Cut cut = {maxu64(share_of(q.top_p, mass), 1ull), q.k};   // (the first entry always)
+            cut_at(cut);
         }
     }
 
-    // sums of the kept weights: of the four entries a thread has in a group, of a wave's 256, of all of them in index order
-    auto kept = [&](float z, int j, double& w) {
-        if (!(z > -INFINITY) || !inside(border, z, j)) return false;
-        w = exact_weight(z);
-        return !(by_m && w < (double)min_p);
-    };
-    const int groups = row.groups();
-    u64* sums = sh.mass;             // [group][wave]: of up to 128 groups; further ones join the last
+    const u64 least = least_of(q, weigh(zmax));
     int n_kept = 0;
-    for (int i = tid; i < kCutBins; i += NT) sums[i] = 0ull;
-    __syncthreads();
-    constexpr int kGroups = kCutBins / NW;
-    const int fold = (groups + kGroups - 1) / kGroups;               // groups that share a sum
-    row.each_group([&](int q, int j, const float (&v)[4]) {
-        u64 s = 0;
+    auto kept = [&](float v, int j, u64 w) { return v > -INFINITY && inside(border, v, j) && w >= least; };
+    auto add_group = [&](int g, u64 s) {
+        s = wave_sum_u64(s);
+        if (lane == 0) sums[g * NW + wave] = s;
+    };
+    if constexpr (E > 0) {
+        if (!q.by_p) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            double w;
-            if (kept(v[i], j + i, w)) {
-                s += whole(w);
+            for (int e = 0; e < E; ++e) {
+                if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                weights[e] = z[e] > -INFINITY && inside(border, z[e], entry<E>(e, tid)) ? weigh(z[e]) : 0ull;
+            }
+        }
+#pragma unroll
+        for (int g = 0; g < E / 4; ++g) {
+            u64 s = 0ull;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int e = 4 * g + i;
+                const bool k = kept(z[e], entry<E>(e, tid), weights[e]);
+                weights[e] = k ? weights[e] : 0ull;
+                s += weights[e];
+                n_kept += k ? 1 : 0;
+            }
+            add_group(g, s);
+        }
+    } else {
+        for (int g = 0; g < groups; ++g) {
+            float v[4];
+            u64 s = 0ull;
+            const int j = g * 4 * NT + 4 * tid;
+            src.four(j, v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (!(v[i] > -INFINITY) || !inside(border, v[i], j + i)) continue;
+                const u64 w = weigh(v[i]);
+                if (w < least) continue;
+                s += w;
                 ++n_kept;
             }
+            add_group(g, s);
         }
-        for (int d = 1; d < 64; d <<= 1) s += __shfl_xor(s, d);
-        if (lane == 0) atomicAdd(&sums[fold == 1 ? q * NW + wave : q / fold * NW], s);
-    });
+    }
+    n_kept = wave_sum_i(n_kept);
+    if (lane == 0) sh.isum[wave] = n_kept;
     __syncthreads();
-    u64 total;
-    const u64 m0 = sums[2 * tid], m1 = sums[2 * tid + 1];
-    const u64 before = block_before(m0 + m1, sh.sum, total);
-    int all;
-    (void)block_before(n_kept, sh.isum, all);
-    const u64 target = min((u64)(fmax((double)a.u[r], 0.0) * (double)total), total - 1);   // the first sum above it
-    if (before <= target && target < before + m0 + m1) {
-        const bool second = target >= before + m0;
-        sh.b_bin = 2 * tid + (second ? 1 : 0);
-        sh.b_mass = second ? before + m0 : before;
+    u64 base, target, total;
+    int chunk;
+    if constexpr (E > 0) {           // up to 64 sums: every wave looks for itself
+        const u64 s = lane < groups * NW ? sums[lane] : 0ull, upto = wave_incl_scan_u64(s);
+        total = lane_u64(upto, 63);
+        target = target_of(a, r, total);
+        chunk = __ffsll(__ballot(target < upto)) - 1;
+        base = lane_u64(upto - s, chunk);
+#pragma unroll
+        for (int g = 0; g < E / 4; ++g)
+            if (g * NW + wave == chunk) {
+                const int j = g * 4 * NT + 4 * tid;
+                const float v[4] = {z[4 * g], z[4 * g + 1], z[4 * g + 2], z[4 * g + 3]};
+                draw_of_chunk(a, r, j, v, [&](float, int at) { return weights[4 * g + (at - j)]; }, weigh, base, target, total);
+            }
+    } else {
+        chunk = pick_chunk(a, r, sums, groups * NW, sh, base, target, total);
+        if (wave == 0) {
+            float v[4];
+            const int j = chunk * kChunk + 4 * lane;
+            src.four(j, v);
+            draw_of_chunk(a, r, j, v, [&](float x, int at) {
+                if (!(x > -INFINITY) || !inside(border, x, at)) return 0ull;
+                const u64 w = weigh(x);
+                return w >= least ? w : 0ull;
+            }, weigh, base, target, total);
+        }
+    }
+    if (tid == 0 && a.out_kept) {
+        int all = 0;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) all += sh.isum[w];
+        a.out_kept[r] = all;
+    }
+}
+
+template <int E> __global__ __launch_bounds__(NT) void sample_filtered_kernel(FilterArgs a) {
+    __shared__ CutShared sh;
+    __shared__ u64 sums[E > 0 ? 64 : kChunks];
+    const int r = blockIdx.x;
+    if (a.skip && a.skip[r] < 0) {
+        if (threadIdx.x == 0) give(a, r, -1, 0.f, 0);
+        return;
+    }
+    whole_row<E>(a, r, sh, sums);
+}
+
+// ---- Long rows in parts of E * 1024 entries.  Their bins are cells of a fixed grid of z, 1024 of them from the cell of the largest entry down (of a
+// part, so that a part needs to know nothing of the others; the last one holds what lies behind), and weights are relative to the
+// upper end of the largest's cell: parts are brought together by moving bins and scaling masses.
+constexpr int kPartBins = 1024, kPartList = 512, kMostParts = 32, kList = 4096;
+constexpr float kCells = 32.f;       // cells of a unit of z
+constexpr int kFar = 1 << 29;        // cells from here on are not told apart
+__device__ __forceinline__ int cell_of(float z) { return (int)fminf(fmaxf(floorf(z * kCells), -1073741824.f), 1073741824.f); }
+__device__ __forceinline__ double ref_of(int top) { return (top + 1) * (double)(1.f / kCells); }
+
+struct PartHead {
+    u64 mass, best;                  // of all entries; the largest with the lowest index (greedy rows)
+    float zmax;
+    int top, valid, n_list, n_kept, pad;
+};
+struct RowHead {
+    u64 total, k_before, p_before;   // of all entries; before the bins that the cuts lie in
+    unsigned k_ahead, k_m;
+    int k_bin, p_first, p_last, pad;
+};
+struct RowRoom {
+    PartHead* head;
+    RowHead* row;
+    u64 *mass, *sums;                // [part][bin]; [part][chunk]
+    unsigned* count;                 // [part][bin]
+    int2* list;                      // [part][kPartList]: z, index
+};
+__host__ __device__ inline size_t part_bytes(int E) { return sizeof(PartHead) + kPartBins * 12 + kPartList * 8 + (size_t)E * 32; }
+__host__ __device__ inline size_t row_bytes(int parts, int E) { return sizeof(RowHead) + parts * part_bytes(E); }
+__device__ __forceinline__ RowRoom room_of(const FilterArgs& a, int row, int E) {
+    char* p = a.room + row * row_bytes(a.parts, E);
+    RowRoom r;
+    r.row = reinterpret_cast<RowHead*>(p);
+    r.head = reinterpret_cast<PartHead*>(p + sizeof(RowHead));
+    r.mass = reinterpret_cast<u64*>(r.head + a.parts);
+    r.sums = r.mass + (size_t)a.parts * kPartBins;
+    r.list = reinterpret_cast<int2*>(r.sums + (size_t)a.parts * E * 4);
+    r.count = reinterpret_cast<unsigned*>(r.list + (size_t)a.parts * kPartList);
+    return r;
+}
+template <int E> struct PartRow {
+    float z[E];
+    int j0;
+    __device__ __forceinline__ void load(const Source& s, int part) {
+        j0 = part * E * NT + 4 * (int)threadIdx.x;
+#pragma unroll
+        for (int g = 0; g < E / 4; ++g) {
+            float v[4];
+            s.four(j0 + g * 4 * NT, v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[4 * g + i] = v[i];
+        }
+    }
+    __device__ __forceinline__ int index(int e) const { return j0 + (e >> 2) * 4 * NT + (e & 3); }
+};
+
+template <int E> __global__ __launch_bounds__(NT) void filter_bins_kernel(FilterArgs a, int row0) {
+    __shared__ u64 mass[kPartBins], slot[NW];
+    __shared__ unsigned count[kPartBins];
+    __shared__ double steps[kSteps];
+    __shared__ float top[NW];
+    const int row = (int)blockIdx.x / a.parts, part = (int)blockIdx.x - row * a.parts, r = row0 + row, tid = threadIdx.x, lane = tid & 63, wave = wave_id();
+    if (a.skip && a.skip[r] < 0) return;
+    const Asked q = asked_of(a, r);
+    const Source src = source_of(a, r, q);
+    PartRow<E> p;
+    p.load(src, part);
+    const RowRoom room = room_of(a, row, E);
+    if (q.greedy) {
+        u64 best = 0ull;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (p.z[e] > -INFINITY) best = maxu64(best, ((u64)fkey(p.z[e]) << 32) | (0xFFFFFFFFu - (unsigned)p.index(e)));
+        best = max1(best, slot);
+        if (tid == 0) room.head[part].best = best;
+        return;
+    }
+    mass[tid] = 0ull;
+    count[tid] = 0u;
+    fill_steps(steps);
+    float zmax = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < E; ++e) zmax = fmaxf(zmax, p.z[e]);
+    zmax = wave_max_f(zmax);
+    if (lane == 0) top[wave] = zmax;
+    __syncthreads();
+    zmax = top[lane & 15];
+    ROW_ALLREDUCE(zmax, fmaxf, dpp_f)
+    zmax = lane_f(zmax, 0);
+    const int cell = cell_of(zmax);
+    const bool bins = (q.by_k || q.by_p) && cell < kFar && cell > -kFar;
+    if (bins) {
+        const Weigh weigh = {ref_of(cell), magic_of(a.unit), steps};
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (p.z[e] > -INFINITY) {
+                const int b = min(cell - cell_of(p.z[e]), kPartBins - 1);
+                atomicAdd(&count[b], 1u);
+                if (q.by_p) atomicAdd(&mass[b], weigh(p.z[e]));
+            }
+        __syncthreads();
+        const u64 m = mass[tid];
+        const int c = (int)count[tid];
+        room.mass[part * kPartBins + tid] = m;
+        room.count[part * kPartBins + tid] = (unsigned)c;
+        const u64 wm = wave_sum_u64(m);
+        const int wc = wave_sum_i(c);
+        if (lane == 0) { slot[wave] = wm; top[wave] = __int_as_float(wc); }
+        __syncthreads();
+    }
+    if (tid == 0) {
+        PartHead h = {};
+        if (bins)
+            for (int w = 0; w < NW; ++w) {
+                h.mass += slot[w];
+                h.valid += __float_as_int(top[w]);
+            }
+        h.zmax = zmax;
+        h.top = cell;
+        room.head[part] = h;
+    }
+}
+
+// The largest entry of a row's parts and its cell; whether there is anything to draw, and whether any part's largest entry is off the grid.
+struct Top { float zmax; int cell; bool any, far; };
+__device__ __forceinline__ Top row_top(const FilterArgs& a, const RowRoom& room) {
+    const int lane = threadIdx.x & 63;
+    const float z = lane < a.parts ? room.head[lane].zmax : -INFINITY;
+    Top t;
+    t.zmax = wave_max_f(z);
+    t.cell = cell_of(t.zmax);
+    t.any = t.zmax > -INFINITY;
+    t.far = __ballot(z > -INFINITY && (cell_of(z) >= kFar || cell_of(z) <= -kFar)) != 0ull;
+    return t;
+}
+
+struct PartShared {
+    u64 mass[kPartBins];
+    unsigned count[kPartBins];
+    double scale[kMostParts], steps[kSteps];
+    int down[kMostParts];
+    u64 rest_mass;
+    int rest, n_list, n_kept;
+    RowHead head;
+};
+
+template <int E> __global__ __launch_bounds__(NT) void filter_parts_kernel(FilterArgs a, int row0) {
+    __shared__ PartShared ps;
+    const int row = (int)blockIdx.x / a.parts, part = (int)blockIdx.x - row * a.parts, r = row0 + row, tid = threadIdx.x, lane = tid & 63, wave = wave_id();
+    if (a.skip && a.skip[r] < 0) return;
+    const Asked q = asked_of(a, r);
+    if (q.greedy) return;
+    const Source src = source_of(a, r, q);
+    PartRow<E> p;
+    p.load(src, part);
+    const RowRoom room = room_of(a, row, E);
+    const Top t = row_top(a, room);
+    if (!t.any || t.far) return;
+    const int top = t.cell;
+    fill_steps(ps.steps);
+    const Weigh weigh = {ref_of(top), magic_of(a.unit), ps.steps};
+    if (tid == 0) { ps.n_list = 0; ps.n_kept = 0; ps.rest = 0; ps.rest_mass = 0ull; ps.head = RowHead{}; ps.head.k_bin = ps.head.p_first = kPartBins; }
+    __syncthreads();
+    if (q.by_k || q.by_p) {
+        if (tid < a.parts) {
+            const PartHead h = room.head[tid];
+            const int d = h.zmax > -INFINITY ? top - h.top : kFar;
+            const double f = d == 0 ? 1.0 : exp_below(-(double)d * (double)(1.f / kCells), ps.steps);
+            ps.down[tid] = d;
+            ps.scale[tid] = f;
+            if (d < kFar) {
+                atomicAdd(&ps.rest, h.valid);
+                atomicAdd(&ps.rest_mass, d == 0 ? h.mass : (u64)((double)h.mass * f));
+            }
+        }
+        __syncthreads();
+        u64 m = 0ull;
+        unsigned c = 0u;
+        if (tid < kPartBins - 1)     // (the last bin: what is left)
+            for (int i = 0; i < a.parts; ++i) {
+                const int b = tid - ps.down[i];
+                if (b < 0) continue;
+                c += room.count[i * kPartBins + b];
+                const u64 x = room.mass[i * kPartBins + b];
+                m += b == tid ? x : (u64)((double)x * ps.scale[i]);
+            }
+        ps.mass[tid] = m;
+        ps.count[tid] = c;
+        const u64 wm = wave_sum_u64(m);
+        const int wc = wave_sum_i((int)c);
+        const u64 total = ps.rest_mass;
+        __syncthreads();
+        if (lane == 0) {
+            atomicAdd(&ps.rest, -wc);
+            atomicAdd(&ps.rest_mass, 0ull - wm);
+        }
+        __syncthreads();
+        if (tid == 0) {
+            ps.count[kPartBins - 1] = (unsigned)ps.rest;
+            ps.mass[kPartBins - 1] = (long long)ps.rest_mass > 0 ? ps.rest_mass : 0ull;
+        }
+        __syncthreads();
+        if (wave == 0) {
+            RowHead h = {};
+            u64 low = total, high = total;
+            if (q.by_k) {
+                const Cut cut = {1ull << 63, q.k};
+                const Picked p = pick_bin<kPartBins>(ps.count, ps.mass, cut, 0u, 0ull);
+                h.k_bin = p.bin;
+                h.k_m = p.m;
+                h.k_ahead = p.ahead;
+                low = h.k_before = p.before;
+                high = low + ps.mass[h.k_bin];
+            }
+            if (q.by_p) {            // (what scaling the parts' masses has rounded is far below 2^-30)
+                const u64 first = share_of(q.top_p, low), last = share_of(q.top_p, high);
+                const Cut c0 = {maxu64(first - (first >> 30), 1ull), q.k}, c1 = {last + (last >> 30) + 1ull, q.k};
+                const Picked p = pick_bin<kPartBins>(ps.count, ps.mass, c0, 0u, 0ull);
+                h.p_first = p.bin;
+                h.p_before = p.before;
+                h.p_last = pick_bin<kPartBins>(ps.count, ps.mass, c1, 0u, 0ull).bin;
+            }
+            h.total = total;
+            if (lane == 0) {
+                ps.head = h;
+                if (part == 0) *room.row = h;
+            }
+        }
+        __syncthreads();
+    }
+    const RowHead h = ps.head;
+    const int sure = q.by_p ? h.p_first : (q.by_k ? h.k_bin : kPartBins);    // bins before this one are kept, but for min-p
+    const u64 least = least_of(q, weigh(t.zmax));
+    int n_kept = 0;
+#pragma unroll
+    for (int g = 0; g < E / 4; ++g) {
+        u64 s = 0ull;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float z = p.z[4 * g + i];
+            if (!(z > -INFINITY)) continue;
+            const int b = min(top - cell_of(z), kPartBins - 1);
+            if (b < sure) {
+                const u64 w = weigh(z);
+                if (w >= least) {
+                    s += w;
+                    ++n_kept;
+                }
+            } else if ((q.by_k && b == h.k_bin) || (q.by_p && b <= h.p_last)) {
+                const int at = atomicAdd(&ps.n_list, 1);
+                if (at < kPartList) room.list[part * kPartList + at] = make_int2(__float_as_int(z), p.index(4 * g + i));
+            }
+        }
+        s = wave_sum_u64(s);
+        if (lane == 0) room.sums[(part * (E / 4) + g) * NW + wave] = s;
+    }
+    n_kept = wave_sum_i(n_kept);
+    if (lane == 0) atomicAdd(&ps.n_kept, n_kept);
+    __syncthreads();
+    if (tid == 0) {
+        room.head[part].n_list = ps.n_list;
+        room.head[part].n_kept = ps.n_kept;
+    }
+}
+
+struct ListShared {
+    float z[kList];
+    int at[kList], from[kMostParts + 1], kept;
+};
+
+template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(FilterArgs a, int row0) {
+    __shared__ CutShared sh;
+    __shared__ ListShared ls;
+    __shared__ u64 sums[kChunks];
+    const int row = blockIdx.x, r = row0 + row, tid = threadIdx.x, lane = tid & 63, wave = wave_id();
+    if (a.skip && a.skip[r] < 0) {
+        if (tid == 0) give(a, r, -1, 0.f, 0);
+        return;
+    }
+    const Asked q = asked_of(a, r);
+    const RowRoom room = room_of(a, row, E);
+    if (q.greedy) {
+        u64 best = max1(tid < a.parts ? room.head[tid].best : 0ull, sh.sum);
+        if (tid == 0) best == 0ull ? give(a, r, -1, 0.f, 0) : give(a, r, (int)(0xFFFFFFFFu - (unsigned)best), 1.f, 1);
+        return;
+    }
+    const Top t = row_top(a, room);
+    if (!t.any) {
+        if (tid == 0) give(a, r, -1, 0.f, 0);
+        return;
+    }
+    const int top = t.cell;
+    bool far = t.far;
+    const int listed = lane < a.parts && !far ? room.head[lane].n_list : 0, upto = wave_incl_scan_i(listed), n_list = __builtin_amdgcn_readlane(upto, 63);
+    far = far || n_list > kList || __ballot(listed > kPartList) != 0ull;
+    if (far) {
+        whole_row<0>(a, r, sh, sums);
+        return;
+    }
+    if (wave == 0 && lane < a.parts) ls.from[lane] = upto - listed;
+    if (tid == 0) { ls.kept = 0; sh.n = 0; sh.winner = 0ull; sh.within = 0ull; }
+    fill_steps(sh.steps);
+    for (int i = tid; i < kBinCount; i += NT) { sh.fine[i] = 0u; sh.fine_mass[i] = 0ull; }
+    const int chunks = a.parts * E * 4;
+    for (int i = tid; i < chunks; i += NT) sums[i] = room.sums[i];
+    __syncthreads();
+    for (int i = wave; i < a.parts; i += NW) {
+        const int n = room.head[i].n_list;
+        for (int k = lane; k < n; k += 64) {
+            const int2 e = room.list[i * kPartList + k];
+            ls.z[ls.from[i] + k] = __int_as_float(e.x);
+            ls.at[ls.from[i] + k] = e.y;
+        }
+        if (lane == 0) atomicAdd(&ls.kept, room.head[i].n_kept);
     }
     __syncthreads();
-    const int where = sh.b_bin;
-    u64 base = sh.b_mass;
-    row.each_group([&](int q, int j, const float (&v)[4]) {
-        if (fold == 1) {
-            if (q * NW + wave != where) return;                      // one wave's 256 entries of one group
-        } else if (q / fold * NW != where) return;                   // the groups of one sum
-        u64 w[4], s = 0;
-        double x[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[i] = 0.0;
-            w[i] = kept(v[i], j + i, x[i]) ? whole(x[i]) : 0;
-            s += w[i];
+    const Weigh weigh = {ref_of(top), magic_of(a.unit), sh.steps};
+    const u64 least = least_of(q, weigh(t.zmax));
+    Border border = {0u, 0x7FFFFFFF};
+    if (q.by_k || q.by_p) {
+        const RowHead h = *room.row;
+        auto bin = [&](float z) { return min(top - cell_of(z), kPartBins - 1); };
+        auto range_of = [&](int first, int last) {       // of the keys of bins first .. last
+            Range x = {};
+            x.hi = fkey((float)ref_of(top - first)) + 1u;
+            x.lo = last == kPartBins - 1 ? 0u : fkey((float)ref_of(top - last - 1)) - 1u;
+            x.last = 0x7FFFFFFF;
+            return x;
+        };
+        u64 mass = h.total;
+        if (q.by_k) {
+            const Cut cut = {1ull << 63, q.k};
+            Range x = range_of(h.k_bin, h.k_bin);
+            x.before = h.k_before; x.ahead = h.k_ahead; x.m = h.k_m;
+            const Found f = find_border([&](auto f) {
+                for (int i = tid; i < n_list; i += NT)
+                    if (bin(ls.z[i]) == h.k_bin) f(ls.at[i], ls.z[i]);
+            }, weigh, q.by_p, cut, x, sh);
+            border = f.border;
+            mass = f.mass;
+            __syncthreads();
         }
-        u64 at, sum = 0;
-        if (fold == 1) {
-            u64 y = s;
-            for (int d = 1; d < 64; d <<= 1) {
-                const u64 o = __shfl_up(y, d);
-                if (lane >= d) y += o;
-            }
-            at = base + y - s;
-        } else {
-            at = base + block_before(s, sh.sum, sum);
-            base += sum;
+        if (q.by_p) {
+            const Border most = border;
+            auto in = [&](int i) {
+                const int b = bin(ls.z[i]);
+                return b >= h.p_first && b <= h.p_last && inside(most, ls.z[i], ls.at[i]);
+            };
+            if (tid == 0) { sh.n = 0; sh.winner = 0ull; sh.within = 0ull; }
+            __syncthreads();
+            int m = 0;
+            for (int i = 0; i < n_list; i += NT) m += __syncthreads_count(i + tid < n_list && in(i + tid));
+            const Cut cut = {maxu64(share_of(q.top_p, mass), 1ull), 0xFFFFFFFFu};
+            Range x = range_of(h.p_first, h.p_last);
+            x.before = h.p_before; x.m = (unsigned)m;
+            border = find_border([&](auto f) {
+                for (int i = tid; i < n_list; i += NT)
+                    if (in(i)) f(ls.at[i], ls.z[i]);
+            }, weigh, true, cut, x, sh).border;
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (at <= target && target < at + w[i]) {
-                a.out_token[r] = j + i;
-                if (a.out_prob) a.out_prob[r] = (float)(x[i] * __hiloint2double((1023 + unit) << 20, 0) / (double)total);
-            }
-            at += w[i];
+        int n = 0;
+        for (int i = tid; i < n_list; i += NT) {
+            if (!inside(border, ls.z[i], ls.at[i])) continue;
+            const u64 w = weigh(ls.z[i]);
+            if (w < least) continue;
+            atomicAdd(&sums[ls.at[i] / kChunk], w);
+            ++n;
         }
-    });
-    if (tid == 0 && a.out_kept) a.out_kept[r] = all;
+        n = wave_sum_i(n);
+        if (lane == 0) atomicAdd(&ls.kept, n);
+        __syncthreads();
+    }
+    u64 base, target, total;
+    const int chunk = pick_chunk(a, r, sums, chunks, sh, base, target, total);
+    if (wave == 0) {
+        const Source src = source_of(a, r, q);
+        float v[4];
+        const int j = chunk * kChunk + 4 * lane;
+        src.four(j, v);
+        draw_of_chunk(a, r, j, v, [&](float x, int at) {
+            if (!(x > -INFINITY) || !inside(border, x, at)) return 0ull;
+            const u64 w = weigh(x);
+            return w >= least ? w : 0ull;
+        }, weigh, base, target, total);
+    }
+    if (tid == 0 && a.out_kept) a.out_kept[r] = ls.kept;
+}
+
+// Rows in parts, as many at a time as kPartsAtOnce parts (so that the workspace does not grow with the rows).
+constexpr int kPartsAtOnce = 2048;
+struct Cutting { int E, parts, rows; };          // entries of a thread (0: rows are not cut), parts of a row, rows at a time
+inline Cutting cutting_of(int rows, int n) {
+    Cutting c = {0, 1, rows};
+    if (n <= 16 * NT) return c;
+    c.E = n <= kMostParts * 8 * NT ? 8 : 32;
+    c.parts = (n + c.E * NT - 1) / (c.E * NT);
+    c.rows = std::min(rows, kPartsAtOnce / c.parts);
+    return c;
+}
+template <int E> void launch_parts(FilterArgs a, const Cutting& c, int rows, hipStream_t stream) {
+    for (int r = 0; r < rows; r += c.rows) {
+        const int n = std::min(c.rows, rows - r);
+        filter_bins_kernel<E><<<(unsigned)(n * c.parts), NT, 0, stream>>>(a, r);
+        filter_parts_kernel<E><<<(unsigned)(n * c.parts), NT, 0, stream>>>(a, r);
+        filter_draw_kernel<E><<<(unsigned)n, NT, 0, stream>>>(a, r);
+    }
 }
 
 int status() { return hipGetLastError() == hipSuccess ? HAWK_OK : HAWK_EDEVICE; }
@@ -450,18 +1025,22 @@ int status() { return hipGetLastError() == hipSuccess ? HAWK_OK : HAWK_EDEVICE; 
 }  // namespace
 
 size_t sample_filtered_workspace_bytes(int rows, int n) {
-    (void)rows; (void)n;
-    return 0;
+    if (rows < 1 || rows > (1 << 22) || n < 1 || n > (1 << 20)) return 0;
+    const Cutting c = cutting_of(rows, n);
+    return c.E ? c.rows * row_bytes(c.parts, c.E) : 0;
 }
 
 int launch_sample_filtered(const void* logits, int dtype, int64_t row_stride, const int32_t* skip, const float* u, const float* temperature,
                            const int32_t* top_k, const float* top_p, const float* min_p, int rows, int n, int32_t* out_token, float* out_prob,
                            int32_t* out_kept, void* workspace, size_t workspace_bytes, hipStream_t stream) {
-    (void)workspace; (void)workspace_bytes;
     if (!is_type(dtype) || rows < 0 || rows > (1 << 22) || n < 1 || n > (1 << 20) || row_stride < n) return HAWK_EINVAL;
     if (rows == 0) return HAWK_OK;
     if (!logits || !u || !out_token || (reinterpret_cast<uintptr_t>(logits) & (type_bytes(dtype) - 1))) return HAWK_EINVAL;
+    const Cutting c = cutting_of(rows, n);
+    if (c.E && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15))) return HAWK_EINVAL;
+    if (c.E && workspace_bytes < c.rows * row_bytes(c.parts, c.E)) return HAWK_ENOMEM;
     FilterArgs a = {};
+    a.parts = c.parts; a.room = static_cast<char*>(workspace);
     a.logits = static_cast<const char*>(logits); a.row_stride = row_stride; a.dtype = dtype; a.n = n;
     a.skip = skip; a.u = u; a.temperature = temperature; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p;
     a.out_token = out_token; a.out_prob = out_prob; a.out_kept = out_kept;
@@ -469,9 +1048,9 @@ int launch_sample_filtered(const void* logits, int dtype, int64_t row_stride, co
     while ((1 << log) < n) ++log;
     a.unit = std::min(51, 62 - log);
     if (n <= 4 * NT) sample_filtered_kernel<4><<<(unsigned)rows, NT, 0, stream>>>(a);
+    else if (n <= 8 * NT) sample_filtered_kernel<8><<<(unsigned)rows, NT, 0, stream>>>(a);
     else if (n <= 16 * NT) sample_filtered_kernel<16><<<(unsigned)rows, NT, 0, stream>>>(a);
-    else if (n <= 64 * NT) sample_filtered_kernel<64><<<(unsigned)rows, NT, 0, stream>>>(a);
-    else sample_filtered_kernel<0><<<(unsigned)rows, NT, 0, stream>>>(a);
+    else c.E == 8 ? launch_parts<8>(a, c, rows, stream) : launch_parts<32>(a, c, rows, stream);
     return status();
 }
 
