@@ -30,11 +30,13 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int kBinCount = 2048;
-constexpr float kPerUnit = 64.f;     // bins of a unit of z
+constexpr int kBinCount = 1024, kFine = 512;     // linear bins; those of a closer look
+constexpr float kPerUnit = 32.f;     // bins of a unit of z
+constexpr int kPartBins = 512;       // bins of a part of a long row
 constexpr int kFew = 256;            // entries that are ranked against each other
 constexpr int kChunk = 256;          // entries that a wave has of four a lane: sums of kept weights are held for each
 constexpr int kChunks = 4096;        // of 2^20 entries
+constexpr int kTop = 2 * NT;         // entries of a top-k that goes on as a list, two a thread
 
 struct FilterArgs {
     const char* logits;
@@ -49,11 +51,9 @@ struct FilterArgs {
     char* room;
 };
 
-struct Border { unsigned key; int at; };     // entries are inside if their key is larger, or equal and their index not above `at`
-__device__ __forceinline__ bool inside(const Border& b, float z, int j) {
-    const unsigned k = fkey(z);
-    return k > b.key || (k == b.key && j <= b.at);
-}
+struct Border { float z; int at; };  // entries are inside if z is larger, or equal and their index not above `at`
+__device__ __forceinline__ bool inside(const Border& b, float z, int j) { return z > b.z || (z == b.z && j <= b.at); }
+constexpr Border kNoBorder = {-3.4028235e38f, 0x7FFFFFFF};       // of all entries there are (minus infinity: none)
 // An entry is before a cut if fewer than K entries and a mass below M lie before it, in order.
 struct Cut { u64 M; unsigned K; };
 // Where the border lies: entries and mass before, m entries with keys lo..hi, of equal keys with indices first..last.
@@ -62,11 +62,11 @@ struct Found { Border border; u64 mass; };   // mass: of all entries up to the b
 
 struct Picked { int bin; unsigned m, ahead; u64 before; };   // a bin: its entries; entries and mass before it
 struct CutShared {
-    u64 mass[kBinCount], fine_mass[kBinCount];
-    unsigned count[kBinCount], fine[kBinCount];      // fine: zero between uses
-    u64 w[kFew], winner, within, base;
+    u64 mass[kBinCount], fine_mass[kFine];
+    unsigned count[kBinCount], fine[kFine];          // fine: zero between uses
+    u64 w[kFew], base;
     unsigned key[kFew];
-    int at[kFew], n, chunk;
+    int at[kFew], order[kFew], n, chunk;
     Picked picked;
     double steps[kSteps];
     u64 sum[NW];
@@ -102,7 +102,9 @@ struct Weigh {
     double ref, magic;
     const double* steps;
     __device__ __forceinline__ double real(float z) const { return exp_below((double)z - ref, steps); }
-    __device__ __forceinline__ u64 operator()(float z) const { return (u64)__double_as_longlong(real(z) + magic) & 0xFFFFFFFFFFFFFull; }
+    __device__ __forceinline__ u64 operator()(float z) const {   // (below -690 it is 0 whatever the weight)
+        return (u64)__double_as_longlong(exp_near(fmax((double)z - ref, -690.0), steps) + magic) & 0xFFFFFFFFFFFFFull;
+    }
 };
 __device__ __forceinline__ double magic_of(int unit) { return __hiloint2double((1075 - unit) << 20, 0); }
 
@@ -220,15 +222,13 @@ template <int NB> __device__ __forceinline__ Picked pick_bin(const unsigned* cou
     const Picked out = {L * PER + at, (unsigned)__builtin_amdgcn_readlane(c1, at), (unsigned)__builtin_amdgcn_readlane((int)a1, at), lane_u64(b1, at)};
     return out;
 }
-// The same for a workgroup: the first wave looks, all threads have the result and find the words of a ranking cleared.  Ends with a barrier.
-__device__ __forceinline__ Picked pick_for_all(const unsigned* count, const u64* mass, const Cut& cut, unsigned ahead, u64 before, CutShared& sh) {
+// The same for a workgroup: the first wave looks, all threads have the result, and sh.n is zero.  Ends with a barrier.
+template <int NB> __device__ __forceinline__ Picked pick_for_all(const unsigned* count, const u64* mass, const Cut& cut, unsigned ahead, u64 before, CutShared& sh) {
     if (wave_id() == 0) {
-        const Picked p = pick_bin<kBinCount>(count, mass, cut, ahead, before);
+        const Picked p = pick_bin<NB>(count, mass, cut, ahead, before);
         if ((threadIdx.x & 63) == 0) {
             sh.picked = p;
             sh.n = 0;
-            sh.winner = 0ull;
-            sh.within = 0ull;
         }
     }
     __syncthreads();
@@ -236,14 +236,14 @@ __device__ __forceinline__ Picked pick_for_all(const unsigned* count, const u64*
 }
 
 // The border of a cut within a range.  each(f): f(index, z) of this thread's entries that may be in it.  masses: weights count.  All threads
-// call; sh.n, winner, within are zero; ends with a barrier.
+// call, sh.n is zero; what it leaves in sh is read until the next barrier.
 template <class Each>
 __device__ __forceinline__ Found find_border(const Each& each, const Weigh& weigh, bool masses, const Cut& cut, Range r, CutShared& sh) {
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
     while (r.m > (unsigned)kFew) {
         const bool by_key = r.lo < r.hi;
         const unsigned span = by_key ? r.hi - r.lo : (unsigned)(r.last - r.first);
-        const int s = max(0, 32 - __clz((int)span) - 11);
+        const int s = max(0, 32 - __clz((int)span) - 9);     // (nine bits: kFine bins)
         each([&](int j, float z) {
             const unsigned k = fkey(z);
             if (k < r.lo || k > r.hi || (!by_key && (j < r.first || j > r.last))) return;
@@ -252,7 +252,7 @@ __device__ __forceinline__ Found find_border(const Each& each, const Weigh& weig
             if (masses) atomicAdd(&sh.fine_mass[d], weigh(z));
         });
         __syncthreads();
-        const Picked p = pick_for_all(sh.fine, sh.fine_mass, cut, r.ahead, r.before, sh);
+        const Picked p = pick_for_all<kFine>(sh.fine, sh.fine_mass, cut, r.ahead, r.before, sh);
         const unsigned d = (unsigned)p.bin, up = ((d + 1u) << s) - 1u;
         r.m = p.m;
         r.ahead = p.ahead;
@@ -266,7 +266,7 @@ __device__ __forceinline__ Found find_border(const Each& each, const Weigh& weig
             r.first = first + (int)(d << s);
             r.last = (int)min((unsigned)r.last, (unsigned)first + up);
         }
-        for (int i = tid; i < kBinCount; i += NT) { sh.fine[i] = 0u; sh.fine_mass[i] = 0ull; }
+        if (tid < kFine) { sh.fine[tid] = 0u; sh.fine_mass[tid] = 0ull; }
         __syncthreads();
     }
     each([&](int j, float z) {
@@ -279,44 +279,58 @@ __device__ __forceinline__ Found find_border(const Each& each, const Weigh& weig
         sh.w[i] = masses ? weigh(z) : 0ull;
     });
     __syncthreads();
-    // a wave has every sixteenth entry, its lanes compare it with all others
-    const int m = (int)r.m;
+    // A wave ranks every sixteenth entry, its lanes compare it with all others.
+    const int m = min((int)r.m, kFew);
     unsigned k[kFew / 64];
     int at[kFew / 64];
-    u64 w[kFew / 64];
 #pragma unroll
     for (int c = 0; c < kFew / 64; ++c) {
         const int i = c * 64 + lane;
         k[c] = i < m ? sh.key[i] : 0u;
         at[c] = i < m ? sh.at[i] : 0x7FFFFFFF;
-        w[c] = i < m ? sh.w[i] : 0ull;
     }
-    u64 best = 0ull, within = 0ull;
-    for (int i = wave; i < m; i += NW) {
-        const unsigned mk = sh.key[i];
-        const int ma = sh.at[i];
-        int rank = 0;
-        u64 sum = 0ull;
 #pragma unroll
-        for (int c = 0; c < kFew / 64; ++c) {
-            if (c * 64 >= m) break;
-            const bool ahead = k[c] > mk || (k[c] == mk && at[c] < ma);
-            rank += __popcll(__ballot(ahead));
-            sum += ahead ? w[c] : 0ull;
+    for (int c = 0; c < kFew / 64; ++c)
+#pragma unroll
+        for (int t = 0; t < 64 / NW; ++t) {
+            const int i = c * 64 + t * NW + wave;
+            if (i >= m) break;
+            const unsigned mk = (unsigned)__builtin_amdgcn_readlane((int)k[c], t * NW + wave);
+            const int ma = __builtin_amdgcn_readlane(at[c], t * NW + wave);
+            int rank = 0;
+#pragma unroll
+            for (int x = 0; x < kFew / 64; ++x) {
+                if (x * 64 >= m) break;
+                rank += __popcll(__ballot(k[x] > mk || (k[x] == mk && at[x] < ma)));
+            }
+            if (lane == 0) sh.order[rank] = i;
         }
-        if (masses) sum = wave_sum_u64(sum);
-        if (r.before + sum < cut.M && r.ahead + (unsigned)rank < cut.K) {
-            best = maxu64(best, ((u64)(unsigned)(rank + 1) << 32) | (unsigned)i);
-            within += sh.w[i];
-        }
-    }
-    if (lane == 0 && best) {
-        atomicMax(&sh.winner, best);
-        atomicAdd(&sh.within, within);
-    }
     __syncthreads();
-    const int i = (int)(unsigned)sh.winner;
-    const Found out = {{sh.key[i], sh.at[i]}, r.before + sh.within};
+    // Then in order: every wave finds the last entry before the cut, a lane has four neighbours.
+    u64 w[4], own = 0ull;
+    int n_in = 0;
+    if (masses) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            w[c] = 4 * lane + c < m ? sh.w[sh.order[4 * lane + c]] : 0ull;
+            own += w[c];
+        }
+        u64 sum = r.before + wave_incl_scan_u64(own) - own;
+        own = 0ull;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const int x = 4 * lane + c;
+            const bool in = x < m && sum < cut.M && r.ahead + (unsigned)x < cut.K;
+            sum += w[c];
+            own += in ? w[c] : 0ull;
+            n_in += __popcll(__ballot(in));
+        }
+        own = wave_sum_u64(own);
+    } else {
+        n_in = (int)min((unsigned)m, cut.K - r.ahead);
+    }
+    const int i = sh.order[max(n_in, 1) - 1];
+    const Found out = {{key_to_float(sh.key[i]), sh.at[i]}, r.before + own};
     return out;
 }
 
@@ -395,8 +409,111 @@ __device__ __forceinline__ int pick_chunk(const FilterArgs& a, int r, const u64*
     return sh.chunk;
 }
 
+// The entries inside a top-k's border, in index order: with a thousand of sixteen thousand left, exponentials and sums are one or two a thread
+// instead of sixteen.
+struct TopList {
+    float z[kTop];
+    int at[kTop], total[64];
+};
+// z: the row's entries as whole_row has them.  All threads call; returns how many there are.  Ends with a barrier.
+template <int E> __device__ __forceinline__ int make_list(const float (&z)[E], const Border& border, TopList& list) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
+    u64 own = 0ull;                  // counts of the groups, 16 bits each
+#pragma unroll
+    for (int e = 0; e < E; ++e) own += inside(border, z[e], entry<E>(e, tid)) ? 1ull << 16 * (e / 4) : 0ull;
+    const u64 upto = wave_incl_scan_u64(own);
+    if (lane == 63)
+#pragma unroll
+        for (int g = 0; g < E / 4; ++g) list.total[g * NW + wave] = (int)(upto >> 16 * g & 0xFFFFull);
+    __syncthreads();
+    const int t = lane < E / 4 * NW ? list.total[lane] : 0, sum = wave_incl_scan_i(t), n = __builtin_amdgcn_readlane(sum, 63);
+#pragma unroll
+    for (int g = 0; g < E / 4; ++g) {
+        int at = __builtin_amdgcn_readlane(sum - t, g * NW + wave) + (int)((upto - own) >> 16 * g & 0xFFFFull);
+#pragma unroll
+        for (int e = 4 * g; e < 4 * g + 4; ++e)
+            if (inside(border, z[e], entry<E>(e, tid))) {
+                list.z[at & (kTop - 1)] = z[e];
+                list.at[at & (kTop - 1)] = entry<E>(e, tid);
+                ++at;
+            }
+    }
+    __syncthreads();
+    return n;
+}
+
+// The draw from n entries of a list, two neighbours a thread.  sh.count and sh.mass: the counts of all entries, and zeros.
+__device__ __forceinline__ void draw_of_list(const FilterArgs& a, int r, const Asked& q, float zmax, const Weigh& weigh, int n, const TopList& list, CutShared& sh) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
+    float z[2];
+    int at[2];
+    u64 w[2];
+    sh.count[tid] = 0u;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const bool there = 2 * tid + i < n;
+        z[i] = there ? list.z[2 * tid + i] : -INFINITY;
+        at[i] = there ? list.at[2 * tid + i] : 0;
+        w[i] = there ? weigh(z[i]) : 0ull;
+    }
+    Border border = kNoBorder;
+    if (q.by_p) {
+        u64 mass = wave_sum_u64(w[0] + w[1]);
+        if (lane == 0) sh.sum[wave] = mass;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (z[i] > -INFINITY) {
+                const int b = bin_of(zmax, z[i]);
+                atomicAdd(&sh.count[b], 1u);
+                atomicAdd(&sh.mass[b], w[i]);
+            }
+        mass = 0ull;
+#pragma unroll
+        for (int v = 0; v < NW; ++v) mass += sh.sum[v];
+        __syncthreads();
+        const Cut cut = {maxu64(share_of(q.top_p, mass), 1ull), 0xFFFFFFFFu};
+        const Picked p = pick_for_all<kBinCount>(sh.count, sh.mass, cut, 0u, 0ull, sh);
+        border = find_border([&](auto f) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (z[i] > -INFINITY && bin_of(zmax, z[i]) == p.bin) f(at[i], z[i]);
+        }, weigh, true, cut, bin_range(zmax, p), sh).border;
+    }
+    const u64 least = least_of(q, weigh(zmax));
+    int n_kept = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const bool kept = inside(border, z[i], at[i]) && w[i] >= least;
+        w[i] = kept ? w[i] : 0ull;
+        n_kept += __popcll(__ballot(kept));
+    }
+    const u64 upto = wave_incl_scan_u64(w[0] + w[1]);
+    if (lane == 63) {
+        sh.sum[wave] = upto;
+        sh.isum[wave] = n_kept;
+    }
+    __syncthreads();
+    u64 before = 0ull, total = 0ull;
+    int all = 0;
+#pragma unroll
+    for (int v = 0; v < NW; ++v) {
+        before += v < wave ? sh.sum[v] : 0ull;
+        total += sh.sum[v];
+        all += sh.isum[v];
+    }
+    before += upto - w[0] - w[1];
+    const u64 target = target_of(a, r, total);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (before <= target && target < before + w[i])
+            give(a, r, at[i], (float)(weigh.real(z[i]) * __hiloint2double((1023 + a.unit) << 20, 0) / (double)total), all);
+        before += w[i];
+    }
+}
+
 // One workgroup, one row.  E entries a thread in registers: group q of four starts at q * 4096 + 4 * thread; E = 0: read again for every look.
-template <int E> __device__ __forceinline__ void whole_row(const FilterArgs& a, int r, CutShared& sh, u64* sums) {
+template <int E> __device__ __forceinline__ void whole_row(const FilterArgs& a, int r, CutShared& sh, u64* sums, TopList& list) {
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
     const Asked q = asked_of(a, r);
     Source src = source_of(a, r, q);
@@ -437,7 +554,10 @@ template <int E> __device__ __forceinline__ void whole_row(const FilterArgs& a, 
     __syncthreads();
     load();
     fill_steps(sh.steps);
-    for (int i = tid; i < kBinCount; i += NT) { sh.count[i] = 0u; sh.mass[i] = 0ull; sh.fine[i] = 0u; sh.fine_mass[i] = 0ull; }
+    static_assert(kBinCount == NT && kPartBins <= NT && kFine <= NT, "a thread has a bin");
+    sh.count[tid] = 0u;
+    sh.mass[tid] = 0ull;
+    if (tid < kFine) { sh.fine[tid] = 0u; sh.fine_mass[tid] = 0ull; }
 
     if (q.greedy) {                  // the largest entry, lowest index first
         u64 best = 0ull;
@@ -464,8 +584,22 @@ template <int E> __device__ __forceinline__ void whole_row(const FilterArgs& a, 
         load();
     }
     const Weigh weigh = {(double)zmax, magic_of(a.unit), sh.steps};
-
-    Border border = {0u, 0x7FFFFFFF};
+    if constexpr (E > 0) {
+        if (q.by_k && q.k <= (unsigned)kTop) {
+            each([&](int, float v) { atomicAdd(&sh.count[bin_of(zmax, v)], 1u); });
+            __syncthreads();
+            const Cut cut = {1ull << 63, q.k};
+            const Picked p = pick_for_all<kBinCount>(sh.count, sh.mass, cut, 0u, 0ull, sh);
+            const Border border = find_border([&](auto f) {
+                each([&](int j, float v) {
+                    if (bin_of(zmax, v) == p.bin) f(j, v);
+                });
+            }, weigh, false, cut, bin_range(zmax, p), sh).border;
+            draw_of_list(a, r, q, zmax, weigh, make_list<E>(z, border, list), list, sh);
+            return;
+        }
+    }
+    Border border = kNoBorder;
     if (q.by_k || q.by_p) {
         if constexpr (E > 0) {
 #pragma unroll
@@ -488,7 +622,7 @@ template <int E> __device__ __forceinline__ void whole_row(const FilterArgs& a, 
         __syncthreads();
         u64 mass = 0ull;
         auto cut_at = [&](const Cut& cut) {
-            const Picked p = pick_for_all(sh.count, sh.mass, cut, 0u, 0ull, sh);
+            const Picked p = pick_for_all<kBinCount>(sh.count, sh.mass, cut, 0u, 0ull, sh);
             const int b = p.bin;
             const Range range = bin_range(zmax, p);
             auto in_bin = [&](auto f) {
@@ -504,8 +638,7 @@ template <int E> __device__ __forceinline__ void whole_row(const FilterArgs& a, 
             const Cut cut = {1ull << 63, q.k};
             cut_at(cut);
         } else {
-            u64 own = sh.mass[tid] + sh.mass[tid + NT];
-            own = wave_sum_u64(own);
+            const u64 own = wave_sum_u64(sh.mass[tid]);
             if (lane == 0) sh.sum[wave] = own;
             __syncthreads();
 #pragma unroll
@@ -520,7 +653,7 @@ template <int E> __device__ __forceinline__ void whole_row(const FilterArgs& a, 
 
     const u64 least = least_of(q, weigh(zmax));
     int n_kept = 0;
-    auto kept = [&](float v, int j, u64 w) { return v > -INFINITY && inside(border, v, j) && w >= least; };
+    auto kept = [&](float v, int j, u64 w) { return inside(border, v, j) && w >= least; };
     auto add_group = [&](int g, u64 s) {
         s = wave_sum_u64(s);
         if (lane == 0) sums[g * NW + wave] = s;
@@ -530,7 +663,7 @@ template <int E> __device__ __forceinline__ void whole_row(const FilterArgs& a, 
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);
-                weights[e] = z[e] > -INFINITY && inside(border, z[e], entry<E>(e, tid)) ? weigh(z[e]) : 0ull;
+                weights[e] = inside(border, z[e], entry<E>(e, tid)) ? weigh(z[e]) : 0ull;
             }
         }
 #pragma unroll
@@ -554,7 +687,7 @@ template <int E> __device__ __forceinline__ void whole_row(const FilterArgs& a, 
             src.four(j, v);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (!(v[i] > -INFINITY) || !inside(border, v[i], j + i)) continue;
+                if (!inside(border, v[i], j + i)) continue;
                 const u64 w = weigh(v[i]);
                 if (w < least) continue;
                 s += w;
@@ -588,7 +721,7 @@ template <int E> __device__ __forceinline__ void whole_row(const FilterArgs& a, 
             const int j = chunk * kChunk + 4 * lane;
             src.four(j, v);
             draw_of_chunk(a, r, j, v, [&](float x, int at) {
-                if (!(x > -INFINITY) || !inside(border, x, at)) return 0ull;
+                if (!inside(border, x, at)) return 0ull;
                 const u64 w = weigh(x);
                 return w >= least ? w : 0ull;
             }, weigh, base, target, total);
@@ -604,20 +737,21 @@ template <int E> __device__ __forceinline__ void whole_row(const FilterArgs& a, 
 
 template <int E> __global__ __launch_bounds__(NT) void sample_filtered_kernel(FilterArgs a) {
     __shared__ CutShared sh;
-    __shared__ u64 sums[E > 0 ? 64 : kChunks];
+    __shared__ u64 sums[64];
+    __shared__ TopList list;
     const int r = blockIdx.x;
     if (a.skip && a.skip[r] < 0) {
         if (threadIdx.x == 0) give(a, r, -1, 0.f, 0);
         return;
     }
-    whole_row<E>(a, r, sh, sums);
+    whole_row<E>(a, r, sh, sums, list);
 }
 
-// ---- Long rows in parts of E * 1024 entries.  Their bins are cells of a fixed grid of z, 1024 of them from the cell of the largest entry down (of a
+// ---- Long rows in parts of E * 1024 entries.  Their bins are cells of a fixed grid of z, 512 of them from the cell of the largest entry down (of a
 // part, so that a part needs to know nothing of the others; the last one holds what lies behind), and weights are relative to the
 // upper end of the largest's cell: parts are brought together by moving bins and scaling masses.
-constexpr int kPartBins = 1024, kPartList = 512, kMostParts = 32, kList = 4096;
-constexpr float kCells = 32.f;       // cells of a unit of z
+constexpr int kPartList = 512, kMostParts = 32, kList = 4096;
+constexpr float kCells = 16.f;       // cells of a unit of z
 constexpr int kFar = 1 << 29;        // cells from here on are not told apart
 __device__ __forceinline__ int cell_of(float z) { return (int)fminf(fmaxf(floorf(z * kCells), -1073741824.f), 1073741824.f); }
 __device__ __forceinline__ double ref_of(int top) { return (top + 1) * (double)(1.f / kCells); }
@@ -689,8 +823,10 @@ template <int E> __global__ __launch_bounds__(NT) void filter_bins_kernel(Filter
         if (tid == 0) room.head[part].best = best;
         return;
     }
-    mass[tid] = 0ull;
-    count[tid] = 0u;
+    if (tid < kPartBins) {
+        mass[tid] = 0ull;
+        count[tid] = 0u;
+    }
     fill_steps(steps);
     float zmax = -INFINITY;
 #pragma unroll
@@ -713,10 +849,12 @@ template <int E> __global__ __launch_bounds__(NT) void filter_bins_kernel(Filter
                 if (q.by_p) atomicAdd(&mass[b], weigh(p.z[e]));
             }
         __syncthreads();
-        const u64 m = mass[tid];
-        const int c = (int)count[tid];
-        room.mass[part * kPartBins + tid] = m;
-        room.count[part * kPartBins + tid] = (unsigned)c;
+        const u64 m = tid < kPartBins ? mass[tid] : 0ull;
+        const int c = tid < kPartBins ? (int)count[tid] : 0;
+        if (tid < kPartBins) {
+            if (q.by_p) room.mass[part * kPartBins + tid] = m;
+            room.count[part * kPartBins + tid] = (unsigned)c;
+        }
         const u64 wm = wave_sum_u64(m);
         const int wc = wave_sum_i(c);
         if (lane == 0) { slot[wave] = wm; top[wave] = __int_as_float(wc); }
@@ -790,16 +928,33 @@ template <int E> __global__ __launch_bounds__(NT) void filter_parts_kernel(Filte
         __syncthreads();
         u64 m = 0ull;
         unsigned c = 0u;
-        if (tid < kPartBins - 1)     // (the last bin: what is left)
-            for (int i = 0; i < a.parts; ++i) {
-                const int b = tid - ps.down[i];
-                if (b < 0) continue;
-                c += room.count[i * kPartBins + b];
-                const u64 x = room.mass[i * kPartBins + b];
-                m += b == tid ? x : (u64)((double)x * ps.scale[i]);
+        // eight parts' bins are requested at a time (the last bin is what is left)
+        for (int i0 = 0; i0 < a.parts; i0 += 8) {
+            unsigned cs[8];
+            u64 ms[8];
+            int bs[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int part_i = min(i0 + i, a.parts - 1), at = part_i * kPartBins;
+                bs[i] = i0 + i < a.parts && tid < kPartBins - 1 ? tid - ps.down[part_i] : -1;
+                cs[i] = 0u;
+                ms[i] = 0ull;
+                if (tid < kPartBins) {
+                    cs[i] = room.count[at + max(bs[i], 0)];
+                    if (q.by_p) ms[i] = room.mass[at + max(bs[i], 0)];
+                }
             }
-        ps.mass[tid] = m;
-        ps.count[tid] = c;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (bs[i] < 0) continue;
+                c += cs[i];
+                m += bs[i] == tid ? ms[i] : (u64)((double)ms[i] * ps.scale[i0 + i]);
+            }
+        }
+        if (tid < kPartBins) {
+            ps.mass[tid] = m;
+            ps.count[tid] = c;
+        }
         const u64 wm = wave_sum_u64(m);
         const int wc = wave_sum_i((int)c);
         const u64 total = ps.rest_mass;
@@ -879,13 +1034,14 @@ template <int E> __global__ __launch_bounds__(NT) void filter_parts_kernel(Filte
 
 struct ListShared {
     float z[kList];
-    int at[kList], from[kMostParts + 1], kept;
+    int at[kList], kept;
 };
 
 template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(FilterArgs a, int row0) {
     __shared__ CutShared sh;
-    __shared__ ListShared ls;
+    __shared__ union { ListShared list; TopList top; } both;     // (a row that is read again needs no list)
     __shared__ u64 sums[kChunks];
+    ListShared& ls = both.list;
     const int row = blockIdx.x, r = row0 + row, tid = threadIdx.x, lane = tid & 63, wave = wave_id();
     if (a.skip && a.skip[r] < 0) {
         if (tid == 0) give(a, r, -1, 0.f, 0);
@@ -905,32 +1061,30 @@ template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(Filter
     }
     const int top = t.cell;
     bool far = t.far;
-    const int listed = lane < a.parts && !far ? room.head[lane].n_list : 0, upto = wave_incl_scan_i(listed), n_list = __builtin_amdgcn_readlane(upto, 63);
+    const int listed = lane < a.parts && !far ? room.head[lane].n_list : 0, sure = lane < a.parts && !far ? room.head[lane].n_kept : 0, upto = wave_incl_scan_i(listed), n_list = __builtin_amdgcn_readlane(upto, 63);
     far = far || n_list > kList || __ballot(listed > kPartList) != 0ull;
     if (far) {
-        whole_row<0>(a, r, sh, sums);
+        whole_row<0>(a, r, sh, sums, both.top);
         return;
     }
-    if (wave == 0 && lane < a.parts) ls.from[lane] = upto - listed;
-    if (tid == 0) { ls.kept = 0; sh.n = 0; sh.winner = 0ull; sh.within = 0ull; }
+    const int n_sure = wave_sum_i(sure);
+    if (tid == 0) { ls.kept = n_sure; sh.n = 0; }
     fill_steps(sh.steps);
-    for (int i = tid; i < kBinCount; i += NT) { sh.fine[i] = 0u; sh.fine_mass[i] = 0ull; }
+    if (tid < kFine) { sh.fine[tid] = 0u; sh.fine_mass[tid] = 0ull; }
     const int chunks = a.parts * E * 4;
     for (int i = tid; i < chunks; i += NT) sums[i] = room.sums[i];
-    __syncthreads();
     for (int i = wave; i < a.parts; i += NW) {
-        const int n = room.head[i].n_list;
+        const int n = __builtin_amdgcn_readlane(listed, i), from = __builtin_amdgcn_readlane(upto, i) - n;
         for (int k = lane; k < n; k += 64) {
             const int2 e = room.list[i * kPartList + k];
-            ls.z[ls.from[i] + k] = __int_as_float(e.x);
-            ls.at[ls.from[i] + k] = e.y;
+            ls.z[from + k] = __int_as_float(e.x);
+            ls.at[from + k] = e.y;
         }
-        if (lane == 0) atomicAdd(&ls.kept, room.head[i].n_kept);
     }
     __syncthreads();
     const Weigh weigh = {ref_of(top), magic_of(a.unit), sh.steps};
     const u64 least = least_of(q, weigh(t.zmax));
-    Border border = {0u, 0x7FFFFFFF};
+    Border border = kNoBorder;
     if (q.by_k || q.by_p) {
         const RowHead h = *room.row;
         auto bin = [&](float z) { return min(top - cell_of(z), kPartBins - 1); };
@@ -960,7 +1114,7 @@ template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(Filter
                 const int b = bin(ls.z[i]);
                 return b >= h.p_first && b <= h.p_last && inside(most, ls.z[i], ls.at[i]);
             };
-            if (tid == 0) { sh.n = 0; sh.winner = 0ull; sh.within = 0ull; }
+            if (tid == 0) sh.n = 0;
             __syncthreads();
             int m = 0;
             for (int i = 0; i < n_list; i += NT) m += __syncthreads_count(i + tid < n_list && in(i + tid));
@@ -992,7 +1146,7 @@ template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(Filter
         const int j = chunk * kChunk + 4 * lane;
         src.four(j, v);
         draw_of_chunk(a, r, j, v, [&](float x, int at) {
-            if (!(x > -INFINITY) || !inside(border, x, at)) return 0ull;
+            if (!inside(border, x, at)) return 0ull;
             const u64 w = weigh(x);
             return w >= least ? w : 0ull;
         }, weigh, base, target, total);

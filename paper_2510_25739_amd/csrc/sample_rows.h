@@ -53,14 +53,17 @@ constexpr int kSteps = 64;
 __device__ __forceinline__ void fill_steps(double* steps) {   // ends without a barrier
     if (threadIdx.x < kSteps) steps[threadIdx.x] = exp2((double)threadIdx.x / kSteps);
 }
-__device__ __forceinline__ double exp_below(double x, const double* steps) {
+__device__ __forceinline__ double exp_near(double x, const double* steps) {   // -700 <= x <= 0
     const double shifted = fma(x, 0x1.71547652b82fep+6, 0x1.8p52), n = shifted - 0x1.8p52;
     const double r = fma(n, -0x1.abc9e3b39803fp-62, fma(n, -0x1.62e42fefa39efp-7, x));
     const double p = r * fma(r, fma(r, fma(r, fma(r, 1.0 / 120, 1.0 / 24), 1.0 / 6), 0.5), 1.0);
     const int i = __double2loint(shifted);
     const double t = steps[i & (kSteps - 1)], v = fma(t, p, t);
-    const bool some = x >= -700.0;
-    return __hiloint2double(some ? __double2hiint(v) + (int)((unsigned)(i & -kSteps) << 14) : 0, some ? __double2loint(v) : 0);
+    return __hiloint2double(__double2hiint(v) + (int)((unsigned)(i & -kSteps) << 14), __double2loint(v));
+}
+__device__ __forceinline__ double exp_below(double x, const double* steps) {
+    const double v = exp_near(x, steps);
+    return x >= -700.0 ? v : 0.0;
 }
 
 // Order-preserving key of a float (larger value <=> larger key); -0 and +0 share a key.
