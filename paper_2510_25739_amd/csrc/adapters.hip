@@ -102,7 +102,7 @@ struct ApplyArgs {
     char* out;
     const float* scale;
     int64_t a_adapter, a_row, b_adapter, b_row, x_row, base_row, out_row;   // elements
-    int n_adapters, rank, d_in, d_out, rows, tiles, out_type;
+    int n_adapters, rank, d_in, d_out, rows, tiles;
     Divisor parts;                   // workgroups of a tile
 };
 
@@ -147,79 +147,193 @@ template <int TYPE> __device__ __forceinline__ unsigned short cut(float& x) {
     return u;
 }
 
-// NR: groups of 16 of the rank.  P: parts of h.  NW waves.
-template <int TYPE, int NR, int P, int NW>
-__global__ __launch_bounds__(64 * NW, NR <= 4 ? 4 : 2) void adapter_apply_kernel(ApplyArgs a) {
+// 16 bytes of a type as they lie in memory: requested in one place, used in another.
+template <int TYPE> struct Piece {
+    static constexpr int kN = 16 / Of<TYPE>::kBytes;
+    v4u w;
+    __device__ __forceinline__ void load(const char* base, int64_t at) { w = *reinterpret_cast<const v4u*>(base + at * Of<TYPE>::kBytes); }
+    __device__ __forceinline__ void store(char* base, int64_t at) const { *reinterpret_cast<v4u*>(base + at * Of<TYPE>::kBytes) = w; }
+    __device__ __forceinline__ void widen(float (&x)[kN]) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (TYPE == HAWK_FP32) x[i] = __uint_as_float(w[i]);
+            else widen2(w[i], TYPE, x[2 * i], x[2 * i + 1]);
+        }
+    }
+    __device__ __forceinline__ void narrow(const float (&x)[kN]) {   // to nearest, ties to even
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (TYPE == HAWK_FP32) w[i] = __float_as_uint(x[i]);
+            else w[i] = narrow2(x[2 * i], x[2 * i + 1], TYPE);
+        }
+    }
+};
+// Between a wave's writes to shared memory and its other lanes' reads of them: the hardware keeps their order, the compiler has to as well.
+__device__ __forceinline__ void wave_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// TYPE: of x and the weights; OUT: of base and out.  NR: groups of 16 of the rank.  NW waves.
+// x, A, base and out pass between memory and registers as rows' whole 128 bytes, eight rows (four of 256) an instruction, and change places
+// with the matrix units' layout - a lane has 16 bytes of one of 16 rows - in shared memory of the wave's own: read in that layout, with 64
+// bytes of 16 rows an instruction, memory gave 3.3 instead of 4.4 TB/s, and x, base and out together, 4400 rows of 4096, took 35 instead of
+// 28 us.
+template <int TYPE, int OUT, int NR, int NW>
+__global__ __launch_bounds__(64 * NW, NR <= 2 ? 4 : 2) void adapter_apply_kernel(ApplyArgs a) {
     using T = Of<TYPE>;
-    constexpr int ES = T::kBytes, VEC = 16 / ES, STEP = 4 * VEC;               // features of a lane's piece, of a product
+    constexpr int ES = T::kBytes, VEC = 16 / ES;                               // values of a piece
     constexpr int RP = 16 * NR, LD = RP + 4;                                   // the rank, rounded up
+    constexpr int P = TYPE == HAWK_FP32 ? 1 : (TYPE == HAWK_BF16 && OUT == HAWK_FP32 ? 3 : 2);   // parts of h
     constexpr bool PAIR = TYPE != HAWK_FP32 && NR == 1;                        // two parts of h share a product's 32 features
     constexpr int KS = TYPE == HAWK_FP32 ? NR : (NR + 1) / 2;                  // products over the rank
     constexpr int PP = PAIR ? (P + 1) / 2 : P;
-    __shared__ float parts[NW][NR][kTile][16];                                 // [wave][..][row][..]
+    constexpr int D1 = NR == 1 ? 4 : (NR == 2 ? 2 : 1);                        // stages of x and A that are requested ahead
+    constexpr int D2 = KS == 1 && OUT != HAWK_FP32 ? 2 : 1;                   // columns that are
+    constexpr int LR = OUT == HAWK_FP32 ? 16 : 8, NI = LR / 4;                 // lanes of a row of 64 columns, instructions of 16 rows
+    constexpr int kStage = 16 * (1 + NR) * 128, kSum = NR * 1024, kDelta = 16 * 68 * 4;
+    constexpr int kOwn = kStage > kSum ? (kStage > kDelta ? kStage : kDelta) : (kSum > kDelta ? kSum : kDelta);
+    __shared__ __align__(16) char own[NW][kOwn];                               // of a wave: a stage, its part of h, a block of B h
     __shared__ float h[kTile][LD];
     __shared__ float factor[kTile];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), m16 = lane & 15, g = lane >> 4;
-    const int part = (int)blockIdx.x / a.tiles, tile = (int)blockIdx.x - part * a.tiles;
-    if (tile >= a.plan[0]) return;
+    // the parts of a tile on one XCD (workgroups go round the eight of them), so that its rows and its adapter come from that one's L2
+    const int turn = (int)blockIdx.x >> 3, eight = turn / a.parts, part = turn - eight * a.parts.d, tile = eight * 8 + ((int)blockIdx.x & 7);
+    if (tile >= min(a.plan[0], a.tiles)) return;
     const int32_t* entry = a.plan + kHead + tile * kEntry;
     const int who = __builtin_amdgcn_readfirstlane(entry[0]);
-    int row = entry[1 + m16];
-    if (row >= a.rows) row = -1;
     const bool none = who < 0 || who >= a.n_adapters;
-    if (none && a.base == a.out) return;
-    const int64_t at = row < 0 ? 0 : row;
+    auto row_of = [&](int i) {
+        const int r = entry[1 + i];
+        return r < a.rows ? r : -1;
+    };
+    int row[NI];                         // of base and out
+#pragma unroll
+    for (int i = 0; i < NI; ++i) row[i] = row_of(i * (16 / NI) + lane / LR);
+    const int groups = (a.d_out + 63) >> 6, step = a.parts.d * NW, piece = (lane & (LR - 1)) * Piece<OUT>::kN;
+    int q = part * NW + wave;
+    if (none) {                          // base alone
+        if (a.base == a.out) return;
+        for (; q < groups; q += step)
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const int c = q * 64 + piece;
+                if (c >= a.d_out || row[i] < 0) continue;
+                Piece<OUT> y = {};
+                if (a.base) y.load(a.base, row[i] * a.base_row + c);
+                y.store(a.out, row[i] * a.out_row + c);
+            }
+        return;
+    }
+    char* mine = own[wave];
+    auto place = [&](int r, int p) { return r * 128 + ((p ^ r) & 7) * 16; };   // of a stage: pieces turned by the row, so that lanes do not meet
 
+    // h^T = A x^T, the waves in turns of 128 bytes of every row
     f32x4 acc[NR];
 #pragma unroll
     for (int j = 0; j < NR; ++j) acc[j] = (f32x4){0.f, 0.f, 0.f, 0.f};
-    if (!none) {
-        const char* x = a.x + at * a.x_row * ES;
-        const char* w = a.a + (who * a.a_adapter + m16 * a.a_row) * ES;
-        for (int k0 = wave * STEP; k0 < a.d_in; k0 += NW * STEP) {
-            const int k = k0 + g * VEC;
-            v4u xv = {0u, 0u, 0u, 0u};
-            const bool there = k < a.d_in;
-            if (there && row >= 0) xv = *reinterpret_cast<const v4u*>(x + (int64_t)k * ES);
+    {
+        const int r8 = lane >> 3, bytes = a.d_in * ES, stages = (bytes + 127) >> 7;
+        const int xr[2] = {row_of(r8), row_of(8 + r8)};
+        const char* x[2];
+        const char* w[2 * NR];
 #pragma unroll
-            for (int j = 0; j < NR; ++j) {
-                v4u wv = {0u, 0u, 0u, 0u};
-                if (there && j * 16 + m16 < a.rank) wv = *reinterpret_cast<const v4u*>(w + (j * 16 * a.a_row + k) * ES);
-                acc[j] = T::mul(wv, xv, acc[j]);
+        for (int i = 0; i < 2; ++i) x[i] = a.x + (int64_t)max(xr[i], 0) * a.x_row * ES;
+#pragma unroll
+        for (int i = 0; i < 2 * NR; ++i) w[i] = a.a + (who * a.a_adapter + min(8 * i + r8, a.rank - 1) * a.a_row) * ES;   // (rows behind the rank: see h)
+        struct Stage { v4u x[2], w[2 * NR]; } ahead[D1];
+        auto request = [&](int t, Stage& st) {
+            const int at = t * 128 + (lane & 7) * 16;
+            const bool in = at < bytes;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                st.x[i] = (v4u){0u, 0u, 0u, 0u};
+                if (in && xr[i] >= 0) st.x[i] = *reinterpret_cast<const v4u*>(x[i] + at);
+            }
+#pragma unroll
+            for (int i = 0; i < 2 * NR; ++i) {
+                st.w[i] = (v4u){0u, 0u, 0u, 0u};
+                if (in) st.w[i] = *reinterpret_cast<const v4u*>(w[i] + at);
+            }
+        };
+#pragma unroll
+        for (int d = 0; d < D1; ++d) request(wave + d * NW, ahead[d]);
+        for (int t = wave; t < stages; t += D1 * NW)
+#pragma unroll
+            for (int d = 0; d < D1; ++d) {
+                if (t + d * NW >= stages) break;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) *reinterpret_cast<v4u*>(mine + place(8 * i + r8, lane)) = ahead[d].x[i];
+#pragma unroll
+                for (int i = 0; i < 2 * NR; ++i) *reinterpret_cast<v4u*>(mine + place(16 + 8 * i + r8, lane)) = ahead[d].w[i];
+                wave_order();
+                request(t + (d + D1) * NW, ahead[d]);
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const v4u xv = *reinterpret_cast<const v4u*>(mine + place(m16, 4 * s + g));
+#pragma unroll
+                    for (int j = 0; j < NR; ++j) acc[j] = T::mul(*reinterpret_cast<const v4u*>(mine + place(16 + 16 * j + m16, 4 * s + g)), xv, acc[j]);
+                }
+                wave_order();
+            }
+#pragma unroll
+        for (int j = 0; j < NR; ++j) *reinterpret_cast<f32x4*>(mine + j * 1024 + m16 * 64 + g * 16) = acc[j];   // [..][row][..]
+    }
+
+    // 64 columns a wave: row mu of block i of the product stands for column 16 i + mu.  The first ones' weights and base are on their way while h is
+    // put together, the next ones' while a wave works on its.
+    const char* wb = a.b + who * a.b_adapter * ES;
+    struct Columns {
+        v4u w[4][KS];
+        Piece<OUT> y[NI];
+    } ahead[D2];
+    auto request = [&](int q, Columns& c) {
+        if (q >= groups) return;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int col = min(q * 64 + 16 * i + m16, a.d_out - 1);
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {   // (behind the rank, where h is zero: the last weights)
+                const int j = min(PAIR ? 8 * (g & 1) : 4 * VEC * k + VEC * g, a.rank - VEC);
+                c.w[i][k] = *reinterpret_cast<const v4u*>(wb + (col * a.b_row + j) * ES);
             }
         }
 #pragma unroll
-        for (int j = 0; j < NR; ++j) *reinterpret_cast<f32x4*>(&parts[wave][j][m16][4 * g]) = acc[j];
-    }
-    __syncthreads();
-    if (!none) {
-        for (int i = threadIdx.x; i < kTile * RP; i += 64 * NW) {
-            const int j = i / (kTile * 16), r = (i >> 4) & 15, c = i & 15;
-            float s = 0.f;
-#pragma unroll
-            for (int v = 0; v < NW; ++v) s += parts[v][j][r][c];
-            h[r][j * 16 + c] = j * 16 + c < a.rank ? s : 0.f;   // (zero weights of an infinite x are no zeros)
+        for (int i = 0; i < NI; ++i) {
+            c.y[i].w = (v4u){0u, 0u, 0u, 0u};
+            if (a.base && row[i] >= 0 && q * 64 + piece < a.d_out) c.y[i].load(a.base, row[i] * a.base_row + q * 64 + piece);
         }
+    };
+#pragma unroll
+    for (int d = 0; d < D2; ++d) request(q + d * step, ahead[d]);
+
+    __syncthreads();
+    for (int i = threadIdx.x; i < kTile * RP; i += 64 * NW) {
+        const int j = i / (kTile * 16), r = (i >> 4) & 15, c = i & 15;
+        float s = 0.f;
+#pragma unroll
+        for (int v = 0; v < NW; ++v) s += *reinterpret_cast<const float*>(own[v] + i * 4);
+        h[r][j * 16 + c] = j * 16 + c < a.rank ? s : 0.f;
     }
     __syncthreads();
-    // scale[a], and of fp16 the power of two that brings a row's largest h below 2^14: half a step of a part of the smallest is then
-    // 2^-39 of the largest, and nothing overflows
-    if (threadIdx.x < 64) {
-        float top = 0.f;
-        if (TYPE == HAWK_FP16 && !none)
+    // of fp16 the power of two that brings a row's largest h below 2^14: half a step of a part of the smallest is then 2^-39 of the largest,
+    // and nothing overflows
+    if (TYPE == HAWK_FP16) {
+        if (threadIdx.x < 64) {
+            float top = 0.f;
             for (int j = g; j < RP; j += 4) {
                 const float v = fabsf(h[m16][j]);
                 top = fmaxf(top, v <= 3.4028235e38f ? v : 0.f);
             }
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        int e = 0;
-        if (TYPE == HAWK_FP16 && top > 0.f) e = max(ilogbf(top) - 13, -126);
-        if (lane < kTile) factor[lane] = __uint_as_float((unsigned)(e + 127) << 23);
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const int e = top > 0.f ? max(ilogbf(top) - 13, -126) : 0;
+            if (lane < kTile) factor[lane] = __uint_as_float((unsigned)(e + 127) << 23);
+        }
+        __syncthreads();
     }
-    __syncthreads();
     v4u hv[PP][KS];
-    const float up = factor[m16], s = none ? 0.f : (a.scale ? a.scale[who] * up : up), down = 1.f / up;
+    const float up = TYPE == HAWK_FP16 ? factor[m16] : 1.f, scale = a.scale ? a.scale[who] * up : up, down = 1.f / up;
     if (TYPE == HAWK_FP32) {
 #pragma unroll
         for (int k = 0; k < KS; ++k) hv[0][k] = *reinterpret_cast<const v4u*>(&h[m16][k * 16 + 4 * g]);
@@ -244,46 +358,43 @@ __global__ __launch_bounds__(64 * NW, NR <= 4 ? 4 : 2) void adapter_apply_kernel
                 }
         }
     }
-
-    // 64 columns a wave: row mu of block i of the product stands for column 16 (mu / 4) + 4 i + mu % 4, so that a lane's results are 16 neighbours
-    const char* wb = none ? nullptr : a.b + who * a.b_adapter * ES;
-    const int od = a.out_type, groups = (a.d_out + 63) >> 6;
-    for (int q = part * NW + wave; q < groups; q += a.parts.d * NW) {
-        const int c0 = q * 64, mine = c0 + 16 * g;
-        f32x4 o[4];
+    for (; q < groups; q += D2 * step)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
-        if (!none) {
+        for (int d = 0; d < D2; ++d) {
+            const int at = q + d * step;
+            if (at >= groups) break;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int c = c0 + 16 * (m16 >> 2) + 4 * i + (m16 & 3);
+                f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int k = 0; k < KS; ++k) {
-                    const int j = PAIR ? 8 * (g & 1) : k * STEP + VEC * g;
-                    v4u wv = {0u, 0u, 0u, 0u};
-                    if (c < a.d_out && j < a.rank) wv = *reinterpret_cast<const v4u*>(wb + (c * a.b_row + j) * ES);
+                for (int k = 0; k < KS; ++k)
 #pragma unroll
-                    for (int p = 0; p < PP; ++p) o[i] = T::mul(wv, hv[p][k], o[i]);
+                    for (int p = 0; p < PP; ++p) o = T::mul(ahead[d].w[i][k], hv[p][k], o);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] *= scale;
+                *reinterpret_cast<f32x4*>(mine + (m16 * 68 + 16 * i + 4 * g) * 4) = o;   // [row][column]
+            }
+            wave_order();
+            Piece<OUT> y[NI];
+#pragma unroll
+            for (int i = 0; i < NI; ++i) y[i] = ahead[d].y[i];
+            request(at + D2 * step, ahead[d]);
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                float v[Piece<OUT>::kN];
+                y[i].widen(v);
+                const float* o = reinterpret_cast<const float*>(mine) + (i * (16 / NI) + lane / LR) * 68 + piece;
+#pragma unroll
+                for (int e = 0; e < Piece<OUT>::kN; e += 4) {
+                    const f32x4 b = *reinterpret_cast<const f32x4*>(o + e);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[e + k] += b[k];
                 }
+                y[i].narrow(v);
+                if (row[i] >= 0 && at * 64 + piece < a.d_out) y[i].store(a.out, row[i] * a.out_row + at * 64 + piece);
             }
+            wave_order();
         }
-        if (row < 0) continue;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            if (mine + 8 * i >= a.d_out) continue;
-            float y[8];
-            if (a.base) load8(a.base, at * a.base_row + mine + 8 * i, od, y);
-            else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = 0.f;
-            }
-            if (!none) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = fmaf(o[2 * i + (e >> 2)][e & 3], s, y[e]);
-            }
-            store8(a.out, at * a.out_row + mine + 8 * i, od, y);
-        }
-    }
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -292,14 +403,17 @@ bool matrix_ok(const hawk_matrix* m, int width) {
     return m && m->data && aligned16(m->data) && is_type(m->dtype) && !(m->row_stride & 7) && m->row_stride >= 0 && width > 0;
 }
 
-template <int TYPE, int NR, int P> void launch_of(const ApplyArgs& a, unsigned grid, hipStream_t stream) {
-    adapter_apply_kernel<TYPE, NR, P, 8><<<grid, 512, 0, stream>>>(a);
+constexpr int kWaves = 8;
+template <int TYPE, int OUT> void launch_rank(const ApplyArgs& a, unsigned grid, hipStream_t stream) {
+    auto kern = a.rank <= 16 ? adapter_apply_kernel<TYPE, OUT, 1, kWaves>
+                             : (a.rank <= 32 ? adapter_apply_kernel<TYPE, OUT, 2, kWaves>
+                                             : (a.rank <= 64 ? adapter_apply_kernel<TYPE, OUT, 4, kWaves> : adapter_apply_kernel<TYPE, OUT, 8, kWaves>));
+    kern<<<grid, 64 * kWaves, 0, stream>>>(a);
 }
-template <int TYPE, int P> void launch_rank(const ApplyArgs& a, unsigned grid, hipStream_t stream) {
-    if (a.rank <= 16) launch_of<TYPE, 1, P>(a, grid, stream);
-    else if (a.rank <= 32) launch_of<TYPE, 2, P>(a, grid, stream);
-    else if (a.rank <= 64) launch_of<TYPE, 4, P>(a, grid, stream);
-    else launch_of<TYPE, 8, P>(a, grid, stream);
+template <int TYPE> void launch_typed(const ApplyArgs& a, int out, unsigned grid, hipStream_t stream) {
+    if (out == HAWK_FP32) launch_rank<TYPE, HAWK_FP32>(a, grid, stream);
+    else if (out == HAWK_BF16) launch_rank<TYPE, HAWK_BF16>(a, grid, stream);
+    else launch_rank<TYPE, HAWK_FP16>(a, grid, stream);
 }
 
 }  // namespace
@@ -340,17 +454,18 @@ int launch_adapter_apply(const hawk_adapters* w, const void* plan, size_t plan_b
     a.x = static_cast<const char*>(x->data); a.base = base ? static_cast<const char*>(base->data) : nullptr; a.out = static_cast<char*>(out->data);
     a.a_adapter = w->a_adapter_stride; a.a_row = w->a_row_stride; a.b_adapter = w->b_adapter_stride; a.b_row = w->b_row_stride;
     a.x_row = x->row_stride; a.base_row = base ? base->row_stride : 0; a.out_row = out->row_stride;
-    a.n_adapters = w->n_adapters; a.rank = w->rank; a.d_in = w->d_in; a.d_out = w->d_out; a.rows = rows; a.out_type = out->dtype;
+    a.n_adapters = w->n_adapters; a.rank = w->rank; a.d_in = w->d_in; a.d_out = w->d_out; a.rows = rows;
     a.tiles = most_tiles(rows, w->n_adapters);
-    const int groups = (a.d_out + 63) / 64;
-    const int parts = std::max(1, std::min((groups + 7) / 8, 512 / std::max(1, a.tiles)));
+    // Every part of a tile's columns makes the tile's h again, so as many as there are idle units to do it (us with 1 / 2 / 3 / 4 / 6 / 8 parts: 6 tiles of
+    // 1280 by 3456, rank 16, 8.9 / 6.7 / 6.1 / 5.5 / 5.4 / 4.8; 64 of 4096 by 11008, rank 32, 23.2 / 16.8 / 15.6 / 15.3 / 17.7 / 16.6; 280 of 4096 by 4096,
+    // rank 16, 31.6 / 32.1 / 34.1 / 36.6 / 42.8 / 49; 50 of 1280 by 1000, rank 128, 18.3 / 14.9 / 15.1 / 26.2 / 26.3 / 34).
+    const int groups = (a.d_out + 63) / 64, parts = std::max(1, std::min((groups + kWaves - 1) / kWaves, 256 / std::max(1, a.tiles)));
     a.parts = divisor(parts);
-    const int64_t grid = (int64_t)a.tiles * parts;
+    const int64_t grid = (int64_t)(a.tiles + 7) / 8 * 8 * parts;
     if (grid > (1 << 22)) return HAWK_EINVAL;
-    const bool exact = out->dtype == HAWK_FP32;
-    if (w->dtype == HAWK_FP32) launch_rank<HAWK_FP32, 1>(a, (unsigned)grid, stream);
-    else if (w->dtype == HAWK_BF16) exact ? launch_rank<HAWK_BF16, 3>(a, (unsigned)grid, stream) : launch_rank<HAWK_BF16, 2>(a, (unsigned)grid, stream);
-    else launch_rank<HAWK_FP16, 2>(a, (unsigned)grid, stream);
+    if (w->dtype == HAWK_FP32) launch_typed<HAWK_FP32>(a, out->dtype, (unsigned)grid, stream);
+    else if (w->dtype == HAWK_BF16) launch_typed<HAWK_BF16>(a, out->dtype, (unsigned)grid, stream);
+    else launch_typed<HAWK_FP16>(a, out->dtype, (unsigned)grid, stream);
     return status();
 }
 
