@@ -33,9 +33,9 @@ typedef unsigned long long u64;
 constexpr int kBinCount = 1024, kFine = 512;     // linear bins; those of a closer look
 constexpr float kPerUnit = 32.f;     // bins of a unit of z
 constexpr int kPartBins = 512;       // bins of a part of a long row
-constexpr int kFew = 256;            // entries that are ranked against each other
+constexpr int kFew = 64;             // entries that are ranked against each other (a look at 220 takes 1.6 us, ranking them 4)
 constexpr int kChunk = 256;          // entries that a wave has of four a lane: sums of kept weights are held for each
-constexpr int kChunks = 4096;        // of 2^20 entries
+constexpr int kMostEntries = 1 << 20, kChunks = kMostEntries / kChunk;
 constexpr int kTop = 2 * NT;         // entries of a top-k that goes on as a list, two a thread
 
 struct FilterArgs {
@@ -65,7 +65,7 @@ struct CutShared {
     u64 mass[kBinCount], fine_mass[kFine];
     unsigned count[kBinCount], fine[kFine];          // fine: zero between uses
     u64 w[kFew], base;
-    unsigned key[kFew];
+    unsigned key[kFew], lo, hi;
     int at[kFew], order[kFew], n, chunk;
     Picked picked;
     double steps[kSteps];
@@ -192,45 +192,46 @@ __device__ __forceinline__ void give(const FilterArgs& a, int r, int token, floa
 // The smallest weight that min_p keeps, top: the largest one's.
 __device__ __forceinline__ u64 least_of(const Asked& q, u64 top) { return q.min_p >= 1.f ? top : (q.min_p > 0.f ? share_of(q.min_p, top) : 0ull); }
 
-// One wave: of NB bins the last one that is not empty and begins before the cut, with what it has
-// and what lies before it, the same in every lane; there is one.  A lane has neighbouring bins and reads them in an order in which lanes do
-// not meet.
-template <int NB> __device__ __forceinline__ Picked pick_bin(const unsigned* count, const u64* mass, const Cut& cut, unsigned ahead, u64 before) {
-    constexpr int PER = NB / 64;
-    const int lane = threadIdx.x & 63;
-    int c = 0;
-    u64 m = 0;
-#pragma unroll 8
-    for (int j = 0; j < PER; ++j) {
-        const int b = lane * PER + ((j + lane) & (PER - 1));
-        c += (int)count[b];
-        m += mass[b];
+// Bins of which each thread has one, in order: its entries and mass, what lies before it, and all entries.  One barrier.
+struct Bin { unsigned m, ahead, all; u64 mass, before; };
+__device__ __forceinline__ Bin scan_bins(unsigned m, u64 mass, bool masses, int (&counts)[NW], u64 (&sums)[NW]) {
+    const int lane = threadIdx.x & 63, wave = wave_id(), upto = wave_incl_scan_i((int)m);
+    const u64 mass_upto = masses ? wave_incl_scan_u64(mass) : 0ull;
+    if (lane == 63) {
+        counts[wave] = upto;
+        if (masses) sums[wave] = mass_upto;
     }
-    const int cb = wave_incl_scan_i(c) - c;
-    const u64 mb = wave_incl_scan_u64(m) - m;
-    u64 who = __ballot(c > 0 && before + mb < cut.M && ahead + (unsigned)cb < cut.K);
-    const int L = who ? 63 - __clzll((long long)who) : 0;
-    ahead += (unsigned)__builtin_amdgcn_readlane(cb, L);
-    before += lane_u64(mb, L);
-    const int b = L * PER + lane;
-    const int c1 = lane < PER ? (int)count[b] : 0;
-    const u64 m1 = lane < PER ? mass[b] : 0ull;
-    const unsigned a1 = ahead + (unsigned)(wave_incl_scan_i(c1) - c1);
-    const u64 b1 = before + (wave_incl_scan_u64(m1) - m1);
-    who = __ballot(c1 > 0 && b1 < cut.M && a1 < cut.K);
-    const int at = who ? 63 - __clzll((long long)who) : 0;
-    const Picked out = {L * PER + at, (unsigned)__builtin_amdgcn_readlane(c1, at), (unsigned)__builtin_amdgcn_readlane((int)a1, at), lane_u64(b1, at)};
-    return out;
+    __syncthreads();
+    Bin b;
+    int base;
+    b.m = m;
+    b.mass = mass;
+    b.all = (unsigned)wave_base_i(counts, wave, base);
+    b.ahead = (unsigned)(base + upto) - m;
+    b.before = 0ull;
+    if (masses) {
+        const u64 s = lane < NW ? sums[lane] : 0ull, x = wave_incl_scan_u64(s);
+        b.before = (wave > 0 ? lane_u64(x, wave - 1) : 0ull) + mass_upto - mass;
+    }
+    return b;
 }
-// The same for a workgroup: the first wave looks, all threads have the result, and sh.n is zero.  Ends with a barrier.
-template <int NB> __device__ __forceinline__ Picked pick_for_all(const unsigned* count, const u64* mass, const Cut& cut, unsigned ahead, u64 before, CutShared& sh) {
-    if (wave_id() == 0) {
-        const Picked p = pick_bin<NB>(count, mass, cut, ahead, before);
-        if ((threadIdx.x & 63) == 0) {
-            sh.picked = p;
-            sh.n = 0;
-        }
+// Whether the bin holds the cut's border: it begins before the cut, and the cut is in it or there is nothing behind.
+__device__ __forceinline__ bool holds(const Bin& b, const Cut& cut) {
+    return b.m > 0u && b.ahead < cut.K && b.before < cut.M && (b.ahead + b.m >= cut.K || b.before + b.mass >= cut.M || b.ahead + b.m == b.all);
+}
+// Of the NB bins the one that holds a cut's border; all threads have the result, and sh.n is zero.  Two barriers, one of them at the end.
+template <int NB>
+__device__ __forceinline__ Picked pick_bin(const unsigned* count, const u64* mass, bool masses, const Cut& cut, unsigned ahead, u64 before, CutShared& sh) {
+    const int tid = threadIdx.x;
+    Bin b = scan_bins(tid < NB ? count[tid] : 0u, tid < NB && masses ? mass[tid] : 0ull, masses, sh.isum, sh.sum);
+    b.ahead += ahead;
+    b.all += ahead;
+    b.before += before;
+    if (holds(b, cut)) {
+        const Picked p = {tid, b.m, b.ahead, b.before};
+        sh.picked = p;
     }
+    if (tid == 0) sh.n = 0;
     __syncthreads();
     return sh.picked;
 }
@@ -238,8 +239,29 @@ template <int NB> __device__ __forceinline__ Picked pick_for_all(const unsigned*
 // The border of a cut within a range.  each(f): f(index, z) of this thread's entries that may be in it.  masses: weights count.  All threads
 // call, sh.n is zero; what it leaves in sh is read until the next barrier.
 template <class Each>
-__device__ __forceinline__ Found find_border(const Each& each, const Weigh& weigh, bool masses, const Cut& cut, Range r, CutShared& sh) {
+__device__ __forceinline__ Found find_border(const Each& each, const Weigh& weigh, bool masses, const Cut& cut, Range r, CutShared& sh, bool ties = false) {
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
+    // logits of 16 bits: the many are a few values at most, and what the range really spans saves a look or two
+    if (ties && r.m > (unsigned)kFew) {
+        unsigned lo = 0xFFFFFFFFu, hi = 0u;
+        each([&](int, float z) {
+            lo = min(lo, fkey(z));
+            hi = max(hi, fkey(z));
+        });
+        if (tid == 0) { sh.lo = 0xFFFFFFFFu; sh.hi = 0u; }
+        __syncthreads();
+        for (int d = 1; d < 64; d <<= 1) {
+            lo = min(lo, (unsigned)__shfl_xor((int)lo, d));
+            hi = max(hi, (unsigned)__shfl_xor((int)hi, d));
+        }
+        if (lane == 0) {
+            atomicMin(&sh.lo, lo);
+            atomicMax(&sh.hi, hi);
+        }
+        __syncthreads();
+        r.lo = sh.lo;
+        r.hi = sh.hi;
+    }
     while (r.m > (unsigned)kFew) {
         const bool by_key = r.lo < r.hi;
         const unsigned span = by_key ? r.hi - r.lo : (unsigned)(r.last - r.first);
@@ -252,7 +274,7 @@ __device__ __forceinline__ Found find_border(const Each& each, const Weigh& weig
             if (masses) atomicAdd(&sh.fine_mass[d], weigh(z));
         });
         __syncthreads();
-        const Picked p = pick_for_all<kFine>(sh.fine, sh.fine_mass, cut, r.ahead, r.before, sh);
+        const Picked p = pick_bin<kFine>(sh.fine, sh.fine_mass, masses, cut, r.ahead, r.before, sh);
         const unsigned d = (unsigned)p.bin, up = ((d + 1u) << s) - 1u;
         r.m = p.m;
         r.ahead = p.ahead;
@@ -281,53 +303,24 @@ __device__ __forceinline__ Found find_border(const Each& each, const Weigh& weig
     __syncthreads();
     // A wave ranks every sixteenth entry, its lanes compare it with all others.
     const int m = min((int)r.m, kFew);
-    unsigned k[kFew / 64];
-    int at[kFew / 64];
+    const unsigned k = lane < m ? sh.key[lane] : 0u;
+    const int at = lane < m ? sh.at[lane] : 0x7FFFFFFF;
 #pragma unroll
-    for (int c = 0; c < kFew / 64; ++c) {
-        const int i = c * 64 + lane;
-        k[c] = i < m ? sh.key[i] : 0u;
-        at[c] = i < m ? sh.at[i] : 0x7FFFFFFF;
+    for (int t = 0; t < kFew / NW; ++t) {
+        const int i = t * NW + wave;
+        if (i >= m) break;
+        const unsigned mk = (unsigned)__builtin_amdgcn_readlane((int)k, i);
+        const int ma = __builtin_amdgcn_readlane(at, i), rank = __popcll(__ballot(k > mk || (k == mk && at < ma)));
+        if (lane == 0) sh.order[rank] = i;
     }
-#pragma unroll
-    for (int c = 0; c < kFew / 64; ++c)
-#pragma unroll
-        for (int t = 0; t < 64 / NW; ++t) {
-            const int i = c * 64 + t * NW + wave;
-            if (i >= m) break;
-            const unsigned mk = (unsigned)__builtin_amdgcn_readlane((int)k[c], t * NW + wave);
-            const int ma = __builtin_amdgcn_readlane(at[c], t * NW + wave);
-            int rank = 0;
-#pragma unroll
-            for (int x = 0; x < kFew / 64; ++x) {
-                if (x * 64 >= m) break;
-                rank += __popcll(__ballot(k[x] > mk || (k[x] == mk && at[x] < ma)));
-            }
-            if (lane == 0) sh.order[rank] = i;
-        }
     __syncthreads();
-    // Then in order: every wave finds the last entry before the cut, a lane has four neighbours.
-    u64 w[4], own = 0ull;
-    int n_in = 0;
+    // Then in order: every wave finds the last entry before the cut.
+    u64 own = 0ull;
+    int n_in = (int)min((unsigned)m, cut.K - r.ahead);
     if (masses) {
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            w[c] = 4 * lane + c < m ? sh.w[sh.order[4 * lane + c]] : 0ull;
-            own += w[c];
-        }
-        u64 sum = r.before + wave_incl_scan_u64(own) - own;
-        own = 0ull;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const int x = 4 * lane + c;
-            const bool in = x < m && sum < cut.M && r.ahead + (unsigned)x < cut.K;
-            sum += w[c];
-            own += in ? w[c] : 0ull;
-            n_in += __popcll(__ballot(in));
-        }
-        own = wave_sum_u64(own);
-    } else {
-        n_in = (int)min((unsigned)m, cut.K - r.ahead);
+        const u64 w = lane < m ? sh.w[sh.order[lane]] : 0ull, upto = wave_incl_scan_u64(w);
+        n_in = min(n_in, __popcll(__ballot(lane < m && r.before + upto - w < cut.M)));
+        own = lane_u64(upto, max(n_in, 1) - 1);
     }
     const int i = sh.order[max(n_in, 1) - 1];
     const Found out = {{key_to_float(sh.key[i]), sh.at[i]}, r.before + own};
@@ -346,7 +339,7 @@ __device__ __forceinline__ Range bin_range(float zmax, const Picked& p) {
     r.hi = b == 0 ? fkey(zmax) : fkey((float)top) + 1u;
     r.lo = b == kBinCount - 1 ? 0u : fkey((float)low) - 1u;
     r.first = 0;
-    r.last = 0x7FFFFFFF;
+    r.last = kMostEntries - 1;
     return r;
 }
 
@@ -419,8 +412,11 @@ struct TopList {
 template <int E> __device__ __forceinline__ int make_list(const float (&z)[E], const Border& border, TopList& list) {
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
     u64 own = 0ull;                  // counts of the groups, 16 bits each
+    unsigned in = 0u;
 #pragma unroll
-    for (int e = 0; e < E; ++e) own += inside(border, z[e], entry<E>(e, tid)) ? 1ull << 16 * (e / 4) : 0ull;
+    for (int e = 0; e < E; ++e) in |= inside(border, z[e], entry<E>(e, tid)) ? 1u << e : 0u;
+#pragma unroll
+    for (int g = 0; g < E / 4; ++g) own |= (u64)__popc(in >> 4 * g & 15u) << 16 * g;
     const u64 upto = wave_incl_scan_u64(own);
     if (lane == 63)
 #pragma unroll
@@ -432,7 +428,7 @@ template <int E> __device__ __forceinline__ int make_list(const float (&z)[E], c
         int at = __builtin_amdgcn_readlane(sum - t, g * NW + wave) + (int)((upto - own) >> 16 * g & 0xFFFFull);
 #pragma unroll
         for (int e = 4 * g; e < 4 * g + 4; ++e)
-            if (inside(border, z[e], entry<E>(e, tid))) {
+            if (in >> e & 1u) {
                 list.z[at & (kTop - 1)] = z[e];
                 list.at[at & (kTop - 1)] = entry<E>(e, tid);
                 ++at;
@@ -473,7 +469,7 @@ __device__ __forceinline__ void draw_of_list(const FilterArgs& a, int r, const A
         for (int v = 0; v < NW; ++v) mass += sh.sum[v];
         __syncthreads();
         const Cut cut = {maxu64(share_of(q.top_p, mass), 1ull), 0xFFFFFFFFu};
-        const Picked p = pick_for_all<kBinCount>(sh.count, sh.mass, cut, 0u, 0ull, sh);
+        const Picked p = pick_bin<kBinCount>(sh.count, sh.mass, true, cut, 0u, 0ull, sh);
         border = find_border([&](auto f) {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
@@ -589,7 +585,7 @@ template <int E> __device__ __forceinline__ void whole_row(const FilterArgs& a, 
             each([&](int, float v) { atomicAdd(&sh.count[bin_of(zmax, v)], 1u); });
             __syncthreads();
             const Cut cut = {1ull << 63, q.k};
-            const Picked p = pick_for_all<kBinCount>(sh.count, sh.mass, cut, 0u, 0ull, sh);
+            const Picked p = pick_bin<kBinCount>(sh.count, sh.mass, false, cut, 0u, 0ull, sh);
             const Border border = find_border([&](auto f) {
                 each([&](int j, float v) {
                     if (bin_of(zmax, v) == p.bin) f(j, v);
@@ -622,7 +618,7 @@ template <int E> __device__ __forceinline__ void whole_row(const FilterArgs& a, 
         __syncthreads();
         u64 mass = 0ull;
         auto cut_at = [&](const Cut& cut) {
-            const Picked p = pick_for_all<kBinCount>(sh.count, sh.mass, cut, 0u, 0ull, sh);
+            const Picked p = pick_bin<kBinCount>(sh.count, sh.mass, q.by_p, cut, 0u, 0ull, sh);
             const int b = p.bin;
             const Range range = bin_range(zmax, p);
             auto in_bin = [&](auto f) {
@@ -887,12 +883,9 @@ __device__ __forceinline__ Top row_top(const FilterArgs& a, const RowRoom& room)
 }
 
 struct PartShared {
-    u64 mass[kPartBins];
-    unsigned count[kPartBins];
-    double scale[kMostParts], steps[kSteps];
-    int down[kMostParts];
-    u64 rest_mass;
-    int rest, n_list, n_kept;
+    u64 sums[NW], high;
+    double steps[kSteps];
+    int counts[NW], n_list, n_kept;
     RowHead head;
 };
 
@@ -911,21 +904,24 @@ template <int E> __global__ __launch_bounds__(NT) void filter_parts_kernel(Filte
     const int top = t.cell;
     fill_steps(ps.steps);
     const Weigh weigh = {ref_of(top), magic_of(a.unit), ps.steps};
-    if (tid == 0) { ps.n_list = 0; ps.n_kept = 0; ps.rest = 0; ps.rest_mass = 0ull; ps.head = RowHead{}; ps.head.k_bin = ps.head.p_first = kPartBins; }
+    if (tid == 0) { ps.n_list = 0; ps.n_kept = 0; ps.head = RowHead{}; ps.head.k_bin = ps.head.p_first = kPartBins; }
     __syncthreads();
     if (q.by_k || q.by_p) {
-        if (tid < a.parts) {
-            const PartHead h = room.head[tid];
-            const int d = h.zmax > -INFINITY ? top - h.top : kFar;
-            const double f = d == 0 ? 1.0 : exp_below(-(double)d * (double)(1.f / kCells), ps.steps);
-            ps.down[tid] = d;
-            ps.scale[tid] = f;
-            if (d < kFar) {
-                atomicAdd(&ps.rest, h.valid);
-                atomicAdd(&ps.rest_mass, d == 0 ? h.mass : (u64)((double)h.mass * f));
+        // lane i: how far part i's bins are moved, and what its masses are multiplied by
+        int down = kFar, valid = 0;
+        double scale = 0.0;
+        u64 mass = 0ull;
+        if (lane < a.parts) {
+            const PartHead h = room.head[lane];
+            if (h.zmax > -INFINITY) {
+                down = top - h.top;
+                scale = down == 0 ? 1.0 : exp_below(-(double)down * (double)(1.f / kCells), ps.steps);
+                valid = h.valid;
+                mass = down == 0 ? h.mass : (u64)((double)h.mass * scale);
             }
         }
-        __syncthreads();
+        const unsigned all = (unsigned)wave_sum_i(valid);
+        const u64 total = wave_sum_u64(mass);
         u64 m = 0ull;
         unsigned c = 0u;
         // eight parts' bins are requested at a time (the last bin is what is left)
@@ -936,7 +932,7 @@ template <int E> __global__ __launch_bounds__(NT) void filter_parts_kernel(Filte
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int part_i = min(i0 + i, a.parts - 1), at = part_i * kPartBins;
-                bs[i] = i0 + i < a.parts && tid < kPartBins - 1 ? tid - ps.down[part_i] : -1;
+                bs[i] = i0 + i < a.parts && tid < kPartBins - 1 ? tid - __builtin_amdgcn_readlane(down, part_i) : -1;
                 cs[i] = 0u;
                 ms[i] = 0ull;
                 if (tid < kPartBins) {
@@ -946,56 +942,46 @@ template <int E> __global__ __launch_bounds__(NT) void filter_parts_kernel(Filte
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
+                const double f = lane_d(scale, min(i0 + i, a.parts - 1));
                 if (bs[i] < 0) continue;
                 c += cs[i];
-                m += bs[i] == tid ? ms[i] : (u64)((double)ms[i] * ps.scale[i0 + i]);
+                m += bs[i] == tid ? ms[i] : (u64)((double)ms[i] * f);
             }
         }
-        if (tid < kPartBins) {
-            ps.mass[tid] = m;
-            ps.count[tid] = c;
+        Bin b = scan_bins(c, m, q.by_p, ps.counts, ps.sums);
+        b.all = all;
+        if (tid == kPartBins - 1) {
+            b.m = all - b.ahead;
+            b.mass = total > b.before ? total - b.before : 0ull;
+        } else if (tid >= kPartBins) {
+            b.m = 0u;
         }
-        const u64 wm = wave_sum_u64(m);
-        const int wc = wave_sum_i((int)c);
-        const u64 total = ps.rest_mass;
-        __syncthreads();
-        if (lane == 0) {
-            atomicAdd(&ps.rest, -wc);
-            atomicAdd(&ps.rest_mass, 0ull - wm);
-        }
-        __syncthreads();
-        if (tid == 0) {
-            ps.count[kPartBins - 1] = (unsigned)ps.rest;
-            ps.mass[kPartBins - 1] = (long long)ps.rest_mass > 0 ? ps.rest_mass : 0ull;
-        }
-        __syncthreads();
-        if (wave == 0) {
-            RowHead h = {};
-            u64 low = total, high = total;
-            if (q.by_k) {
-                const Cut cut = {1ull << 63, q.k};
-                const Picked p = pick_bin<kPartBins>(ps.count, ps.mass, cut, 0u, 0ull);
-                h.k_bin = p.bin;
-                h.k_m = p.m;
-                h.k_ahead = p.ahead;
-                low = h.k_before = p.before;
-                high = low + ps.mass[h.k_bin];
+        u64 low = total, high = total;
+        const Cut by_k = {1ull << 63, q.k};
+        if (tid == 0) ps.head.total = total;
+        if (q.by_k) {
+            if (holds(b, by_k)) {
+                ps.head.k_bin = tid;
+                ps.head.k_m = b.m;
+                ps.head.k_ahead = b.ahead;
+                ps.head.k_before = b.before;
+                ps.high = b.before + b.mass;
             }
-            if (q.by_p) {            // (what scaling the parts' masses has rounded is far below 2^-30)
-                const u64 first = share_of(q.top_p, low), last = share_of(q.top_p, high);
-                const Cut c0 = {maxu64(first - (first >> 30), 1ull), q.k}, c1 = {last + (last >> 30) + 1ull, q.k};
-                const Picked p = pick_bin<kPartBins>(ps.count, ps.mass, c0, 0u, 0ull);
-                h.p_first = p.bin;
-                h.p_before = p.before;
-                h.p_last = pick_bin<kPartBins>(ps.count, ps.mass, c1, 0u, 0ull).bin;
+            __syncthreads();
+            low = ps.head.k_before;
+            high = ps.high;
+        }
+        if (q.by_p) {                // (what scaling the parts' masses has rounded is far below 2^-30)
+            const u64 first = share_of(q.top_p, low), last = share_of(q.top_p, high);
+            const Cut c0 = {maxu64(first - (first >> 30), 1ull), q.k}, c1 = {last + (last >> 30) + 1ull, q.k};
+            if (holds(b, c0)) {
+                ps.head.p_first = tid;
+                ps.head.p_before = b.before;
             }
-            h.total = total;
-            if (lane == 0) {
-                ps.head = h;
-                if (part == 0) *room.row = h;
-            }
+            if (holds(b, c1)) ps.head.p_last = tid;
         }
         __syncthreads();
+        if (part == 0 && tid == 0) *room.row = ps.head;
     }
     const RowHead h = ps.head;
     const int sure = q.by_p ? h.p_first : (q.by_k ? h.k_bin : kPartBins);    // bins before this one are kept, but for min-p
@@ -1092,7 +1078,7 @@ template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(Filter
             Range x = {};
             x.hi = fkey((float)ref_of(top - first)) + 1u;
             x.lo = last == kPartBins - 1 ? 0u : fkey((float)ref_of(top - last - 1)) - 1u;
-            x.last = 0x7FFFFFFF;
+            x.last = kMostEntries - 1;
             return x;
         };
         u64 mass = h.total;
@@ -1103,7 +1089,7 @@ template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(Filter
             const Found f = find_border([&](auto f) {
                 for (int i = tid; i < n_list; i += NT)
                     if (bin(ls.z[i]) == h.k_bin) f(ls.at[i], ls.z[i]);
-            }, weigh, q.by_p, cut, x, sh);
+            }, weigh, q.by_p, cut, x, sh, a.dtype != HAWK_FP32);
             border = f.border;
             mass = f.mass;
             __syncthreads();
@@ -1124,7 +1110,7 @@ template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(Filter
             border = find_border([&](auto f) {
                 for (int i = tid; i < n_list; i += NT)
                     if (in(i)) f(ls.at[i], ls.z[i]);
-            }, weigh, true, cut, x, sh).border;
+            }, weigh, true, cut, x, sh, a.dtype != HAWK_FP32).border;
         }
         int n = 0;
         for (int i = tid; i < n_list; i += NT) {
@@ -1179,7 +1165,7 @@ int status() { return hipGetLastError() == hipSuccess ? HAWK_OK : HAWK_EDEVICE; 
 }  // namespace
 
 size_t sample_filtered_workspace_bytes(int rows, int n) {
-    if (rows < 1 || rows > (1 << 22) || n < 1 || n > (1 << 20)) return 0;
+    if (rows < 1 || rows > (1 << 22) || n < 1 || n > kMostEntries) return 0;
     const Cutting c = cutting_of(rows, n);
     return c.E ? c.rows * row_bytes(c.parts, c.E) : 0;
 }
@@ -1187,7 +1173,7 @@ size_t sample_filtered_workspace_bytes(int rows, int n) {
 int launch_sample_filtered(const void* logits, int dtype, int64_t row_stride, const int32_t* skip, const float* u, const float* temperature,
                            const int32_t* top_k, const float* top_p, const float* min_p, int rows, int n, int32_t* out_token, float* out_prob,
                            int32_t* out_kept, void* workspace, size_t workspace_bytes, hipStream_t stream) {
-    if (!is_type(dtype) || rows < 0 || rows > (1 << 22) || n < 1 || n > (1 << 20) || row_stride < n) return HAWK_EINVAL;
+    if (!is_type(dtype) || rows < 0 || rows > (1 << 22) || n < 1 || n > kMostEntries || row_stride < n) return HAWK_EINVAL;
     if (rows == 0) return HAWK_OK;
     if (!logits || !u || !out_token || (reinterpret_cast<uintptr_t>(logits) & (type_bytes(dtype) - 1))) return HAWK_EINVAL;
     const Cutting c = cutting_of(rows, n);
