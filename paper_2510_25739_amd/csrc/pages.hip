@@ -93,39 +93,46 @@ struct TakeArgs {
 // The pages that are written next.  First what every sequence lacks: places among those of entries n_past .. n_past + n_new - 1 that have no
 // page or one that other places have too.  Then the free pages in ascending order, as many as are lacking.  Then they are handed
 // out, sequences and places in ascending order, a sequence that would need more than there are (and all behind it) left as it
-// was.  The counts that decide are those before the call: they are changed at the end.
+// was.  The counts that decide are those before the call: they are changed at the end.  72 sequences, 64 of which lack 2 pages of 700: NEW us, nearly
+// all of it dependent latencies.
 __global__ __launch_bounds__(kWide) void paged_take_kernel(TakeArgs a) {
-    __shared__ int sums[kWide / 64 + 1];
+    __shared__ int sums[kWide / 64 + 1], given, moves;
     const PagedView& c = a.c;
     const int tid = threadIdx.x, per = kWide >> a.lanes, width = 1 << a.lanes, l = tid & (width - 1), group = (tid & 63) & ~(width - 1);
     const unsigned long long mine = width == 64 ? ~0ull : ((1ull << width) - 1ull) << group, before = mine & ((1ull << (tid & 63)) - 1ull);
-    struct Span { int first, stop, inside; };        // places that are written; entries of the first one that stay
-    auto span = [&](int s) {
-        Span t = {0, 0, 0};
-        if (s < c.n_seq) {
-            const int past = a.n_past[s], add = a.n_new[s];
-            if (past >= 0 && add > 0 && past < c.capacity) {
-                t.first = page_of(c, past);
-                t.stop = pages_for((int64_t)past + add, c);
-                t.inside = past - t.first * c.page_size;
-            }
-        }
-        return t;
-    };
+    const bool once = c.n_seq <= per;                // what is found out at first still holds when pages are handed out
     auto lacks = [&](int s, int p, int& page) {
         page = a.table[s * c.table_stride + p];
         if (!in_pool(c, page)) { page = -1; return true; }
         return a.refs[page] > 1;
     };
+    // A sequence's places that are written, entries of the first one that stay, pages it lacks; the lane's first place.
+    int first = 0, stop = 0, inside = 0, need = 0, page0 = -1;
+    bool lack0 = false;
+    auto look = [&](int s) {
+        first = stop = inside = need = 0;
+        lack0 = false;
+        if (s < c.n_seq) {
+            const int past = a.n_past[s], add = a.n_new[s];
+            if (past >= 0 && add > 0 && past < c.capacity) {
+                first = page_of(c, past);
+                stop = pages_for((int64_t)past + add, c);
+                inside = past - first * c.page_size;
+            }
+        }
+        if (first + l < stop) need = lack0 = lacks(s, first + l, page0);
+        int page;
+        for (int p = first + l + width; p < stop; p += width) need += lacks(s, p, page) ? 1 : 0;
+        for (int w = 1; w < width; w <<= 1) need += __shfl_xor(need, w);
+    };
     int wanted = 0;                                  // of this thread's sequences
     for (int s0 = 0; s0 < c.n_seq; s0 += per) {
-        const int s = s0 + (tid >> a.lanes);
-        const Span t = span(s);
-        int page;
-        for (int p = t.first + l; p < t.stop; p += width) wanted += lacks(s, p, page) ? 1 : 0;
+        look(s0 + (tid >> a.lanes));
+        wanted += l == 0 ? need : 0;
     }
+    if (tid == 0) given = moves = 0;
     int total, n_free = 0;
-    block_before(wanted, sums, total);
+    const int begin = block_before(wanted, sums, total);
     for (int p0 = 0; p0 < c.n_pages && n_free < total; p0 += kWide * kEach) {
         const int at = p0 + tid * kEach;
         unsigned bits = 0u;
@@ -136,45 +143,43 @@ __global__ __launch_bounds__(kWide) void paged_take_kernel(TakeArgs a) {
         n_free += all;
     }
     __syncthreads();
-    int asked = 0, moves = 0, given = 0;             // of the sequences before this round's; given: of those that are served
+    int asked = 0;                                   // of the sequences before this round's
     for (int s0 = 0; s0 < c.n_seq; s0 += per) {
         const int s = s0 + (tid >> a.lanes);
-        const Span t = span(s);
-        int page, need = 0;
-        for (int p = t.first + l; p < t.stop; p += width) need += lacks(s, p, page) ? 1 : 0;
-        for (int w = 1; w < width; w <<= 1) need += __shfl_xor(need, w);
-        int all, k = asked + block_before(l == 0 ? need : 0, sums, all);
-        k = __shfl(k, group);                        // (the group's first lane counts for it)
-        asked += all;
-        const bool served = k + need <= n_free;
-        const bool bring = served && t.inside > 0 && t.stop > t.first && lacks(s, t.first, page) && page >= 0;
-        int brought, m = moves + block_before(bring && l == 0 ? 1 : 0, sums, brought);
-        moves += brought;
-        int gave;
-        block_before(served && l == 0 ? need : 0, sums, gave);
-        given += gave;
-        if (s < c.n_seq && l == 0) a.short_by[s] = served ? 0 : need;
-        if (bring && l == 0) {
-            // (the first place is the first that lacks a page: the first page of the sequence's)
-            const Move mv = {page, a.free[k], t.inside};
-            a.moves.move[m] = mv;
+        int k = begin;
+        if (!once) {
+            look(s);
+            int all;
+            k = asked + block_before(l == 0 ? need : 0, sums, all);
+            asked += all;
         }
-        if (served) {
-            for (int p0 = t.first; p0 < t.stop; p0 += width) {
-                const int p = p0 + l;
-                const bool take = p < t.stop && lacks(s, p, page);
-                const unsigned long long who = __ballot(take);
-                if (take) {
-                    const int at = k + __popcll(who & before), to = a.free[at];
-                    a.old[at] = page;
-                    a.table[s * c.table_stride + p] = to;
-                }
-                k += __popcll(who & mine);
+        k = __shfl(k, group);                        // (the group's first lane counts for it)
+        const bool served = k + need <= n_free;
+        if (l == 0 && s < c.n_seq) {
+            a.short_by[s] = served ? 0 : need;
+            if (served && need > 0) atomicMax(&given, k + need);
+            if (served && inside > 0 && lack0 && page0 >= 0) {
+                // (the first place is the first that lacks a page, and gets the first page; copies may be made in any order)
+                const Move mv = {page0, a.free[k], inside};
+                a.moves.move[atomicAdd(&moves, 1)] = mv;
             }
         }
+        if (!served || need == 0) continue;
+        for (int p0 = first; p0 < stop; p0 += width) {
+            const int p = p0 + l;
+            int page = page0;
+            const bool take = p < stop && (p0 == first ? lack0 : lacks(s, p, page));
+            const unsigned long long who = __ballot(take);
+            if (take) {
+                const int at = k + __popcll(who & before), to = a.free[at];
+                a.old[at] = page;
+                a.table[s * c.table_stride + p] = to;
+            }
+            k += __popcll(who & mine);
+        }
     }
-    if (tid == 0) *a.moves.count = moves;
     __syncthreads();
+    if (tid == 0) *a.moves.count = moves;
     for (int i = tid; i < given; i += kWide) {
         a.refs[a.free[i]] = 1;
         if (a.old[i] >= 0) atomicAdd(&a.refs[a.old[i]], -1);
@@ -232,6 +237,7 @@ struct CopyArgs {
     const int32_t *src, *dst;       // pages of a list of the caller's (moves.count null)
     MoveList moves;
     int n, esz;
+    int64_t batches;                // of the pieces of a whole page
     Divisor units, heads, pieces;   // of a page: layers times two pools times heads; heads; 16-byte pieces of an entry
     // tables on the way
     const int* map;                 // [n_pages]; null: none
@@ -239,9 +245,11 @@ struct CopyArgs {
     int64_t table_out_stride, places;
 };
 
-// A wave moves one head's keys or values of one page and layer: up to 8 KB requested at once, then stored.  Waves stay for as many units as fill
+// A wave moves 512 neighbouring pieces of 16 bytes of one page - heads one behind the other, of all layers and both pools -, eight a lane, requested
+// together and then stored.  Parts of pages are as small as one entry: a wave that had one head of one layer at a time moved 640 bytes between
+// two latencies (64 copies of 5 entries on average, 36 layers of 20 heads of 64: 36 us, so NEW).  Workgroups stay for as many pieces as fill
 // the chip a few times.
-constexpr int kCopyWaves = 8192;
+constexpr int kCopyWaves = 8192, kBatch = 512;
 __global__ __launch_bounds__(256) void paged_copy_kernel(CopyArgs a) {
     const int lane = threadIdx.x & 63;
     if (a.map) {
@@ -251,31 +259,59 @@ __global__ __launch_bounds__(256) void paged_copy_kernel(CopyArgs a) {
         }
     }
     const int count = a.moves.count ? min(*a.moves.count, a.n) : a.n;
-    const int64_t units = (int64_t)count * a.units.d;
-    for (int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); u < units; u += (int64_t)gridDim.x * 4) {
-        const int m = __builtin_amdgcn_readfirstlane((int)(u / a.units.d)), rest = __builtin_amdgcn_readfirstlane((int)(u - (int64_t)m * a.units.d));
-        const int lk = rest / a.heads, head = rest - lk * a.heads.d;
+    const int64_t xs = a.from.entry_stride * a.esz, ys = a.to.entry_stride * a.esz;
+    const int64_t items = (int64_t)count * a.batches;
+    for (int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); u < items; u += (int64_t)gridDim.x * 4) {
+        const int m = __builtin_amdgcn_readfirstlane((int)(u / a.batches)), batch = __builtin_amdgcn_readfirstlane((int)(u - (int64_t)m * a.batches));
         Move mv = {-1, -1, a.from.page_size};
         if (a.moves.count) mv = a.moves.move[m];
         else { mv.from = a.src[m]; mv.to = a.dst[m]; }
         if (!in_pool(a.from, mv.from) || !in_pool(a.to, mv.to)) continue;
-        const char* x = ((lk & 1) ? a.from.v : a.from.k) + (lk >> 1) * a.from_layer + (mv.from * a.from.page_stride + head * a.from.head_stride) * a.esz;
-        char* y = ((lk & 1) ? a.to.v : a.to.k) + (lk >> 1) * a.to_layer + (mv.to * a.to.page_stride + head * a.to.head_stride) * a.esz;
-        const int total = mv.n * a.pieces.d;
-        const int64_t xs = a.from.entry_stride * a.esz, ys = a.to.entry_stride * a.esz;
-        for (int i0 = lane; i0 < total; i0 += 512) {
-            v4u w[8];
+        // pieces of a head's entries; the batch's first head and its place in it
+        const int per = mv.n * a.pieces.d, unit0 = (int)((int64_t)batch * kBatch / per), left = a.units.d - unit0;
+        const int at0 = (int)((int64_t)batch * kBatch - (int64_t)unit0 * per);
+        if (left <= 0) continue;
+        const int64_t x0 = mv.from * a.from.page_stride, y0 = mv.to * a.to.page_stride;
+        auto head_at = [&](int unit, const char*& from, char*& to) {
+            const int lk = unit / a.heads, head = unit - lk * a.heads.d;
+            from = ((lk & 1) ? a.from.v : a.from.k) + (lk >> 1) * a.from_layer + (x0 + head * a.from.head_stride) * a.esz;
+            to = ((lk & 1) ? a.to.v : a.to.k) + (lk >> 1) * a.to_layer + (y0 + head * a.to.head_stride) * a.esz;
+        };
+        v4u w[8];
+        if (at0 + kBatch <= per) {       // all of one head
+            const char* from;
+            char* to;
+            head_at(unit0, from, to);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int i = i0 + 64 * j, e = i / a.pieces, p = i - e * a.pieces.d;
-                if (i < total) w[j] = *reinterpret_cast<const v4u*>(x + e * xs + p * 16);
+                const int i = at0 + lane + 64 * j, e = i / a.pieces, p = (i - e * a.pieces.d) * 16;
+                w[j] = *reinterpret_cast<const v4u*>(from + e * xs + p);
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int i = i0 + 64 * j, e = i / a.pieces, p = i - e * a.pieces.d;
-                if (i < total) *reinterpret_cast<v4u*>(y + e * ys + p * 16) = w[j];
+                const int i = at0 + lane + 64 * j, e = i / a.pieces, p = (i - e * a.pieces.d) * 16;
+                *reinterpret_cast<v4u*>(to + e * ys + p) = w[j];
+            }
+            continue;
+        }
+        // at0 + 511 < per + 512: the quotients by per are 0 and 1, or of numbers below 1024 and exact by 2^20 / per rounded up
+        const unsigned magic = per < kBatch ? ((1u << 20) + per - 1u) / (unsigned)per : 0u;
+        char* to[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = at0 + lane + 64 * j, q = per < kBatch ? (int)(((unsigned)i * magic) >> 20) : (i >= per ? 1 : 0);
+            to[j] = nullptr;
+            if (q < left) {
+                const int k = i - q * per, e = k / a.pieces, p = (k - e * a.pieces.d) * 16;
+                const char* from;
+                head_at(unit0 + q, from, to[j]);
+                to[j] += e * ys + p;
+                w[j] = *reinterpret_cast<const v4u*>(from + e * xs + p);
             }
         }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (to[j]) *reinterpret_cast<v4u*>(to[j]) = w[j];
     }
 }
 
@@ -287,7 +323,8 @@ size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 // A cache whose pages can be copied in all layers.
 bool whole_view(const hawk_paged_cache* c, PagedView* v) {
     return paged_view(c, 0, v) && !(c->n_layers > 1 && c->layer_stride < c->head_dim) && (int64_t)c->n_layers * 2 * c->n_heads <= (1 << 25) &&
-           (int64_t)c->page_size * (c->head_dim * (int)type_bytes(c->dtype) / 16) <= (1 << 30) && (int64_t)c->n_seq * c->max_pages <= (1 << 30);
+           (int64_t)c->page_size * (c->head_dim * (int)type_bytes(c->dtype) / 16) <= (1 << 30) && (int64_t)c->n_seq * c->max_pages <= (1 << 30) &&
+           (int64_t)c->page_size * (c->head_dim * (int)type_bytes(c->dtype) / 16) * c->n_layers * 2 * c->n_heads <= (int64_t)kBatch << 30;
 }
 void copy_sides(const hawk_paged_cache* from, const hawk_paged_cache* to, CopyArgs* a) {
     a->esz = (int)type_bytes(from->dtype);
@@ -296,6 +333,7 @@ void copy_sides(const hawk_paged_cache* from, const hawk_paged_cache* to, CopyAr
     a->units = divisor(from->n_layers * 2 * from->n_heads);
     a->heads = divisor(from->n_heads);
     a->pieces = divisor(from->head_dim * a->esz / 16);
+    a->batches = ((int64_t)from->page_size * a->pieces.d * a->units.d + kBatch - 1) / kBatch;
 }
 void launch_copy(const CopyArgs& a, int64_t most, hipStream_t stream) {   // most: units there can be
     const int64_t waves = std::min<int64_t>(kCopyWaves, std::max<int64_t>(most, 1));
@@ -363,7 +401,7 @@ int launch_paged_take(const hawk_paged_cache* cache, int32_t* refs, const int32_
     m.moves = a.moves;
     m.n = a.c.n_seq;
     copy_sides(cache, cache, &m);
-    launch_copy(m, (int64_t)m.n * m.units.d, stream);
+    launch_copy(m, m.n * m.batches, stream);
     return status();
 }
 
@@ -383,7 +421,7 @@ int launch_paged_compact(const hawk_paged_cache* cache, const int32_t* refs, int
     m.places = (int64_t)m.from.n_seq * m.from.max_pages;
     copy_sides(cache, cache, &m);
     paged_holes_kernel<<<1, kWide, 0, stream>>>(m.from, refs, refs_out, r.to, r.a, r.b, m.moves, n_used);
-    launch_copy(m, std::max<int64_t>((int64_t)m.n * m.units.d, (m.places + 63) / 64), stream);
+    launch_copy(m, std::max<int64_t>(m.n * m.batches, (m.places + 63) / 64), stream);
     return status();
 }
 
@@ -397,7 +435,7 @@ int launch_paged_copy(const hawk_paged_cache* from, const hawk_paged_cache* to, 
     if (!src || !dst) return HAWK_EINVAL;
     m.src = src; m.dst = dst; m.n = n;
     copy_sides(from, to, &m);
-    launch_copy(m, (int64_t)n * m.units.d, stream);
+    launch_copy(m, n * m.batches, stream);
     return status();
 }
 
