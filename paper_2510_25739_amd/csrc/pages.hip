@@ -93,7 +93,7 @@ struct TakeArgs {
 // The pages that are written next.  First what every sequence lacks: places among those of entries n_past .. n_past + n_new - 1 that have no
 // page or one that other places have too.  Then the free pages in ascending order, as many as are lacking.  Then they are handed
 // out, sequences and places in ascending order, a sequence that would need more than there are (and all behind it) left as it
-// was.  The counts that decide are those before the call: they are changed at the end.  72 sequences, 64 of which lack 2 pages of 700: NEW us, nearly
+// was.  The counts that decide are those before the call: they are changed at the end.  72 sequences, 64 of which lack 2 pages of 700: 8 us, nearly
 // all of it dependent latencies.
 __global__ __launch_bounds__(kWide) void paged_take_kernel(TakeArgs a) {
     __shared__ int sums[kWide / 64 + 1], given, moves;
@@ -247,9 +247,10 @@ struct CopyArgs {
 
 // A wave moves 512 neighbouring pieces of 16 bytes of one page - heads one behind the other, of all layers and both pools -, eight a lane, requested
 // together and then stored.  Parts of pages are as small as one entry: a wave that had one head of one layer at a time moved 640 bytes between
-// two latencies (64 copies of 5 entries on average, 36 layers of 20 heads of 64: 36 us, so NEW).  Workgroups stay for as many pieces as fill
-// the chip a few times.
-constexpr int kCopyWaves = 8192, kBatch = 512;
+// two latencies (64 copies of 5 entries on average, 36 layers of 20 heads of 64: 36 us, so 26).  Workgroups stay for as many pieces as make the
+// waves asked for: where there may be nothing to copy (a take), and where there are whole pages (us with 8192 / 16384 / 65536 waves: those 64
+// with fork and take 38 / 36.3 / 37, 48 pages of 16.8 MB 344 / 337 / 326).
+constexpr int kPartWaves = 16384, kPageWaves = 65536, kBatch = 512;
 __global__ __launch_bounds__(256) void paged_copy_kernel(CopyArgs a) {
     const int lane = threadIdx.x & 63;
     if (a.map) {
@@ -335,8 +336,8 @@ void copy_sides(const hawk_paged_cache* from, const hawk_paged_cache* to, CopyAr
     a->pieces = divisor(from->head_dim * a->esz / 16);
     a->batches = ((int64_t)from->page_size * a->pieces.d * a->units.d + kBatch - 1) / kBatch;
 }
-void launch_copy(const CopyArgs& a, int64_t most, hipStream_t stream) {   // most: units there can be
-    const int64_t waves = std::min<int64_t>(kCopyWaves, std::max<int64_t>(most, 1));
+void launch_copy(const CopyArgs& a, int64_t most, int waves_most, hipStream_t stream) {   // most: batches there can be
+    const int64_t waves = std::min<int64_t>(waves_most, std::max<int64_t>(most, 1));
     paged_copy_kernel<<<(unsigned)((waves + 3) / 4), 256, 0, stream>>>(a);
 }
 
@@ -401,7 +402,7 @@ int launch_paged_take(const hawk_paged_cache* cache, int32_t* refs, const int32_
     m.moves = a.moves;
     m.n = a.c.n_seq;
     copy_sides(cache, cache, &m);
-    launch_copy(m, m.n * m.batches, stream);
+    launch_copy(m, m.n * m.batches, kPartWaves, stream);
     return status();
 }
 
@@ -421,7 +422,7 @@ int launch_paged_compact(const hawk_paged_cache* cache, const int32_t* refs, int
     m.places = (int64_t)m.from.n_seq * m.from.max_pages;
     copy_sides(cache, cache, &m);
     paged_holes_kernel<<<1, kWide, 0, stream>>>(m.from, refs, refs_out, r.to, r.a, r.b, m.moves, n_used);
-    launch_copy(m, std::max<int64_t>(m.n * m.batches, (m.places + 63) / 64), stream);
+    launch_copy(m, std::max<int64_t>(m.n * m.batches, (m.places + 63) / 64), kPageWaves, stream);
     return status();
 }
 
@@ -435,7 +436,7 @@ int launch_paged_copy(const hawk_paged_cache* from, const hawk_paged_cache* to, 
     if (!src || !dst) return HAWK_EINVAL;
     m.src = src; m.dst = dst; m.n = n;
     copy_sides(from, to, &m);
-    launch_copy(m, n * m.batches, stream);
+    launch_copy(m, n * m.batches, kPageWaves, stream);
     return status();
 }
 
