@@ -175,7 +175,7 @@ __device__ __forceinline__ void wave_order() {
 }
 
 // TYPE: of x and the weights; OUT: of base and out.  NR: groups of 16 of the rank.  NW waves.
-// x, A, base and out pass between memory and registers as rows' whole 128 bytes, eight rows (four of 256) an instruction, and change places
+// x, A, B, base and out pass between memory and registers as rows' whole 128 bytes, eight rows (four of 256) an instruction, and change places
 // with the matrix units' layout - a lane has 16 bytes of one of 16 rows - in shared memory of the wave's own: read in that layout, with 64
 // bytes of 16 rows an instruction, memory gave 3.3 instead of 4.4 TB/s, and x, base and out together, 4400 rows of 4096, took 35 instead of
 // 28 us.
@@ -188,11 +188,15 @@ __global__ __launch_bounds__(64 * NW, NR <= 2 ? 4 : 2) void adapter_apply_kernel
     constexpr bool PAIR = TYPE != HAWK_FP32 && NR == 1;                        // two parts of h share a product's 32 features
     constexpr int KS = TYPE == HAWK_FP32 ? NR : (NR + 1) / 2;                  // products over the rank
     constexpr int PP = PAIR ? (P + 1) / 2 : P;
-    constexpr int D1 = NR == 1 ? 4 : (NR == 2 ? 2 : 1);                        // stages of x and A that are requested ahead
-    constexpr int D2 = KS == 1 && OUT != HAWK_FP32 ? 2 : 1;                   // columns that are
+    constexpr int D1 = NR <= 2 ? 2 : 1;                                        // stages of x and A that are requested ahead
+    constexpr int D2 = NR == 1 && OUT != HAWK_FP32 ? 2 : 1;                   // columns that are
     constexpr int LR = OUT == HAWK_FP32 ? 16 : 8, NI = LR / 4;                 // lanes of a row of 64 columns, instructions of 16 rows
+    // B of 32 bits, twice a stage's size, goes straight into the operands' places
+    constexpr bool VIA = TYPE != HAWK_FP32;
+    constexpr int PR = VIA ? RP / VEC : 4 * KS;                                // pieces of B that a lane brings for 64 columns (VIA: of a row)
     constexpr int kStage = 16 * (1 + NR) * 128, kSum = NR * 1024, kDelta = 16 * 68 * 4;
     constexpr int kOwn = kStage > kSum ? (kStage > kDelta ? kStage : kDelta) : (kSum > kDelta ? kSum : kDelta);
+    static_assert(!VIA || 64 * PR * 16 <= kOwn, "64 columns' weights fit");
     __shared__ __align__(16) char own[NW][kOwn];                               // of a wave: a stage, its part of h, a block of B h
     __shared__ float h[kTile][LD];
     __shared__ float factor[kTile];
@@ -284,19 +288,17 @@ __global__ __launch_bounds__(64 * NW, NR <= 2 ? 4 : 2) void adapter_apply_kernel
     // put together, the next ones' while a wave works on its.
     const char* wb = a.b + who * a.b_adapter * ES;
     struct Columns {
-        v4u w[4][KS];
+        v4u w[PR];
         Piece<OUT> y[NI];
     } ahead[D2];
+    auto weight_at = [&](int col, int p) { return (col * PR + (PR >= 8 ? p ^ (col & (PR - 1)) : p)) * 16; };   // of 64 columns' weights
     auto request = [&](int q, Columns& c) {
         if (q >= groups) return;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int col = min(q * 64 + 16 * i + m16, a.d_out - 1);
-#pragma unroll
-            for (int k = 0; k < KS; ++k) {   // (behind the rank, where h is zero: the last weights)
-                const int j = min(PAIR ? 8 * (g & 1) : 4 * VEC * k + VEC * g, a.rank - VEC);
-                c.w[i][k] = *reinterpret_cast<const v4u*>(wb + (col * a.b_row + j) * ES);
-            }
+        for (int i = 0; i < PR; ++i) {       // (behind the rank, where h is zero: the last weights)
+            const int n = lane + 64 * i;
+            const int col = min(q * 64 + (VIA ? n / PR : 16 * (i / KS) + m16), a.d_out - 1), j = min((VIA ? n % PR : 4 * (i % KS) + g) * VEC, a.rank - VEC);
+            c.w[i] = *reinterpret_cast<const v4u*>(wb + (col * a.b_row + j) * ES);
         }
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
@@ -363,16 +365,28 @@ __global__ __launch_bounds__(64 * NW, NR <= 2 ? 4 : 2) void adapter_apply_kernel
         for (int d = 0; d < D2; ++d) {
             const int at = q + d * step;
             if (at >= groups) break;
+            if constexpr (VIA) {
+#pragma unroll
+                for (int i = 0; i < PR; ++i) *reinterpret_cast<v4u*>(mine + weight_at((lane + 64 * i) / PR, (lane + 64 * i) % PR)) = ahead[d].w[i];
+                wave_order();
+            }
+            f32x4 o[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                f32x4 o = {0.f, 0.f, 0.f, 0.f};
+                o[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int k = 0; k < KS; ++k)
+                for (int k = 0; k < KS; ++k) {
+                    const v4u w = VIA ? *reinterpret_cast<const v4u*>(mine + weight_at(16 * i + m16, PAIR ? g & 1 : 4 * k + g)) : ahead[d].w[(i * KS + k) % PR];
 #pragma unroll
-                    for (int p = 0; p < PP; ++p) o = T::mul(ahead[d].w[i][k], hv[p][k], o);
+                    for (int p = 0; p < PP; ++p) o[i] = T::mul(w, hv[p][k], o[i]);
+                }
+            }
+            wave_order();
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] *= scale;
-                *reinterpret_cast<f32x4*>(mine + (m16 * 68 + 16 * i + 4 * g) * 4) = o;   // [row][column]
+            for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[i][e] *= scale;
+                *reinterpret_cast<f32x4*>(mine + (m16 * 68 + 16 * i + 4 * g) * 4) = o[i];   // [row][column]
             }
             wave_order();
             Piece<OUT> y[NI];
