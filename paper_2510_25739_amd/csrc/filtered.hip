@@ -1146,8 +1146,10 @@ struct Cutting { int E, parts, rows; };          // entries of a thread (0: rows
 inline Cutting cutting_of(int rows, int n) {
     Cutting c = {0, 1, rows};
     if (n <= 16 * NT) return c;
-    c.E = n <= kMostParts * 8 * NT ? 8 : 32;
-    c.parts = (n + c.E * NT - 1) / (c.E * NT);
+    c.E = 8;
+    auto parts = [&](int E) { return (n + E * NT - 1) / (E * NT); };
+    while (c.E < 32 && (parts(c.E) > kMostParts || (int64_t)rows * parts(c.E) > 256)) c.E *= 2;
+    c.parts = parts(c.E);
     c.rows = std::min(rows, kPartsAtOnce / c.parts);
     return c;
 }
@@ -1190,7 +1192,9 @@ int launch_sample_filtered(const void* logits, int dtype, int64_t row_stride, co
     if (n <= 4 * NT) sample_filtered_kernel<4><<<(unsigned)rows, NT, 0, stream>>>(a);
     else if (n <= 8 * NT) sample_filtered_kernel<8><<<(unsigned)rows, NT, 0, stream>>>(a);
     else if (n <= 16 * NT) sample_filtered_kernel<16><<<(unsigned)rows, NT, 0, stream>>>(a);
-    else c.E == 8 ? launch_parts<8>(a, c, rows, stream) : launch_parts<32>(a, c, rows, stream);
+    else if (c.E == 8) launch_parts<8>(a, c, rows, stream);
+    else if (c.E == 16) launch_parts<16>(a, c, rows, stream);
+    else launch_parts<32>(a, c, rows, stream);
     return status();
 }
 

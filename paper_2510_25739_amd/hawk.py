@@ -711,35 +711,39 @@ class AdapterPlan:
             raise HawkError(rc, where)
 
     def _matrix(self, what, t, width):
-        if t.dim() != 2 or t.get_device() != self._dev or t.shape[0] != self.rows or t.shape[1] != width or (t.stride(1) != 1 and self.rows):
+        st = t.stride()
+        if t.get_device() != self._dev or t.shape != (self.rows, width) or (st[1] != 1 and self.rows):
             raise HawkError(-1, "hawk_adapter_apply", f"{what} must be a tensor [rows, {width}] on the plan's device, the last axis contiguous")
-        return _PACK_MATRIX(t.data_ptr(), t.stride(0) if self.rows > 1 else (width + 7) // 8 * 8, _dtype_of(t))
+        return _PACK_MATRIX(t.data_ptr(), st[0] if self.rows > 1 else (width + 7) // 8 * 8, _DTYPES.get(t.dtype, -1))
 
     def apply(self, x, a, b, base=None, scale=None, out=None, dtype=None):
         """hawk_adapter_apply: base + scale[i] * B_i (A_i x) of every row, i its adapter.  x [rows, d_in], a [n_adapters, rank, d_in],
         b [n_adapters, d_out, rank] of one type; base [rows, d_out] (None: zero) and out of one type; scale [n_adapters] fp32 (None: 1).
         out: where the result goes, base itself allowed (None: a new tensor of base's type, or of `dtype`, or of x's, whose rows
         of no sequence are not written)."""
-        where = "hawk_adapter_apply"
-        if a.dim() != 3 or b.dim() != 3 or a.get_device() != self._dev or b.get_device() != self._dev or a.dtype is not b.dtype:
+        where, dev, n = "hawk_adapter_apply", self._dev, self.n_adapters
+        if a.dim() != 3 or b.dim() != 3 or a.get_device() != dev or b.get_device() != dev or a.dtype is not b.dtype:
             raise HawkError(-1, where, "a [n_adapters, rank, d_in] and b [n_adapters, d_out, rank] must be tensors of one type on the plan's device")
-        n, rank, d_in = a.shape
-        d_out = b.shape[1]
+        na, rank, d_in = a.shape
+        nb, d_out, rank_b = b.shape
         (sa, ja, ia), (sb, jb, ib) = a.stride(), b.stride()
-        if n != self.n_adapters or b.shape[0] != n or b.shape[2] != rank or (n and (ia != 1 or ib != 1)):
+        if na != n or nb != n or rank_b != rank or ((ia != 1 or ib != 1) and n):
             raise HawkError(-1, where, "a [n_adapters, rank, d_in] and b [n_adapters, d_out, rank] must have the plan's adapters and last axes that are contiguous")
-        s = None
+        s = 0
         if scale is not None:
-            if scale.dtype is not self._f32 or scale.get_device() != self._dev or scale.shape != (n,) or not scale.is_contiguous():
+            if scale.dtype is not self._f32 or scale.get_device() != dev or scale.shape != (n,) or not scale.is_contiguous():
                 raise HawkError(-1, where, "scale must be a contiguous fp32 tensor [n_adapters] on the plan's device")
             s = scale.data_ptr()
+        kind = _dtype_of(a)
         hx = self._matrix("x", x, d_in)
         hb = self._matrix("base", base, d_out) if base is not None else None
         if out is None:
             out = x.new_empty((self.rows, d_out), dtype=dtype if dtype is not None else (base.dtype if base is not None else x.dtype))
-        ho = self._matrix("out", out, d_out)
-        w = _PACK_ADAPTERS(a.data_ptr(), b.data_ptr(), sa if n > 1 else 0, ja, sb if n > 1 else 0, jb, s or 0, _dtype_of(a), n, rank, d_in, d_out)
-        rc = _call_on(self._dev, self._L.hawk_adapter_apply, w, self._ptr, self._n, self.rows, hx, hb, ho)
+            ho = _PACK_MATRIX(out.data_ptr(), d_out, _DTYPES.get(out.dtype, -1))
+        else:
+            ho = self._matrix("out", out, d_out)
+        w = _PACK_ADAPTERS(a.data_ptr(), b.data_ptr(), sa if n > 1 else 0, ja, sb if n > 1 else 0, jb, s, kind, n, rank, d_in, d_out)
+        rc = _call_on(dev, self._L.hawk_adapter_apply, w, self._ptr, self._n, self.rows, hx, hb, ho)
         if rc != 0:
             raise HawkError(rc, where)
         return out
