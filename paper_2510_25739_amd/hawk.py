@@ -460,6 +460,7 @@ class PagedCache:
         self._dev, self._hd, self._kv = k.get_device(), head_dim, n_heads
         self._dtype, self._f32, self._i32, self._i64 = k.dtype, _float32(), _int32(), _int64()
         self._room = {}     # workspace of an attention by (rows, q heads, max_len)
+        self._refs_shape = (n_pages,)
         self.table = table
 
     @property
@@ -592,41 +593,43 @@ class PagedCache:
             raise HawkError(rc, where)
 
     def _refs(self, where, refs):
-        self._fits(where, "refs must be a contiguous int32 tensor [n_pages] on the cache's device", refs, self._i32, (self._c.n_pages,))
+        self._fits(where, "refs must be a contiguous int32 tensor [n_pages] on the cache's device", refs, self._i32, self._refs_shape)
         return refs.data_ptr()
 
     def _pages_workspace(self, like):
-        if self._pages_room is None:
-            self._pages_room = self._L.hawk_paged_pages_workspace_bytes(self._ref)
-        return like.new_empty((max(self._pages_room, 16),), dtype=_uint8())
+        """Workspace of a take or compact, from an int32 tensor's memory, and its bytes."""
+        n = self._pages_room
+        if n is None:
+            n = self._pages_room = max(self._L.hawk_paged_pages_workspace_bytes(self._ref), 16)
+        return like.new_empty((n // 4,)), n
 
     def fork(self, refs, n_past, src, dst):
         """hawk_paged_fork: sequences dst [n] int32 share from now on the pages of the entries that sequences src [n] have committed; the
         table, refs [n_pages] and n_past [n_seq] change in place."""
-        where, i32 = "hawk_paged_fork", self._i32
-        what = "src and dst must be contiguous int32 tensors [n], n_past [n_seq], on the cache's device"
-        n = src.shape[0] if src.dim() == 1 else -1
-        self._fits(where, what, src, i32, (n,))
-        self._fits(where, what, dst, i32, (n,))
-        self._fits(where, what, n_past, i32, self._past_shape)
-        rc = _call_on(self._dev, self._L.hawk_paged_fork, self._ref, self._refs(where, refs), n_past.data_ptr(), src.data_ptr(), dst.data_ptr(), n)
+        where, i32, dev, shape = "hawk_paged_fork", self._i32, self._dev, src.shape
+        if not (src.dtype is i32 and dst.dtype is i32 and n_past.dtype is i32 and src.get_device() == dev and dst.get_device() == dev
+                and n_past.get_device() == dev and len(shape) == 1 and dst.shape == shape and n_past.shape == self._past_shape
+                and src.is_contiguous() and dst.is_contiguous() and n_past.is_contiguous()):
+            raise HawkError(-1, where, "src and dst must be contiguous int32 tensors [n], n_past [n_seq], on the cache's device")
+        rc = _call_on(dev, self._L.hawk_paged_fork, self._ref, self._refs(where, refs), n_past.data_ptr(), src.data_ptr(), dst.data_ptr(), shape[0])
         if rc != 0:
             raise HawkError(rc, where)
 
     def take(self, refs, n_past, n_new, short_by=None):
         """hawk_paged_take: pages for the next n_new [n_seq] int32 entries of every sequence, shared ones copied first; the table and refs change
         in place.  Returns short_by [n_seq] int32: 0, or how many pages a sequence needs that was left as it was because there were too few."""
-        where, i32 = "hawk_paged_take", self._i32
+        where, i32, dev, shape = "hawk_paged_take", self._i32, self._dev, self._past_shape
         what = "n_past, n_new and short_by must be contiguous int32 tensors [n_seq] on the cache's device"
-        self._fits(where, what, n_past, i32, self._past_shape)
-        self._fits(where, what, n_new, i32, self._past_shape)
+        if not (n_past.dtype is i32 and n_new.dtype is i32 and n_past.get_device() == dev and n_new.get_device() == dev and n_past.shape == shape
+                and n_new.shape == shape and n_past.is_contiguous() and n_new.is_contiguous()):
+            raise HawkError(-1, where, what)
         if short_by is None:
-            short_by = n_past.new_empty(self._past_shape)
+            short_by = n_past.new_empty(shape)
         else:
-            self._fits(where, what, short_by, i32, self._past_shape)
-        ws = self._pages_workspace(n_past)
-        rc = _call_on(self._dev, self._L.hawk_paged_take, self._ref, self._refs(where, refs), n_past.data_ptr(), n_new.data_ptr(), short_by.data_ptr(),
-                      ws.data_ptr(), ws.shape[0])
+            self._fits(where, what, short_by, i32, shape)
+        at = self._refs(where, refs)
+        ws, n = self._pages_workspace(n_past)
+        rc = _call_on(dev, self._L.hawk_paged_take, self._ref, at, n_past.data_ptr(), n_new.data_ptr(), short_by.data_ptr(), ws.data_ptr(), n)
         if rc != 0:
             raise HawkError(rc, where)
         return short_by
@@ -656,9 +659,9 @@ class PagedCache:
             n_used = refs.new_empty((1,))
         else:
             self._fits(where, "n_used must be an int32 tensor [1] on the cache's device", n_used, i32, (1,))
-        ws = self._pages_workspace(refs)
-        rc = _call_on(self._dev, self._L.hawk_paged_compact, self._ref, ptr, table.data_ptr(), self._c.table_stride, self._refs(where, refs_out),
-                      n_used.data_ptr(), ws.data_ptr(), ws.shape[0])
+        to = self._refs(where, refs_out)
+        ws, n = self._pages_workspace(refs)
+        rc = _call_on(self._dev, self._L.hawk_paged_compact, self._ref, ptr, table.data_ptr(), self._c.table_stride, to, n_used.data_ptr(), ws.data_ptr(), n)
         if rc != 0:
             raise HawkError(rc, where)
         return table, refs_out, n_used
