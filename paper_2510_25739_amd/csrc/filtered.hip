@@ -746,7 +746,8 @@ template <int E> __global__ __launch_bounds__(NT) void sample_filtered_kernel(Fi
 // ---- Long rows in parts of E * 1024 entries.  Their bins are cells of a fixed grid of z, 512 of them from the cell of the largest entry down (of a
 // part, so that a part needs to know nothing of the others; the last one holds what lies behind), and weights are relative to the
 // upper end of the largest's cell: parts are brought together by moving bins and scaling masses.
-constexpr int kPartList = 512, kMostParts = 32, kList = 4096;
+constexpr int kMostParts = 32, kList = 4096;     // parts of a row; entries of the borders' bins that shared memory holds
+__host__ __device__ constexpr int part_list(int E) { return 256 * E; }        // those of a part: a quarter of its entries
 constexpr float kCells = 16.f;       // cells of a unit of z
 constexpr int kFar = 1 << 29;        // cells from here on are not told apart
 __device__ __forceinline__ int cell_of(float z) { return (int)fminf(fmaxf(floorf(z * kCells), -1073741824.f), 1073741824.f); }
@@ -767,9 +768,9 @@ struct RowRoom {
     RowHead* row;
     u64 *mass, *sums;                // [part][bin]; [part][chunk]
     unsigned* count;                 // [part][bin]
-    int2* list;                      // [part][kPartList]: z, index
+    int2* list;                      // [part][part_list]: z, index
 };
-__host__ __device__ inline size_t part_bytes(int E) { return sizeof(PartHead) + kPartBins * 12 + kPartList * 8 + (size_t)E * 32; }
+__host__ __device__ inline size_t part_bytes(int E) { return sizeof(PartHead) + kPartBins * 12 + (size_t)part_list(E) * 8 + (size_t)E * 32; }
 __host__ __device__ inline size_t row_bytes(int parts, int E) { return sizeof(RowHead) + parts * part_bytes(E); }
 __device__ __forceinline__ RowRoom room_of(const FilterArgs& a, int row, int E) {
     char* p = a.room + row * row_bytes(a.parts, E);
@@ -779,7 +780,7 @@ __device__ __forceinline__ RowRoom room_of(const FilterArgs& a, int row, int E) 
     r.mass = reinterpret_cast<u64*>(r.head + a.parts);
     r.sums = r.mass + (size_t)a.parts * kPartBins;
     r.list = reinterpret_cast<int2*>(r.sums + (size_t)a.parts * E * 4);
-    r.count = reinterpret_cast<unsigned*>(r.list + (size_t)a.parts * kPartList);
+    r.count = reinterpret_cast<unsigned*>(r.list + (size_t)a.parts * part_list(E));
     return r;
 }
 template <int E> struct PartRow {
@@ -1003,7 +1004,7 @@ template <int E> __global__ __launch_bounds__(NT) void filter_parts_kernel(Filte
                 }
             } else if ((q.by_k && b == h.k_bin) || (q.by_p && b <= h.p_last)) {
                 const int at = atomicAdd(&ps.n_list, 1);
-                if (at < kPartList) room.list[part * kPartList + at] = make_int2(__float_as_int(z), p.index(4 * g + i));
+                if (at < part_list(E)) room.list[part * part_list(E) + at] = make_int2(__float_as_int(z), p.index(4 * g + i));
             }
         }
         s = wave_sum_u64(s);
@@ -1020,7 +1021,7 @@ template <int E> __global__ __launch_bounds__(NT) void filter_parts_kernel(Filte
 
 struct ListShared {
     float z[kList];
-    int at[kList], kept;
+    int at[kList], kept, m;
 };
 
 template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(FilterArgs a, int row0) {
@@ -1048,25 +1049,39 @@ template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(Filter
     const int top = t.cell;
     bool far = t.far;
     const int listed = lane < a.parts && !far ? room.head[lane].n_list : 0, sure = lane < a.parts && !far ? room.head[lane].n_kept : 0, upto = wave_incl_scan_i(listed), n_list = __builtin_amdgcn_readlane(upto, 63);
-    far = far || n_list > kList || __ballot(listed > kPartList) != 0ull;
+    far = far || __ballot(listed > part_list(E)) != 0ull;
     if (far) {
         whole_row<0>(a, r, sh, sums, both.top);
         return;
     }
     const int n_sure = wave_sum_i(sure);
-    if (tid == 0) { ls.kept = n_sure; sh.n = 0; }
+    if (tid == 0) { ls.kept = n_sure; ls.m = 0; sh.n = 0; }
     fill_steps(sh.steps);
     if (tid < kFine) { sh.fine[tid] = 0u; sh.fine_mass[tid] = 0ull; }
     const int chunks = a.parts * E * 4;
     for (int i = tid; i < chunks; i += NT) sums[i] = room.sums[i];
-    for (int i = wave; i < a.parts; i += NW) {
+    const bool held = n_list <= kList;
+    for (int i = wave; held && i < a.parts; i += NW) {
         const int n = __builtin_amdgcn_readlane(listed, i), from = __builtin_amdgcn_readlane(upto, i) - n;
         for (int k = lane; k < n; k += 64) {
-            const int2 e = room.list[i * kPartList + k];
+            const int2 e = room.list[i * part_list(E) + k];
             ls.z[from + k] = __int_as_float(e.x);
             ls.at[from + k] = e.y;
         }
     }
+    auto each_listed = [&](auto f) {     // f(index, z)
+        if (held) {
+            for (int i = tid; i < n_list; i += NT) f(ls.at[i], ls.z[i]);
+        } else {
+            for (int i = 0; i < a.parts; ++i) {
+                const int n = __builtin_amdgcn_readlane(listed, i);
+                for (int k = tid; k < n; k += NT) {
+                    const int2 e = room.list[i * part_list(E) + k];
+                    f(e.y, __int_as_float(e.x));
+                }
+            }
+        }
+    };
     __syncthreads();
     const Weigh weigh = {ref_of(top), magic_of(a.unit), sh.steps};
     const u64 least = least_of(q, weigh(t.zmax));
@@ -1087,8 +1102,9 @@ template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(Filter
             Range x = range_of(h.k_bin, h.k_bin);
             x.before = h.k_before; x.ahead = h.k_ahead; x.m = h.k_m;
             const Found f = find_border([&](auto f) {
-                for (int i = tid; i < n_list; i += NT)
-                    if (bin(ls.z[i]) == h.k_bin) f(ls.at[i], ls.z[i]);
+                each_listed([&](int at, float z) {
+                    if (bin(z) == h.k_bin) f(at, z);
+                });
             }, weigh, q.by_p, cut, x, sh, a.dtype != HAWK_FP32);
             border = f.border;
             mass = f.mass;
@@ -1096,30 +1112,34 @@ template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(Filter
         }
         if (q.by_p) {
             const Border most = border;
-            auto in = [&](int i) {
-                const int b = bin(ls.z[i]);
-                return b >= h.p_first && b <= h.p_last && inside(most, ls.z[i], ls.at[i]);
+            auto in = [&](int at, float z) {
+                const int b = bin(z);
+                return b >= h.p_first && b <= h.p_last && inside(most, z, at);
             };
+            int m = 0;
+            each_listed([&](int at, float z) { m += in(at, z) ? 1 : 0; });
+            m = wave_sum_i(m);
+            if (lane == 0) atomicAdd(&ls.m, m);
             if (tid == 0) sh.n = 0;
             __syncthreads();
-            int m = 0;
-            for (int i = 0; i < n_list; i += NT) m += __syncthreads_count(i + tid < n_list && in(i + tid));
+            m = ls.m;
             const Cut cut = {maxu64(share_of(q.top_p, mass), 1ull), 0xFFFFFFFFu};
             Range x = range_of(h.p_first, h.p_last);
             x.before = h.p_before; x.m = (unsigned)m;
             border = find_border([&](auto f) {
-                for (int i = tid; i < n_list; i += NT)
-                    if (in(i)) f(ls.at[i], ls.z[i]);
+                each_listed([&](int at, float z) {
+                    if (in(at, z)) f(at, z);
+                });
             }, weigh, true, cut, x, sh, a.dtype != HAWK_FP32).border;
         }
         int n = 0;
-        for (int i = tid; i < n_list; i += NT) {
-            if (!inside(border, ls.z[i], ls.at[i])) continue;
-            const u64 w = weigh(ls.z[i]);
-            if (w < least) continue;
-            atomicAdd(&sums[ls.at[i] / kChunk], w);
+        each_listed([&](int at, float z) {
+            if (!inside(border, z, at)) return;
+            const u64 w = weigh(z);
+            if (w < least) return;
+            atomicAdd(&sums[at / kChunk], w);
             ++n;
-        }
+        });
         n = wave_sum_i(n);
         if (lane == 0) atomicAdd(&ls.kept, n);
         __syncthreads();

@@ -124,6 +124,13 @@ def test_far_tails_and_wide_ranges(H, n):
     check(H, z, k=[0, n // 2, n // 2, n - 5, 0, 300, 0], p=[0.9, 1, 1, 1, 0.999, 0.9, 1], m=[0, 0, 0, 0, 0, 0, 1e-6], T=[1, 1, 1, 1, 0.1, 3, 1])
 
 
+@pytest.mark.parametrize("n", [16384, 40000, 200003, 1 << 20])
+@pytest.mark.parametrize("scale", [0.01, 0.2, 1.0, 8.0])
+def test_narrow_and_wide_rows(H, n, scale):
+    # thousands of entries where the border lies, or all of them
+    check(H, logits(n, 5, n, scale), k=[0, n // 3, 0, 5000, n // 2], p=[0.9, 1, 0.3, 0.9, 0.95], m=[0, 0, 0.3, 0, 0])
+
+
 @pytest.mark.parametrize("n", [300, 16384, 70000])
 def test_infinities_and_nan(H, n):
     z = logits(n, 10, n)
