@@ -14,7 +14,11 @@
 // Up to 16384 entries one workgroup of 1024 threads has a row in its registers (sample_filtered_kernel).  Longer rows are cut into parts, a
 // workgroup each, in three launches: the parts' bins (filter_bins_kernel); sums of what is kept for certain, and the entries of the bins
 // that a border may be in (filter_parts_kernel); the borders and the draw, a workgroup a row (filter_draw_kernel).  A row whose border bins hold
-// too many entries for that, or whose logits are beyond the bins' grid, is read again and again by that last workgroup alone.
+// more than a quarter of a part, or whose logits are beyond the bins' grid, is read again and again by that last workgroup alone.
+//
+// What bounds it: latencies.  One row of 16384 entries, 15.4 us, is twelve steps of a workgroup with a barrier behind each; 96 rows of
+// which some have no top-k, 21 us, half of that the exponentials of 16 entries a thread; 48 rows of 65536, 38 us, three launches whose workgroups
+// are done in 5, 9 and 7 us.
 #include "filtered.h"
 #include "paged.h"
 #include "sample_rows.h"
@@ -33,6 +37,7 @@ typedef unsigned long long u64;
 constexpr int kBinCount = 1024, kFine = 512;     // linear bins; those of a closer look
 constexpr float kPerUnit = 32.f;     // bins of a unit of z
 constexpr int kPartBins = 512;       // bins of a part of a long row
+constexpr int kLooks = 7;             // closer looks there can be: 32 bits of a key and 20 of an index, nine at a time
 constexpr int kFew = 64;             // entries that are ranked against each other (a look at 220 takes 1.6 us, ranking them 4)
 constexpr int kChunk = 256;          // entries that a wave has of four a lane: sums of kept weights are held for each
 constexpr int kMostEntries = 1 << 20, kChunks = kMostEntries / kChunk;
@@ -262,7 +267,7 @@ __device__ __forceinline__ Found find_border(const Each& each, const Weigh& weig
         r.lo = sh.lo;
         r.hi = sh.hi;
     }
-    while (r.m > (unsigned)kFew) {
+    for (int look = 0; look < kLooks && r.m > (unsigned)kFew; ++look) {
         const bool by_key = r.lo < r.hi;
         const unsigned span = by_key ? r.hi - r.lo : (unsigned)(r.last - r.first);
         const int s = max(0, 32 - __clz((int)span) - 9);     // (nine bits: kFine bins)
