@@ -529,7 +529,7 @@ int64_t hawk_paged_entry(const hawk_paged_cache* cache, const int32_t* table_row
  * page (images of one prompt): a page that more than one place has is never written, hawk_paged_take gives the writer one of its own first.
  * Counts below 0 are free pages; what the arrays hold is checked as everywhere: no page outside the pool is read, written or counted.
  *
- * hawk_paged_fork: sequence dst[i] becomes a second holder of what sequence src[i] has committed (i < n, n <= n_seq): its row of the table gets
+ * hawk_paged_fork: sequence dst[i] becomes a second holder of what sequence src[i] has committed (i < n, n <= n_seq, 2^23 at most): its row of the table gets
  *   the pages of the first n_past[src[i]] entries, n_past[dst[i]] that length, and the pages it held until now are given back.  A pair
  *   is left out if either number is no sequence, both are the same, an earlier pair has the same dst, or its src is the dst of any pair.
  * hawk_paged_take: pages for entries n_past[s] .. n_past[s] + n_new[s] - 1 of every sequence with n_new[s] > 0 (those up to max_pages *
@@ -540,7 +540,7 @@ int64_t hawk_paged_entry(const hawk_paged_cache* cache, const int32_t* table_row
  * hawk_paged_trim: the pages behind the first n_past[s] entries are given back (n_past[s] = 0: all of them; negative: the sequence is left alone).
  * hawk_paged_compact: the pages in use (refs > 0), U of them, come to lie in pages 0 .. U - 1: those behind are moved, in all layers, in
  *   ascending order into the free ones before, in ascending order.  table_out (row s table_out_stride places behind row s - 1) and refs_out
- *   get the table and the counts as they are then, in place or elsewhere; places of pages that are not in use become -1.  n_used: U.
+ *   get the table and the counts as they are then, in place (the table with its own stride) or elsewhere; places of pages that are not in use become -1.  n_used: U.
  *   No entry that the old table leads to is overwritten.
  * hawk_paged_copy: page src[i] of one pool goes to page dst[i] of another (or the same) of equal type, layers, heads, head_dim and page_size, all
  *   layers, i < n, n <= 2^20; pairs with a page outside its pool are left out.  A page that is written twice, or written and read, holds either.

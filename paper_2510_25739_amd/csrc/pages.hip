@@ -269,9 +269,10 @@ __global__ __launch_bounds__(256) void paged_copy_kernel(CopyArgs a) {
         else { mv.from = a.src[m]; mv.to = a.dst[m]; }
         if (!in_pool(a.from, mv.from) || !in_pool(a.to, mv.to)) continue;
         // pieces of a head's entries; the batch's first head and its place in it
-        const int per = mv.n * a.pieces.d, unit0 = (int)((int64_t)batch * kBatch / per), left = a.units.d - unit0;
-        const int at0 = (int)((int64_t)batch * kBatch - (int64_t)unit0 * per);
-        if (left <= 0) continue;
+        const int per = mv.n * a.pieces.d;
+        const int64_t head0 = (int64_t)batch * kBatch / per;         // (of a page of 2^30 pieces a part can be one: up to 2^39)
+        if (head0 >= a.units.d) continue;
+        const int unit0 = (int)head0, left = a.units.d - unit0, at0 = (int)((int64_t)batch * kBatch - head0 * per);
         const int64_t x0 = mv.from * a.from.page_stride, y0 = mv.to * a.to.page_stride;
         auto head_at = [&](int unit, const char*& from, char*& to) {
             const int lk = unit / a.heads, head = unit - lk * a.heads.d;
@@ -367,7 +368,7 @@ int launch_paged_fork(const hawk_paged_cache* cache, int32_t* refs, int32_t* n_p
     PagedView c;
     if (!paged_view(cache, 0, &c) || n < 0 || n > c.n_seq) return HAWK_EINVAL;
     if (n == 0) return HAWK_OK;
-    if (!refs || !n_past || !src || !dst) return HAWK_EINVAL;
+    if (!refs || !n_past || !src || !dst || n > (1 << 23)) return HAWK_EINVAL;
     paged_fork_kernel<<<(unsigned)n, 256, 0, stream>>>(c, const_cast<int32_t*>(c.table), refs, n_past, src, dst, n);
     return status();
 }
@@ -411,6 +412,7 @@ int launch_paged_compact(const hawk_paged_cache* cache, const int32_t* refs, int
     CopyArgs m = {};
     if (!whole_view(cache, &m.from) || !refs || !refs_out || !n_used || !workspace || !aligned16(workspace)) return HAWK_EINVAL;
     if (m.from.n_seq > 0 && (!table_out || table_out_stride < m.from.max_pages)) return HAWK_EINVAL;
+    if (m.from.n_seq > 1 && table_out == cache->table && table_out_stride != cache->table_stride) return HAWK_EINVAL;
     const Room r = room_of(cache, workspace);
     if (workspace_bytes < r.bytes) return HAWK_ENOMEM;
     m.to = m.from;

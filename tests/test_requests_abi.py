@@ -66,9 +66,11 @@ def test_bad_page_calls_are_refused(L):
             refused(which, **{name: None})
     refused("fork", n=-1)
     refused("fork", n=4)                # more pairs than sequences
+    refused("fork", n=(1 << 23) + 1, c=cache(n_seq=1 << 24))
     refused("copy", n=-1)
     refused("copy", n=(1 << 20) + 1)
     refused("compact", stride=7)
+    refused("compact", stride=9)         # in place, but rows that would be written over rows not yet read
     for which in ("take", "compact"):
         refused(which, ws=ONE + 8)
         refused(which, -3, nws=need - 1)
