@@ -736,11 +736,11 @@ template <int E> __device__ __forceinline__ void whole_row(const FilterArgs& a, 
     }
 }
 
-template <int E> __global__ __launch_bounds__(NT) void sample_filtered_kernel(FilterArgs a) {
+template <int E> __global__ __launch_bounds__(NT) void sample_filtered_kernel(FilterArgs a, int row0) {
     __shared__ CutShared sh;
     __shared__ u64 sums[64];
     __shared__ TopList list;
-    const int r = blockIdx.x;
+    const int r = row0 + (int)blockIdx.x;
     if (a.skip && a.skip[r] < 0) {
         if (threadIdx.x == 0) give(a, r, -1, 0.f, 0);
         return;
@@ -1165,7 +1165,10 @@ template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(Filter
     if (tid == 0 && a.out_kept) a.out_kept[r] = ls.kept;
 }
 
-// Rows in parts, as many at a time as kPartsAtOnce parts (so that the workspace does not grow with the rows).
+// Rows in parts, as many at a time as kPartsAtOnce parts (so that the workspace does not grow with the rows).  Parts as small as keep them one to a
+// unit: a larger part takes its unit longer, more parts than units take turns (us with 8 / 16 / 32 entries a thread: 16 rows of 65536,
+// 128 / 64 / 32 parts, 29.9 / 34.9 / 47.6; 48 of them, 384 / 192 / 96, 40.8 / 36.7 / 47.8; 512 of them 204 / 185 / 164; 2 of 200003 35.9 / 41.6 / 58.9; 32 of
+// them, 800 / 416 / 224, 79.8 / 69.1 / 64).
 constexpr int kPartsAtOnce = 2048;
 struct Cutting { int E, parts, rows; };          // entries of a thread (0: rows are not cut), parts of a row, rows at a time
 inline Cutting cutting_of(int rows, int n) {
@@ -1177,6 +1180,10 @@ inline Cutting cutting_of(int rows, int n) {
     c.parts = parts(c.E);
     c.rows = std::min(rows, kPartsAtOnce / c.parts);
     return c;
+}
+template <int E> void launch_rows(const FilterArgs& a, int rows, hipStream_t stream) {
+    constexpr int kMost = 1 << 21;               // a launch has fewer than 2^32 threads
+    for (int r = 0; r < rows; r += kMost) sample_filtered_kernel<E><<<(unsigned)std::min(kMost, rows - r), NT, 0, stream>>>(a, r);
 }
 template <int E> void launch_parts(FilterArgs a, const Cutting& c, int rows, hipStream_t stream) {
     for (int r = 0; r < rows; r += c.rows) {
@@ -1214,9 +1221,9 @@ int launch_sample_filtered(const void* logits, int dtype, int64_t row_stride, co
     int log = 0;
     while ((1 << log) < n) ++log;
     a.unit = std::min(51, 62 - log);
-    if (n <= 4 * NT) sample_filtered_kernel<4><<<(unsigned)rows, NT, 0, stream>>>(a);
-    else if (n <= 8 * NT) sample_filtered_kernel<8><<<(unsigned)rows, NT, 0, stream>>>(a);
-    else if (n <= 16 * NT) sample_filtered_kernel<16><<<(unsigned)rows, NT, 0, stream>>>(a);
+    if (n <= 4 * NT) launch_rows<4>(a, rows, stream);
+    else if (n <= 8 * NT) launch_rows<8>(a, rows, stream);
+    else if (n <= 16 * NT) launch_rows<16>(a, rows, stream);
     else if (c.E == 8) launch_parts<8>(a, c, rows, stream);
     else if (c.E == 16) launch_parts<16>(a, c, rows, stream);
     else launch_parts<32>(a, c, rows, stream);

@@ -186,6 +186,20 @@ def test_skipped_rows_and_many_rows(H):
     assert H.sample_filtered(e, torch.empty(0, device=DEV))[0].shape == (0,)
 
 
+def test_the_most_rows_there_can_be(H):
+    import torch
+    rows = 1 << 22                                       # more workgroups than one launch has
+    r = np.random.RandomState(3)
+    x = torch.from_numpy(r.randn(5).astype(np.float32)).to(DEV).repeat(rows, 1)
+    u = torch.arange(rows, dtype=torch.int32, device=DEV).remainder(1 << 12).float() / (1 << 12)
+    skip = torch.zeros(rows, dtype=torch.int32, device=DEV)
+    skip[:-4096] = -1                                    # (one pass over u)
+    token, _, kept = H.sample_filtered(x, u, skip=skip)
+    want = [draw(x[0].cpu().numpy(), v, 1.0, 0, 1.0, 0.0)[0] for v in u[-4096:].cpu().numpy()]
+    assert token[-4096:].tolist() == want and bool((kept[-4096:] == 5).all())
+    assert bool((token[:-4096] == -1).all()) and bool((kept[:-4096] == 0).all())
+
+
 def test_draws_follow_the_cut_distribution(H):
     # 2^16 draws of one row: counts within five standard deviations of what the probabilities say (one in 10^6 a token, 9 tokens)
     import torch
