@@ -49,6 +49,7 @@ struct FilterArgs {
     const int32_t *skip, *top_k;
     const float *u, *temperature, *top_p, *min_p;
     int dtype, n, unit;              // unit: S
+    unsigned apart;                  // fp32 steps between scaled logits that differ, at least (see find_border)
     int32_t *out_token, *out_kept;
     float* out_prob;
     // rows in parts
@@ -244,10 +245,12 @@ __device__ __forceinline__ Picked pick_bin(const unsigned* count, const u64* mas
 // The border of a cut within a range.  each(f): f(index, z) of this thread's entries that may be in it.  masses: weights count.  All threads
 // call, sh.n is zero; what it leaves in sh is read until the next barrier.
 template <class Each>
-__device__ __forceinline__ Found find_border(const Each& each, const Weigh& weigh, bool masses, const Cut& cut, Range r, CutShared& sh, bool ties = false) {
+__device__ __forceinline__ Found find_border(const Each& each, const Weigh& weigh, bool masses, const Cut& cut, Range r, CutShared& sh, unsigned apart) {
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
-    // logits of 16 bits: the many are a few values at most, and what the range really spans saves a look or two
-    if (ties && r.m > (unsigned)kFew) {
+    // keys of which there is one value at most: different ones of logits of 16 bits are `apart` (but for those too small to keep their distance)
+    auto single = [&]() { return r.lo == r.hi || (r.hi - r.lo < apart && (r.lo >= 0x80800000u || r.hi <= 0x7F7FFFFFu)); };
+    // logits of 16 bits: the many are a few values at most; where bins are wider than that, what the range really spans saves a look or two
+    if (apart > 1u && r.m > (unsigned)kFew && (r.hi - r.lo) >> 9 >= apart) {
         unsigned lo = 0xFFFFFFFFu, hi = 0u;
         each([&](int, float z) {
             lo = min(lo, fkey(z));
@@ -268,7 +271,7 @@ __device__ __forceinline__ Found find_border(const Each& each, const Weigh& weig
         r.hi = sh.hi;
     }
     for (int look = 0; look < kLooks && r.m > (unsigned)kFew; ++look) {
-        const bool by_key = r.lo < r.hi;
+        const bool by_key = !single();
         const unsigned span = by_key ? r.hi - r.lo : (unsigned)(r.last - r.first);
         const int s = max(0, 32 - __clz((int)span) - 9);     // (nine bits: kFine bins)
         each([&](int j, float z) {
@@ -298,7 +301,7 @@ __device__ __forceinline__ Found find_border(const Each& each, const Weigh& weig
     }
     each([&](int j, float z) {
         const unsigned k = fkey(z);
-        if (k < r.lo || k > r.hi || (r.lo == r.hi && (j < r.first || j > r.last))) return;
+        if (k < r.lo || k > r.hi || j < r.first || j > r.last) return;
         const int i = atomicAdd(&sh.n, 1);
         if (i >= kFew) return;       // (there are r.m of them)
         sh.key[i] = k;
@@ -479,7 +482,7 @@ __device__ __forceinline__ void draw_of_list(const FilterArgs& a, int r, const A
 #pragma unroll
             for (int i = 0; i < 2; ++i)
                 if (z[i] > -INFINITY && bin_of(zmax, z[i]) == p.bin) f(at[i], z[i]);
-        }, weigh, true, cut, bin_range(zmax, p), sh).border;
+        }, weigh, true, cut, bin_range(zmax, p), sh, 1u).border;
     }
     const u64 least = least_of(q, weigh(zmax));
     int n_kept = 0;
@@ -595,7 +598,7 @@ template <int E> __device__ __forceinline__ void whole_row(const FilterArgs& a, 
                 each([&](int j, float v) {
                     if (bin_of(zmax, v) == p.bin) f(j, v);
                 });
-            }, weigh, false, cut, bin_range(zmax, p), sh).border;
+            }, weigh, false, cut, bin_range(zmax, p), sh, 1u).border;
             draw_of_list(a, r, q, zmax, weigh, make_list<E>(z, border, list), list, sh);
             return;
         }
@@ -631,7 +634,7 @@ template <int E> __device__ __forceinline__ void whole_row(const FilterArgs& a, 
                     if (bin_of(zmax, v) == b) f(j, v);
                 });
             };
-            const Found found = find_border(in_bin, weigh, q.by_p, cut, range, sh);
+            const Found found = find_border(in_bin, weigh, q.by_p, cut, range, sh, E > 0 ? 1u : a.apart);
             border = found.border;
             mass = found.mass;
         };
@@ -1110,7 +1113,7 @@ template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(Filter
                 each_listed([&](int at, float z) {
                     if (bin(z) == h.k_bin) f(at, z);
                 });
-            }, weigh, q.by_p, cut, x, sh, a.dtype != HAWK_FP32);
+            }, weigh, q.by_p, cut, x, sh, a.apart);
             border = f.border;
             mass = f.mass;
             __syncthreads();
@@ -1135,7 +1138,7 @@ template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(Filter
                 each_listed([&](int at, float z) {
                     if (in(at, z)) f(at, z);
                 });
-            }, weigh, true, cut, x, sh, a.dtype != HAWK_FP32).border;
+            }, weigh, true, cut, x, sh, a.apart).border;
         }
         int n = 0;
         each_listed([&](int at, float z) {
@@ -1221,6 +1224,8 @@ int launch_sample_filtered(const void* logits, int dtype, int64_t row_stride, co
     int log = 0;
     while ((1 << log) < n) ++log;
     a.unit = std::min(51, 62 - log);
+    // neighbours of 8 (11) bits are 2^15 (2^12) steps of 24 bits apart at least, times any number; each product is rounded by half a step
+    a.apart = dtype == HAWK_BF16 ? (1u << 15) - 1u : (dtype == HAWK_FP16 ? (1u << 12) - 1u : 1u);
     if (n <= 4 * NT) launch_rows<4>(a, rows, stream);
     else if (n <= 8 * NT) launch_rows<8>(a, rows, stream);
     else if (n <= 16 * NT) launch_rows<16>(a, rows, stream);

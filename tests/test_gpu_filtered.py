@@ -186,6 +186,22 @@ def test_skipped_rows_and_many_rows(H):
     assert H.sample_filtered(e, torch.empty(0, device=DEV))[0].shape == (0,)
 
 
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("n", [16384, 20001, 150000])
+def test_many_alike_of_16_bits(H, n, dtype):
+    # borders among thousands of equal logits whose neighbours are as near as the type has them, divided by temperatures that keep them
+    # apart, bring them as near as 24 bits do, and (the last two) make them one, or numbers below the smallest of 24 bits
+    import torch
+    r = np.random.RandomState(n)
+    t = getattr(torch, dtype)
+    for centre, T in ((1.0, 1.0), (-1.99, 1.0), (0.07, 0.7), (3.0, 1.4142135), (-0.004, 0.0078), (1.0, 1e-3), (1.0, 3e37), (1.5, 3e38)):
+        step = torch.finfo(t).eps * abs(centre)
+        x = (centre + step * r.randint(-3, 4, (6, n))).astype(np.float32)
+        x[3:] = -x[3:]
+        x = torch.from_numpy(x).to(t).float().numpy()
+        check(H, x, T=T, k=[0, 100, n // 2, 0, n // 3, 0], p=[0.5, 1.0, 0.7, 0.03, 1.0, 0.9], dtype=dtype)
+
+
 def test_the_most_rows_there_can_be(H):
     import torch
     rows = 1 << 22                                       # more workgroups than one launch has
