@@ -321,17 +321,18 @@ __global__ __launch_bounds__(64 * NW, NR <= 2 ? 4 : 2) void adapter_apply_kernel
     // of fp16 the power of two that brings a row's largest h below 2^14: half a step of a part of the smallest is then 2^-39 of the largest,
     // and nothing overflows
     if (TYPE == HAWK_FP16) {
-        if (threadIdx.x < 64) {
-            float top = 0.f;
-            for (int j = g; j < RP; j += 4) {
-                const float v = fabsf(h[m16][j]);
-                top = fmaxf(top, v <= 3.4028235e38f ? v : 0.f);
-            }
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const int e = top > 0.f ? max(ilogbf(top) - 13, -126) : 0;
-            if (lane < kTile) factor[lane] = __uint_as_float((unsigned)(e + 127) << 23);
+        constexpr int N = 64 * NW / kTile;           // threads of a row
+        const int r = (int)threadIdx.x / N;
+        float top = 0.f;
+#pragma unroll
+        for (int j = threadIdx.x % N; j < RP; j += N) {
+            const float v = fabsf(h[r][j]);
+            top = fmaxf(top, v <= 3.4028235e38f ? v : 0.f);
         }
+#pragma unroll
+        for (int d = 1; d < N; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+        const int e = top > 0.f ? max(ilogbf(top) - 13, -126) : 0;
+        if (threadIdx.x % N == 0) factor[r] = __uint_as_float((unsigned)(e + 127) << 23);
         __syncthreads();
     }
     v4u hv[PP][KS];
