@@ -93,8 +93,8 @@ struct TakeArgs {
 // The pages that are written next.  First what every sequence lacks: places among those of entries n_past .. n_past + n_new - 1 that have no
 // page or one that other places have too.  Then the free pages in ascending order, as many as are lacking.  Then they are handed
 // out, sequences and places in ascending order, a sequence that would need more than there are (and all behind it) left as it
-// was.  The counts that decide are those before the call: they are changed at the end.  72 sequences, 64 of which lack 2 pages of 700: 8 us, nearly
-// all of it dependent latencies.
+// was.  The counts that decide are those before the call: they are changed at the end.  72 sequences, 64 of which lack 2 pages of 700: 6.4 us, nearly
+// all of it dependent latencies (8.2 with the counts requested once it was known how many are lacking).
 __global__ __launch_bounds__(kWide) void paged_take_kernel(TakeArgs a) {
     __shared__ int sums[kWide / 64 + 1], given, moves;
     const PagedView& c = a.c;
@@ -125,6 +125,22 @@ __global__ __launch_bounds__(kWide) void paged_take_kernel(TakeArgs a) {
         for (int p = first + l + width; p < stop; p += width) need += lacks(s, p, page) ? 1 : 0;
         for (int w = 1; w < width; w <<= 1) need += __shfl_xor(need, w);
     };
+    // Free pages among neighbouring counts: the first ones are requested before it is known how many are lacking.
+    auto free_among = [&](int at) {
+        unsigned bits = 0u;
+        if (at + kEach <= c.n_pages) {
+            typedef int i4 __attribute__((ext_vector_type(4), aligned(4)));
+            i4 v[kEach / 4];
+#pragma unroll
+            for (int j = 0; j < kEach / 4; ++j) v[j] = *reinterpret_cast<const i4*>(a.refs + at + 4 * j);
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) bits |= v[j / 4][j % 4] == 0 ? 1u << j : 0u;
+        } else {
+            for (int j = 0; j < kEach && at + j < c.n_pages; ++j) bits |= a.refs[at + j] == 0 ? 1u << j : 0u;
+        }
+        return bits;
+    };
+    const unsigned bits0 = free_among(tid * kEach);
     int wanted = 0;                                  // of this thread's sequences
     for (int s0 = 0; s0 < c.n_seq; s0 += per) {
         look(s0 + (tid >> a.lanes));
@@ -135,9 +151,7 @@ __global__ __launch_bounds__(kWide) void paged_take_kernel(TakeArgs a) {
     const int begin = block_before(wanted, sums, total);
     for (int p0 = 0; p0 < c.n_pages && n_free < total; p0 += kWide * kEach) {
         const int at = p0 + tid * kEach;
-        unsigned bits = 0u;
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) bits |= at + j < c.n_pages && a.refs[min(at + j, c.n_pages - 1)] == 0 ? 1u << j : 0u;
+        unsigned bits = p0 == 0 ? bits0 : free_among(at);
         int all, k = n_free + block_before(__popc(bits), sums, all);
         for (; bits && k < total; bits &= bits - 1u) a.free[k++] = at + __ffs(bits) - 1;
         n_free += all;
