@@ -89,6 +89,24 @@ __device__ __forceinline__ u64 wave_sum_u64(u64 v) {
     ROW_ALLREDUCE(v, addu, dpp_u64)
     return (lane_u64(v, 0) + lane_u64(v, 16)) + (lane_u64(v, 32) + lane_u64(v, 48));
 }
+// Sums over the wave of four numbers a lane: halves of two change places, so that one addition is for both, then rows.  Lanes of row 0 have the
+// first's sum, of row 2 the second's, of row 1 the third's, of row 3 the fourth's.
+__device__ __forceinline__ u64 swap_add32(u64 a, u64 b) {
+    const auto lo = __builtin_amdgcn_permlane32_swap((unsigned)a, (unsigned)b, false, false);
+    const auto hi = __builtin_amdgcn_permlane32_swap((unsigned)(a >> 32), (unsigned)(b >> 32), false, false);
+    return ((u64)hi[0] << 32 | lo[0]) + ((u64)hi[1] << 32 | lo[1]);
+}
+__device__ __forceinline__ u64 swap_add16(u64 a, u64 b) {
+    const auto lo = __builtin_amdgcn_permlane16_swap((unsigned)a, (unsigned)b, false, false);
+    const auto hi = __builtin_amdgcn_permlane16_swap((unsigned)(a >> 32), (unsigned)(b >> 32), false, false);
+    return ((u64)hi[0] << 32 | lo[0]) + ((u64)hi[1] << 32 | lo[1]);
+}
+__device__ __forceinline__ u64 wave_sums_u64(u64 a, u64 b, u64 c, u64 d) {
+    u64 v = swap_add16(swap_add32(a, b), swap_add32(c, d));
+    ROW_ALLREDUCE(v, addu, dpp_u64)
+    return v;
+}
+__device__ __forceinline__ int which_of_four(int lane) { return (lane >> 5) + 2 * (lane >> 4 & 1); }
 __device__ __forceinline__ int wave_sum_i(int v) {
     ROW_ALLREDUCE(v, addi, dpp_i)
     return (__builtin_amdgcn_readlane(v, 0) + __builtin_amdgcn_readlane(v, 16)) + (__builtin_amdgcn_readlane(v, 32) + __builtin_amdgcn_readlane(v, 48));
@@ -670,18 +688,20 @@ template <int E> __device__ __forceinline__ void whole_row(const FilterArgs& a, 
                 weights[e] = inside(border, z[e], entry<E>(e, tid)) ? weigh(z[e]) : 0ull;
             }
         }
+        u64 s[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
-        for (int g = 0; g < E / 4; ++g) {
-            u64 s = 0ull;
+        for (int e = 0; e < E; ++e) {
+            const bool k = kept(z[e], entry<E>(e, tid), weights[e]);
+            weights[e] = k ? weights[e] : 0ull;
+            s[e / 4] += weights[e];
+            n_kept += k ? 1 : 0;
+        }
+        if constexpr (E == 16) {
+            const u64 v = wave_sums_u64(s[0], s[1], s[2], s[3]);
+            if ((lane & 15) == 0) sums[which_of_four(lane) * NW + wave] = v;
+        } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int e = 4 * g + i;
-                const bool k = kept(z[e], entry<E>(e, tid), weights[e]);
-                weights[e] = k ? weights[e] : 0ull;
-                s += weights[e];
-                n_kept += k ? 1 : 0;
-            }
-            add_group(g, s);
+            for (int g = 0; g < E / 4; ++g) add_group(g, s[g]);
         }
     } else {
         for (int g = 0; g < groups; ++g) {
@@ -996,9 +1016,11 @@ template <int E> __global__ __launch_bounds__(NT) void filter_parts_kernel(Filte
     const int sure = q.by_p ? h.p_first : (q.by_k ? h.k_bin : kPartBins);    // bins before this one are kept, but for min-p
     const u64 least = least_of(q, weigh(t.zmax));
     int n_kept = 0;
+    u64 sums[4];
 #pragma unroll
     for (int g = 0; g < E / 4; ++g) {
-        u64 s = 0ull;
+        u64& s = sums[g & 3];
+        s = 0ull;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float z = p.z[4 * g + i];
@@ -1015,8 +1037,13 @@ template <int E> __global__ __launch_bounds__(NT) void filter_parts_kernel(Filte
                 if (at < part_list(E)) room.list[part * part_list(E) + at] = make_int2(__float_as_int(z), p.index(4 * g + i));
             }
         }
-        s = wave_sum_u64(s);
-        if (lane == 0) room.sums[(part * (E / 4) + g) * NW + wave] = s;
+        if constexpr (E == 8) {
+            s = wave_sum_u64(s);
+            if (lane == 0) room.sums[(part * (E / 4) + g) * NW + wave] = s;
+        } else if ((g & 3) == 3) {
+            const u64 v = wave_sums_u64(sums[0], sums[1], sums[2], sums[3]);
+            if ((lane & 15) == 0) room.sums[(part * (E / 4) + g - 3 + which_of_four(lane)) * NW + wave] = v;
+        }
     }
     n_kept = wave_sum_i(n_kept);
     if (lane == 0) atomicAdd(&ps.n_kept, n_kept);
