@@ -870,7 +870,7 @@ template <int E> __global__ __launch_bounds__(NT) void filter_bins_kernel(Filter
         for (int e = 0; e < E; ++e)
             if (p.z[e] > -INFINITY) {
                 const int b = min(cell - cell_of(p.z[e]), kPartBins - 1);
-                atomicAdd(&count[b], 1u);
+                if (q.by_k) atomicAdd(&count[b], 1u);
                 if (q.by_p) atomicAdd(&mass[b], weigh(p.z[e]));
             }
         __syncthreads();
@@ -878,7 +878,7 @@ template <int E> __global__ __launch_bounds__(NT) void filter_bins_kernel(Filter
         const int c = tid < kPartBins ? (int)count[tid] : 0;
         if (tid < kPartBins) {
             if (q.by_p) room.mass[part * kPartBins + tid] = m;
-            room.count[part * kPartBins + tid] = (unsigned)c;
+            if (q.by_k) room.count[part * kPartBins + tid] = (unsigned)c;
         }
         const u64 wm = wave_sum_u64(m);
         const int wc = wave_sum_i(c);
@@ -912,8 +912,9 @@ __device__ __forceinline__ Top row_top(const FilterArgs& a, const RowRoom& room)
 }
 
 struct PartShared {
-    u64 sums[NW], high;
-    double steps[kSteps];
+    u64 sums[NW], most_mass;
+    double steps[kSteps], high[kPartBins], low[kPartBins];
+    unsigned count[kPartBins];
     int counts[NW], n_list, n_kept;
     RowHead head;
 };
@@ -951,41 +952,57 @@ template <int E> __global__ __launch_bounds__(NT) void filter_parts_kernel(Filte
         }
         const unsigned all = (unsigned)wave_sum_i(valid);
         const u64 total = wave_sum_u64(mass);
-        u64 m = 0ull;
+        // Two threads a bin, each with every second part, four parts' bins requested at a time.  The halves of a mass are scaled and added as doubles,
+        // whole numbers where parts are not moved: a third of the instructions of a whole mass, there and back for every part.
+        static_assert(NT == 2 * kPartBins, "two threads a bin");
+        const int half = wave >> 3, bin = tid & (kPartBins - 1);
         unsigned c = 0u;
-        // eight parts' bins are requested at a time (the last bin is what is left)
-        for (int i0 = 0; i0 < a.parts; i0 += 8) {
-            unsigned cs[8];
-            u64 ms[8];
-            int bs[8];
+        u64 m = 0ull;
+        double high = 0.0, low = 0.0;
+        for (int i0 = half; i0 < a.parts; i0 += 8) {
+            unsigned cs[4];
+            u64 ms[4];
+            bool there[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int part_i = min(i0 + i, a.parts - 1), at = part_i * kPartBins;
-                bs[i] = i0 + i < a.parts && tid < kPartBins - 1 ? tid - __builtin_amdgcn_readlane(down, part_i) : -1;
-                cs[i] = 0u;
-                ms[i] = 0ull;
-                if (tid < kPartBins) {
-                    cs[i] = room.count[at + max(bs[i], 0)];
-                    if (q.by_p) ms[i] = room.mass[at + max(bs[i], 0)];
-                }
+            for (int j = 0; j < 4; ++j) {
+                const int i = min(i0 + 2 * j, a.parts - 1), from = bin - __builtin_amdgcn_readlane(down, i), at = i * kPartBins + max(from, 0);
+                there[j] = i0 + 2 * j < a.parts && from >= 0;
+                cs[j] = q.by_k ? room.count[at] : 0u;
+                ms[j] = q.by_p ? room.mass[at] : 0ull;
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const double f = lane_d(scale, min(i0 + i, a.parts - 1));
-                if (bs[i] < 0) continue;
-                c += cs[i];
-                m += bs[i] == tid ? ms[i] : (u64)((double)ms[i] * f);
+            for (int j = 0; j < 4; ++j) {
+                const double f = there[j] ? lane_d(scale, min(i0 + 2 * j, a.parts - 1)) : 0.0;
+                c += there[j] ? cs[j] : 0u;
+                high = fma((double)(unsigned)(ms[j] >> 32), f, high);
+                low = fma((double)(unsigned)ms[j], f, low);
             }
         }
+        if (half == 1) {
+            ps.high[bin] = high;
+            ps.low[bin] = low;
+            ps.count[bin] = c;
+        }
+        __syncthreads();
+        if (half == 0) {
+            high += ps.high[bin];
+            low += ps.low[bin];
+            c += ps.count[bin];
+            const double whole = floor(high);
+            m = ((u64)whole << 32) + (u64)fma(high - whole, 0x1p32, low);
+            if (!q.by_k) c = m > 0ull ? 1u : 0u;     // (entries are not counted then: a border by mass is in a bin that has some)
+        } else {
+            c = 0u;
+        }
         Bin b = scan_bins(c, m, q.by_p, ps.counts, ps.sums);
-        b.all = all;
+        b.all = q.by_k ? all : 0xFFFFFFFFu;
         if (tid == kPartBins - 1) {
-            b.m = all - b.ahead;
             b.mass = total > b.before ? total - b.before : 0ull;
+            b.m = q.by_k ? all - b.ahead : (b.mass > 0ull ? 1u : 0u);
         } else if (tid >= kPartBins) {
             b.m = 0u;
         }
-        u64 low = total, high = total;
+        u64 least_mass = total, most_mass = total;       // that a top-k keeps
         const Cut by_k = {1ull << 63, q.k};
         if (tid == 0) ps.head.total = total;
         if (q.by_k) {
@@ -994,14 +1011,14 @@ template <int E> __global__ __launch_bounds__(NT) void filter_parts_kernel(Filte
                 ps.head.k_m = b.m;
                 ps.head.k_ahead = b.ahead;
                 ps.head.k_before = b.before;
-                ps.high = b.before + b.mass;
+                ps.most_mass = b.before + b.mass;
             }
             __syncthreads();
-            low = ps.head.k_before;
-            high = ps.high;
+            least_mass = ps.head.k_before;
+            most_mass = ps.most_mass;
         }
         if (q.by_p) {                // (what scaling the parts' masses has rounded is far below 2^-30)
-            const u64 first = share_of(q.top_p, low), last = share_of(q.top_p, high);
+            const u64 first = share_of(q.top_p, least_mass), last = share_of(q.top_p, most_mass);
             const Cut c0 = {maxu64(first - (first >> 30), 1ull), q.k}, c1 = {last + (last >> 30) + 1ull, q.k};
             if (holds(b, c0)) {
                 ps.head.p_first = tid;
