@@ -3,7 +3,9 @@
 // Rows are grouped by adapter into tiles of 16, once a step (the plan), so that an adapter that many requests use is read once for 16 of
 // their rows.  One launch a projection: a workgroup has a tile and some of the columns.  Its waves share the sum over d_in - both
 // operands of A x go from memory straight into the matrix units' registers, 16 bytes a lane -, their parts are added in shared memory, and
-// B h is added to base on the way out.  Both products are computed transposed (h^T = A x^T, out^T = B h^T): a result lane then has neighbouring
+// B h is added to base on the way out.  What bounds it: of single tokens memory (200 rows of 64 adapters of rank 32, 4096 by 11008, 67 MB, 15.1 us in
+// turn with other inputs: 4.4 TB/s) and of prompts (4724 rows of 4096 by 4096, 117 MB, 32 us cold, 24 with what the last-level cache holds of a repeated
+// input); of few rows a chain of latencies (plan, x and A, h, B; one row 3.5 us, of which 3 are a launch).  Both products are computed transposed (h^T = A x^T, out^T = B h^T): a result lane then has neighbouring
 // elements of one row.
 #include "adapters.h"
 #include "paged.h"
@@ -177,8 +179,8 @@ __device__ __forceinline__ void wave_order() {
 // TYPE: of x and the weights; OUT: of base and out.  NR: groups of 16 of the rank.  NW waves.
 // x, A, B, base and out pass between memory and registers as rows' whole 128 bytes, eight rows (four of 256) an instruction, and change places
 // with the matrix units' layout - a lane has 16 bytes of one of 16 rows - in shared memory of the wave's own: read in that layout, with 64
-// bytes of 16 rows an instruction, memory gave 3.3 instead of 4.4 TB/s, and x, base and out together, 4400 rows of 4096, took 35 instead of
-// 28 us.
+// bytes of 16 rows an instruction, memory gave 3.3 instead of 4.4 TB/s, and x, base and out together, 4400 rows of 4096 without their products, took 35
+// instead of 28 us.
 template <int TYPE, int OUT, int NR, int NW>
 __global__ __launch_bounds__(64 * NW, NR <= 2 ? 4 : 2) void adapter_apply_kernel(ApplyArgs a) {
     using T = Of<TYPE>;
@@ -471,9 +473,9 @@ int launch_adapter_apply(const hawk_adapters* w, const void* plan, size_t plan_b
     a.x_row = x->row_stride; a.base_row = base ? base->row_stride : 0; a.out_row = out->row_stride;
     a.n_adapters = w->n_adapters; a.rank = w->rank; a.d_in = w->d_in; a.d_out = w->d_out; a.rows = rows;
     a.tiles = most_tiles(rows, w->n_adapters);
-    // Every part of a tile's columns makes the tile's h again, so as many as there are idle units to do it (us with 1 / 2 / 3 / 4 / 6 / 8 parts: 6 tiles of
-    // 1280 by 3456, rank 16, 8.9 / 6.7 / 6.1 / 5.5 / 5.4 / 4.8; 64 of 4096 by 11008, rank 32, 23.2 / 16.8 / 15.6 / 15.3 / 17.7 / 16.6; 280 of 4096 by 4096,
-    // rank 16, 31.6 / 32.1 / 34.1 / 36.6 / 42.8 / 49; 50 of 1280 by 1000, rank 128, 18.3 / 14.9 / 15.1 / 26.2 / 26.3 / 34).
+    // Every part of a tile's columns makes the tile's h again, so as many as there are idle units to do it (us with 1 / 2 / 3 / 4 / 6 / 8 parts, by the tiles there can be: 15 of
+    // 1280 by 3456, rank 16, 8.8 / 6.6 / 6.0 / 5.4 / 5.3 / 4.7; 77 of 4096 by 11008, rank 32, 27.0 / 18.3 / 15.6 / 15.4 / 17.6 / 16.9; 304 of 4096 by 4096,
+    // rank 16, 31.5 / 30.9 / 33.7 / 37.3 / 43.3 / 48; 80 of 1280 by 1000, rank 128, 15.6 / 13.1 / 13.2 / 23.3 / 23.4 / 29.8).
     const int groups = (a.d_out + 63) / 64, parts = std::max(1, std::min((groups + kWaves - 1) / kWaves, 256 / std::max(1, a.tiles)));
     a.parts = divisor(parts);
     const int64_t grid = (int64_t)(a.tiles + 7) / 8 * 8 * parts;

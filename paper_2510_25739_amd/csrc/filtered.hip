@@ -16,9 +16,10 @@
 // that a border may be in (filter_parts_kernel); the borders and the draw, a workgroup a row (filter_draw_kernel).  A row whose border bins hold
 // more than a quarter of a part, or whose logits are beyond the bins' grid, is read again and again by that last workgroup alone.
 //
-// What bounds it: latencies.  One row of 16384 entries, 15.4 us, is twelve steps of a workgroup with a barrier behind each; 96 rows of
-// which some have no top-k, 21 us, half of that the exponentials of 16 entries a thread; 48 rows of 65536, 38 us, three launches whose workgroups
-// are done in 5, 9 and 7 us.
+// What bounds it: not memory (48 rows of 65536 are 2.6 us of it) but a workgroup's instructions and barriers.  One row of 16384 entries, 15.4 us, is
+// a dozen steps of sixteen waves with a barrier behind each, 1450 vector instructions a wave, which take 10 us to issue; 96 rows of which some have no top-k
+// 21 us, the exponentials of 16 entries a thread among them; 48 rows of 65536 36.7 us, three launches of 10.8, 14.4 and 10.8, of which nearly 4 each is
+// a launch; 4 of 200003, 16 bits, 38 us.
 #include "filtered.h"
 #include "paged.h"
 #include "sample_rows.h"
@@ -1214,8 +1215,8 @@ template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(Filter
 
 // Rows in parts, as many at a time as kPartsAtOnce parts (so that the workspace does not grow with the rows).  Parts as small as keep them one to a
 // unit: a larger part takes its unit longer, more parts than units take turns (us with 8 / 16 / 32 entries a thread: 16 rows of 65536,
-// 128 / 64 / 32 parts, 29.9 / 34.9 / 47.6; 48 of them, 384 / 192 / 96, 40.8 / 36.7 / 47.8; 512 of them 204 / 185 / 164; 2 of 200003 35.9 / 41.6 / 58.9; 32 of
-// them, 800 / 416 / 224, 79.8 / 69.1 / 64).
+// 128 / 64 / 32 parts, 29.5 / 34.4 / 46.1; 48 of them, 384 / 192 / 96, 39.3 / 36.0 / 46.4; 512 of them 195 / 178 / 158; 2 of 200003 33.1 / 39.7 / 56.5; 32 of
+// them, 800 / 416 / 224, 73.6 / 67.3 / 61.7).
 constexpr int kPartsAtOnce = 2048;
 struct Cutting { int E, parts, rows; };          // entries of a thread (0: rows are not cut), parts of a row, rows at a time
 inline Cutting cutting_of(int rows, int n) {
