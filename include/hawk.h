@@ -567,7 +567,8 @@ int hawk_paged_copy(const hawk_paged_cache* from, const hawk_paged_cache* to, co
  * elements, pointers 16-byte aligned.  x and the weights of one type, base and out of one (any) type; out overlaps nothing but base,
  * and that only as a whole.  A x and B h are summed in fp32; A x enters the second product with 16 bits (bf16; 24 if out is fp32), 22 bits below
  * a row's largest (fp16) or 24 (fp32); the sum is rounded once to out's type.  Weights are finite numbers; an infinity or NaN in a row of x
- * stays in that row. */
+ * stays in that row.  workspace (16-byte aligned, may be NULL where the size function, of the weights' sizes and rows, says 0):
+ * hawk_adapter_apply_workspace_bytes; nothing in it has to be cleared or is kept. */
 typedef struct {
     const void *a, *b;
     int64_t a_adapter_stride, a_row_stride, b_adapter_stride, b_row_stride;
@@ -584,7 +585,8 @@ size_t hawk_adapter_plan_bytes(int rows, int n_adapters);
 int hawk_adapter_plan(const int32_t* row_start, const int32_t* adapter, int n_seq, int rows, int n_adapters, void* plan, size_t plan_bytes,
                       void* stream);
 int hawk_adapter_apply(const hawk_adapters* weights, const void* plan, size_t plan_bytes, int rows, const hawk_matrix* x, const hawk_matrix* base,
-                       const hawk_matrix* out, void* stream);
+                       const hawk_matrix* out, void* workspace, size_t workspace_bytes, void* stream);
+size_t hawk_adapter_apply_workspace_bytes(const hawk_adapters* weights, int rows);
 
 /* One draw per row from logits that the caller has, each row with parameters of its own (arrays of rows values in device memory; NULL: the
  * value in brackets): temperature [1], top_k [0], top_p [1], min_p [0].

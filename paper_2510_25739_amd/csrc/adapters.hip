@@ -1,7 +1,8 @@
 // Low-rank adapters of many requests beside a shared projection: out[r] = base[r] + scale[a] B_a (A_a x[r]), a the adapter of row r's sequence.
 //
 // Rows are grouped by adapter into tiles of 16, once a step (the plan), so that an adapter that many requests use is read once for 16 of
-// their rows.  One launch a projection: a workgroup has a tile and some of the columns.  Its waves share the sum over d_in - both
+// their rows.  One launch a projection: a workgroup has a tile and some of the columns (two launches, the first of
+// sums over parts of d_in, where a few tiles' A would be a few units' to read).  Its waves share the sum over d_in - both
 // operands of A x go from memory straight into the matrix units' registers, 16 bytes a lane -, their parts are added in shared memory, and
 // B h is added to base on the way out.  What bounds it: of single tokens memory (200 rows of 64 adapters of rank 32, 4096 by 11008, 67 MB, 15.1 us in
 // turn with other inputs: 4.4 TB/s) and of prompts (4724 rows of 4096 by 4096, 117 MB, 32 us cold, 24 with what the last-level cache holds of a repeated
@@ -106,7 +107,12 @@ struct ApplyArgs {
     int64_t a_adapter, a_row, b_adapter, b_row, x_row, base_row, out_row;   // elements
     int n_adapters, rank, d_in, d_out, rows, tiles;
     Divisor parts;                   // workgroups of a tile
+    int step;                        // kWhole; in two launches kShrink, kExpand
+    int splits;                      // of the sum over d_in (two launches)
+    float* sums;                     // [tile][split][rank / 16, rounded up][row][16]
 };
+
+enum { kWhole, kShrink, kExpand };
 
 template <int TYPE> struct Of;
 template <> struct Of<HAWK_BF16> {
@@ -219,7 +225,7 @@ __global__ __launch_bounds__(64 * NW, NR <= 2 ? 4 : 2) void adapter_apply_kernel
     const int groups = (a.d_out + 63) >> 6, step = a.parts.d * NW, piece = (lane & (LR - 1)) * Piece<OUT>::kN;
     int q = part * NW + wave;
     if (none) {                          // base alone
-        if (a.base == a.out) return;
+        if (a.base == a.out || a.step == kShrink) return;
         for (; q < groups; q += step)
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
@@ -234,12 +240,13 @@ __global__ __launch_bounds__(64 * NW, NR <= 2 ? 4 : 2) void adapter_apply_kernel
     char* mine = own[wave];
     auto place = [&](int r, int p) { return r * 128 + ((p ^ r) & 7) * 16; };   // of a stage: pieces turned by the row, so that lanes do not meet
 
-    // h^T = A x^T, the waves in turns of 128 bytes of every row
-    f32x4 acc[NR];
+    // h^T = A x^T, the waves (of a tile's workgroups, where they share the sum) in turns of 128 bytes of every row
+    if (a.step != kExpand) {
+        f32x4 acc[NR];
 #pragma unroll
-    for (int j = 0; j < NR; ++j) acc[j] = (f32x4){0.f, 0.f, 0.f, 0.f};
-    {
+        for (int j = 0; j < NR; ++j) acc[j] = (f32x4){0.f, 0.f, 0.f, 0.f};
         const int r8 = lane >> 3, bytes = a.d_in * ES, stages = (bytes + 127) >> 7;
+        const int first = a.step == kShrink ? q : wave, turn = a.step == kShrink ? step : NW;
         const int xr[2] = {row_of(r8), row_of(8 + r8)};
         const char* x[2];
         const char* w[2 * NR];
@@ -263,17 +270,17 @@ __global__ __launch_bounds__(64 * NW, NR <= 2 ? 4 : 2) void adapter_apply_kernel
             }
         };
 #pragma unroll
-        for (int d = 0; d < D1; ++d) request(wave + d * NW, ahead[d]);
-        for (int t = wave; t < stages; t += D1 * NW)
+        for (int d = 0; d < D1; ++d) request(first + d * turn, ahead[d]);
+        for (int t = first; t < stages; t += D1 * turn)
 #pragma unroll
             for (int d = 0; d < D1; ++d) {
-                if (t + d * NW >= stages) break;
+                if (t + d * turn >= stages) break;
 #pragma unroll
                 for (int i = 0; i < 2; ++i) *reinterpret_cast<v4u*>(mine + place(8 * i + r8, lane)) = ahead[d].x[i];
 #pragma unroll
                 for (int i = 0; i < 2 * NR; ++i) *reinterpret_cast<v4u*>(mine + place(16 + 8 * i + r8, lane)) = ahead[d].w[i];
                 wave_order();
-                request(t + (d + D1) * NW, ahead[d]);
+                request(t + (d + D1) * turn, ahead[d]);
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
                     const v4u xv = *reinterpret_cast<const v4u*>(mine + place(m16, 4 * s + g));
@@ -308,17 +315,32 @@ __global__ __launch_bounds__(64 * NW, NR <= 2 ? 4 : 2) void adapter_apply_kernel
             if (a.base && row[i] >= 0 && q * 64 + piece < a.d_out) c.y[i].load(a.base, row[i] * a.base_row + q * 64 + piece);
         }
     };
+    if (a.step != kShrink)
 #pragma unroll
-    for (int d = 0; d < D2; ++d) request(q + d * step, ahead[d]);
+        for (int d = 0; d < D2; ++d) request(q + d * step, ahead[d]);
 
     __syncthreads();
     for (int i = threadIdx.x; i < kTile * RP; i += 64 * NW) {
         const int j = i / (kTile * 16), r = (i >> 4) & 15, c = i & 15;
         float s = 0.f;
+        if (a.step == kExpand) {
+            const float* from = a.sums + (int64_t)tile * a.splits * (kTile * RP) + i;
+            for (int k0 = 0; k0 < a.splits; k0 += 8) {
+                float v[8];
 #pragma unroll
-        for (int v = 0; v < NW; ++v) s += *reinterpret_cast<const float*>(own[v] + i * 4);
-        h[r][j * 16 + c] = j * 16 + c < a.rank ? s : 0.f;
+                for (int k = 0; k < 8; ++k) v[k] = k0 + k < a.splits ? from[(k0 + k) * (kTile * RP)] : 0.f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) s += v[k];
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < NW; ++v) s += *reinterpret_cast<const float*>(own[v] + i * 4);
+            s = j * 16 + c < a.rank ? s : 0.f;
+            if (a.step == kShrink) a.sums[((int64_t)tile * a.splits + part) * (kTile * RP) + i] = s;
+        }
+        h[r][j * 16 + c] = s;
     }
+    if (a.step == kShrink) return;
     __syncthreads();
     // of fp16 the power of two that brings a row's largest h below 2^14: half a step of a part of the smallest is then 2^-39 of the largest,
     // and nothing overflows
@@ -433,7 +455,34 @@ template <int TYPE> void launch_typed(const ApplyArgs& a, int out, unsigned grid
     else launch_rank<TYPE, HAWK_FP16>(a, grid, stream);
 }
 
+// In how many workgroups a tile's sum over d_in is made, in a launch of its own (0: in every one that has some of its columns).  A unit reads A at 75 GB/s,
+// whatever lies behind it; s of them save (s - 1) / s of that and cost a launch, 1.7 us in a graph and 5 for the host (us in one launch / two, in a
+// graph: one row, 4096 by 4096, rank 32 7.6 / 6.1, 64 11.0 / 8.2, 128 20.2 / 13.4; 11008 by 4096, rank 16 10.3 / 5.9, 32 13.6 / 6.6, 128 38.5 / 17.1; three workgroups a
+// tile, 64 rows of 64 adapters, 4096 by 4096, rank 64 16.3 / 18.1, 11008 by 4096, rank 32 17.9 / 16.2, 128 73 / 61; two, 1500 rows, 4096 by 4096, rank 128
+// 30.4 / 30.8, 11008 by 4096, rank 64 29.5 / 26.2).  The border is where calls that are not captured lose nothing either (one row of 4096 by 4096, rank 64
+// 11.4 / 13.3; of 11008, rank 32 13.8 / 12.9).
+constexpr int64_t kSplitBytes = 400 << 10;
+int splits_of(const hawk_adapters* w, int tiles) {
+    const int64_t row = w->d_in * (int64_t)type_bytes(w->dtype), stages = (row + 127) / 128;
+    const int64_t most = std::min<int64_t>(256 / std::max(tiles, 1), (stages + kWaves - 1) / kWaves);
+    return most >= 2 && row * w->rank * (most - 1) >= kSplitBytes * (most + 1) ? (int)most : 0;
+}
+size_t sums_bytes(const hawk_adapters* w, int tiles, int splits) {
+    const int nr = w->rank <= 16 ? 1 : (w->rank <= 32 ? 2 : (w->rank <= 64 ? 4 : 8));
+    return (size_t)tiles * splits * kTile * 16 * nr * sizeof(float);
+}
+bool weights_ok(const hawk_adapters* w) {
+    return w && is_type(w->dtype) && w->n_adapters >= 0 && w->rank >= 8 && w->rank <= 128 && w->rank % 8 == 0 && w->d_in >= 8 && w->d_in % 8 == 0 &&
+           w->d_out >= 8 && w->d_out % 8 == 0 && w->d_in <= (1 << 24) && w->d_out <= (1 << 24);
+}
+
 }  // namespace
+
+size_t adapter_apply_workspace_bytes(const hawk_adapters* w, int rows) {
+    if (!weights_ok(w) || rows < 1 || adapter_plan_bytes(rows, w->n_adapters) == 0) return 0;
+    const int tiles = most_tiles(rows, w->n_adapters);
+    return sums_bytes(w, tiles, splits_of(w, tiles));
+}
 
 size_t adapter_plan_bytes(int rows, int n_adapters) {
     if (rows < 0 || rows > (1 << 22) || n_adapters < 0 || n_adapters > kMostAdapters) return 0;
@@ -450,10 +499,8 @@ int launch_adapter_plan(const int32_t* row_start, const int32_t* adapter, int n_
 }
 
 int launch_adapter_apply(const hawk_adapters* w, const void* plan, size_t plan_bytes, int rows, const hawk_matrix* x, const hawk_matrix* base,
-                         const hawk_matrix* out, hipStream_t stream) {
-    if (!w || rows < 0 || !is_type(w->dtype) || w->n_adapters < 0 || w->rank < 8 || w->rank > 128 || w->rank % 8 || w->d_in < 8 || w->d_in % 8 ||
-        w->d_out < 8 || w->d_out % 8 || w->d_in > (1 << 24) || w->d_out > (1 << 24))
-        return HAWK_EINVAL;
+                         const hawk_matrix* out, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    if (!weights_ok(w) || rows < 0) return HAWK_EINVAL;
     if ((w->a_adapter_stride | w->a_row_stride | w->b_adapter_stride | w->b_row_stride) & 7) return HAWK_EINVAL;
     if (w->a_adapter_stride < 0 || w->b_adapter_stride < 0 || w->a_row_stride < w->d_in || w->b_row_stride < w->rank) return HAWK_EINVAL;
     const size_t need = adapter_plan_bytes(rows, w->n_adapters);
@@ -477,12 +524,24 @@ int launch_adapter_apply(const hawk_adapters* w, const void* plan, size_t plan_b
     // 1280 by 3456, rank 16, 8.8 / 6.6 / 6.0 / 5.4 / 5.3 / 4.7; 77 of 4096 by 11008, rank 32, 27.0 / 18.3 / 15.6 / 15.4 / 17.6 / 16.9; 304 of 4096 by 4096,
     // rank 16, 31.5 / 30.9 / 33.7 / 37.3 / 43.3 / 48; 80 of 1280 by 1000, rank 128, 15.6 / 13.1 / 13.2 / 23.3 / 23.4 / 29.8).
     const int groups = (a.d_out + 63) / 64, parts = std::max(1, std::min((groups + kWaves - 1) / kWaves, 256 / std::max(1, a.tiles)));
-    a.parts = divisor(parts);
-    const int64_t grid = (int64_t)(a.tiles + 7) / 8 * 8 * parts;
-    if (grid > (1 << 22)) return HAWK_EINVAL;
-    if (w->dtype == HAWK_FP32) launch_typed<HAWK_FP32>(a, out->dtype, (unsigned)grid, stream);
-    else if (w->dtype == HAWK_BF16) launch_typed<HAWK_BF16>(a, out->dtype, (unsigned)grid, stream);
-    else launch_typed<HAWK_FP16>(a, out->dtype, (unsigned)grid, stream);
+    auto launch = [&](int step, int n) {
+        a.step = step;
+        a.parts = divisor(n);
+        const unsigned grid = (unsigned)((a.tiles + 7) / 8 * 8 * n);
+        if (w->dtype == HAWK_FP32) launch_typed<HAWK_FP32>(a, out->dtype, grid, stream);
+        else if (w->dtype == HAWK_BF16) launch_typed<HAWK_BF16>(a, out->dtype, grid, stream);
+        else launch_typed<HAWK_FP16>(a, out->dtype, grid, stream);
+    };
+    a.splits = splits_of(w, a.tiles);
+    if (a.splits == 0) {
+        launch(kWhole, parts);
+    } else {
+        if (!workspace || !aligned16(workspace)) return HAWK_EINVAL;
+        if (workspace_bytes < sums_bytes(w, a.tiles, a.splits)) return HAWK_ENOMEM;
+        a.sums = static_cast<float*>(workspace);
+        launch(kShrink, a.splits);
+        launch(kExpand, parts);
+    }
     return status();
 }
 

@@ -639,9 +639,11 @@ int hawk_adapter_plan(const int32_t* row_start, const int32_t* adapter, int n_se
     return hawk::launch_adapter_plan(row_start, adapter, n_seq, rows, n_adapters, plan, plan_bytes, static_cast<hipStream_t>(stream));
 }
 
+size_t hawk_adapter_apply_workspace_bytes(const hawk_adapters* weights, int rows) { return hawk::adapter_apply_workspace_bytes(weights, rows); }
+
 int hawk_adapter_apply(const hawk_adapters* weights, const void* plan, size_t plan_bytes, int rows, const hawk_matrix* x, const hawk_matrix* base,
-                       const hawk_matrix* out, void* stream) {
-    return hawk::launch_adapter_apply(weights, plan, plan_bytes, rows, x, base, out, static_cast<hipStream_t>(stream));
+                       const hawk_matrix* out, void* workspace, size_t workspace_bytes, void* stream) {
+    return hawk::launch_adapter_apply(weights, plan, plan_bytes, rows, x, base, out, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
 }
 
 size_t hawk_sample_filtered_workspace_bytes(int rows, int n) { return hawk::sample_filtered_workspace_bytes(rows, n); }

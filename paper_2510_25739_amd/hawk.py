@@ -140,7 +140,8 @@ EXPORTS = {
     "hawk_paged_copy": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p]),
     "hawk_adapter_plan_bytes": (C.c_size_t, [C.c_int, C.c_int]),
     "hawk_adapter_plan": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
-    "hawk_adapter_apply": (C.c_int, [C.c_void_p, C.c_void_p, C.c_size_t, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "hawk_adapter_apply_workspace_bytes": (C.c_size_t, [C.c_void_p, C.c_int]),
+    "hawk_adapter_apply": (C.c_int, [C.c_void_p, C.c_void_p, C.c_size_t, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "hawk_sample_filtered_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int]),
     "hawk_sample_filtered": (C.c_int, [C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                        C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
@@ -702,6 +703,7 @@ class AdapterPlan:
         self._dev, self._i32, self._f32 = row_start.get_device(), _int32(), _float32()
         self._plan = row_start.new_empty((n,), dtype=_uint8())
         self._ptr, self._n = self._plan.data_ptr(), n
+        self._room = {}     # workspace of an apply by (rank, d_in, type)
         self.update(row_start, adapter)
 
     def update(self, row_start, adapter):
@@ -746,7 +748,11 @@ class AdapterPlan:
         else:
             ho = self._matrix("out", out, d_out)
         w = _PACK_ADAPTERS(a.data_ptr(), b.data_ptr(), sa if n > 1 else 0, ja, sb if n > 1 else 0, jb, s, kind, n, rank, d_in, d_out)
-        rc = _call_on(dev, self._L.hawk_adapter_apply, w, self._ptr, self._n, self.rows, hx, hb, ho)
+        nws = self._room.get((rank, d_in, kind))
+        if nws is None:
+            nws = self._room[rank, d_in, kind] = self._L.hawk_adapter_apply_workspace_bytes(w, self.rows)
+        ws = x.new_empty((nws,), dtype=_uint8()) if nws else None
+        rc = _call_on(dev, self._L.hawk_adapter_apply, w, self._ptr, self._n, self.rows, hx, hb, ho, ws.data_ptr() if nws else None, nws)
         if rc != 0:
             raise HawkError(rc, where)
         return out

@@ -124,6 +124,59 @@ def test_groupings(H, rows, adapter, n):
     check(c, c.plan(H).apply(c.dev("x"), c.dev("a"), c.dev("b"), base=c.dev("base"), scale=c.dev("scale")))
 
 
+def shared(H, c):
+    """Whether a tile's sum over d_in is shared by several workgroups (two launches)."""
+    import ctypes
+    from paper_2510_25739_amd import hawk
+    w = hawk.HawkAdapters(dtype=hawk._dtype_of(c.a), n_adapters=c.n, rank=c.rank, d_in=c.d_in, d_out=c.d_out)
+    return H.load_library().hawk_adapter_apply_workspace_bytes(ctypes.byref(w), c.total) > 0
+
+
+WIDE = [("bf16", "bf16", 128, 4096, 264), ("bf16", "fp32", 64, 11008, 72), ("bf16", "bf16", 32, 12296, 1000), ("fp16", "fp16", 120, 5000, 136),
+        ("fp16", "fp32", 64, 8192, 40), ("fp32", "fp32", 40, 8200, 264), ("fp32", "bf16", 128, 2056, 200), ("bf16", "fp16", 16, 40000, 64)]
+
+
+@pytest.mark.parametrize("x,out,rank,d_in,d_out", WIDE)
+@pytest.mark.parametrize("rows,adapter,n", [([1], [0], 1), ([1, 6, 0, 17, 33, 2], [2, 0, 1, -1, 2, 1], 3), ([200, 130], [1, 0], 2)])
+def test_sums_that_workgroups_share(H, x, out, rank, d_in, d_out, rows, adapter, n):
+    c = Case(rank + d_in, rows, adapter, n, rank, d_in, d_out, x, out, extra=3)
+    assert shared(H, c)
+    kept = c.dev("base")
+    got = c.plan(H).apply(c.dev("x"), c.dev("a"), c.dev("b"), base=kept, scale=c.dev("scale"), out=kept)
+    check(c, got, c.base)
+
+
+def test_shared_sums_on_two_streams_and_replayed(H):
+    import torch
+    cs = [Case(s, [1, 6, 3], [1, 0, 1], 2, 128, 4096, 264) for s in (1, 2)]
+    assert all(shared(H, c) for c in cs)
+    plan = cs[0].plan(H)                                 # both have the same rows: one plan
+    dev = [[c.dev(k) for k in ("x", "a", "b", "base", "scale")] for c in cs]
+    run = lambda d: plan.apply(d[0], d[1], d[2], base=d[3], scale=d[4])
+    one = [run(d) for d in dev]
+    for c, y in zip(cs, one):
+        check(c, y)
+    streams = [torch.cuda.Stream() for _ in dev]
+    torch.cuda.synchronize()
+    many = [[], []]
+    for _ in range(20):
+        for s, d, m in zip(streams, dev, many):
+            with torch.cuda.stream(s):
+                m.append(run(d))
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, w) for m, w in zip(many, one) for y in m)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = [run(d) for d in dev]
+    for _ in range(3):
+        for y in outs:
+            y.zero_()
+        graph.replay()
+        again = run(dev[0])
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], one[0]) and torch.equal(outs[1], one[1]) and torch.equal(again, one[0])
+
+
 @pytest.mark.parametrize("base,scale", [(True, False), (False, True), (False, False)])
 def test_without_a_base_or_a_scale(H, base, scale):
     c = Case(5, [4, 30, 9], [1, -1, 0], 2, 16, 128, 200, base=base, scale=scale)

@@ -122,7 +122,7 @@ def test_bad_adapter_calls_are_refused(L):
 
     def apply(w=None, plan=ONE, nbytes=need, rows=5, x=None, base=None, out=None, **kw):
         ref = lambda m: None if m is None else C.byref(m)
-        return L.hawk_adapter_apply(ref(w or adapters(**kw)), plan, nbytes, rows, ref(x or matrix(64)), ref(base), ref(out or matrix(40, data=1 << 20)), None)
+        return L.hawk_adapter_apply(ref(w or adapters(**kw)), plan, nbytes, rows, ref(x or matrix(64)), ref(base), ref(out or matrix(40, data=1 << 20)), None, 0, None)
 
     for kw in (dict(rank=0), dict(rank=12), dict(rank=136, b_row_stride=136), dict(d_in=0), dict(d_in=60), dict(d_in=72), dict(d_out=44), dict(d_out=0),
                dict(dtype=5), dict(n_adapters=-1), dict(a=None), dict(b=None), dict(a=ONE + 2), dict(b=ONE + 8), dict(a_row_stride=68),
@@ -133,6 +133,22 @@ def test_bad_adapter_calls_are_refused(L):
         assert apply(**kw) == -1, kw
     assert apply(nbytes=need - 1) == -3
     assert apply(rows=0, a=None, b=None, n_adapters=0, plan=None, x=matrix(64, data=None)) == 0
+
+
+def test_sums_shared_by_workgroups_need_a_workspace(L):
+    def size(rows=5, **kw):
+        return L.hawk_adapter_apply_workspace_bytes(C.byref(adapters(**kw)), rows)
+
+    wide = dict(rank=128, d_in=4096, a_row_stride=4096, b_row_stride=128)
+    need = size(**wide)
+    assert need > 0 and need % 16 == 0
+    assert size() == 0 and size(rank=128) == 0 and size(rows=4096, **wide) == 0      # a little to read, or many tiles
+    assert size(rows=0, **wide) == 0 and size(rows=-1, **wide) == 0 and size(rows=5, **{**wide, "rank": 12}) == 0
+    w, plan = C.byref(adapters(**wide)), L.hawk_adapter_plan_bytes(5, 3)
+    x, out = matrix(4096), matrix(40, data=1 << 20)
+    for ws, n, code in ((None, need, -1), (ONE + 8, need, -1), (ONE, need - 1, -3), (ONE, 0, -3)):
+        assert L.hawk_adapter_apply(w, ONE, plan, 5, C.byref(x), None, C.byref(out), ws, n, None) == code
+    assert L.hawk_adapter_apply(w, ONE, plan, 0, C.byref(x), None, C.byref(out), None, 0, None) == 0
 
 
 def test_bad_filtered_draws_are_refused(L):
