@@ -1,13 +1,14 @@
 // Low-rank adapters of many requests beside a shared projection: out[r] = base[r] + scale[a] B_a (A_a x[r]), a the adapter of row r's sequence.
 //
 // Rows are grouped by adapter into tiles of 16, once a step (the plan), so that an adapter that many requests use is read once for 16 of
-// their rows.  One launch a projection: a workgroup has a tile and some of the columns (two launches, the first of
-// sums over parts of d_in, where a few tiles' A would be a few units' to read).  Its waves share the sum over d_in - both
-// operands of A x go from memory straight into the matrix units' registers, 16 bytes a lane -, their parts are added in shared memory, and
-// B h is added to base on the way out.  What bounds it: of single tokens memory (200 rows of 64 adapters of rank 32, 4096 by 11008, 67 MB, 15.1 us in
-// turn with other inputs: 4.4 TB/s) and of prompts (4724 rows of 4096 by 4096, 117 MB, 32 us cold, 24 with what the last-level cache holds of a repeated
-// input); of few rows a chain of latencies (plan, x and A, h, B; one row 3.5 us, of which 3 are a launch).  Both products are computed transposed (h^T = A x^T, out^T = B h^T): a result lane then has neighbouring
-// elements of one row.
+// their rows.  One launch a projection: a workgroup has a tile and some of the columns.  Its waves share the sum over d_in, their parts are
+// added in shared memory, and B h is added to base on the way out.  Where a few tiles' A would be a few units' to read, the sums are a launch of their
+// own, shared by more workgroups (splits_of).  Both products are computed transposed (h^T = A x^T, out^T = B h^T): a result lane then has
+// neighbouring elements of one row.
+//
+// What bounds it: of single tokens memory (200 rows of 64 adapters of rank 32, 4096 by 11008, 67 MB, 15.1 us with other inputs in turn: 4.4 TB/s), of prompts
+// as well (4724 rows of 4096 by 4096, 117 MB, 32 us with other inputs in turn, 24 of one input that the last-level cache holds part of); of few rows a
+// chain of latencies (plan, x and A, h, B; one row 3.8 us, of which a launch is 3).
 #include "adapters.h"
 #include "paged.h"
 
