@@ -13,8 +13,8 @@
 //
 // Up to 16384 entries one workgroup of 1024 threads has a row in its registers (sample_filtered_kernel).  Longer rows are cut into parts, a
 // workgroup each, in three launches: the parts' bins (filter_bins_kernel); sums of what is kept for certain, and the entries of the bins
-// that a border may be in (filter_parts_kernel); the borders and the draw, a workgroup a row (filter_draw_kernel).  A row whose border bins hold
-// more than a quarter of a part, or whose logits are beyond the bins' grid, is read again and again by that last workgroup alone.
+// that a border may be in (filter_parts_kernel); the borders and the draw, a workgroup a row (filter_draw_kernel).  Where the border's bins
+// hold more than a quarter of a part that last workgroup looks for it in the row itself; rows whose logits are beyond the bins' grid are its alone.
 //
 // What bounds it: not memory (48 rows of 65536 are 2.6 us of it) but a workgroup's instructions and barriers.  One row of 16384 entries, 15.4 us, is
 // a dozen steps of sixteen waves with a barrier behind each, 1450 vector instructions a wave, which take 10 us to issue; 96 rows of which some have no top-k
@@ -1100,20 +1100,21 @@ template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(Filter
         return;
     }
     const int top = t.cell;
-    bool far = t.far;
-    const int listed = lane < a.parts && !far ? room.head[lane].n_list : 0, sure = lane < a.parts && !far ? room.head[lane].n_kept : 0, upto = wave_incl_scan_i(listed), n_list = __builtin_amdgcn_readlane(upto, 63);
-    far = far || __ballot(listed > part_list(E)) != 0ull;
-    if (far) {
+    if (t.far) {
         whole_row<0>(a, r, sh, sums, both.top);
         return;
     }
+    const Source src = source_of(a, r, q);
+    const int listed = lane < a.parts ? room.head[lane].n_list : 0, sure = lane < a.parts ? room.head[lane].n_kept : 0;
+    const int upto = wave_incl_scan_i(listed), n_list = __builtin_amdgcn_readlane(upto, 63);
+    const bool cut_short = __ballot(listed > part_list(E)) != 0ull;      // some are only in the row itself
     const int n_sure = wave_sum_i(sure);
     if (tid == 0) { ls.kept = n_sure; ls.m = 0; sh.n = 0; }
     fill_steps(sh.steps);
     if (tid < kFine) { sh.fine[tid] = 0u; sh.fine_mass[tid] = 0ull; }
     const int chunks = a.parts * E * 4;
     for (int i = tid; i < chunks; i += NT) sums[i] = room.sums[i];
-    const bool held = n_list <= kList;
+    const bool held = n_list <= kList && !cut_short;
     for (int i = wave; held && i < a.parts; i += NW) {
         const int n = __builtin_amdgcn_readlane(listed, i), from = __builtin_amdgcn_readlane(upto, i) - n;
         for (int k = lane; k < n; k += 64) {
@@ -1125,12 +1126,27 @@ template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(Filter
     auto each_listed = [&](auto f) {     // f(index, z)
         if (held) {
             for (int i = tid; i < n_list; i += NT) f(ls.at[i], ls.z[i]);
+        } else if (cut_short) {
+            for (int j = 4 * tid; j < a.n; j += 4 * NT) {
+                float v[4];
+                src.four(j, v);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (v[i] > -INFINITY) f(j + i, v[i]);
+            }
         } else {
-            for (int i = 0; i < a.parts; ++i) {
-                const int n = __builtin_amdgcn_readlane(listed, i);
-                for (int k = tid; k < n; k += NT) {
-                    const int2 e = room.list[i * part_list(E) + k];
-                    f(e.y, __int_as_float(e.x));
+            for (int i0 = 0; i0 < a.parts; i0 += 4) {            // four loads on their way together
+                int n[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) n[i] = i0 + i < a.parts ? __builtin_amdgcn_readlane(listed, min(i0 + i, a.parts - 1)) : 0;
+                const int most = max(max(n[0], n[1]), max(n[2], n[3]));
+                for (int k = tid; k < most; k += NT) {
+                    int2 e[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) e[i] = k < n[i] ? room.list[(i0 + i) * part_list(E) + k] : make_int2(0, 0);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (k < n[i]) f(e[i].y, __int_as_float(e[i].x));
                 }
             }
         }
@@ -1169,13 +1185,16 @@ template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(Filter
                 const int b = bin(z);
                 return b >= h.p_first && b <= h.p_last && inside(most, z, at);
             };
-            int m = 0;
-            each_listed([&](int at, float z) { m += in(at, z) ? 1 : 0; });
-            m = wave_sum_i(m);
-            if (lane == 0) atomicAdd(&ls.m, m);
-            if (tid == 0) sh.n = 0;
-            __syncthreads();
-            m = ls.m;
+            int m = n_list;          // (those before its bins are not listed, those behind neither, but for a top-k's bin)
+            if (q.by_k) {
+                m = 0;
+                each_listed([&](int at, float z) { m += in(at, z) ? 1 : 0; });
+                m = wave_sum_i(m);
+                if (lane == 0) atomicAdd(&ls.m, m);
+                if (tid == 0) sh.n = 0;
+                __syncthreads();
+                m = ls.m;
+            }
             const Cut cut = {maxu64(share_of(q.top_p, mass), 1ull), 0xFFFFFFFFu};
             Range x = range_of(h.p_first, h.p_last);
             x.before = h.p_before; x.m = (unsigned)m;
@@ -1186,8 +1205,9 @@ template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(Filter
             }, weigh, true, cut, x, sh, a.apart).border;
         }
         int n = 0;
+        const int first = q.by_p ? h.p_first : h.k_bin;          // entries of bins before it are among the sums
         each_listed([&](int at, float z) {
-            if (!inside(border, z, at)) return;
+            if (!inside(border, z, at) || (cut_short && bin(z) < first)) return;
             const u64 w = weigh(z);
             if (w < least) return;
             atomicAdd(&sums[at / kChunk], w);
@@ -1200,7 +1220,6 @@ template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(Filter
     u64 base, target, total;
     const int chunk = pick_chunk(a, r, sums, chunks, sh, base, target, total);
     if (wave == 0) {
-        const Source src = source_of(a, r, q);
         float v[4];
         const int j = chunk * kChunk + 4 * lane;
         src.four(j, v);
