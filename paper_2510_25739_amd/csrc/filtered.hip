@@ -18,8 +18,8 @@
 //
 // What bounds it: not memory (48 rows of 65536 are 2.6 us of it) but a workgroup's instructions and barriers.  One row of 16384 entries, 15.4 us, is
 // a dozen steps of sixteen waves with a barrier behind each, 1450 vector instructions a wave, which take 10 us to issue; 96 rows of which some have no top-k
-// 21 us, the exponentials of 16 entries a thread among them; 48 rows of 65536 36.7 us, three launches of 10.8, 14.4 and 10.8, of which nearly 4 each is
-// a launch; 4 of 200003, 16 bits, 38 us.
+// 21 us, the exponentials of 16 entries a thread among them; 48 rows of 65536 36.4 us, three launches of 9.7, 14.2 and 10.9, of which nearly 4 each is
+// a launch; 4 of 200003, 16 bits, 37 us.
 #include "filtered.h"
 #include "paged.h"
 #include "sample_rows.h"
