@@ -565,7 +565,7 @@ int hawk_paged_copy(const hawk_paged_cache* from, const hawk_paged_cache* to, co
  * hawk_adapter_apply: A_i is rank rows of d_in elements, element (j, k) at a + i * a_adapter_stride + j * a_row_stride + k; B_i d_out rows of rank
  * elements, likewise.  scale fp32 [n_adapters] (NULL: 1).  rank, d_in, d_out multiples of 8, rank at most 128; strides multiples of 8
  * elements, pointers 16-byte aligned.  x and the weights of one type, base and out of one (any) type; out overlaps nothing but base,
- * and that only as a whole.  A x and B h are summed in fp32; A x enters the second product with 16 bits (bf16; 24 if out is fp32), 22 bits below
+ * and that only as a whole (over x or part of base it is refused).  A x and B h are summed in fp32; A x enters the second product with 16 bits (bf16; 24 if out is fp32), 22 bits below
  * a row's largest (fp16) or 24 (fp32); the sum is rounded once to out's type.  Weights are finite numbers; an infinity or NaN in a row of x
  * stays in that row.  workspace (16-byte aligned, may be NULL where the size function, of the weights' sizes and rows, says 0):
  * hawk_adapter_apply_workspace_bytes; nothing in it has to be cleared or is kept. */

@@ -510,7 +510,13 @@ int launch_adapter_apply(const hawk_adapters* w, const void* plan, size_t plan_b
     if (w->n_adapters > 0 && (!w->a || !w->b || !aligned16(w->a) || !aligned16(w->b))) return HAWK_EINVAL;
     if (!matrix_ok(x, w->d_in) || !matrix_ok(out, w->d_out) || (base && !matrix_ok(base, w->d_out))) return HAWK_EINVAL;
     if (x->dtype != w->dtype || (base && base->dtype != out->dtype) || (rows > 1 && out->row_stride < w->d_out)) return HAWK_EINVAL;
-    if (base && base->data == out->data && rows > 1 && base->row_stride != out->row_stride) return HAWK_EINVAL;
+    // a tile's workgroups read its rows of x while others write theirs of out; base and out of one piece are read and written by the same lane
+    auto over = [&](const hawk_matrix* m, int width) {
+        const int64_t es = type_bytes(m->dtype), eo = type_bytes(out->dtype);
+        return rows_meet(m->data, m->row_stride * es, width * es, out->data, out->row_stride * eo, w->d_out * eo, rows);
+    };
+    const bool in_place = base && base->data == out->data && (rows < 2 || base->row_stride == out->row_stride);
+    if (over(x, w->d_in) || (base && !in_place && over(base, w->d_out))) return HAWK_EINVAL;
     if (!plan || !aligned16(plan)) return HAWK_EINVAL;
     if (plan_bytes < need) return HAWK_ENOMEM;
     ApplyArgs a = {};

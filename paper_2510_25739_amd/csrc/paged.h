@@ -4,6 +4,8 @@
 
 #include "hawk_internal.h"
 
+#include <algorithm>
+
 namespace hawk {
 
 // n / d for n below 2^31 and a d of the host's: with s = ceil(log2 d) and M = ceil(2^(31 + s) / d) < 2^32 the product n M / 2^(31 + s) is
@@ -48,6 +50,23 @@ __host__ __device__ inline int64_t entry_at(const PagedView& c, const int32_t* t
 
 inline bool is_type(int dtype) { return dtype == HAWK_FP32 || dtype == HAWK_BF16 || dtype == HAWK_FP16; }
 inline size_t type_bytes(int dtype) { return dtype == HAWK_FP32 ? 4 : 2; }
+// Whether rows a and rows b, each `rows` pieces of so many bytes that start so many bytes apart, have a byte in common.  Columns of one buffer
+// lie between one another's rows and have none.
+inline bool rows_meet(const void* a, int64_t a_step, int64_t a_bytes, const void* b, int64_t b_step, int64_t b_bytes, int rows) {
+    const int64_t d = (int64_t)(reinterpret_cast<uintptr_t>(b) - reinterpret_cast<uintptr_t>(a)), last = rows - 1;
+    if (rows < 2) a_step = b_step = 0;
+    if (rows < 1 || d >= last * a_step + a_bytes || d + last * b_step + b_bytes <= 0) return false;
+    // whether a step of a's, from the first to the last, starts in lo + 1 .. hi - 1
+    auto starts = [&](int64_t lo, int64_t hi, int64_t first) {
+        if (a_step == 0) return lo < 0 && hi > 0;
+        const int64_t q = lo / a_step - (lo % a_step < 0 ? 1 : 0), k = std::max(q + 1, first);
+        return k <= last && k * a_step < hi;
+    };
+    if (a_step == b_step) return starts(d - a_bytes, d + b_bytes, -last);
+    for (int64_t i = 0; i <= last; ++i)
+        if (starts(d + i * b_step - a_bytes, d + i * b_step + b_bytes, 0)) return true;
+    return false;
+}
 bool paged_view(const hawk_paged_cache* c, int layer, PagedView* out);     // false: bad argument
 bool heads_view(const hawk_heads* h, HeadsView* out);
 // An output whose vectors do not overlap because of a stride alone.

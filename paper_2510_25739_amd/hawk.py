@@ -731,8 +731,8 @@ class AdapterPlan:
     def apply(self, x, a, b, base=None, scale=None, out=None, dtype=None):
         """hawk_adapter_apply: base + scale[i] * B_i (A_i x) of every row, i its adapter.  x [rows, d_in], a [n_adapters, rank, d_in],
         b [n_adapters, d_out, rank] of one type; base [rows, d_out] (None: zero) and out of one type; scale [n_adapters] fp32 (None: 1).
-        out: where the result goes, base itself allowed (None: a new tensor of base's type, or of `dtype`, or of x's, whose rows
-        of no sequence are not written)."""
+        out: where the result goes, base itself allowed, nothing that lies over x or over part of base (None: a new tensor of base's
+        type, or of `dtype`, or of x's, whose rows of no sequence are not written)."""
         where, dev, n = "hawk_adapter_apply", self._dev, self.n_adapters
         if a.dim() != 3 or b.dim() != 3 or a.get_device() != dev or b.get_device() != dev or a.dtype is not b.dtype:
             raise HawkError(-1, where, "a [n_adapters, rank, d_in] and b [n_adapters, d_out, rank] must be tensors of one type on the plan's device")
