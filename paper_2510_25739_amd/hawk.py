@@ -709,7 +709,7 @@ class AdapterPlan:
         self._dev, self._i32, self._f32 = row_start.get_device(), _int32(), _float32()
         self._plan = row_start.new_empty((n,), dtype=_uint8())
         self._ptr, self._n = self._plan.data_ptr(), n
-        self._room = {}     # workspace of an apply by (rank, d_in, type)
+        self._room = {}     # workspace of an apply by (rank, d_in, d_out, type)
         self._like = _empty_like()
         self.update(row_start, adapter)
 
@@ -758,9 +758,10 @@ class AdapterPlan:
         else:
             ho = self._matrix("out", out, d_out)
         w = _PACK_ADAPTERS(a.data_ptr(), b.data_ptr(), sa if n > 1 else 0, ja, sb if n > 1 else 0, jb, s, kind, n, rank, d_in, d_out)
-        nws = self._room.get((rank, d_in, kind))
+        key = (rank, d_in, d_out, kind)                  # (all that the size is made of: it is 0 where they are refused)
+        nws = self._room.get(key)
         if nws is None:
-            nws = self._room[rank, d_in, kind] = self._L.hawk_adapter_apply_workspace_bytes(w, self.rows)
+            nws = self._room[key] = self._L.hawk_adapter_apply_workspace_bytes(w, self.rows)
         ws = x.new_empty((nws,), dtype=_uint8()) if nws else None
         rc = _call_on(dev, self._L.hawk_adapter_apply, w, self._ptr, self._n, self.rows, hx, hb, ho, ws.data_ptr() if nws else None, nws)
         if rc != 0:
