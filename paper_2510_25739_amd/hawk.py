@@ -282,6 +282,11 @@ def _empty_like():
     return torch.empty_like
 
 
+def _raw_stream():
+    import torch  # device memory and stream only
+    return torch._C._cuda_getCurrentRawStream
+
+
 def _uint8():
     import torch
     return torch.uint8
@@ -708,16 +713,28 @@ class AdapterPlan:
             raise HawkError(-1, "hawk_adapter_plan_bytes", "rows or n_adapters out of range")
         self._dev, self._i32, self._f32 = row_start.get_device(), _int32(), _float32()
         self._plan = row_start.new_empty((n,), dtype=_uint8())
+        self._now = _raw_stream()
+        self._streams = {self._now(self._dev) if self._dev >= 0 else 0}
         self._ptr, self._n = self._plan.data_ptr(), n
         self._room = {}     # workspace of an apply by (rank, d_in, d_out, type)
         self._like = _empty_like()
         self.update(row_start, adapter)
+
+    def _on_stream(self):
+        """The plan's memory belongs to the stream it was made on; another one that works with it is noted, so that the memory is not given to
+        others before that work is done, whenever the plan is dropped."""
+        now = self._now(self._dev)
+        if now not in self._streams:
+            import torch  # device memory and stream only
+            self._plan.record_stream(torch.cuda.current_stream(self._dev))
+            self._streams.add(now)
 
     def update(self, row_start, adapter):
         where, n = "hawk_adapter_plan", adapter.shape[0] if adapter.dim() == 1 else -1
         for t, shape in ((row_start, (n + 1,)), (adapter, (n,))):
             if self._dev < 0 or t.dtype is not self._i32 or t.get_device() != self._dev or t.shape != shape or not t.is_contiguous():
                 raise HawkError(-1, where, "row_start [n_seq + 1] and adapter [n_seq] must be contiguous int32 tensors on one device")
+        self._on_stream()
         rc = _call_on(self._dev, self._L.hawk_adapter_plan, row_start.data_ptr(), adapter.data_ptr(), n, self.rows, self.n_adapters, self._ptr, self._n)
         if rc != 0:
             raise HawkError(rc, where)
@@ -763,6 +780,7 @@ class AdapterPlan:
         if nws is None:
             nws = self._room[key] = self._L.hawk_adapter_apply_workspace_bytes(w, self.rows)
         ws = x.new_empty((nws,), dtype=_uint8()) if nws else None
+        self._on_stream()
         rc = _call_on(dev, self._L.hawk_adapter_apply, w, self._ptr, self._n, self.rows, hx, hb, ho, ws.data_ptr() if nws else None, nws)
         if rc != 0:
             raise HawkError(rc, where)
