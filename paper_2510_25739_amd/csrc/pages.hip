@@ -134,9 +134,9 @@ __global__ __launch_bounds__(kWide) void paged_take_kernel(TakeArgs a) {
 #pragma unroll
             for (int j = 0; j < kEach / 4; ++j) v[j] = *reinterpret_cast<const i4*>(a.refs + at + 4 * j);
 #pragma unroll
-            for (int j = 0; j < kEach; ++j) bits |= v[j / 4][j % 4] == 0 ? 1u << j : 0u;
+            for (int j = 0; j < kEach; ++j) bits |= v[j / 4][j % 4] <= 0 ? 1u << j : 0u;
         } else {
-            for (int j = 0; j < kEach && at + j < c.n_pages; ++j) bits |= a.refs[at + j] == 0 ? 1u << j : 0u;
+            for (int j = 0; j < kEach && at + j < c.n_pages; ++j) bits |= a.refs[at + j] <= 0 ? 1u << j : 0u;
         }
         return bits;
     };
@@ -228,8 +228,10 @@ __global__ __launch_bounds__(kWide) void paged_holes_kernel(PagedView c, const i
         for (int j = 0; j < real; ++j) to[at + j] = (bits >> j) & 1u ? at + j : -1;
     }
     __syncthreads();
-    if (refs_out != refs)
-        for (int p = tid; p < c.n_pages; p += kWide) refs_out[p] = max(refs[p], 0);
+    for (int p = tid; p < c.n_pages; p += kWide) {   // (in place only what is below 0)
+        const int r = refs[p];
+        if (refs_out != refs || r < 0) refs_out[p] = max(r, 0);
+    }
     __syncthreads();
     for (int i = tid; i < behind; i += kWide) {
         const Move mv = {src[i], dst[i], c.page_size};
