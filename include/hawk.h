@@ -540,7 +540,7 @@ int64_t hawk_paged_entry(const hawk_paged_cache* cache, const int32_t* table_row
  * hawk_paged_trim: the pages behind the first n_past[s] entries are given back (n_past[s] = 0: all of them; negative: the sequence is left alone).
  * hawk_paged_compact: the pages in use (refs > 0), U of them, come to lie in pages 0 .. U - 1: those behind are moved, in all layers, in
  *   ascending order into the free ones before, in ascending order.  table_out (row s table_out_stride places behind row s - 1) and refs_out
- *   get the table and the counts as they are then, in place (the table with its own stride) or elsewhere; places of pages that are not in use become -1.  n_used: U.
+ *   get the table and the counts as they are then, in place (the table with its own stride) or elsewhere (over part of the old ones they are refused); places of pages that are not in use become -1.  n_used: U.
  *   No entry that the old table leads to is overwritten.
  * hawk_paged_copy: page src[i] of one pool goes to page dst[i] of another (or the same) of equal type, layers, heads, head_dim and page_size, all
  *   layers, i < n, n <= 2^20; pairs with a page outside its pool are left out.  A page that is written twice, or written and read, holds either.

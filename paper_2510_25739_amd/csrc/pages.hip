@@ -428,7 +428,11 @@ int launch_paged_compact(const hawk_paged_cache* cache, const int32_t* refs, int
     CopyArgs m = {};
     if (!whole_view(cache, &m.from) || !refs || !refs_out || !n_used || !workspace || !aligned16(workspace)) return HAWK_EINVAL;
     if (m.from.n_seq > 0 && (!table_out || table_out_stride < m.from.max_pages)) return HAWK_EINVAL;
-    if (m.from.n_seq > 1 && table_out == cache->table && table_out_stride != cache->table_stride) return HAWK_EINVAL;
+    // in place every thread writes what it has read itself; what lies over the old table or counts in any other way would be written before it is read
+    const bool same_table = table_out == cache->table && (m.from.n_seq < 2 || table_out_stride == cache->table_stride);
+    if (!same_table && rows_meet(cache->table, cache->table_stride * 4, cache->max_pages * 4ll, table_out, table_out_stride * 4, cache->max_pages * 4ll, cache->n_seq))
+        return HAWK_EINVAL;
+    if (refs_out != refs && rows_meet(refs, 0, cache->n_pages * 4ll, refs_out, 0, cache->n_pages * 4ll, 1)) return HAWK_EINVAL;
     const Room r = room_of(cache, workspace);
     if (workspace_bytes < r.bytes) return HAWK_ENOMEM;
     m.to = m.from;

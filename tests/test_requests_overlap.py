@@ -61,3 +61,30 @@ def test_every_arrangement_of_a_few_rows(L):
         covered = lambda p, stride, n, es: {p + r * stride * es + b for r in range(rows) for b in range(0, n * es, 2)}
         meet = bool(covered(at, sx, d_in, 2) & covered(at + shift, so, d_out, width[tout]))
         assert apply(L, (at, sx), (at + shift, so), rows=rows, d_in=d_in, d_out=d_out, tout=tout) == (-1 if meet else -3), (rows, sx, so, tout, shift)
+
+
+def cache(at, stride=8, **kw):
+    return hawk.HawkPagedCache(**{**dict(k=1 << 30, v=1 << 31, layer_stride=1 << 20, page_stride=16 * 2 * 64, head_stride=16 * 64, entry_stride=64, table=at,
+                                         table_stride=stride, dtype=hawk.HAWK_FP16, n_layers=2, n_pages=10, page_size=16, n_heads=2, head_dim=64, n_seq=3,
+                                         max_pages=8), **kw})
+
+
+def compact(L, table, out, refs=1 << 18, refs_out=1 << 19, n_seq=3):
+    """table, out: (address, row stride).  -1: refused; -3: the workspace is too small, which is looked at last."""
+    return L.hawk_paged_compact(C.byref(cache(*table, n_seq=n_seq)), refs, out[0], out[1], refs_out, 1 << 21, 1 << 22, 16, None)
+
+
+def test_tables_and_counts_that_lie_over_one_another_in_part_are_refused(L):
+    at = 1 << 16
+    assert compact(L, (at, 8), (at, 8)) == -3                                        # in place
+    assert compact(L, (at, 8), (at + 3 * 32, 8)) == -3                               # one behind the other
+    assert compact(L, (at, 8), (at + 32, 8)) == -1                                   # a row further
+    assert compact(L, (at + 4, 8), (at, 8)) == -1
+    assert compact(L, (at, 16), (at + 32, 16)) == -3                                 # side by side in one array
+    assert compact(L, (at, 16), (at + 28, 16)) == -1
+    assert compact(L, (at, 16), (at, 8)) == -1 and compact(L, (at, 16), (at, 8), n_seq=1) == -3
+    assert compact(L, (at, 8), (at, 8), refs=1 << 18, refs_out=1 << 18) == -3
+    for by in (-36, -4, 4, 36):
+        assert compact(L, (at, 8), (at, 8), refs_out=(1 << 18) + by) == -1
+    for by in (-40, 40):
+        assert compact(L, (at, 8), (at, 8), refs_out=(1 << 18) + by) == -3
