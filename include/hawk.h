@@ -545,7 +545,8 @@ int64_t hawk_paged_entry(const hawk_paged_cache* cache, const int32_t* table_row
  * hawk_paged_copy: page src[i] of one pool goes to page dst[i] of another (or the same) of equal type, layers, heads, head_dim and page_size, all
  *   layers, i < n, n <= 2^20; pairs with a page outside its pool are left out.  A page that is written twice, or written and read, holds either.
  * workspace of take and compact (16-byte aligned): hawk_paged_pages_workspace_bytes; nothing in it has to be cleared or is kept.
- * n_seq * max_pages <= 2^30, a page of one head at most 2^30 times 16 bytes, layers apart from one another. */
+ * take, compact and copy: n_pages <= 2^31 - 2^15, n_seq * max_pages <= 2^30, a page of one head at most 2^30 times 16 bytes, layers apart from one
+ * another. */
 size_t hawk_paged_pages_workspace_bytes(const hawk_paged_cache* cache);
 int hawk_paged_fork(const hawk_paged_cache* cache, int32_t* refs, int32_t* n_past, const int32_t* src, const int32_t* dst, int n, void* stream);
 int hawk_paged_take(const hawk_paged_cache* cache, int32_t* refs, const int32_t* n_past, const int32_t* n_new, int32_t* short_by,

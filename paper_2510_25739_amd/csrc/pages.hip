@@ -338,9 +338,11 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 
 int status() { return hipGetLastError() == hipSuccess ? HAWK_OK : HAWK_EDEVICE; }
 size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 
+// Lookups go through the counts in rounds of kWide * kEach: numbers of a round that begins behind the last page are still below 2^31.
+constexpr int kMostPages = 0x7FFFFFFF - (2 * kWide * kEach - 1);
 // A cache whose pages can be copied in all layers.
 bool whole_view(const hawk_paged_cache* c, PagedView* v) {
-    return paged_view(c, 0, v) && !(c->n_layers > 1 && c->layer_stride < c->head_dim) && (int64_t)c->n_layers * 2 * c->n_heads <= (1 << 25) &&
+    return paged_view(c, 0, v) && c->n_pages <= kMostPages && !(c->n_layers > 1 && c->layer_stride < c->head_dim) && (int64_t)c->n_layers * 2 * c->n_heads <= (1 << 25) &&
            (int64_t)c->page_size * (c->head_dim * (int)type_bytes(c->dtype) / 16) <= (1 << 30) && (int64_t)c->n_seq * c->max_pages <= (1 << 30) &&
            (int64_t)c->page_size * (c->head_dim * (int)type_bytes(c->dtype) / 16) * c->n_layers * 2 * c->n_heads <= (int64_t)kBatch << 30;
 }
