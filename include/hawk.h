@@ -529,7 +529,7 @@ int64_t hawk_paged_entry(const hawk_paged_cache* cache, const int32_t* table_row
  * page (images of one prompt): a page that more than one place has is never written, hawk_paged_take gives the writer one of its own first.
  * Counts below 0 are free pages; what the arrays hold is checked as everywhere: no page outside the pool is read, written or counted.
  *
- * hawk_paged_fork: sequence dst[i] becomes a second holder of what sequence src[i] has committed (i < n, n <= n_seq, 2^23 at most): its row of the table gets
+ * hawk_paged_fork: sequence dst[i] becomes a second holder of what sequence src[i] has committed (i < n, n <= n_seq, 2^18 at most): its row of the table gets
  *   the pages of the first n_past[src[i]] entries, n_past[dst[i]] that length, and the pages it held until now are given back.  A pair
  *   is left out if either number is no sequence, both are the same, an earlier pair has the same dst, or its src is the dst of any pair.
  * hawk_paged_take: pages for entries n_past[s] .. n_past[s] + n_new[s] - 1 of every sequence with n_new[s] > 0 (those up to max_pages *

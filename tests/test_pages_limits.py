@@ -16,3 +16,9 @@ def test_pools_whose_page_numbers_would_wrap_are_refused(L):   # noqa: F811
         assert L.hawk_paged_take(r, ONE, ONE, ONE, ONE, ONE, 16, None) == code          # (a workspace that is too small)
         assert L.hawk_paged_compact(r, ONE, ONE, 8, ONE, ONE, ONE, 16, None) == code
     assert L.hawk_paged_copy(r, r, ONE, ONE, 1, None) == -1
+
+
+def test_forks_of_more_pairs_than_are_compared_in_a_moment_are_refused(L):   # noqa: F811
+    r = C.byref(cache(n_seq=1 << 24))
+    for n in ((1 << 18) + 1, 1 << 20, 1 << 23):
+        assert L.hawk_paged_fork(r, ONE, ONE, ONE, ONE, n, None) == -1
