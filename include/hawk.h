@@ -597,8 +597,8 @@ size_t hawk_adapter_apply_workspace_bytes(const hawk_adapters* weights, int rows
  *   The token is the first in ascending index at which the sum of kept weights exceeds u times their whole, u in [0, 1).
  * temperature 0 (or below, or NaN): the largest entry, lowest index first.  A NaN is never drawn, nor is minus infinity; entries of plus infinity
  * are alike and everything else beside them is nothing.  A row with nothing to draw gives token -1.
- * Weights are held as multiples of 2^-S of the largest (of a number up to e^(1/16) times the largest where n > 16384), S = min(51, 62 - log2 n
- * rounded up), and summed exactly.
+ * w >= min_p is decided in 64 bits.  For sums weights are held as multiples of 2^-S of the largest (of a number up to e^(1/16) times the
+ * largest where n > 16384), S = min(51, 62 - log2 n rounded up), and summed exactly.
  * logits: n values of dtype (any of the three types), row r starting r * row_stride elements in, n 1..2^20, rows <= 2^22; skip (may be NULL) [rows]: a row
  * with a negative entry is not read and gives token -1.  out_prob (may be NULL): the probability with which the token was drawn, kept weights
  * alone; out_kept (may be NULL): how many entries were kept; both 0 where there is no token.

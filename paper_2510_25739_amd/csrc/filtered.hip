@@ -214,8 +214,14 @@ __device__ __forceinline__ void give(const FilterArgs& a, int r, int token, floa
     if (a.out_prob) a.out_prob[r] = prob;
     if (a.out_kept) a.out_kept[r] = kept;
 }
-// The smallest weight that min_p keeps, top: the largest one's.
-__device__ __forceinline__ u64 least_of(const Asked& q, u64 top) { return q.min_p >= 1.f ? top : (q.min_p > 0.f ? share_of(q.min_p, top) : 0ull); }
+// The smallest z that min_p keeps, in 64 bits: held weights are too coarse for it, multiples of 2^-48 against a min_p that may be 2^-149.  zmax + log(min_p)
+// is rounded to the nearest z, which is inside or the last one outside.
+__device__ __forceinline__ float lowest_of(const Asked& q, float zmax, const double* steps) {
+    if (!(q.min_p > 0.f)) return -INFINITY;
+    if (q.min_p >= 1.f) return zmax;
+    const float z = (float)((double)zmax + log((double)q.min_p));
+    return exp_below((double)z - (double)zmax, steps) >= (double)q.min_p ? z : key_to_float(fkey(z) + 1u);
+}
 
 // Bins of which each thread has one, in order: its entries and mass, what lies before it, and all entries.  One barrier.
 struct Bin { unsigned m, ahead, all; u64 mass, before; };
@@ -503,11 +509,11 @@ __device__ __forceinline__ void draw_of_list(const FilterArgs& a, int r, const A
                 if (z[i] > -INFINITY && bin_of(zmax, z[i]) == p.bin) f(at[i], z[i]);
         }, weigh, true, cut, bin_range(zmax, p), sh, 1u).border;
     }
-    const u64 least = least_of(q, weigh(zmax));
+    const float lowest = lowest_of(q, zmax, sh.steps);
     int n_kept = 0;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const bool kept = inside(border, z[i], at[i]) && w[i] >= least;
+        const bool kept = inside(border, z[i], at[i]) && z[i] >= lowest;
         w[i] = kept ? w[i] : 0ull;
         n_kept += __popcll(__ballot(kept));
     }
@@ -674,9 +680,9 @@ template <int E> __device__ __forceinline__ void whole_row(const FilterArgs& a, 
         }
     }
 
-    const u64 least = least_of(q, weigh(zmax));
+    const float lowest = lowest_of(q, zmax, sh.steps);
     int n_kept = 0;
-    auto kept = [&](float v, int j, u64 w) { return inside(border, v, j) && w >= least; };
+    auto kept = [&](float v, int j) { return inside(border, v, j) && v >= lowest; };
     auto add_group = [&](int g, u64 s) {
         s = wave_sum_u64(s);
         if (lane == 0) sums[g * NW + wave] = s;
@@ -686,13 +692,13 @@ template <int E> __device__ __forceinline__ void whole_row(const FilterArgs& a, 
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);
-                weights[e] = inside(border, z[e], entry<E>(e, tid)) ? weigh(z[e]) : 0ull;
+                weights[e] = kept(z[e], entry<E>(e, tid)) ? weigh(z[e]) : 0ull;
             }
         }
         u64 s[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const bool k = kept(z[e], entry<E>(e, tid), weights[e]);
+            const bool k = kept(z[e], entry<E>(e, tid));
             weights[e] = k ? weights[e] : 0ull;
             s[e / 4] += weights[e];
             n_kept += k ? 1 : 0;
@@ -712,10 +718,8 @@ template <int E> __device__ __forceinline__ void whole_row(const FilterArgs& a, 
             src.four(j, v);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (!inside(border, v[i], j + i)) continue;
-                const u64 w = weigh(v[i]);
-                if (w < least) continue;
-                s += w;
+                if (!kept(v[i], j + i)) continue;
+                s += weigh(v[i]);
                 ++n_kept;
             }
             add_group(g, s);
@@ -745,11 +749,7 @@ template <int E> __device__ __forceinline__ void whole_row(const FilterArgs& a, 
             float v[4];
             const int j = chunk * kChunk + 4 * lane;
             src.four(j, v);
-            draw_of_chunk(a, r, j, v, [&](float x, int at) {
-                if (!inside(border, x, at)) return 0ull;
-                const u64 w = weigh(x);
-                return w >= least ? w : 0ull;
-            }, weigh, base, target, total);
+            draw_of_chunk(a, r, j, v, [&](float x, int at) { return kept(x, at) ? weigh(x) : 0ull; }, weigh, base, target, total);
         }
     }
     if (tid == 0 && a.out_kept) {
@@ -1032,7 +1032,7 @@ template <int E> __global__ __launch_bounds__(NT) void filter_parts_kernel(Filte
     }
     const RowHead h = ps.head;
     const int sure = q.by_p ? h.p_first : (q.by_k ? h.k_bin : kPartBins);    // bins before this one are kept, but for min-p
-    const u64 least = least_of(q, weigh(t.zmax));
+    const float lowest = lowest_of(q, t.zmax, ps.steps);
     int n_kept = 0;
     u64 sums[4];
 #pragma unroll
@@ -1045,9 +1045,8 @@ template <int E> __global__ __launch_bounds__(NT) void filter_parts_kernel(Filte
             if (!(z > -INFINITY)) continue;
             const int b = min(top - cell_of(z), kPartBins - 1);
             if (b < sure) {
-                const u64 w = weigh(z);
-                if (w >= least) {
-                    s += w;
+                if (z >= lowest) {
+                    s += weigh(z);
                     ++n_kept;
                 }
             } else if ((q.by_k && b == h.k_bin) || (q.by_p && b <= h.p_last)) {
@@ -1153,7 +1152,7 @@ template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(Filter
     };
     __syncthreads();
     const Weigh weigh = {ref_of(top), magic_of(a.unit), sh.steps};
-    const u64 least = least_of(q, weigh(t.zmax));
+    const float lowest = lowest_of(q, t.zmax, sh.steps);
     Border border = kNoBorder;
     if (q.by_k || q.by_p) {
         const RowHead h = *room.row;
@@ -1207,10 +1206,8 @@ template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(Filter
         int n = 0;
         const int first = q.by_p ? h.p_first : h.k_bin;          // entries of bins before it are among the sums
         each_listed([&](int at, float z) {
-            if (!inside(border, z, at) || (cut_short && bin(z) < first)) return;
-            const u64 w = weigh(z);
-            if (w < least) return;
-            atomicAdd(&sums[at / kChunk], w);
+            if (!inside(border, z, at) || z < lowest || (cut_short && bin(z) < first)) return;
+            atomicAdd(&sums[at / kChunk], weigh(z));
             ++n;
         });
         n = wave_sum_i(n);
@@ -1223,11 +1220,7 @@ template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(Filter
         float v[4];
         const int j = chunk * kChunk + 4 * lane;
         src.four(j, v);
-        draw_of_chunk(a, r, j, v, [&](float x, int at) {
-            if (!inside(border, x, at)) return 0ull;
-            const u64 w = weigh(x);
-            return w >= least ? w : 0ull;
-        }, weigh, base, target, total);
+        draw_of_chunk(a, r, j, v, [&](float x, int at) { return inside(border, x, at) && x >= lowest ? weigh(x) : 0ull; }, weigh, base, target, total);
     }
     if (tid == 0 && a.out_kept) a.out_kept[r] = ls.kept;
 }
