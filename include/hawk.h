@@ -598,7 +598,9 @@ size_t hawk_adapter_apply_workspace_bytes(const hawk_adapters* weights, int rows
  * temperature 0 (or below, or NaN): the largest entry, lowest index first.  A NaN is never drawn, nor is minus infinity; entries of plus infinity
  * are alike and everything else beside them is nothing.  A row with nothing to draw gives token -1.
  * w >= min_p is decided in 64 bits.  For sums weights are held as multiples of 2^-S of the largest (of a number up to e^(1/16) times the
- * largest where n > 16384), S = min(51, 62 - log2 n rounded up), and summed exactly.
+ * largest where n > 16384), S = min(51, 62 - log2 n rounded up).  The draw sums them exactly, and so does a top-p of n <= 16384; in longer rows a
+ * top-p's mass is summed in parts, each with multiples of 2^-S of its own largest, which are brought together in doubles: off by n 2^-S of the
+ * largest weight at most, the same for the same row whenever it is drawn from with as many rows.
  * logits: n values of dtype (any of the three types), row r starting r * row_stride elements in, n 1..2^20, rows <= 2^22; skip (may be NULL) [rows]: a row
  * with a negative entry is not read and gives token -1.  out_prob (may be NULL): the probability with which the token was drawn, kept weights
  * alone; out_kept (may be NULL): how many entries were kept; both 0 where there is no token.

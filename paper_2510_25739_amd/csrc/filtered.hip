@@ -6,7 +6,7 @@
 //
 // Weights are whole multiples of 2^-S of the reference's (S as large as n of them still sum up in 64 bits: 48 for 16384 entries), rounded to
 // nearest, so that a sum has one value whatever the order it is made in, and masses can be counted in bins by atomics.  What that
-// rounding moves is n 2^-(S + 1) at most, 2^-35 for 16384 entries; the sum of random errors is a hundredth of it.
+// rounding moves is n 2^-(S + 1) at most, 2^-35 for 16384 entries; the sum of random errors is a hundredth of it.  (Rows in parts: below.)
 //
 // The border of a cut - its last entry - is found by bins: linear ones of z below the maximum first, then, while more than a few entries share the
 // border's bin, bins of the keys' bits in that range and, among equal ones, of the index.  The few are ranked against each other.
@@ -774,7 +774,8 @@ template <int E> __global__ __launch_bounds__(NT) void sample_filtered_kernel(Fi
 
 // ---- Long rows in parts of E * 1024 entries.  Their bins are cells of a fixed grid of z, 512 of them from the cell of the largest entry down (of a
 // part, so that a part needs to know nothing of the others; the last one holds what lies behind), and weights are relative to the
-// upper end of the largest's cell: parts are brought together by moving bins and scaling masses.
+// upper end of the largest's cell: parts are brought together by moving bins and scaling masses, in doubles (where a part's largest is in the
+// row's cell they are the same whole numbers).  Between the borders' bins sums are whole numbers of the row's unit again.
 constexpr int kMostParts = 32, kList = 4096;     // parts of a row; entries of the borders' bins that shared memory holds
 __host__ __device__ constexpr int part_list(int E) { return 256 * E; }        // those of a part: a quarter of its entries
 constexpr float kCells = 16.f;       // cells of a unit of z
@@ -935,7 +936,7 @@ template <int E> __global__ __launch_bounds__(NT) void filter_parts_kernel(Filte
     const int top = t.cell;
     fill_steps(ps.steps);
     const Weigh weigh = {ref_of(top), magic_of(a.unit), ps.steps};
-    if (tid == 0) { ps.n_list = 0; ps.n_kept = 0; ps.head = RowHead{}; ps.head.k_bin = ps.head.p_first = kPartBins; }
+    if (tid == 0) { ps.n_list = 0; ps.n_kept = 0; ps.head = RowHead{}; ps.head.k_bin = ps.head.p_first = kPartBins; ps.head.p_last = kPartBins - 1; }
     __syncthreads();
     if (q.by_k || q.by_p) {
         // lane i: how far part i's bins are moved, and what its masses are multiplied by
@@ -1018,9 +1019,13 @@ template <int E> __global__ __launch_bounds__(NT) void filter_parts_kernel(Filte
             least_mass = ps.head.k_before;
             most_mass = ps.most_mass;
         }
-        if (q.by_p) {                // (what scaling the parts' masses has rounded is far below 2^-30)
-            const u64 first = share_of(q.top_p, least_mass), last = share_of(q.top_p, most_mass);
-            const Cut c0 = {maxu64(first - (first >> 30), 1ull), q.k}, c1 = {last + (last >> 30) + 1ull, q.k};
+        if (q.by_p) {
+            // The cut's mass is `first` at least and, by the parts' sums, `last` at most.  The border is looked for with weights relative to the row's
+            // maximum, each rounded to a unit, a part's own to a smaller one: sums of the same entries differ by a unit an entry at most, by one a
+            // bin and part where scaled masses are rounded down, and by 2^-46 of the whole (exponentials are off by 2^-51, the sum of 32 products by
+            // 2^-48).  That twice: for the cut's mass and for the sum that has to reach it.  A wider bracket lists a few more entries.
+            const u64 first = share_of(q.top_p, least_mass), last = share_of(q.top_p, most_mass), off = (u64)a.n + kPartBins + kMostParts + (total >> 46);
+            const Cut c0 = {maxu64(first, 1ull), q.k}, c1 = {last + 2ull * off + 1ull, q.k};
             if (holds(b, c0)) {
                 ps.head.p_first = tid;
                 ps.head.p_before = b.before;
