@@ -1,7 +1,7 @@
 """Calls on one plan of adapters behind one another: refused ones before others, rows that are one row for all, other streams than the plan's."""
 import pytest
 
-from test_gpu_adapters import DEV, Case, H, check, i32, shared   # noqa: F401
+from test_gpu_adapters import DEV, Case, H, check, dt, i32, shared   # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -81,3 +81,18 @@ def test_columns_of_one_buffer(H):   # noqa: F811
         c.plan(H).apply(one[:, :64], c.dev("a"), c.dev("b"), out=one[:, 56:104])
     with pytest.raises(H.HawkError):
         c.plan(H).apply(one[:, :64], c.dev("a"), c.dev("b"), base=one[:, 112:160], out=one[:, 104:152])
+
+
+@pytest.mark.parametrize("out", ["fp16", "fp32"])
+@pytest.mark.parametrize("where", ["x", "weights", "parts"])
+def test_small_halves(H, out, where):   # noqa: F811
+    # numbers below the smallest normal half: in x, in both weights, and as the second parts of A x in a row with one large value
+    c = Case(36, [5, 18], [0, 1], 2, 16, 256, 72, "fp16", out, base=False, spread=2.0 ** -16 if where == "x" else 1.0)
+    if where == "weights":
+        c.a, c.b = (c.a.float() * 2.0 ** -13).to(c.a.dtype), (c.b.float() * 2.0 ** -17).to(c.b.dtype)
+        c.scale = c.scale * 2.0 ** 20
+    elif where == "parts":
+        c.a[:, 1:] = (c.a[:, 1:].float() * 2.0 ** -13).to(c.a.dtype)
+        c.a[:, 0] = (c.a[:, 0].float() * 2.0 ** 12).to(c.a.dtype)
+        c.b[:, :, 0] = 0                                 # (the large one has no part in the result)
+    check(c, c.plan(H).apply(c.dev("x"), c.dev("a"), c.dev("b"), scale=c.dev("scale"), dtype=dt(out)))
