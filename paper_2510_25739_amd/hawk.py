@@ -282,11 +282,6 @@ def _empty_like():
     return torch.empty_like
 
 
-def _raw_stream():
-    import torch  # device memory and stream only
-    return torch._C._cuda_getCurrentRawStream
-
-
 def _uint8():
     import torch
     return torch.uint8
@@ -425,6 +420,21 @@ def _call_on(index, fn, *args):
         return fn(*args, stream)
     with _torch.cuda.device(index):
         return fn(*args, stream)
+
+
+def _call_at(index, stream, fn, *args):
+    """_call_on where torch's current stream of device `index` is known already (_raw_stream)."""
+    if _torch._C._cuda_getDevice() == index:
+        return fn(*args, stream)
+    with _torch.cuda.device(index):
+        return fn(*args, stream)
+
+
+def _raw_stream():
+    global _torch
+    import torch  # device memory and stream only
+    _torch = torch
+    return torch._C._cuda_getCurrentRawStream
 
 
 def rotary_table(n_pos: int, rot_dim: int, theta: float = 10000.0, device: str = "cuda:0"):
@@ -703,7 +713,8 @@ class PagedCache:
 class AdapterPlan:
     """Which rows of a step have which low-rank adapter (hawk_adapter_plan): rows row_start[s] .. row_start[s + 1] - 1 of sequence s,
     adapter[s] (-1: none), int32 device tensors [n_seq + 1] and [n_seq].  Made once a step and used for every projection of every layer
-    (apply); update lays out another step of as many rows and adapters in the same memory, in a captured graph as well."""
+    (apply), on any stream that waits for the one it was made on; update lays out another step of as many rows and adapters in the same
+    memory, in a captured graph as well."""
 
     def __init__(self, row_start, adapter, rows: int, n_adapters: int):
         self._L = load_library()
@@ -720,22 +731,21 @@ class AdapterPlan:
         self._like = _empty_like()
         self.update(row_start, adapter)
 
-    def _on_stream(self):
+    def _note_stream(self, stream):
         """The plan's memory belongs to the stream it was made on; another one that works with it is noted, so that the memory is not given to
         others before that work is done, whenever the plan is dropped."""
-        now = self._now(self._dev)
-        if now not in self._streams:
-            import torch  # device memory and stream only
-            self._plan.record_stream(torch.cuda.current_stream(self._dev))
-            self._streams.add(now)
+        self._plan.record_stream(_torch.cuda.current_stream(self._dev))
+        self._streams.add(stream)
 
     def update(self, row_start, adapter):
         where, n = "hawk_adapter_plan", adapter.shape[0] if adapter.dim() == 1 else -1
         for t, shape in ((row_start, (n + 1,)), (adapter, (n,))):
             if self._dev < 0 or t.dtype is not self._i32 or t.get_device() != self._dev or t.shape != shape or not t.is_contiguous():
                 raise HawkError(-1, where, "row_start [n_seq + 1] and adapter [n_seq] must be contiguous int32 tensors on one device")
-        self._on_stream()
-        rc = _call_on(self._dev, self._L.hawk_adapter_plan, row_start.data_ptr(), adapter.data_ptr(), n, self.rows, self.n_adapters, self._ptr, self._n)
+        stream = self._now(self._dev)
+        if stream not in self._streams:
+            self._note_stream(stream)
+        rc = _call_at(self._dev, stream, self._L.hawk_adapter_plan, row_start.data_ptr(), adapter.data_ptr(), n, self.rows, self.n_adapters, self._ptr, self._n)
         if rc != 0:
             raise HawkError(rc, where)
 
@@ -780,8 +790,10 @@ class AdapterPlan:
         if nws is None:
             nws = self._room[key] = self._L.hawk_adapter_apply_workspace_bytes(w, self.rows)
         ws = x.new_empty((nws,), dtype=_uint8()) if nws else None
-        self._on_stream()
-        rc = _call_on(dev, self._L.hawk_adapter_apply, w, self._ptr, self._n, self.rows, hx, hb, ho, ws.data_ptr() if nws else None, nws)
+        stream = self._now(dev)
+        if stream not in self._streams:
+            self._note_stream(stream)
+        rc = _call_at(dev, stream, self._L.hawk_adapter_apply, w, self._ptr, self._n, self.rows, hx, hb, ho, ws.data_ptr() if nws else None, nws)
         if rc != 0:
             raise HawkError(rc, where)
         return out
