@@ -537,13 +537,15 @@ int64_t hawk_paged_entry(const hawk_paged_cache* cache, const int32_t* table_row
  *   with the entries before n_past[s] copied in all layers (every holder that writes in one call gets its own, the last one too).  Free
  *   pages are taken in ascending order, sequences and places in ascending order; a sequence that needs more than are left, and every one behind
  *   it that needs any, is left as it was.  short_by [n_seq]: 0, or for a sequence that was left how many pages it needs.
- * hawk_paged_trim: the pages behind the first n_past[s] entries are given back (n_past[s] = 0: all of them; negative: the sequence is left alone).
+ * hawk_paged_trim: the pages behind the first n_past[s] entries are given back (n_past[s] = 0: all of them; negative: the sequence is left alone);
+ *   n_seq * (max_pages / 256, rounded up) <= 2^23.
  * hawk_paged_compact: the pages in use (refs > 0), U of them, come to lie in pages 0 .. U - 1: those behind are moved, in all layers, in
  *   ascending order into the free ones before, in ascending order.  table_out (row s table_out_stride places behind row s - 1) and refs_out
  *   get the table and the counts as they are then, in place (the table with its own stride) or elsewhere (over part of the old ones they are refused); places of pages that are not in use become -1.  n_used: U.
  *   No entry that the old table leads to is overwritten.
  * hawk_paged_copy: page src[i] of one pool goes to page dst[i] of another (or the same) of equal type, layers, heads, head_dim and page_size, all
- *   layers, i < n, n <= 2^20; pairs with a page outside its pool are left out.  A page that is written twice, or written and read, holds either.
+ *   layers, i < n, n <= 2^20; pairs with a page outside its pool are left out.  A page that is written twice, or written and read, holds pieces of
+ *   either.
  * workspace of take and compact (16-byte aligned): hawk_paged_pages_workspace_bytes; nothing in it has to be cleared or is kept.
  * take, compact and copy: n_pages <= 2^31 - 2^15, n_seq * max_pages <= 2^30, a page of one head at most 2^30 times 16 bytes, layers apart from one
  * another. */
@@ -604,8 +606,8 @@ size_t hawk_adapter_apply_workspace_bytes(const hawk_adapters* weights, int rows
  * logits: n values of dtype (any of the three types), row r starting r * row_stride elements in, n 1..2^20, rows <= 2^22; skip (may be NULL) [rows]: a row
  * with a negative entry is not read and gives token -1.  out_prob (may be NULL): the probability with which the token was drawn, kept weights
  * alone; out_kept (may be NULL): how many entries were kept; both 0 where there is no token.
- * workspace (16-byte aligned, may be NULL where the size function says 0): hawk_sample_filtered_workspace_bytes; nothing in it has to be cleared
- * or is kept. */
+ * workspace (16-byte aligned, may be NULL where the size function says 0, up to 150 MB for many long rows): hawk_sample_filtered_workspace_bytes;
+ * nothing in it has to be cleared or is kept. */
 size_t hawk_sample_filtered_workspace_bytes(int rows, int n);
 int hawk_sample_filtered(const void* logits, int dtype, int64_t row_stride, const int32_t* skip, const float* u, const float* temperature,
                          const int32_t* top_k, const float* top_p, const float* min_p, int rows, int n, int32_t* out_token, float* out_prob,

@@ -6,9 +6,10 @@
 // own, shared by more workgroups (splits_of).  Both products are computed transposed (h^T = A x^T, out^T = B h^T): a result lane then has
 // neighbouring elements of one row.
 //
-// What bounds it: of single tokens memory (200 rows of 64 adapters of rank 32, 4096 by 11008, 67 MB, 15.1 us with other inputs in turn: 4.4 TB/s), of prompts
+// What bounds it: of single tokens memory (200 rows of 64 adapters of rank 32, 4096 by 11008, 67 MB, 15.0 us with other inputs in turn: 4.5 TB/s), of prompts
 // as well (4724 rows of 4096 by 4096, 117 MB, 32 us with other inputs in turn, 24 of one input that the last-level cache holds part of); of few rows a
-// chain of latencies (plan, x and A, h, B; one row 3.8 us, of which a launch is 3).
+// chain of latencies (plan, x and A, h, B; one row 3.8 us, where a call that launches nothing but an empty kernel takes 3.7); of large ranks the way of all of A
+// into every tile's unit (1219 rows of rank 128, 1280 by 1000, 13.4 us: 412 KB a unit are 5.5 of it).
 #include "adapters.h"
 #include "paged.h"
 
@@ -32,6 +33,9 @@ constexpr int kHead = 4, kEntry = 1 + kTile;
 __host__ __device__ inline int most_tiles(int rows, int n_adapters) { return rows / kTile + (rows < n_adapters + 1 ? rows : n_adapters + 1); }
 __host__ __device__ inline size_t plan_words(int rows, int n_adapters) { return kHead + (size_t)most_tiles(rows, n_adapters) * kEntry; }
 
+// Once a step, in one workgroup: 96 rows of 8 adapters 4.3 us, 200 single tokens of 64 8.6, 4724 rows of four prompts 13.2; it grows with the rows, and
+// with the adapters that a wave's rows have (65536 rows: 102 us of 16 prompts, 550 of single tokens of 64 adapters; 2^20 of 256 13 ms).
+//
 // Which rows have which adapter.  A row belongs to the last sequence that starts at or before it, if that one goes as far.  A row's number
 // among its adapter's rows is whatever the counters give it: which rows share a tile has no part in any row's result.
 __global__ __launch_bounds__(kPlanThreads) void adapter_plan_kernel(const int32_t* row_start, const int32_t* adapter, int n_seq, int rows, int n_adapters,

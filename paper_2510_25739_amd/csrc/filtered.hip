@@ -16,10 +16,10 @@
 // that a border may be in (filter_parts_kernel); the borders and the draw, a workgroup a row (filter_draw_kernel).  Where the border's bins
 // hold more than a quarter of a part that last workgroup looks for it in the row itself; rows whose logits are beyond the bins' grid are its alone.
 //
-// What bounds it: not memory (48 rows of 65536 are 2.6 us of it) but a workgroup's instructions and barriers.  One row of 16384 entries, 15.4 us, is
-// a dozen steps of sixteen waves with a barrier behind each, 1450 vector instructions a wave, which take 10 us to issue; 96 rows of which some have no top-k
-// 21 us, the exponentials of 16 entries a thread among them; 48 rows of 65536 36.4 us, three launches of 9.7, 14.2 and 10.9, of which nearly 4 each is
-// a launch; 4 of 200003, 16 bits, 37 us.
+// What bounds it: not memory (48 rows of 65536 are 2.6 us of it) but a workgroup's instructions and barriers.  One row of 16384 entries, 15.5 us, is
+// a dozen steps of sixteen waves with a barrier behind each, 1440 vector instructions a wave, which take 9.6 us to issue; 96 rows of which some have no top-k
+// 21.6 us, the exponentials of 16 entries a thread among them; 48 rows of 65536 34.5 us one call among others, three launches of 10.7, 14.3 and 11.0 by
+// themselves, of which nearly 4 each is a launch; 4 of 200003, 16 bits, 33.9 us.
 #include "filtered.h"
 #include "paged.h"
 #include "sample_rows.h"
@@ -1240,6 +1240,7 @@ template <int E> __global__ __launch_bounds__(NT) void filter_draw_kernel(Filter
 // unit: a larger part takes its unit longer, more parts than units take turns (us with 8 / 16 / 32 entries a thread: 16 rows of 65536,
 // 128 / 64 / 32 parts, 29.5 / 34.4 / 46.1; 48 of them, 384 / 192 / 96, 39.3 / 36.0 / 46.4; 512 of them 195 / 178 / 158; 2 of 200003 33.1 / 39.7 / 56.5; 32 of
 // them, 800 / 416 / 224, 73.6 / 67.3 / 61.7).
+// 2048 parts of 72 KB are 150 MB.
 constexpr int kPartsAtOnce = 2048;
 struct Cutting { int E, parts, rows; };          // entries of a thread (0: rows are not cut), parts of a row, rows at a time
 inline Cutting cutting_of(int rows, int n) {

@@ -724,7 +724,7 @@ class AdapterPlan:
             raise HawkError(-1, "hawk_adapter_plan_bytes", "rows or n_adapters out of range")
         self._dev, self._i32, self._f32 = row_start.get_device(), _int32(), _float32()
         self._plan = row_start.new_empty((n,), dtype=_uint8())
-        self._now = _raw_stream()
+        self._now, self._apply = _raw_stream(), self._L.hawk_adapter_apply
         self._streams = {self._now(self._dev) if self._dev >= 0 else 0}
         self._ptr, self._n = self._plan.data_ptr(), n
         self._room = {}     # workspace of an apply by (rank, d_in, d_out, type)
@@ -793,7 +793,7 @@ class AdapterPlan:
         stream = self._now(dev)
         if stream not in self._streams:
             self._note_stream(stream)
-        rc = _call_at(dev, stream, self._L.hawk_adapter_apply, w, self._ptr, self._n, self.rows, hx, hb, ho, ws.data_ptr() if nws else None, nws)
+        rc = _call_at(dev, stream, self._apply, w, self._ptr, self._n, self.rows, hx, hb, ho, ws.data_ptr() if nws else None, nws)
         if rc != 0:
             raise HawkError(rc, where)
         return out
